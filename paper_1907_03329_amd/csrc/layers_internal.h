@@ -1,0 +1,118 @@
+// What the layer operators (include/esrnn_layers.h) share: element types, aligned and unaligned groups of four channels,
+// the sigmoid in both directions, and the launch functions that layers_api.cpp calls.
+#pragma once
+
+#include "device_utils.h"
+#include "esrnn_layers.h"
+
+namespace esrnn {
+
+template <class E>
+using Vec4 = E __attribute__((ext_vector_type(4)));
+
+// f(element type tag) for the element type of a call (checked before)
+template <class F>
+hipError_t with_element(int dtype, F &&f)
+{
+    switch (dtype) {
+    case ESRNN_F32: return f(float{});
+    case ESRNN_BF16: return f(__bf16{});
+    default: return f(_Float16{});
+    }
+}
+
+template <class E>
+__device__ __forceinline__ f32x4 to_f32(Vec4<E> v)
+{
+    return __builtin_convertvector(v, f32x4);
+}
+template <class E>
+__device__ __forceinline__ Vec4<E> from_f32(f32x4 v)
+{
+    return __builtin_convertvector(v, Vec4<E>);
+}
+
+// A lane has four channels of a row of tiles of 4 W channels, W lanes side by side.  Aligned: neighbours, one wide access.  Else the
+// channels lane, lane + W, ..: every access of the W lanes is one run of neighbouring elements.
+template <bool kAligned, int W>
+struct Channels {
+    int first, count;       // first channel of this lane, and how many exist from the tile's begin
+    __device__ __forceinline__ Channels(int lane, int begin, int C) : first(begin + (kAligned ? 4 * lane : lane)), count(C) {}
+    __device__ __forceinline__ int channel(int k) const { return first + (kAligned ? k : W * k); }
+    __device__ __forceinline__ bool exists(int k) const { return channel(k) < count; }
+    // a channel that can be read in the place of one that does not exist
+    __device__ __forceinline__ int readable(int k) const
+    {
+        return kAligned ? min(first, count - 4) + k : min(channel(k), count - 1);
+    }
+    template <class E>
+    __device__ __forceinline__ Vec4<E> load(const E *row) const
+    {
+        if constexpr (kAligned) return *reinterpret_cast<const Vec4<E> *>(row + readable(0));
+        Vec4<E> v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = row[readable(k)];
+        return v;
+    }
+    template <class E>
+    __device__ __forceinline__ void store(E *row, Vec4<E> v) const
+    {
+        if constexpr (kAligned) {
+            if (exists(0)) *reinterpret_cast<Vec4<E> *>(row + first) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (exists(k)) row[channel(k)] = v[k];
+        }
+    }
+};
+
+// sigmoid(g) and sigmoid(-g), both to a few units in the last place: 1 - sigmoid would lose those of the small one
+struct Sigmoids {
+    float of, of_minus;
+};
+__device__ __forceinline__ Sigmoids sigmoids(float g)
+{
+    const float e = __builtin_amdgcn_exp2f(fabsf(g) * kSigmoidExponent);
+    const float large = fast_rcp(1.0f + e), small = e * large;
+    return g < 0.0f ? Sigmoids{small, large} : Sigmoids{large, small};
+}
+
+inline bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+inline size_t element_bytes(int dtype) { return dtype == ESRNN_F32 ? 4 : 2; }
+
+// ---- gated linear recurrence (recurrence_kernels.hip) ----
+// Positions of a block, the blocks of a sequence, and how many neighbouring blocks a workgroup takes (a segment).
+struct RecurrencePlan {
+    int waves, block, blocks, per_segment, segments;
+};
+RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s);
+struct RecurrenceForward {
+    const void *x, *gate;
+    const int32_t *lengths;
+    const float *initial;
+    void *out;
+    float *last, *saved, *parts;
+};
+struct RecurrenceBackward {
+    const void *x, *gate;
+    const int32_t *lengths;
+    const float *saved;
+    const void *grad_out;
+    const float *grad_last;
+    void *grad_x, *grad_gate;
+    float *grad_initial, *parts;
+};
+hipError_t launch_recurrence_forward(const esrnn_recurrence_shape &s, const RecurrenceForward &a, hipStream_t st);
+hipError_t launch_recurrence_backward(const esrnn_recurrence_shape &s, const RecurrenceBackward &a, hipStream_t st);
+struct RecurrenceStep {
+    const void *x, *gate;
+    long long x_stride, gate_stride, out_stride;
+    const int32_t *slots;
+    float *state;
+    void *out;
+    int rows, pool, C;
+};
+hipError_t launch_recurrence_step(int kind, int dtype, const RecurrenceStep &a, hipStream_t st);
+
+}  // namespace esrnn

@@ -1,0 +1,197 @@
+"""Thin ctypes binding of the layer operators (C ABI in include/esrnn_layers.h): gated linear recurrence, group norm with
+activation, AdamW over many tensors.
+
+Argument marshalling only, as in binding.py: the classes own the buffers of a layer, every call runs in the library's
+kernels on the current stream (or the one given), and a failed call raises EsrnnError.  There is no fallback.
+Tensors that a call names have to live until the stream has run it, as with any work of torch on that stream.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Sequence
+
+from .binding import ESRNN_OK, EsrnnError, load_library
+
+KINDS = {"smooth": 0, "decay": 1}
+ACTIVATIONS = {"none": 0, "silu": 1}
+ADAMW_BLOCK = 256
+
+
+class RecurrenceShape(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("C", C.c_int32), ("kind", C.c_int32), ("dtype", C.c_int32)] + [
+        (name, C.c_int64 * 2) for name in ("x_stride", "gate_stride", "out_stride", "grad_out_stride", "grad_x_stride",
+                                           "grad_gate_stride")]
+
+
+_lib = None
+
+
+def _library():
+    """The library with the signatures of include/esrnn_layers.h."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = load_library()
+    vp, i32, i64, size = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(C.c_size_t)
+    rs = C.POINTER(RecurrenceShape)
+    for name, args in {
+        "esrnn_recurrence_workspace_bytes": [rs, size],
+        "esrnn_recurrence_saved_bytes": [rs, size],
+        "esrnn_recurrence_forward": [rs] + [vp] * 9,
+        "esrnn_recurrence_backward": [rs] + [vp] * 11,
+        "esrnn_recurrence_step": [i32] * 5 + [vp, i64, vp, i64, vp, vp, vp, i64, vp],
+    }.items():
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, C.c_int
+    _lib = lib
+    return lib
+
+
+def _dtype(dtype) -> int:
+    import torch
+    found = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    if found is None:
+        raise ValueError(f"elements are float32, bfloat16 or float16, got {dtype}")
+    return found
+
+
+def _choice(table, name, what):
+    if name not in table:
+        raise ValueError(f"{what} is one of {', '.join(table)}, got {name!r}")
+    return table[name]
+
+
+def _raise(status, what):
+    if status != ESRNN_OK:
+        raise EsrnnError(status, what)
+
+
+def _stream(stream, device):
+    import torch
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+def _bytes(fn, *args) -> int:
+    n = C.c_size_t()
+    _raise(fn(*args, C.byref(n)), fn.__name__)
+    return int(n.value)
+
+
+def _check(t, name, shape, dtype, device, dense=True):
+    """The address of a tensor that has to be there."""
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} has to be {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} has to be contiguous")
+    return t.data_ptr()
+
+
+def _check_optional(t, name, shape, dtype, device):
+    return None if t is None else _check(t, name, shape, dtype, device)
+
+
+def _cuda(device):
+    import torch
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"a GPU is needed, got {device}")
+    return torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+
+
+class GatedRecurrence:
+    """h_t = a_t h_{t-1} + b_t over sequences of up to T positions, C channels each on its own, with gates from the caller:
+    kind "smooth": a = 1 - sigmoid(gate), b = sigmoid(gate) x;  kind "decay": a = sigmoid(gate), b = x.
+
+    Tensors are [B, T, C], with time_major [T, B, C]; x, gate, grad_out (and grad_x, grad_gate, where the caller gives them) may
+    be strided in any way that keeps channels next to each other, as the two halves of one projection's result do.
+    lengths: int32 [B], positions that exist; initial, grad_last: float32 [B, C] or None (zero).
+    Owns out, last, the gradients and what the reverse pass needs, all overwritten by the next call."""
+
+    def __init__(self, B: int, T: int, C_: int, kind: str = "smooth", dtype=None, time_major: bool = False,
+                 training: bool = True, device="cuda"):
+        import torch
+        dtype = torch.float32 if dtype is None else dtype
+        self.device, self.dtype, self.time_major, self.training = _cuda(device), dtype, time_major, training
+        self._lib = _library()
+        s = RecurrenceShape()
+        s.B, s.T, s.C, s.kind, s.dtype = int(B), int(T), int(C_), _choice(KINDS, kind, "kind"), _dtype(dtype)
+        self._shape, self._ref = s, C.byref(s)
+        workspace = _bytes(self._lib.esrnn_recurrence_workspace_bytes, self._ref)
+        saved = _bytes(self._lib.esrnn_recurrence_saved_bytes, self._ref)
+        self.workspace = torch.empty(workspace, dtype=torch.uint8, device=self.device)
+        self._size = torch.Size((T, B, C_) if time_major else (B, T, C_))
+        self._rows = torch.Size((B, C_))
+        self.out = torch.empty(self._size, dtype=dtype, device=self.device)
+        self.last = torch.empty(self._rows, dtype=torch.float32, device=self.device)
+        self._out_ptr, self._last_ptr, self._workspace_ptr = self.out.data_ptr(), self.last.data_ptr(), self.workspace.data_ptr()
+        self._strides(s.out_stride, self.out)
+        self._forward_done = False
+        if training:
+            self.saved = torch.empty(saved // 4, dtype=torch.float32, device=self.device)
+            self.grad_x, self.grad_gate = (torch.empty(self._size, dtype=dtype, device=self.device) for _ in range(2))
+            self.grad_initial = torch.empty(self._rows, dtype=torch.float32, device=self.device)
+
+    def _strides(self, field, t):
+        a, b, _ = t.stride()
+        field[0], field[1] = (b, a) if self.time_major else (a, b)
+
+    def _elements(self, t, name, field):
+        at = _check(t, name, self._size, self.dtype, self.device, dense=False)
+        if t.stride(2) != 1 and self._size[2] != 1:
+            raise ValueError(f"{name}: channels have to lie next to each other")
+        self._strides(field, t)
+        return at
+
+    def _lengths(self, lengths):
+        import torch
+        return _check_optional(lengths, "lengths", self._rows[:1], torch.int32, self.device)
+
+    def forward(self, x, gate, lengths=None, initial=None, stream=None):
+        """(out, last): all states in the element type, zero past the lengths, and the last one of every sequence in float32."""
+        import torch
+        s = self._shape
+        x_ptr, gate_ptr = self._elements(x, "x", s.x_stride), self._elements(gate, "gate", s.gate_stride)
+        _raise(self._lib.esrnn_recurrence_forward(
+            self._ref, x_ptr, gate_ptr, self._lengths(lengths),
+            _check_optional(initial, "initial", self._rows, torch.float32, self.device), self._out_ptr, self._last_ptr,
+            self.saved.data_ptr() if self.training else None, self._workspace_ptr, _stream(stream, self.device)),
+            "esrnn_recurrence_forward")
+        self._forward_done = True
+        return self.out, self.last
+
+    def backward(self, x, gate, grad_out, lengths=None, grad_last=None, grad_x=None, grad_gate=None, stream=None):
+        """(grad_x, grad_gate, grad_initial) for the forward pass last run, which had the same x, gate and lengths."""
+        import torch
+        if not self.training or not self._forward_done:
+            raise EsrnnError(4, "GatedRecurrence.backward")
+        grad_x = self.grad_x if grad_x is None else grad_x
+        grad_gate = self.grad_gate if grad_gate is None else grad_gate
+        s = self._shape
+        x_ptr, gate_ptr = self._elements(x, "x", s.x_stride), self._elements(gate, "gate", s.gate_stride)
+        d_ptr = self._elements(grad_out, "grad_out", s.grad_out_stride)
+        gx_ptr = self._elements(grad_x, "grad_x", s.grad_x_stride)
+        gg_ptr = self._elements(grad_gate, "grad_gate", s.grad_gate_stride)
+        _raise(self._lib.esrnn_recurrence_backward(
+            self._ref, x_ptr, gate_ptr, self._lengths(lengths), self.saved.data_ptr(), d_ptr,
+            _check_optional(grad_last, "grad_last", self._rows, torch.float32, self.device), gx_ptr, gg_ptr,
+            self.grad_initial.data_ptr(), self._workspace_ptr, _stream(stream, self.device)), "esrnn_recurrence_backward")
+        return grad_x, grad_gate, self.grad_initial
+
+
+def recurrence_step(x, gate, state, out, slots=None, kind: str = "smooth", stream=None) -> None:
+    """One position for each row of x, gate, out [rows, C]: state [pool, C] float32 is updated in place and out gets it in the
+    element type.  slots: int32 [rows], the pool's row of every request, distinct (outside the pool: zeros, nothing changes)."""
+    import torch
+    lib, device = _library(), x.device
+    if x.dim() != 2 or state.dim() != 2 or device.type != "cuda":
+        raise ValueError("x has to be [rows, C] and state [pool, C] on a GPU")
+    rows, channels = x.shape
+    for name, t in (("x", x), ("gate", gate), ("out", out)):
+        _check(t, name, x.shape, x.dtype, device, dense=False)
+        if t.stride(1) != 1 and channels != 1:
+            raise ValueError(f"{name}: channels have to lie next to each other")
+    _raise(lib.esrnn_recurrence_step(
+        _choice(KINDS, kind, "kind"), _dtype(x.dtype), rows, state.shape[0], channels, x.data_ptr(), x.stride(0), gate.data_ptr(),
+        gate.stride(0), _check_optional(slots, "slots", x.shape[:1], torch.int32, device),
+        _check(state, "state", torch.Size((state.shape[0], channels)), torch.float32, device), out.data_ptr(), out.stride(0),
+        _stream(stream, device)), "esrnn_recurrence_step")

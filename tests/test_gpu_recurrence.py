@@ -1,0 +1,369 @@
+"""Gated linear recurrence on the GPU against its definition, position by position in 64 bits."""
+import numpy as np
+import pytest
+
+from paper_1907_03329_amd import layers
+
+pytestmark = pytest.mark.gpu
+
+# Largest difference over the largest value of the array.  An element is rounded to its type once (half a unit in the last place: with 24, 8 and 11
+# significant bits at most 2^-24, 2^-8, 2^-11 of it).  The fp32 arithmetic before that: a sigmoid is off by a few 2^-24, every position adds a
+# rounding to a state that forgets the earlier ones at the rate at which it forgets inputs, and gates below allow a memory of some
+# hundred positions: 2e-5 has room for all of it, and a dropped or doubled position is off by 1e-2 or more.
+ROUNDING = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
+ARITHMETIC = 2e-5
+
+
+def definition(kind, x, g, h0, lengths, d=None, dlast=None):
+    """All in float64 numpy, [B, T, C]; the reverse pass written down from the forward one, position by position."""
+    B, T, C = x.shape
+    z, rest = 1.0 / (1.0 + np.exp(-g)), 1.0 / (1.0 + np.exp(g))
+    a, b = (rest, z * x) if kind == "smooth" else (z, x)
+    out, before, h = np.zeros_like(x), np.zeros_like(x), h0.copy()
+    for t in range(T):
+        on = (t < lengths)[:, None]
+        before[:, t] = h
+        h = np.where(on, a[:, t] * h + b[:, t], h)
+        out[:, t] = np.where(on, h, 0.0)
+    if d is None:
+        return out, h
+    gx, gg, mu = np.zeros_like(x), np.zeros_like(x), dlast.copy()
+    for t in range(T - 1, -1, -1):
+        on = (t < lengths)[:, None]
+        lam = d[:, t] + mu
+        if kind == "smooth":
+            gx[:, t] = np.where(on, lam * z[:, t], 0.0)
+            gg[:, t] = np.where(on, lam * (x[:, t] - before[:, t]) * z[:, t] * rest[:, t], 0.0)
+        else:
+            gx[:, t] = np.where(on, lam, 0.0)
+            gg[:, t] = np.where(on, lam * before[:, t] * z[:, t] * rest[:, t], 0.0)
+        mu = np.where(on, a[:, t] * lam, mu)
+    return out, h, gx, gg, mu
+
+
+def close(got, want, dtype="float32", what=""):
+    got = got.double().cpu().numpy()
+    scale = np.abs(want).max() if want.size else 0.0
+    assert np.isfinite(got).all(), what
+    err = np.abs(got - want).max() if want.size else 0.0
+    assert err <= (ROUNDING[dtype] + ARITHMETIC) * scale, (what, err, scale)
+
+
+def tensors(rng, B, T, C, dtype, kind, time_major=False, lengths=None, layout="halves"):
+    """x, gate, grad_out as the caller's program has them, and the same values in float64 [B, T, C]."""
+    import torch
+    dt = getattr(torch, dtype)
+    lead = (T, B) if time_major else (B, T)
+    host = {"x": rng.normal(size=lead + (C,)), "g": rng.normal(size=lead + (C,)) * 1.5 + (2.0 if kind == "decay" else -2.0),
+            "d": rng.normal(size=lead + (C,))}
+    dev = {k: torch.from_numpy(v).to(dt) for k, v in host.items()}
+    turn = (lambda v: v.transpose(1, 0, 2)) if time_major else (lambda v: v)
+    ref = {k: turn(v.double().numpy()) for k, v in dev.items()}
+    if lengths is not None:     # what lies past a length must not matter
+        for b, n in enumerate(lengths):
+            for k in dev:
+                at = (slice(n, None), b) if time_major else (b, slice(n, None))
+                dev[k][at] = float("nan") if b % 2 else float("inf")
+    if layout == "halves":
+        both = torch.cat([dev["x"], dev["g"]], -1).cuda()
+        x, g = both[..., :C], both[..., C:]
+    else:                       # every array with gaps between its rows and a first element that no wide access likes
+        def gaps(v):
+            flat = torch.full((lead[0], lead[1] + 2, C + 3), float("nan"), dtype=dt, device="cuda")
+            view = flat[:, 1:-1, 1:C + 1]
+            view.copy_(v)
+            return view
+        x, g = gaps(dev["x"]), gaps(dev["g"])
+        return x, g, gaps(dev["d"]), ref
+    return x, g, dev["d"].cuda(), ref
+
+
+def check(B, T, C, dtype="float32", kind="smooth", time_major=False, lengths=None, initial=False, layout="halves", seed=0):
+    import torch
+    rng = np.random.default_rng(seed)
+    if isinstance(lengths, str):
+        n = rng.integers(0, T + 1, B)
+        n[rng.integers(B)] = T
+        if B > 1:
+            n[np.flatnonzero(n < T)[:1]] = 0
+        lengths = n
+    x, g, d, ref = tensors(rng, B, T, C, dtype, kind, time_major, lengths, layout)
+    n = np.full(B, T) if lengths is None else np.asarray(lengths)
+    h0 = torch.from_numpy(rng.normal(size=(B, C))).float() if initial else torch.zeros(B, C)
+    dl = torch.from_numpy(rng.normal(size=(B, C))).float() if initial else torch.zeros(B, C)
+    layer = layers.GatedRecurrence(B, T, C, kind=kind, dtype=x.dtype, time_major=time_major)
+    for t in (layer.out, layer.last, layer.saved, layer.grad_x, layer.grad_gate, layer.grad_initial):
+        t.fill_(float("nan"))
+    layer.workspace.fill_(255)
+    lens = None if lengths is None else torch.from_numpy(n.astype(np.int32)).cuda()
+    out, last = layer.forward(x, g, lengths=lens, initial=h0.cuda() if initial else None)
+    gx, gg, gi = layer.backward(x, g, d, lengths=lens, grad_last=dl.cuda() if initial else None)
+    want = definition(kind, ref["x"], ref["g"], h0.double().numpy(), n, ref["d"], dl.double().numpy())
+    turn = (lambda t: t.transpose(0, 1)) if time_major else (lambda t: t)
+    what = (B, T, C, dtype, kind, time_major, layout)
+    close(turn(out), want[0], dtype, ("out",) + what)
+    close(last, want[1], "float32", ("last",) + what)
+    close(turn(gx), want[2], dtype, ("grad_x",) + what)
+    close(turn(gg), want[3], dtype, ("grad_gate",) + what)
+    close(gi, want[4], "float32", ("grad_initial",) + what)
+    if lengths is not None:
+        for b in range(B):
+            for t in (turn(out), turn(gx), turn(gg)):
+                assert not t[b, n[b]:].any()
+    return layer, (x, g, d, lens, h0, dl), (out, last, gx, gg, gi)
+
+
+@pytest.mark.parametrize("kind", ["smooth", "decay"])
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 31, 32, 33, 64, 65, 127, 128, 129, 257, 1000])
+def test_lengths_around_every_piece(kind, T):
+    check(3, T, 68, kind=kind, initial=True, seed=T)
+
+
+@pytest.mark.parametrize("C", [1, 2, 3, 4, 5, 37, 63, 64, 65, 130])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_channels_and_types(C, dtype):
+    check(2, 150, C, dtype=dtype, kind="decay", seed=C)
+    check(2, 20, C, dtype=dtype, kind="smooth", initial=True, seed=C + 1)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("kind", ["smooth", "decay"])
+@pytest.mark.parametrize("time_major", [False, True])
+@pytest.mark.parametrize("T", [50, 300])
+def test_ragged_lengths_with_garbage_behind_them(dtype, kind, time_major, T):
+    check(9, T, 40, dtype=dtype, kind=kind, time_major=time_major, lengths="ragged", initial=True, seed=T)
+    check(9, T, 41, dtype=dtype, kind=kind, time_major=time_major, lengths="ragged", layout="gaps", seed=T + 1)
+
+
+def test_all_sequences_empty():
+    layer, given, (out, last, gx, gg, gi) = check(3, 200, 8, lengths=[0, 0, 0], initial=True)
+    assert (last.cpu() == given[4]).all() and (gi.cpu() == given[5]).all()
+
+
+@pytest.mark.parametrize("B,T,C,dtype", [(1, 5000, 64, "bfloat16"), (2, 4096, 100, "float32"), (1, 40000, 5, "float32"), (3, 2049, 256, "float16")])
+@pytest.mark.parametrize("kind", ["smooth", "decay"])
+def test_few_channels_and_many_positions(B, T, C, dtype, kind):
+    """(several segments a sequence)"""
+    check(B, T, C, dtype=dtype, kind=kind, initial=True, seed=T)
+    check(B, T, C, dtype=dtype, kind=kind, lengths=[T // 3 + 5] * B, seed=T + 1)
+
+
+def test_lengths_outside_the_range_are_clamped():
+    import torch
+    rng = np.random.default_rng(3)
+    x, g, d, ref = tensors(rng, 2, 40, 12, "float32", "smooth")
+    layer = layers.GatedRecurrence(2, 40, 12)
+    out, last = layer.forward(x, g, lengths=torch.tensor([-5, 1000], dtype=torch.int32, device="cuda"))
+    want = definition("smooth", ref["x"], ref["g"], np.zeros((2, 12)), np.array([0, 40]))
+    close(out, want[0])
+    close(last, want[1])
+
+
+def test_gates_at_their_ends():
+    """Gates of +-30 and infinities: a state is kept for ever or replaced at once, and rates near zero and one keep their digits."""
+    import torch
+    T, C = 200, 8
+    g = torch.full((1, T, C), -30.0)
+    g[0, 10], g[0, 20], g[0, 30] = 30.0, float("inf"), float("-inf")
+    g[0, :, 4:] = 9.0       # almost all of x at once, what is left counts in the gradient of the gate
+    x = torch.linspace(-2, 3, T * C).view(1, T, C)
+    d = torch.ones(1, T, C)
+    layer = layers.GatedRecurrence(1, T, C)
+    out, last = layer.forward(x.cuda(), g.cuda())
+    gx, gg, gi = layer.backward(x.cuda(), g.cuda(), d.cuda())
+    with np.errstate(over="ignore"):
+        want = definition("smooth", x.double().numpy(), g.double().numpy(), np.zeros((1, C)), np.array([T]), d.double().numpy(), np.zeros((1, C)))
+    for got, w in zip((out, last, gx, gg, gi), want):
+        close(got, w)
+    wanted = want[3][:, :, 4:]
+    assert np.abs(gg[:, :, 4:].double().cpu().numpy() - wanted).max() <= ARITHMETIC * np.abs(wanted).max()
+
+
+@pytest.mark.parametrize("kind", ["smooth", "decay"])
+@pytest.mark.parametrize("T", [300, 3000])
+def test_what_is_not_finite_stays_behind_its_position(kind, T):
+    import torch
+    rng = np.random.default_rng(5)
+    x, g, d, _ = tensors(rng, 1, T, 8, "float32", kind)
+    layer = layers.GatedRecurrence(1, T, 8, kind=kind)
+    clean = layer.forward(x, g)[0].clone()
+    x[0, 133, 2] = float("nan")
+    out = layer.forward(x, g)[0]
+    assert torch.equal(out[0, :133], clean[0, :133]) and out[0, 133:, 2].isnan().all()
+    keep = [c for c in range(8) if c != 2]
+    assert torch.equal(out[0, :, keep], clean[0, :, keep])
+
+
+@pytest.mark.parametrize("kind", ["smooth", "decay"])
+def test_gradients_against_differences(kind):
+    """Of the library's own forward pass in fp32: central differences with a step of 1e-2 of sums that are linear in the outputs."""
+    import torch
+    rng = np.random.default_rng(7)
+    B, T, C = 2, 140, 5
+    x, g, d, _ = tensors(rng, B, T, C, "float32", kind)
+    x, g = x.contiguous(), g.contiguous()
+    h0, dl = (torch.from_numpy(rng.normal(size=(B, C))).float().cuda() for _ in range(2))
+    lens = torch.tensor([T, 77], dtype=torch.int32, device="cuda")
+    layer = layers.GatedRecurrence(B, T, C, kind=kind)
+
+    def value():
+        out, last = layer.forward(x, g, lengths=lens, initial=h0)
+        return float((out.double() * d.double()).sum() + (last.double() * dl.double()).sum())
+
+    value()
+    grads = [t.clone() for t in layer.backward(x, g, d, lengths=lens, grad_last=dl)]
+    for t, grad in zip((x, g, h0), grads):
+        for _ in range(6):
+            at = tuple(int(rng.integers(n)) for n in t.shape)
+            step, old = 1e-2, float(t[at])
+            t[at] = old + step
+            up = value()
+            t[at] = old - step
+            down = value()
+            t[at] = old
+            # truncation: step^2 / 6 of a third derivative of the size of the gradients; rounding: 1e-7 of sums of ~ 10 over the step
+            assert abs((up - down) / (2 * step) - float(grad[at])) <= 1e-3 * max(1.0, float(grad.abs().max()))
+
+
+def test_equal_calls_are_equal_and_streams_and_graphs_do_not_matter():
+    import torch
+    layer, (x, g, d, lens, h0, dl), results = check(2, 3000, 72, dtype="bfloat16", lengths="ragged", initial=True, seed=11)
+    want = [t.clone() for t in results]
+    side = torch.cuda.Stream()
+    h0, dl = h0.cuda(), dl.cuda()
+    side.wait_stream(torch.cuda.current_stream())
+    layer.forward(x, g, lengths=lens, initial=h0, stream=side)
+    layer.backward(x, g, d, lengths=lens, grad_last=dl, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(results, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        layer.forward(x, g, lengths=lens, initial=h0)
+        layer.backward(x, g, d, lengths=lens, grad_last=dl)
+    for replay in range(3):
+        h0.mul_(1.5)
+        layer.forward(x, g, lengths=lens, initial=h0)
+        eager = [t.clone() for t in (layer.out, layer.last) + layer.backward(x, g, d, lengths=lens, grad_last=dl)]
+        for t in results:
+            t.zero_()
+        layer.workspace.fill_(replay)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(results, eager))
+
+
+def test_gradients_into_the_halves_of_one_array():
+    import torch
+    rng = np.random.default_rng(13)
+    B, T, C = 2, 70, 24
+    x, g, d, ref = tensors(rng, B, T, C, "float32", "smooth")
+    layer = layers.GatedRecurrence(B, T, C)
+    layer.forward(x, g)
+    both = torch.full((B, T, 2 * C), float("nan"), device="cuda")
+    gx, gg, _ = layer.backward(x, g, d, grad_x=both[..., :C], grad_gate=both[..., C:])
+    assert gx.data_ptr() == both.data_ptr()
+    want = definition("smooth", ref["x"], ref["g"], np.zeros((B, C)), np.full(B, T), ref["d"], np.zeros((B, C)))
+    close(both[..., :C], want[2])
+    close(both[..., C:], want[3])
+
+
+def test_one_sequence_read_for_all():
+    import torch
+    rng = np.random.default_rng(17)
+    x, g, d, ref = tensors(rng, 1, 90, 16, "float32", "decay")
+    layer = layers.GatedRecurrence(4, 90, 16, kind="decay")
+    initial = torch.randn(4, 16, device="cuda")
+    out, _ = layer.forward(x.expand(4, -1, -1), g.expand(4, -1, -1), initial=initial)
+    want = definition("decay", np.repeat(ref["x"], 4, 0), np.repeat(ref["g"], 4, 0), initial.double().cpu().numpy(), np.full(4, 90))
+    close(out, want[0])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("kind", ["smooth", "decay"])
+@pytest.mark.parametrize("rows,pool,C", [(1, 1, 1), (7, 64, 1000), (5, 9, 37), (40, 40, 64), (3, 8, 2051)])
+def test_single_positions(dtype, kind, rows, pool, C):
+    import torch
+    rng = np.random.default_rng(rows + C)
+    dt = getattr(torch, dtype)
+    both = torch.from_numpy(rng.normal(size=(rows, 2 * C)) * 1.5).to(dt).cuda()
+    x, g = both[:, :C], both[:, C:]
+    state = torch.from_numpy(rng.normal(size=(pool, C))).float().cuda()
+    slots = rng.permutation(pool)[:rows].astype(np.int32)
+    if rows > 4:
+        slots[2], slots[3] = -1, pool
+    want_state, want = state.double().cpu().numpy(), np.zeros((rows, C))
+    for i, s in enumerate(slots):
+        if 0 <= s < pool:
+            xi, gi = x[i].double().cpu().numpy(), g[i].double().cpu().numpy()
+            want[i] = definition(kind, xi[None, None], gi[None, None], want_state[s][None], np.ones(1))[1][0]
+            want_state[s] = want[i]
+    out = torch.full((rows, C), float("nan"), dtype=dt, device="cuda")
+    layers.recurrence_step(x, g, state, out, slots=torch.from_numpy(slots).cuda(), kind=kind)
+    close(out, want, dtype)
+    close(state, want_state)
+
+
+def test_positions_one_by_one_are_the_whole_sequence():
+    import torch
+    rng = np.random.default_rng(23)
+    x, g, _, ref = tensors(rng, 6, 90, 40, "float32", "smooth")
+    layer = layers.GatedRecurrence(6, 90, 40)
+    state, out = torch.zeros(6, 40, device="cuda"), torch.empty(6, 40, device="cuda")
+    layers.recurrence_step(x[:0, 0], g[:0, 0], state, out[:0])
+    outs = []
+    for t in range(90):
+        layers.recurrence_step(x[:, t], g[:, t], state, out)
+        outs.append(out.clone())
+    whole, last = layer.forward(x, g)
+    scale = float(whole.abs().max())
+    assert float((torch.stack(outs, 1) - whole).abs().max()) <= ARITHMETIC * scale
+    assert float((state - last).abs().max()) <= ARITHMETIC * scale
+
+
+def test_offsets_beyond_32_bits():
+    """Rows of a strided view that lie more than 2^31 elements apart (the gaps are never touched)."""
+    import torch
+    T, C, stride = 3, 8, (1 << 30) + 8
+    big = torch.empty(2 * stride + 4 * C, dtype=torch.bfloat16, device="cuda")
+    view = lambda at: torch.as_strided(big, (1, T, C), (3 * stride, stride, 1), at)  # noqa: E731
+    rng = np.random.default_rng(29)
+    for at in (0, C):
+        view(at).copy_(torch.from_numpy(rng.normal(size=(1, T, C))))
+    layer = layers.GatedRecurrence(1, T, C, dtype=torch.bfloat16)
+    out, _ = layer.forward(view(0), view(C))
+    want = definition("smooth", view(0).double().cpu().numpy(), view(C).double().cpu().numpy(), np.zeros((1, C)), np.array([T]))
+    close(out, want[0], "bfloat16")
+
+
+def test_refusals():
+    import torch
+    from paper_1907_03329_amd.binding import EsrnnError
+    layer = layers.GatedRecurrence(2, 5, 8)
+    x = torch.zeros(2, 5, 8, device="cuda")
+    with pytest.raises(EsrnnError) as e:
+        layer.backward(x, x, x)
+    assert e.value.status == 4
+    for bad in (x[:1], x.half(), x.cpu(), x.transpose(0, 1)):
+        with pytest.raises(ValueError):
+            layer.forward(x, bad)
+    with pytest.raises(ValueError):
+        layer.forward(x, torch.zeros(2, 5, 16, device="cuda")[..., ::2])
+    with pytest.raises(ValueError):
+        layer.forward(x, x, lengths=torch.zeros(2, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        layer.forward(x, x, initial=torch.zeros(2, 9, device="cuda"))
+    with pytest.raises(ValueError):
+        layers.GatedRecurrence(2, 5, 8, kind="other")
+    with pytest.raises(ValueError):
+        layers.GatedRecurrence(2, 5, 8, dtype=torch.float64)
+    with pytest.raises(EsrnnError):
+        layers.GatedRecurrence(0, 5, 8)
+    layer.forward(x, x)
+    with pytest.raises(EsrnnError) as e:        # gradients that would overwrite each other
+        layer.backward(x, x, x, grad_x=torch.zeros(1, 5, 8, device="cuda").expand(2, -1, -1))
+    assert e.value.status == 2
+    with pytest.raises(ValueError):
+        layers.recurrence_step(x[:, 0], x[:, 0], torch.zeros(2, 9, device="cuda"), x[:, 1])
+    with pytest.raises(EsrnnError):             # two requests, one state, no slots
+        layers.recurrence_step(x[:, 0], x[:, 0], torch.zeros(1, 8, device="cuda"), x[:, 1])
