@@ -131,8 +131,8 @@ typedef struct {
 } esrnn_adamw_tensor;
 
 typedef struct {
-    float lr, beta1, beta2, eps;
-    float clip_norm;          /* <= 0: no clipping, and no norm */
+    double lr, beta1, beta2, eps;     /* double: 1 - beta2 and the bias corrections lose digits that a float beta2 has dropped */
+    double clip_norm;         /* <= 0: no clipping, and no norm */
     uint32_t seed;            /* of the rounding of 8-bit moments */
 } esrnn_adamw_config;
 

@@ -1,0 +1,287 @@
+// AdamW over many tensors at once (include/esrnn_layers.h).
+//
+// All tensors are one list of chunks of kChunk elements, a workgroup each, so that a list of any length is one launch (two with
+// clipping: sums of squares in a fixed order first, which every workgroup of the update adds up in the same order).  A chunk finds its
+// tensor through a table in the workspace.  A wave has whole blocks of 256 elements, four neighbours a lane: the block of an 8-bit
+// moment's scale is one wave's, and its largest magnitude takes six steps within the wave.
+//
+// Bound by memory: 30 bytes an element with bf16 gradients, a bf16 copy and fp32 moments (18 with 8-bit moments) against some 25 (70)
+// vector instructions, of which the hash of the random bits takes 13.
+#include <algorithm>
+#include <cmath>
+
+#include "layers_internal.h"
+
+namespace esrnn {
+
+namespace {
+
+// magnitude of e4m3's largest number, and the factor that brings its exponents to those at a float's lower end (exponent bias
+// 7 against 127): the upper 12 bits of the scaled magnitude, denormal or not, are the code
+constexpr float kMostE4m3 = 448.0f, kToCode = 0x1p-120f, kLeastScale = 0x1p-100f;
+
+template <class E>
+__device__ __forceinline__ f32x4 load_group(const void *base, long long at, int left, bool aligned)
+{
+    const E *p = static_cast<const E *>(base) + at;
+    if (aligned && left >= 4) return to_f32<E>(*reinterpret_cast<const Vec4<E> *>(p));
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (k < left) v[k] = (float)p[k];
+    return v;
+}
+template <class E>
+__device__ __forceinline__ void store_group(void *base, long long at, int left, bool aligned, f32x4 v)
+{
+    E *p = static_cast<E *>(base) + at;
+    const Vec4<E> r = from_f32<E>(v);
+    if (aligned && left >= 4) {
+        *reinterpret_cast<Vec4<E> *>(p) = r;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (k < left) p[k] = r[k];
+}
+__device__ __forceinline__ f32x4 load_grad(const AdamWEntry &e, long long at, int left)
+{
+    if (e.grad_dtype == ESRNN_BF16) return load_group<__bf16>(e.grad, at, left, e.aligned);
+    if (e.grad_dtype == ESRNN_F16) return load_group<_Float16>(e.grad, at, left, e.aligned);
+    return load_group<float>(e.grad, at, left, e.aligned);
+}
+
+// the place of one group of four neighbours of this lane in its tensor
+__device__ __forceinline__ int elements_left(const AdamWEntry &e, long long at)
+{
+    return (int)min(max(e.n - at, 0LL), 4LL);
+}
+
+__global__ void __launch_bounds__(1024) adamw_norm_kernel(const AdamWEntry *__restrict__ entries, const int *__restrict__ owner, int chunks,
+                                                          double *__restrict__ partial)
+{
+    constexpr int kGroups = kAdamWChunk / 256;
+    __shared__ double s_wave[16];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    double acc = 0.0;       // (squares of fp32 numbers do not overflow)
+    for (int chunk = __builtin_amdgcn_readfirstlane(blockIdx.x * 16 + wave); chunk < chunks; chunk += gridDim.x * 16) {
+        const AdamWEntry e = entries[owner[chunk]];
+        const long long first = (long long)(chunk - e.first_chunk) * kAdamWChunk + 4 * lane;
+        f32x4 g[kGroups];
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) g[j] = load_grad(e, first + 256 * j, elements_left(e, first + 256 * j));
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc += (double)g[j][k] * (double)g[j][k];
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) acc += __shfl_xor(acc, off, 64);
+    if (lane == 0) s_wave[wave] = acc;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double sum = 0.0;
+        for (int w = 0; w < 16; ++w) sum += s_wave[w];
+        partial[blockIdx.x] = sum;
+    }
+}
+
+// largest of the wave's 64 (bit patterns of magnitudes: a NaN is above infinity, and that above all numbers)
+__device__ __forceinline__ int wave_max_bits(int v)
+{
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v = max(v, __shfl_xor(v, off, 64));
+    return v;
+}
+
+__device__ __forceinline__ unsigned random_word(unsigned long long place, unsigned key)
+{
+    unsigned w = (unsigned)place ^ (unsigned)(place >> 32) * 0xC2B2AE35u ^ key;
+    w = (w ^ w >> 16) * 0x7FEB352Du;
+    w = (w ^ w >> 15) * 0x846CA68Bu;
+    return w ^ w >> 16;
+}
+
+struct Scale {
+    float scale, inverse;
+    bool finite;
+};
+__device__ __forceinline__ Scale scale_of(int most_bits)
+{
+    const float scale = __builtin_bit_cast(float, most_bits) * (1.0f / kMostE4m3);
+    if (most_bits >= 0x7f800000) return {__builtin_nanf(""), 0.0f, false};
+    return scale > kLeastScale ? Scale{scale, 1.0f / scale, true} : Scale{0.0f, 0.0f, true};
+}
+// 16 random bits behind the three of the code's mantissa, of the 20 that are cut off: up with the probability of what is cut off
+__device__ __forceinline__ unsigned code_of(float magnitude, const Scale &s, unsigned bits16)
+{
+    const unsigned y = __builtin_bit_cast(unsigned, magnitude * s.inverse * kToCode);
+    return (y + (bits16 << 4)) >> 20;
+}
+
+// Every operation rounded by itself, as an elementwise program rounds them: which of two codes a moment takes hangs on its last bits.
+__device__ __forceinline__ void moments(f32x4 &m, f32x4 &v, f32x4 g, const AdamWUpdate &u)
+{
+#pragma clang fp contract(off)
+    m = u.beta1 * m + u.new1 * g;
+    v = u.beta2 * v + u.new2 * (g * g);
+}
+
+// kBits: of the moments.
+template <int kBits>
+__global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
+{
+    constexpr int kGroups = kAdamWChunk / 1024;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, chunk = blockIdx.x;
+    const AdamWEntry e = u.entries[u.owner[chunk]];
+    const long long first = (long long)(chunk - e.first_chunk) * kAdamWChunk + wave * (256 * kGroups) + 4 * lane;
+    const long long flat = e.flat + first;      // place in the moments
+
+    int left[kGroups];
+    f32x4 p[kGroups], g[kGroups], m[kGroups], v[kGroups];
+    unsigned m8[kGroups], r8[kGroups];
+    float m_scale[kGroups], r_scale[kGroups];
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j) {
+        const long long at = first + 256 * j;
+        left[j] = elements_left(e, at);
+        const bool block = at - 4 * lane < e.n;     // (uniform: the wave has a block here)
+        p[j] = load_group<float>(e.param, at, left[j], e.aligned);
+        g[j] = load_grad(e, at, left[j]);
+        if (kBits == 32) {
+            m[j] = v[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (block) {
+                m[j] = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(u.m) + flat + 256 * j);
+                v[j] = *reinterpret_cast<const f32x4 *>(u.v + flat + 256 * j);
+            }
+        } else {
+            m8[j] = r8[j] = 0;
+            m_scale[j] = r_scale[j] = 0.0f;
+            if (block) {
+                m8[j] = reinterpret_cast<const unsigned *>(u.m)[(flat + 256 * j) >> 2];
+                r8[j] = reinterpret_cast<const unsigned *>(u.r)[(flat + 256 * j) >> 2];
+                m_scale[j] = u.m_scale[(flat + 256 * j) >> 8];
+                r_scale[j] = u.r_scale[(flat + 256 * j) >> 8];
+            }
+        }
+    }
+    float scale = 1.0f;
+    if (u.partial) {
+        __shared__ double s_sum[4];
+        double sum = (int)threadIdx.x < u.n_partial ? u.partial[threadIdx.x] : 0.0;
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+        if (lane == 0) s_sum[wave] = sum;
+        __syncthreads();
+        const float norm = (float)sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
+        if (u.norm && blockIdx.x == 0 && threadIdx.x == 0) *u.norm = norm;
+        if (!(norm < __builtin_inff())) return;     // infinite or NaN: nothing changes
+        scale = fminf(1.0f, u.clip_norm / (norm + 1e-6f));
+    }
+    const float keep = 1.0f - u.lr * e.weight_decay;
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j) {
+        if (first + 256 * j - 4 * lane >= e.n) break;
+        if (kBits == 8) {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(m8[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(m8[j], true);
+            const auto rlo = __builtin_amdgcn_cvt_pk_f32_fp8(r8[j], false), rhi = __builtin_amdgcn_cvt_pk_f32_fp8(r8[j], true);
+            m[j] = f32x4{lo[0], lo[1], hi[0], hi[1]} * m_scale[j];
+            const f32x4 r = f32x4{rlo[0], rlo[1], rhi[0], rhi[1]} * r_scale[j];
+            v[j] = r * r;
+        }
+        f32x4 root;
+        moments(m[j], v[j], g[j] * scale, u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            root[k] = sqrtf(v[j][k]);
+            p[j][k] = keep * p[j][k] - u.rate * m[j][k] * fast_rcp(root[k] * u.root_correction + u.eps);
+        }
+        const long long at = first + 256 * j;
+        store_group<float>(e.param, at, left[j], e.aligned, p[j]);
+        if (e.copy) {
+            if (e.copy_dtype == ESRNN_BF16) store_group<__bf16>(e.copy, at, left[j], e.aligned, p[j]);
+            else store_group<_Float16>(e.copy, at, left[j], e.aligned, p[j]);
+        }
+        if (kBits == 32) {
+            *reinterpret_cast<f32x4 *>(static_cast<float *>(u.m) + flat + 256 * j) = m[j];
+            *reinterpret_cast<f32x4 *>(u.v + flat + 256 * j) = v[j];
+            continue;
+        }
+        int most_m = 0, most_r = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            most_m = max(most_m, __builtin_bit_cast(int, fabsf(m[j][k])));
+            most_r = max(most_r, __builtin_bit_cast(int, fabsf(root[k])));
+        }
+        const Scale sm = scale_of(wave_max_bits(most_m)), sr = scale_of(wave_max_bits(most_r));
+        unsigned m_codes = 0, r_codes = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned w = random_word((unsigned long long)(flat + 256 * j + k), u.key);
+            const unsigned mc = code_of(fabsf(m[j][k]), sm, w >> 16) | (m[j][k] < 0.0f ? 0x80u : 0u);
+            const float y = root[k] * sr.inverse * kToCode;
+            const unsigned rc = max(code_of(root[k], sr, w & 0xffffu), y > 0.0f ? 1u : 0u);
+            m_codes |= (sm.finite ? mc : 0x7fu) << 8 * k;
+            r_codes |= (sr.finite ? rc : 0x7fu) << 8 * k;
+        }
+        reinterpret_cast<unsigned *>(u.m)[(flat + 256 * j) >> 2] = m_codes;
+        reinterpret_cast<unsigned *>(u.r)[(flat + 256 * j) >> 2] = r_codes;
+        if (lane == 0) {
+            u.m_scale[(flat + 256 * j) >> 8] = sm.scale;
+            u.r_scale[(flat + 256 * j) >> 8] = sr.scale;
+        }
+    }
+}
+
+// The table comes to the device as arguments of launches: no copy from host memory that might still be read after the call.
+struct Some {
+    AdamWEntry entry[kAdamWEntriesAtOnce];
+};
+__global__ void __launch_bounds__(64) adamw_entries_kernel(Some some, int n, AdamWEntry *to)
+{
+    if ((int)threadIdx.x < n) to[threadIdx.x] = some.entry[threadIdx.x];
+}
+__global__ void __launch_bounds__(256) adamw_owners_kernel(const AdamWEntry *entries, int count, int *owner, int chunks)
+{
+    const int chunk = blockIdx.x * 256 + threadIdx.x;
+    if (chunk >= chunks) return;
+    int lo = 0, hi = count;         // the last entry whose first chunk is not behind this one
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (entries[mid].first_chunk <= chunk) lo = mid;
+        else hi = mid;
+    }
+    owner[chunk] = lo;
+}
+
+}  // namespace
+
+hipError_t launch_adamw_bind(const AdamWEntry *host, int count, AdamWEntry *entries, int *owner, int chunks, hipStream_t st)
+{
+    for (int first = 0; first < count; first += kAdamWEntriesAtOnce) {
+        Some some{};
+        const int n = std::min(kAdamWEntriesAtOnce, count - first);
+        std::copy(host + first, host + first + n, some.entry);
+        adamw_entries_kernel<<<1, 64, 0, st>>>(some, n, entries + first);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    adamw_owners_kernel<<<(chunks + 255) / 256, 256, 0, st>>>(entries, count, owner, chunks);
+    return hipGetLastError();
+}
+
+hipError_t launch_adamw_update(AdamWUpdate u, int chunks, double *partial, int state_bits, hipStream_t st)
+{
+    if (u.clip_norm > 0.0f) {
+        u.partial = partial;
+        u.n_partial = std::min((chunks + 15) / 16, kAdamWNormBlocks);
+        adamw_norm_kernel<<<u.n_partial, 1024, 0, st>>>(u.entries, u.owner, chunks, partial);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (state_bits == 32) adamw_update_kernel<32><<<chunks, 256, 0, st>>>(u);
+    else adamw_update_kernel<8><<<chunks, 256, 0, st>>>(u);
+    return hipGetLastError();
+}
+
+}  // namespace esrnn

@@ -1,0 +1,1020 @@
+// Group norm with activation, channels last (include/esrnn_layers.h), forward and reverse.
+//
+//   forward   mean and variance of a group (positions of a sample x neighbouring channels), then  u = xhat scale + shift,  out = act(u)
+//   reverse   du = grad_out act'(u);  P1_c = sum over positions of du, P2_c of du xhat;  grad_shift, grad_scale: their sums over samples;
+//             S1 = sum over the group's channels of scale P1, S2 of scale P2;  grad_x = rstd (scale du - (S1 + xhat S2) / M),
+//             M the elements of the group that exist
+//
+// Three ways, by size alone, all with sums in fp32 and variances from differences to a mean (of the group where the data stay on
+// chip, else of a thread's rows, put together pairwise by count: sums of squares would lose the variance of data far from zero):
+//   sample   a workgroup holds all positions of some groups of a sample in registers: x is read once, one launch
+//   position T = 1: a wave has one or several samples with all their channels; sums over a group pass through the wave's own LDS
+//   stream   anything: sums per channel and chunk of positions, sums per group (and of the gradients over samples), the result; three launches,
+//            x read twice, the second time from the last-level cache where it fits
+#include <algorithm>
+
+#include "layers_internal.h"
+
+namespace esrnn {
+
+namespace {
+
+__device__ __forceinline__ f32x4 splat(float v) { return f32x4{v, v, v, v}; }
+
+struct Norm {
+    const void *x, *grad_out;
+    void *out, *grad_x;
+    const int32_t *lengths;
+    const float *scale, *shift, *stats_in;
+    float *stats, *parts, *grad_scale, *grad_shift;
+    int N, T, C, G, D;          // D channels a group
+    int silu;
+    float eps;
+    int tile, tiles, log_w;     // channels of a workgroup, workgroups of a sample, log2 of the lanes side by side (sample way)
+    int chunk, chunks;          // positions of a workgroup, workgroups along positions (stream way)
+};
+
+__device__ __forceinline__ int length_of(const Norm &a, int n) { return a.lengths ? min(max(a.lengths[n], 0), a.T) : a.T; }
+
+__device__ __forceinline__ float activate(float u, int silu) { return silu ? u * sigmoids(u).of : u; }
+__device__ __forceinline__ float slope(float u, int silu)
+{
+    if (!silu) return 1.0f;
+    const Sigmoids s = sigmoids(u);
+    return s.of * (1.0f + u * s.of_minus);
+}
+
+// The gradient of an input, from du, the sums over its group (by the group's elements) and what is normalised.  The product is rounded before the
+// first sum is taken off, as it was in that sum: a group of one element has no gradient, and gets exactly none.
+__device__ __forceinline__ f32x4 input_gradient(f32x4 rstd, f32x4 scale, f32x4 du, f32x4 s1, f32x4 xhat, f32x4 s2)
+{
+    f32x4 own;
+    {
+#pragma clang fp contract(off)
+        own = scale * du;
+    }
+    return rstd * ((own - s1) - xhat * s2);
+}
+
+// ---- sample ------------------------------------------------------------------------------------------------------
+// Channels of a tile [begin, begin + count), dealt to w = 2^log_w lanes; w and the tile are the launch's.
+template <bool kAligned>
+struct TileChannels {
+    int begin, count, w, lane;
+    __device__ __forceinline__ int at(int k) const { return kAligned ? 4 * lane + k : lane + w * k; }
+    __device__ __forceinline__ bool exists(int k) const { return at(k) < count; }
+    template <class E>
+    __device__ __forceinline__ Vec4<E> load(const E *row) const     // of channel 0; some channel of the tile for those that do not exist
+    {
+        if constexpr (kAligned) return *reinterpret_cast<const Vec4<E> *>(row + begin + min(4 * lane, count - 4));
+        Vec4<E> v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = row[begin + min(at(k), count - 1)];
+        return v;
+    }
+    template <class E>
+    __device__ __forceinline__ void store(E *row, Vec4<E> v) const
+    {
+        if constexpr (kAligned) {
+            if (exists(0)) *reinterpret_cast<Vec4<E> *>(row + begin + 4 * lane) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (exists(k)) row[begin + at(k)] = v[k];
+        }
+    }
+    __device__ __forceinline__ f32x4 parameters(const float *p) const       // (any alignment)
+    {
+        f32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = p[begin + min(at(k), count - 1)];
+        return v;
+    }
+};
+
+// Sums over the workgroup's rows, and over the channels of each group.  NV values a channel.
+template <int NT, int NV, bool kAligned>
+struct TileSums {
+    // channel sums of each wave [slots][NV][tile], sums of groups [groups][NV]
+    float *part, *group;
+    int slots, tile, D;
+    __device__ __forceinline__ void channels(f32x4 (&v)[NV], const TileChannels<kAligned> &ch, int log_w)
+    {
+        const int w = 1 << log_w, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        for (int off = w; off < 64; off *= 2)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[i][k] += __shfl_xor(v[i][k], off, 64);
+        const int slot = w >= 64 ? (int)threadIdx.x >> log_w : wave;
+        if (lane < w)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (ch.exists(k)) part[(slot * NV + i) * tile + ch.at(k)] = v[i][k];
+        __syncthreads();
+    }
+    // behind channels(): a wave a group; weight: of a channel
+    template <class W>
+    __device__ __forceinline__ void groups(W &&weight)
+    {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        int log_d = 0;
+        while ((1 << log_d) < D && log_d < 6) ++log_d;
+        const int c0 = lane & ((1 << log_d) - 1), s0 = lane >> log_d, s_step = 64 >> log_d;
+        for (int g = wave; g * D < tile; g += NT / 64) {
+            float sum[NV] = {};
+            for (int c = c0; c < D; c += 64) {
+                const float f = weight(g * D + c);
+                for (int s = s0; s < slots; s += s_step)
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) sum[i] += f * part[(s * NV + i) * tile + g * D + c];
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                sum[i] = wave_sum(sum[i]);
+                if (lane == 0) group[g * NV + i] = sum[i];
+            }
+        }
+        __syncthreads();
+    }
+};
+
+constexpr int kMostTile = 1024;     // channels of a workgroup of the sample way
+
+template <class E, bool kAligned, int NT, int K, bool kSilu>
+__global__ void __launch_bounds__(NT) norm_sample_forward_kernel(Norm a)
+{
+    __shared__ float part[NT / 64 * 256], group[kMostTile];
+    const int n = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, rows = NT >> a.log_w, row = (int)threadIdx.x >> a.log_w;
+    const TileChannels<kAligned> ch{tile * a.tile, min(a.tile, a.C - tile * a.tile), 1 << a.log_w, (int)threadIdx.x & ((1 << a.log_w) - 1)};
+    const int length = length_of(a, n);
+    const E *x = static_cast<const E *>(a.x) + (size_t)n * a.T * a.C;
+    E *out = static_cast<E *>(a.out) + (size_t)n * a.T * a.C;
+    Vec4<E> xs[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (K == 1 || k * rows < a.T) xs[k] = ch.load(x + (size_t)min(row + k * rows, a.T - 1) * a.C);
+    const f32x4 scale = ch.parameters(a.scale), shift = ch.parameters(a.shift);
+    TileSums<NT, 1, kAligned> sums{part, group, a.log_w >= 6 ? rows : NT / 64, ch.count, a.D};
+    int g[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) g[k] = min(ch.at(k), ch.count - 1) / a.D;
+    const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
+    f32x4 mean, rstd, v[1] = {splat(0.0f)};
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (row + k * rows < length) v[0] += to_f32<E>(xs[k]);
+    sums.channels(v, ch, a.log_w);
+    sums.groups([](int) { return 1.0f; });
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mean[k] = group[g[k]] * inverse;
+    v[0] = splat(0.0f);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (row + k * rows < length) {
+            const f32x4 d = to_f32<E>(xs[k]) - mean;
+            v[0] += d * d;
+        }
+    sums.channels(v, ch, a.log_w);      // (a barrier between the reads of `group` above and its next writes)
+    sums.groups([](int) { return 1.0f; });
+#pragma unroll
+    for (int k = 0; k < 4; ++k) rstd[k] = 1.0f / sqrtf(group[g[k]] * inverse + a.eps);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int t = row + k * rows;
+        if (t >= a.T) break;
+        f32x4 y = (to_f32<E>(xs[k]) - mean) * rstd * scale + shift;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = activate(y[i], kSilu);
+        ch.store(out + (size_t)t * a.C, from_f32<E>(t < length ? y : splat(0.0f)));
+    }
+    if (a.stats && row == 0)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (ch.exists(k) && ch.at(k) % a.D == 0) {
+                float *s = a.stats + ((size_t)n * a.G + tile * a.tile / a.D + g[k]) * 2;
+                s[0] = mean[k];
+                s[1] = rstd[k];
+            }
+}
+
+template <class E, bool kAligned, int NT, int K, bool kSilu>
+__global__ void __launch_bounds__(NT) norm_sample_backward_kernel(Norm a)
+{
+    __shared__ float part[NT / 64 * 256 * 2], group[kMostTile * 2];
+    const int n = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, rows = NT >> a.log_w, row = (int)threadIdx.x >> a.log_w;
+    const TileChannels<kAligned> ch{tile * a.tile, min(a.tile, a.C - tile * a.tile), 1 << a.log_w, (int)threadIdx.x & ((1 << a.log_w) - 1)};
+    const int length = length_of(a, n);
+    const size_t base = (size_t)n * a.T * a.C;
+    const E *x = static_cast<const E *>(a.x) + base, *grad_out = static_cast<const E *>(a.grad_out) + base;
+    E *grad_x = static_cast<E *>(a.grad_x) + base;
+    Vec4<E> xs[K], ds[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (K == 1 || k * rows < a.T) {
+            const size_t at = (size_t)min(row + k * rows, a.T - 1) * a.C;
+            xs[k] = ch.load(x + at);
+            ds[k] = ch.load(grad_out + at);
+        }
+    const f32x4 scale = ch.parameters(a.scale), shift = ch.parameters(a.shift);
+    f32x4 mean, rstd;
+    int g[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        g[k] = min(ch.at(k), ch.count - 1) / a.D;
+        const float *s = a.stats_in + ((size_t)n * a.G + tile * a.tile / a.D + g[k]) * 2;
+        mean[k] = s[0];
+        rstd[k] = s[1];
+    }
+    TileSums<NT, 2, kAligned> sums{part, group, a.log_w >= 6 ? rows : NT / 64, ch.count, a.D};
+    f32x4 v[2] = {splat(0.0f), splat(0.0f)};
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (row + k * rows < length) {
+            const f32x4 xhat = (to_f32<E>(xs[k]) - mean) * rstd, u = xhat * scale + shift;
+            f32x4 du = to_f32<E>(ds[k]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) du[i] *= slope(u[i], kSilu);
+            v[0] += du;
+            v[1] += du * xhat;
+        }
+    sums.channels(v, ch, a.log_w);
+    for (int c = threadIdx.x; c < ch.count; c += NT) {      // sums of the sample, to be added up over the samples
+        float p1 = 0.0f, p2 = 0.0f;
+        for (int s = 0; s < sums.slots; ++s) {
+            p1 += part[(s * 2) * ch.count + c];
+            p2 += part[(s * 2 + 1) * ch.count + c];
+        }
+        a.parts[((size_t)n * 2) * a.C + ch.begin + c] = p1;
+        a.parts[((size_t)n * 2 + 1) * a.C + ch.begin + c] = p2;
+    }
+    sums.groups([&](int c) { return a.scale[ch.begin + c]; });
+    const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
+    f32x4 s1, s2;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        s1[k] = group[2 * g[k]] * inverse;
+        s2[k] = group[2 * g[k] + 1] * inverse;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int t = row + k * rows;
+        if (t >= a.T) break;
+        const f32x4 xhat = (to_f32<E>(xs[k]) - mean) * rstd, u = xhat * scale + shift;
+        f32x4 du = to_f32<E>(ds[k]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) du[i] *= slope(u[i], kSilu);
+        const f32x4 gx = input_gradient(rstd, scale, du, s1, xhat, s2);
+        ch.store(grad_x + (size_t)t * a.C, from_f32<E>(t < length ? gx : splat(0.0f)));
+    }
+}
+
+// ---- position ----------------------------------------------------------------------------------------------------
+// T = 1.  A row of a sample's channels is 2^log_w lanes x J chunks of four channels; a wave has 64 >> log_w rows at once.  What a lane has to add
+// to a group goes through the wave's own part of LDS: as the sum of its four channels where groups consist of such fours (kQuads), else
+// channel by channel.  No other wave takes part, so nothing waits at a barrier.
+template <bool kAligned, bool kQuads, int J>
+struct Row {
+    static_assert(kAligned || !kQuads, "");
+    int C, D, G, log_w, lane, row;      // lane: within the row; row: of the wave's
+    float *entries, *sums;              // LDS of this wave: values to add up, sums of groups
+
+    __device__ __forceinline__ int channel(int j, int k) const
+    {
+        return (j << (log_w + 2)) + (kAligned ? 4 * lane + k : lane + (k << log_w));
+    }
+    __device__ __forceinline__ bool exists(int j, int k) const { return channel(j, k) < C; }
+    template <class E>
+    __device__ __forceinline__ Vec4<E> load(const E *p, int j) const
+    {
+        if constexpr (kAligned) return *reinterpret_cast<const Vec4<E> *>(p + min(channel(j, 0), C - 4));
+        Vec4<E> v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = p[min(channel(j, k), C - 1)];
+        return v;
+    }
+    template <class E>
+    __device__ __forceinline__ void store(E *p, int j, Vec4<E> v) const
+    {
+        if constexpr (kAligned) {
+            if (exists(j, 0)) *reinterpret_cast<Vec4<E> *>(p + channel(j, 0)) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (exists(j, k)) p[channel(j, k)] = v[k];
+        }
+    }
+    __device__ __forceinline__ f32x4 parameters(const float *p, int j) const
+    {
+        f32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = p[min(channel(j, k), C - 1)];
+        return v;
+    }
+    // Entries of a group lie side by side; a word of padding after 32 keeps lanes that read at the distance of a group off each
+    // other's banks.
+    __device__ static __forceinline__ int padded(int i) { return i + (i >> 5); }
+    __device__ __forceinline__ int row_entries() const { return padded((J << (log_w + (kQuads ? 0 : 2))) - 1) + 1; }
+    __device__ __forceinline__ int group(int j, int k) const { return min(channel(j, k), C - 1) / D; }
+
+    // v: what each channel adds.  Afterwards total(j, k) is its group's sum.
+    __device__ __forceinline__ void add_up(const f32x4 (&v)[J]) const
+    {
+        float *mine = entries + row * row_entries();
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (kQuads) mine[padded((j << log_w) + lane)] = (v[j][0] + v[j][1]) + (v[j][2] + v[j][3]);
+            else
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mine[padded(channel(j, k))] = v[j][k];
+        }
+        ordered();
+        const int items = G << (6 - log_w), n = kQuads ? D / 4 : D;
+        int log_s = 0;      // lanes that share a group
+        while (items << (log_s + 1) <= 64 && 1 << log_s < n) ++log_s;
+        const int wave_lane = threadIdx.x & 63, part = wave_lane & ((1 << log_s) - 1);
+        for (int item0 = 0; item0 < items; item0 += 64 >> log_s) {
+            const int item = item0 + (wave_lane >> log_s), r = item / G, g = item - r * G;
+            float sum = 0.0f;
+            if (item < items)
+                for (int i = part; i < n; i += 1 << log_s) sum += entries[r * row_entries() + padded(g * n + i)];
+            for (int off = 1; off < 1 << log_s; off *= 2) sum += __shfl_xor(sum, off, 64);
+            if (item < items && part == 0) sums[item] = sum;
+        }
+        ordered();
+    }
+    __device__ __forceinline__ float total(int g) const { return sums[row * G + g]; }
+    __device__ static __forceinline__ void ordered()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+};
+
+// f32x4 of a value of each channel's group
+template <bool kAligned, bool kQuads, int J, class F>
+__device__ __forceinline__ f32x4 by_group(const int (&g)[J][kQuads ? 1 : 4], int j, F &&f)
+{
+    if constexpr (kQuads) return splat(f(g[j][0]));
+    else return f32x4{f(g[j][0]), f(g[j][1]), f(g[j][2]), f(g[j][3])};
+}
+
+extern __shared__ float s_dynamic[];
+
+template <bool kAligned, bool kQuads, int J>
+__device__ __forceinline__ Row<kAligned, kQuads, J> row_of(const Norm &a)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    Row<kAligned, kQuads, J> r{a.C, a.D, a.G, a.log_w, lane & ((1 << a.log_w) - 1), lane >> a.log_w, nullptr, nullptr};
+    r.entries = s_dynamic + wave * a.tile;      // (floats of a wave)
+    r.sums = r.entries + (64 >> a.log_w) * r.row_entries();
+    return r;
+}
+
+template <class E, bool kAligned, bool kQuads, int J, bool kSilu>
+__global__ void __launch_bounds__(256) norm_position_forward_kernel(Norm a)
+{
+    const auto row = row_of<kAligned, kQuads, J>(a);
+    const int rows = 64 >> a.log_w, wave = threadIdx.x >> 6, step = (int)gridDim.x * 4 * rows;
+    int g[J][kQuads ? 1 : 4];
+    f32x4 scale[J], shift[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+#pragma unroll
+        for (int k = 0; k < (kQuads ? 1 : 4); ++k) g[j][k] = row.group(j, k);
+        scale[j] = row.parameters(a.scale, j);
+        shift[j] = row.parameters(a.shift, j);
+    }
+    const float inverse = 1.0f / (float)a.D;
+    const E *x = static_cast<const E *>(a.x);
+    Vec4<E> next[J];
+    int first = (blockIdx.x * 4 + wave) * rows;     // of this wave's samples (the same in all its lanes)
+    if (first < a.N)
+#pragma unroll
+        for (int j = 0; j < J; ++j) next[j] = row.load(x + (size_t)min(first + row.row, a.N - 1) * a.C, j);
+    for (; first < a.N; first += step) {
+        const int n = min(first + row.row, a.N - 1);
+        const bool here = first + row.row < a.N, valid = length_of(a, n) > 0;
+        f32x4 v[J], part[J], mean[J], rstd[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            v[j] = to_f32<E>(next[j]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) part[j][k] = valid && row.exists(j, k) ? v[j][k] : 0.0f;
+        }
+        if (first + step < a.N)
+#pragma unroll
+            for (int j = 0; j < J; ++j) next[j] = row.load(x + (size_t)min(first + step + row.row, a.N - 1) * a.C, j);
+        row.add_up(part);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            mean[j] = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return row.total(i); }) * inverse;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float d = v[j][k] - mean[j][k];
+                part[j][k] = valid && row.exists(j, k) ? d * d : 0.0f;
+            }
+        }
+        row.ordered();
+        row.add_up(part);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            rstd[j] = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return 1.0f / sqrtf(row.total(i) * inverse + a.eps); });
+            if (!here) continue;
+            f32x4 y = (v[j] - mean[j]) * rstd[j] * scale[j] + shift[j];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = activate(y[k], kSilu);
+            row.store(static_cast<E *>(a.out) + (size_t)n * a.C, j, from_f32<E>(valid ? y : splat(0.0f)));
+            if (!a.stats) continue;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = row.channel(j, k);
+                if (c < a.C && c % a.D == 0) {
+                    float *s = a.stats + ((size_t)n * a.G + g[j][kQuads ? 0 : k]) * 2;
+                    s[0] = mean[j][k];
+                    s[1] = rstd[j][k];
+                }
+            }
+        }
+        row.ordered();
+    }
+}
+
+template <class E, bool kAligned, bool kQuads, int J, bool kSilu>
+__global__ void __launch_bounds__(256) norm_position_backward_kernel(Norm a)
+{
+    const auto row = row_of<kAligned, kQuads, J>(a);
+    const int rows = 64 >> a.log_w, wave = threadIdx.x >> 6, step = (int)gridDim.x * 4 * rows;
+    int g[J][kQuads ? 1 : 4];
+    f32x4 scale[J], shift[J], p1[J], p2[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+#pragma unroll
+        for (int k = 0; k < (kQuads ? 1 : 4); ++k) g[j][k] = row.group(j, k);
+        scale[j] = row.parameters(a.scale, j);
+        shift[j] = row.parameters(a.shift, j);
+        p1[j] = p2[j] = splat(0.0f);
+    }
+    const float inverse = 1.0f / (float)a.D;
+    const E *x = static_cast<const E *>(a.x), *grad_out = static_cast<const E *>(a.grad_out);
+    for (int first = (blockIdx.x * 4 + wave) * rows; first < a.N; first += step) {
+        const int n = min(first + row.row, a.N - 1);
+        const bool here = first + row.row < a.N, valid = length_of(a, n) > 0;
+        const size_t base = (size_t)n * a.C;
+        f32x4 xhat[J], du[J], part[J], s1[J], rstd[J];
+        Vec4<E> xs[J], ds[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            xs[j] = row.load(x + base, j);
+            ds[j] = row.load(grad_out + base, j);
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const float *stats = a.stats_in + (size_t)n * a.G * 2;
+            const f32x4 mean = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return stats[2 * i]; });
+            rstd[j] = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return stats[2 * i + 1]; });
+            xhat[j] = (to_f32<E>(xs[j]) - mean) * rstd[j];
+            du[j] = to_f32<E>(ds[j]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                du[j][k] *= slope(xhat[j][k] * scale[j][k] + shift[j][k], kSilu);
+                if (!(here && valid && row.exists(j, k))) du[j][k] = xhat[j][k] = 0.0f;
+            }
+            p1[j] += du[j];
+            p2[j] += du[j] * xhat[j];
+            {
+#pragma clang fp contract(off)
+                part[j] = scale[j] * du[j];
+            }
+        }
+        row.add_up(part);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            s1[j] = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return row.total(i); }) * inverse;
+            part[j] = part[j] * xhat[j];
+        }
+        row.ordered();
+        row.add_up(part);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const f32x4 s2 = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return row.total(i); }) * inverse;
+            const f32x4 gx = input_gradient(rstd[j], scale[j], du[j], s1[j], xhat[j], s2);
+            if (here) row.store(static_cast<E *>(a.grad_x) + base, j, from_f32<E>(valid ? gx : splat(0.0f)));
+        }
+        row.ordered();
+    }
+    // the wave's rows, then the waves one behind the other: parts [workgroups][2][C]
+    for (int off = 1 << a.log_w; off < 64; off *= 2)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                p1[j][k] += __shfl_xor(p1[j][k], off, 64);
+                p2[j][k] += __shfl_xor(p2[j][k], off, 64);
+            }
+    for (int w = 0; w < 4; ++w) {
+        __syncthreads();
+        if (wave != w || row.row != 0) continue;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (row.exists(j, k)) {
+                    const int c = row.channel(j, k);
+                    s_dynamic[c] = w ? s_dynamic[c] + p1[j][k] : p1[j][k];
+                    s_dynamic[a.C + c] = w ? s_dynamic[a.C + c] + p2[j][k] : p2[j][k];
+                }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.C; c += 256) a.parts[(size_t)blockIdx.x * 2 * a.C + c] = s_dynamic[c];
+}
+
+// Sums over `rows` rows of [rows][2][C]: a workgroup has 64 channels of one of the two and a run of rows, its waves every 16th of them.
+// From workgroups of one run to [runs][2][C]; of a single run, to the gradients.
+__global__ void __launch_bounds__(1024) norm_sum_rows_kernel(const float *__restrict__ parts, int rows, int C, float *to_shift, float *to_scale)
+{
+    __shared__ float s_sum[16][64];
+    const int lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane, wave = threadIdx.x >> 6;
+    const int run = (rows + (int)gridDim.z - 1) / (int)gridDim.z, first = blockIdx.z * run, end = min(first + run, rows);
+    const float *p = parts + (size_t)blockIdx.y * C + min(c, C - 1);
+    float sum[4] = {};
+    for (int r = first + wave; r < end; r += 64)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r + 16 * i < end) sum[i] += p[(size_t)(r + 16 * i) * 2 * C];
+    s_sum[wave][lane] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    __syncthreads();
+    if (wave != 0 || c >= C) return;
+    float all = 0.0f;
+    for (int w = 0; w < 16; ++w) all += s_sum[w][lane];
+    (blockIdx.y ? to_scale : to_shift)[(size_t)blockIdx.z * 2 * C + c] = all;
+}
+
+// ---- stream ------------------------------------------------------------------------------------------------------
+// mean of n values, and the sum of squared differences to it
+struct Moments {
+    float n, mean, square;
+    __device__ __forceinline__ void add(const Moments &o)
+    {
+        const float all = n + o.n, share = all > 0.0f ? o.n / all : 0.0f, delta = o.mean - mean;
+        if (o.n > 0.0f) {
+            mean += delta * share;
+            square += o.square + delta * delta * n * share;
+        }
+        n = all;
+    }
+};
+
+constexpr int kRows = 8;        // positions that a thread has in registers at once
+
+// parts [N][chunks][2][C]: mean and sum of squared differences of a channel over a chunk's positions
+template <class E, bool kAligned>
+__global__ void __launch_bounds__(256) norm_moments_kernel(Norm a)
+{
+    __shared__ float s_mean[16][64], s_square[16][64];
+    __shared__ int s_n[16];
+    const int lane16 = threadIdx.x & 15, row = threadIdx.x >> 4;
+    const int n = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, chunk = blockIdx.y;
+    const Channels<kAligned, 16> ch(lane16, tile * 64, a.C);
+    const int first = chunk * a.chunk, end = min(min(first + a.chunk, a.T), length_of(a, n));
+    const E *x = static_cast<const E *>(a.x) + (size_t)n * a.T * a.C;
+    f32x4 mean = splat(0.0f), square = splat(0.0f);
+    int count = 0;
+    for (int t0 = first; t0 < end; t0 += 16 * kRows) {
+        Vec4<E> xs[kRows];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) xs[k] = ch.load(x + (size_t)min(t0 + row + 16 * k, end - 1) * a.C);
+        int have = 0;
+        f32x4 sum = splat(0.0f), sq = splat(0.0f);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k)
+            if (t0 + row + 16 * k < end) {
+                sum += to_f32<E>(xs[k]);
+                ++have;
+            }
+        if (!have) break;
+        const f32x4 m = sum * (1.0f / (float)have);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k)
+            if (t0 + row + 16 * k < end) {
+                const f32x4 d = to_f32<E>(xs[k]) - m;
+                sq += d * d;
+            }
+        const float share = (float)have / (float)(count + have);
+        const f32x4 delta = m - mean;
+        square += sq + delta * delta * ((float)count * share);
+        mean += delta * share;
+        count += have;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        s_mean[row][kAligned ? 4 * lane16 + k : lane16 + 16 * k] = mean[k];
+        s_square[row][kAligned ? 4 * lane16 + k : lane16 + 16 * k] = square[k];
+    }
+    if (lane16 == 0) s_n[row] = count;
+    __syncthreads();
+    const int c = tile * 64 + (int)threadIdx.x;
+    if (threadIdx.x >= 64 || c >= a.C) return;
+    Moments all{0.0f, 0.0f, 0.0f};
+    for (int r = 0; r < 16; ++r) all.add(Moments{(float)s_n[r], s_mean[r][threadIdx.x], s_square[r][threadIdx.x]});
+    float *p = a.parts + ((size_t)n * a.chunks + chunk) * 2 * a.C + c;
+    p[0] = all.mean;
+    p[a.C] = all.square;
+}
+
+__device__ __forceinline__ int positions_in(const Norm &a, int chunk, int length)
+{
+    return max(min(min((chunk + 1) * a.chunk, a.T), length) - chunk * a.chunk, 0);
+}
+
+// stats [N][G][2]: a wave a group
+__global__ void __launch_bounds__(64) norm_stats_kernel(Norm a)
+{
+    const int n = blockIdx.x / a.G, g = blockIdx.x % a.G, length = length_of(a, n);
+    const float *p = a.parts + (size_t)n * a.chunks * 2 * a.C + g * a.D;
+    Moments all{0.0f, 0.0f, 0.0f};
+    const long long entries = (long long)a.chunks * a.D;
+    for (long long i = threadIdx.x; i < entries; i += 64) {
+        const int chunk = (int)(i / a.D), c = (int)(i % a.D);
+        all.add(Moments{(float)positions_in(a, chunk, length), p[(size_t)chunk * 2 * a.C + c], p[((size_t)chunk * 2 + 1) * a.C + c]});
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        const Moments o{__shfl_xor(all.n, off, 64), __shfl_xor(all.mean, off, 64), __shfl_xor(all.square, off, 64)};
+        // (the same order on both sides of an exchange, for the same bits)
+        Moments lower = threadIdx.x & off ? o : all;
+        lower.add(threadIdx.x & off ? all : o);
+        all = lower;
+    }
+    if (threadIdx.x == 0) {
+        float *s = a.stats + (size_t)blockIdx.x * 2;
+        s[0] = all.mean;
+        s[1] = 1.0f / sqrtf((all.n > 0.0f ? all.square / all.n : 0.0f) + a.eps);
+    }
+}
+
+// mean and rstd of the groups of four channels of a lane
+template <bool kAligned>
+__device__ __forceinline__ void group_stats(const Norm &a, const float *stats, int n, const Channels<kAligned, 16> &ch, f32x4 &mean, f32x4 &rstd)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float *s = stats + ((size_t)n * a.G + ch.readable(k) / a.D) * 2;
+        mean[k] = s[0];
+        rstd[k] = s[1];
+    }
+}
+template <bool kAligned>
+__device__ __forceinline__ f32x4 parameters(const float *p, const Channels<kAligned, 16> &ch)
+{
+    return f32x4{p[ch.readable(0)], p[ch.readable(1)], p[ch.readable(2)], p[ch.readable(3)]};
+}
+
+template <class E, bool kAligned, bool kSilu>
+__global__ void __launch_bounds__(256) norm_apply_kernel(Norm a)
+{
+    const int lane16 = threadIdx.x & 15, row = threadIdx.x >> 4;
+    const int n = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
+    const Channels<kAligned, 16> ch(lane16, tile * 64, a.C);
+    const int length = length_of(a, n), first = blockIdx.y * a.chunk, end = min(first + a.chunk, a.T);
+    const E *x = static_cast<const E *>(a.x) + (size_t)n * a.T * a.C;
+    E *out = static_cast<E *>(a.out) + (size_t)n * a.T * a.C;
+    f32x4 mean, rstd;
+    group_stats(a, a.stats, n, ch, mean, rstd);
+    const f32x4 scale = parameters(a.scale, ch), shift = parameters(a.shift, ch);
+    for (int t0 = first; t0 < end; t0 += 16 * kRows) {
+        Vec4<E> xs[kRows];
+        if (t0 < length)
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) xs[k] = ch.load(x + (size_t)min(t0 + row + 16 * k, length - 1) * a.C);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int t = t0 + row + 16 * k;
+            f32x4 y = (to_f32<E>(xs[k]) - mean) * rstd * scale + shift;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = activate(y[i], kSilu);
+            if (t < end) ch.store(out + (size_t)t * a.C, from_f32<E>(t < length ? y : splat(0.0f)));
+        }
+    }
+}
+
+// parts [N][chunks][2][C]: P1 and P2 of a chunk's positions
+template <class E, bool kAligned, bool kSilu>
+__global__ void __launch_bounds__(256) norm_gradient_sums_kernel(Norm a)
+{
+    __shared__ float s_p1[16][64], s_p2[16][64];
+    const int lane16 = threadIdx.x & 15, row = threadIdx.x >> 4;
+    const int n = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, chunk = blockIdx.y;
+    const Channels<kAligned, 16> ch(lane16, tile * 64, a.C);
+    const int first = chunk * a.chunk, end = min(min(first + a.chunk, a.T), length_of(a, n));
+    const E *x = static_cast<const E *>(a.x) + (size_t)n * a.T * a.C, *grad_out = static_cast<const E *>(a.grad_out) + (size_t)n * a.T * a.C;
+    f32x4 mean, rstd, p1 = splat(0.0f), p2 = splat(0.0f);
+    group_stats(a, a.stats_in, n, ch, mean, rstd);
+    const f32x4 scale = parameters(a.scale, ch), shift = parameters(a.shift, ch);
+    for (int t0 = first; t0 < end; t0 += 16 * kRows) {
+        Vec4<E> xs[kRows], ds[kRows];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const size_t at = (size_t)min(t0 + row + 16 * k, end - 1) * a.C;
+            xs[k] = ch.load(x + at);
+            ds[k] = ch.load(grad_out + at);
+        }
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const f32x4 xhat = (to_f32<E>(xs[k]) - mean) * rstd, u = xhat * scale + shift;
+            f32x4 du = to_f32<E>(ds[k]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) du[i] *= slope(u[i], kSilu);
+            if (t0 + row + 16 * k < end) {
+                p1 += du;
+                p2 += du * xhat;
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        s_p1[row][kAligned ? 4 * lane16 + k : lane16 + 16 * k] = p1[k];
+        s_p2[row][kAligned ? 4 * lane16 + k : lane16 + 16 * k] = p2[k];
+    }
+    __syncthreads();
+    const int c = threadIdx.x & 63, which = threadIdx.x >> 6;
+    if (which >= 2 || tile * 64 + c >= a.C) return;
+    float sum = 0.0f;
+    for (int r = 0; r < 16; ++r) sum += (which ? s_p2 : s_p1)[r][c];
+    a.parts[(((size_t)n * a.chunks + chunk) * 2 + which) * a.C + tile * 64 + c] = sum;
+}
+
+// sums [N][G][2] behind parts: S1 / M and S2 / M, a wave a group
+__global__ void __launch_bounds__(64) norm_group_sums_kernel(Norm a)
+{
+    const int n = blockIdx.x / a.G, g = blockIdx.x % a.G, length = length_of(a, n);
+    const float *p = a.parts + (size_t)n * a.chunks * 2 * a.C + g * a.D, *scale = a.scale + g * a.D;
+    float s1 = 0.0f, s2 = 0.0f;
+    const long long entries = (long long)a.chunks * a.D;
+    for (long long i = threadIdx.x; i < entries; i += 64) {
+        const int chunk = (int)(i / a.D), c = (int)(i % a.D);
+        s1 += scale[c] * p[(size_t)chunk * 2 * a.C + c];
+        s2 += scale[c] * p[((size_t)chunk * 2 + 1) * a.C + c];
+    }
+    s1 = wave_sum(s1);
+    s2 = wave_sum(s2);
+    if (threadIdx.x == 0) {
+        const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
+        float *s = a.parts + (size_t)a.N * a.chunks * 2 * a.C + (size_t)blockIdx.x * 2;
+        s[0] = s1 * inverse;
+        s[1] = s2 * inverse;
+    }
+}
+
+template <class E, bool kAligned, bool kSilu>
+__global__ void __launch_bounds__(256) norm_gradient_kernel(Norm a)
+{
+    const int lane16 = threadIdx.x & 15, row = threadIdx.x >> 4;
+    const int n = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
+    const Channels<kAligned, 16> ch(lane16, tile * 64, a.C);
+    const int length = length_of(a, n), first = blockIdx.y * a.chunk, end = min(first + a.chunk, a.T);
+    const E *x = static_cast<const E *>(a.x) + (size_t)n * a.T * a.C, *grad_out = static_cast<const E *>(a.grad_out) + (size_t)n * a.T * a.C;
+    E *grad_x = static_cast<E *>(a.grad_x) + (size_t)n * a.T * a.C;
+    f32x4 mean, rstd, s1, s2;
+    group_stats(a, a.stats_in, n, ch, mean, rstd);
+    group_stats(a, a.parts + (size_t)a.N * a.chunks * 2 * a.C, n, ch, s1, s2);
+    const f32x4 scale = parameters(a.scale, ch), shift = parameters(a.shift, ch);
+    for (int t0 = first; t0 < end; t0 += 16 * kRows) {
+        Vec4<E> xs[kRows], ds[kRows];
+        if (t0 < length)
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) {
+                const size_t at = (size_t)min(t0 + row + 16 * k, length - 1) * a.C;
+                xs[k] = ch.load(x + at);
+                ds[k] = ch.load(grad_out + at);
+            }
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int t = t0 + row + 16 * k;
+            const f32x4 xhat = (to_f32<E>(xs[k]) - mean) * rstd, u = xhat * scale + shift;
+            f32x4 du = to_f32<E>(ds[k]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) du[i] *= slope(u[i], kSilu);
+            const f32x4 gx = input_gradient(rstd, scale, du, s1, xhat, s2);
+            if (t < end) ch.store(grad_x + (size_t)t * a.C, from_f32<E>(t < length ? gx : splat(0.0f)));
+        }
+    }
+}
+
+// ---- which way, and its sizes ------------------------------------------------------------------------------------
+enum Kind { kPosition, kSample, kStream };
+struct Way {
+    Kind kind;
+    int threads, rows_each;     // sample: of a workgroup; positions a thread
+    int tile, tiles, log_w, chunk, chunks;
+    int pieces;                 // position: chunks of four channels a lane
+    int forward_groups, backward_groups;        // position: workgroups
+    int part_rows;              // rows [2][C] of channel sums that the reverse pass leaves
+};
+
+// Rows are added up in two launches from this many on: one alone reads them with 2 C / 64 workgroups.
+constexpr int kManyRows = 1024, kRuns = 64;
+
+Way way_of(const esrnn_group_norm_shape &s)
+{
+    Way w{};
+    const int D = s.C / s.G;
+    if (s.T == 1) {
+        for (w.log_w = 0; w.log_w < 6 && 4 << w.log_w < s.C; ++w.log_w) {}
+        for (w.pieces = 1; w.pieces << (w.log_w + 2) < s.C && w.pieces < 16; w.pieces *= 2) {}
+        if (w.pieces <= (D % 4 ? 4 : 8)) {
+            w.kind = kPosition;
+            const int rows = 4 * (64 >> w.log_w);       // of a workgroup
+            const int64_t most = ((int64_t)s.N + rows - 1) / rows;
+            w.forward_groups = (int)std::min<int64_t>(most, 2048);
+            w.backward_groups = (int)std::min<int64_t>(most, 512);
+            w.part_rows = w.backward_groups;
+            return w;
+        }
+    }
+    // sample: whole groups side by side up to 64 channels (a run of 128 bytes of bf16), as many positions as fit
+    int groups = std::max(1, std::min(s.G, 64 / D));
+    for (int fewer = groups; fewer > 1; --fewer)        // (whole groups of four channels, if a few groups less give them)
+        if (fewer * D % 4 == 0) {
+            groups = fewer;
+            break;
+        }
+    w.tile = groups * D;
+    for (w.log_w = 0; 4 << w.log_w < w.tile; ++w.log_w) {}
+    w.tiles = (s.G + groups - 1) / groups;
+    for (int threads : {256, 1024})
+        for (int rows : {4, 16})
+            if (w.kind != kSample && w.tile <= kMostTile && threads >> w.log_w >= 1 && (int64_t)s.N * w.tiles * threads <= (int64_t(1) << 31) &&
+                (int64_t)s.T <= (int64_t)(threads >> w.log_w) * rows) {
+                w.kind = kSample;
+                w.threads = threads, w.rows_each = rows;
+            }
+    w.part_rows = s.N;
+    if (w.kind == kSample) return w;
+    w.kind = kStream;
+    w.tiles = (s.C + 63) / 64;
+    const int64_t columns = (int64_t)s.N * w.tiles;
+    int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((s.T + 127) / 128, 2048 / columns));
+    w.chunk = (int)(((s.T + chunks - 1) / chunks + 127) / 128 * 128);
+    w.chunks = (s.T + w.chunk - 1) / w.chunk;
+    w.part_rows = s.N * w.chunks;
+    return w;
+}
+
+Norm norm_of(const esrnn_group_norm_shape &s, const GroupNormArgs &f, const Way &w)
+{
+    Norm a{};
+    a.x = f.x, a.grad_out = f.grad_out, a.out = f.out, a.grad_x = f.grad_x, a.lengths = f.lengths, a.scale = f.scale, a.shift = f.shift;
+    a.stats_in = f.stats_in, a.stats = f.stats, a.parts = f.parts, a.grad_scale = f.grad_scale, a.grad_shift = f.grad_shift;
+    a.N = s.N, a.T = s.T, a.C = s.C, a.G = s.G, a.D = s.C / s.G, a.silu = s.activation == ESRNN_NORM_SILU, a.eps = s.eps;
+    a.tile = w.tile, a.tiles = w.tiles, a.log_w = w.log_w, a.chunk = w.chunk, a.chunks = w.chunks;
+    return a;
+}
+
+template <class F>
+void with_flags(bool aligned, bool silu, F &&f)
+{
+    if (aligned) silu ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
+    else silu ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
+}
+
+
+// LDS of a wave of the position way, in floats: entries of its rows, sums of their groups.
+int position_floats(const esrnn_group_norm_shape &s, const Way &w, bool quads)
+{
+    const int rows = 64 >> w.log_w, entries = w.pieces << (w.log_w + (quads ? 0 : 2));
+    return rows * (entries + (entries - 1) / 32 + s.G);
+}
+
+// f(pieces, aligned, quads) for the instantiations that there are: groups that are no fours of channels have at most four pieces, unless
+// it is only the arrays' alignment that keeps the fours apart.
+template <class F>
+void with_pieces(int pieces, bool aligned, bool quads, F &&f)
+{
+    const auto layout = [&](auto j) {
+        if (aligned && quads) f(j, std::true_type{}, std::true_type{});
+        else if (!aligned) f(j, std::false_type{}, std::false_type{});
+        else if constexpr (j() <= 4) f(j, std::true_type{}, std::false_type{});
+    };
+    switch (pieces) {
+    case 1: return layout(std::integral_constant<int, 1>{});
+    case 2: return layout(std::integral_constant<int, 2>{});
+    case 4: return layout(std::integral_constant<int, 4>{});
+    default: return layout(std::integral_constant<int, 8>{});
+    }
+}
+
+template <class E, bool kSilu>
+void position_forward(const esrnn_group_norm_shape &s, Norm a, const Way &w, bool aligned, hipStream_t st)
+{
+    const bool quads = aligned && a.D % 4 == 0;
+    a.tile = position_floats(s, w, quads);
+    with_pieces(w.pieces, aligned, quads, [&](auto j, auto al, auto q) {
+        norm_position_forward_kernel<E, al(), q(), j(), kSilu><<<w.forward_groups, 256, 16 * a.tile, st>>>(a);
+    });
+}
+
+template <class E, bool kSilu>
+void position_backward(const esrnn_group_norm_shape &s, Norm a, const Way &w, bool aligned, hipStream_t st)
+{
+    const bool quads = aligned && a.D % 4 == 0;
+    a.tile = position_floats(s, w, quads);
+    with_pieces(w.pieces, aligned, quads, [&](auto j, auto al, auto q) {
+        norm_position_backward_kernel<E, al(), q(), j(), kSilu><<<w.backward_groups, 256, std::max(16 * a.tile, 8 * a.C), st>>>(a);
+    });
+}
+
+// The sums over `rows` rows at parts; `more`: room for kRuns rows.
+void sum_rows(const Norm &a, int rows, float *more, hipStream_t st)
+{
+    const unsigned tiles = (a.C + 63) / 64;
+    if (rows >= kManyRows) {
+        norm_sum_rows_kernel<<<dim3(tiles, 2, kRuns), 1024, 0, st>>>(a.parts, rows, a.C, more, more + a.C);
+        norm_sum_rows_kernel<<<dim3(tiles, 2, 1), 1024, 0, st>>>(more, kRuns, a.C, a.grad_shift, a.grad_scale);
+    } else {
+        norm_sum_rows_kernel<<<dim3(tiles, 2, 1), 1024, 0, st>>>(a.parts, rows, a.C, a.grad_shift, a.grad_scale);
+    }
+}
+
+// The workspace: channel sums [part_rows][2][C] of the reverse pass (of the stream way's forward pass: moments), statistics or group sums
+// [N][G][2] of the stream way, runs of channel sums.
+size_t groups_at(const esrnn_group_norm_shape &s, const Way &w) { return (size_t)w.part_rows * 2 * s.C; }
+size_t runs_at(const esrnn_group_norm_shape &s, const Way &w) { return groups_at(s, w) + (w.kind == kStream ? (size_t)s.N * s.G * 2 : 0); }
+
+}  // namespace
+
+size_t group_norm_workspace_floats(const esrnn_group_norm_shape &s)
+{
+    const Way w = way_of(s);
+    return runs_at(s, w) + (w.part_rows >= kManyRows ? (size_t)kRuns * 2 * s.C : 0);
+}
+
+hipError_t launch_group_norm_forward(const esrnn_group_norm_shape &s, const GroupNormArgs &f, hipStream_t st)
+{
+    const Way w = way_of(s);
+    Norm a = norm_of(s, f, w);
+    const size_t group = 4 * element_bytes(s.dtype);
+    const bool aligned = s.C % 4 == 0 && aligned_to(f.x, group) && aligned_to(f.out, group);
+    return with_element(s.dtype, [&](auto e) {
+        using E = decltype(e);
+        with_flags(aligned && (w.kind != kSample || w.tile % 4 == 0), a.silu, [&](auto al, auto silu) {
+            if (w.kind == kPosition) {
+                position_forward<E, silu()>(s, a, w, aligned, st);
+                return;
+            }
+            if (w.kind == kSample) {
+                const unsigned grid = (unsigned)(s.N * w.tiles);
+                if (w.threads == 256 && w.rows_each == 4) norm_sample_forward_kernel<E, al(), 256, 4, silu()><<<grid, 256, 0, st>>>(a);
+                else if (w.threads == 256) norm_sample_forward_kernel<E, al(), 256, 16, silu()><<<grid, 256, 0, st>>>(a);
+                else if (w.rows_each == 4) norm_sample_forward_kernel<E, al(), 1024, 4, silu()><<<grid, 1024, 0, st>>>(a);
+                else norm_sample_forward_kernel<E, al(), 1024, 16, silu()><<<grid, 1024, 0, st>>>(a);
+                return;
+            }
+            if (!a.stats) a.stats = a.parts + groups_at(s, w);
+            const dim3 grid((unsigned)(s.N * w.tiles), w.chunks);
+            norm_moments_kernel<E, al()><<<grid, 256, 0, st>>>(a);
+            norm_stats_kernel<<<(unsigned)(s.N * s.G), 64, 0, st>>>(a);
+            norm_apply_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
+        });
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_group_norm_backward(const esrnn_group_norm_shape &s, const GroupNormArgs &f, hipStream_t st)
+{
+    const Way w = way_of(s);
+    const Norm a = norm_of(s, f, w);
+    const size_t group = 4 * element_bytes(s.dtype);
+    const bool aligned = s.C % 4 == 0 && aligned_to(f.x, group) && aligned_to(f.grad_out, group) && aligned_to(f.grad_x, group);
+    return with_element(s.dtype, [&](auto e) {
+        using E = decltype(e);
+        with_flags(aligned && (w.kind != kSample || w.tile % 4 == 0), a.silu, [&](auto al, auto silu) {
+            float *runs = a.parts + runs_at(s, w);
+            if (w.kind == kPosition) {
+                position_backward<E, silu()>(s, a, w, aligned, st);
+                sum_rows(a, w.part_rows, runs, st);
+                return;
+            }
+            if (w.kind == kSample) {
+                const unsigned grid = (unsigned)(s.N * w.tiles);
+                if (w.threads == 256 && w.rows_each == 4) norm_sample_backward_kernel<E, al(), 256, 4, silu()><<<grid, 256, 0, st>>>(a);
+                else if (w.threads == 256) norm_sample_backward_kernel<E, al(), 256, 16, silu()><<<grid, 256, 0, st>>>(a);
+                else if (w.rows_each == 4) norm_sample_backward_kernel<E, al(), 1024, 4, silu()><<<grid, 1024, 0, st>>>(a);
+                else norm_sample_backward_kernel<E, al(), 1024, 16, silu()><<<grid, 1024, 0, st>>>(a);
+                sum_rows(a, w.part_rows, runs, st);
+                return;
+            }
+            const dim3 grid((unsigned)(s.N * w.tiles), w.chunks);
+            norm_gradient_sums_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
+            norm_group_sums_kernel<<<(unsigned)(s.N * s.G), 64, 0, st>>>(a);
+            sum_rows(a, w.part_rows, runs, st);
+            norm_gradient_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
+        });
+        return hipGetLastError();
+    });
+}
+
+}  // namespace esrnn

@@ -115,4 +115,44 @@ struct RecurrenceStep {
 };
 hipError_t launch_recurrence_step(int kind, int dtype, const RecurrenceStep &a, hipStream_t st);
 
+// ---- AdamW over many tensors (adamw_kernels.hip) ----
+constexpr int kAdamWChunk = 2048, kAdamWNormBlocks = 256, kAdamWEntriesAtOnce = 56;
+struct AdamWEntry {
+    float *param;
+    const void *grad;
+    void *copy;
+    long long n, flat;          // elements; where the tensor begins in the moments
+    float weight_decay;
+    int first_chunk;
+    unsigned char grad_dtype, copy_dtype, aligned;      // aligned: every group of four elements is at a multiple of its size
+};
+struct AdamWUpdate {
+    const AdamWEntry *entries;
+    const int *owner;           // tensor of every chunk
+    const double *partial;      // sums of squares, or null without clipping
+    int n_partial;
+    float lr, beta1, new1, beta2, new2, eps, clip_norm;     // new1 = 1 - beta1, new2 = 1 - beta2
+    float rate, root_correction;        // lr / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
+    unsigned key;               // of the random bits
+    void *m;
+    float *v;
+    void *r;
+    float *m_scale, *r_scale, *norm;
+};
+hipError_t launch_adamw_bind(const AdamWEntry *host, int count, AdamWEntry *entries, int *owner, int chunks, hipStream_t st);
+hipError_t launch_adamw_update(AdamWUpdate u, int chunks, double *partial, int state_bits, hipStream_t st);
+
+// ---- group norm + activation (group_norm_kernels.hip) ----
+struct GroupNormArgs {
+    const void *x, *grad_out;
+    const int32_t *lengths;
+    const float *scale, *shift, *stats_in;
+    void *out, *grad_x;
+    float *stats, *grad_scale, *grad_shift;
+    float *parts;               // the workspace
+};
+size_t group_norm_workspace_floats(const esrnn_group_norm_shape &s);
+hipError_t launch_group_norm_forward(const esrnn_group_norm_shape &s, const GroupNormArgs &a, hipStream_t st);
+hipError_t launch_group_norm_backward(const esrnn_group_norm_shape &s, const GroupNormArgs &a, hipStream_t st);
+
 }  // namespace esrnn

@@ -23,6 +23,19 @@ class RecurrenceShape(C.Structure):
                                            "grad_gate_stride")]
 
 
+class GroupNormShape(C.Structure):
+    _fields_ = [(name, C.c_int32) for name in ("N", "T", "C", "G", "activation", "dtype")] + [("eps", C.c_float)]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("weight_decay", C.c_float),
+                ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32)]
+
+
+class AdamWConfig(C.Structure):
+    _fields_ = [(name, C.c_double) for name in ("lr", "beta1", "beta2", "eps", "clip_norm")] + [("seed", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -40,6 +53,15 @@ def _library():
         "esrnn_recurrence_forward": [rs] + [vp] * 9,
         "esrnn_recurrence_backward": [rs] + [vp] * 11,
         "esrnn_recurrence_step": [i32] * 5 + [vp, i64, vp, i64, vp, vp, vp, i64, vp],
+        "esrnn_group_norm_workspace_bytes": [C.POINTER(GroupNormShape), size],
+        "esrnn_group_norm_forward": [C.POINTER(GroupNormShape)] + [vp] * 8,
+        "esrnn_group_norm_backward": [C.POINTER(GroupNormShape)] + [vp] * 11,
+        "esrnn_adamw_create": [C.POINTER(AdamWTensor), i32, i32, C.POINTER(vp)],
+        "esrnn_adamw_destroy": [vp],
+        "esrnn_adamw_state_elements": [vp, size],
+        "esrnn_adamw_workspace_bytes": [vp, size],
+        "esrnn_adamw_bind": [vp, vp, vp],
+        "esrnn_adamw_update": [vp, C.POINTER(AdamWConfig), i32] + [vp] * 8,
     }.items():
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, C.c_int
@@ -195,3 +217,119 @@ def recurrence_step(x, gate, state, out, slots=None, kind: str = "smooth", strea
         gate.stride(0), _check_optional(slots, "slots", x.shape[:1], torch.int32, device),
         _check(state, "state", torch.Size((state.shape[0], channels)), torch.float32, device), out.data_ptr(), out.stride(0),
         _stream(stream, device)), "esrnn_recurrence_step")
+
+
+class GroupNorm:
+    """Group norm with activation over x [N, T, C], channels last: `groups` groups of neighbouring channels, statistics over the positions
+    of a sample and a group's channels (T = 1: every position by itself), then scale and shift [C] float32, then "silu" or "none".
+    lengths: int32 [N], positions that exist, or None.  Owns out, the gradients and what the reverse pass needs."""
+
+    def __init__(self, N: int, T: int, C_: int, groups: int, activation: str = "silu", eps: float = 1e-5, dtype=None,
+                 training: bool = True, device="cuda"):
+        import torch
+        dtype = torch.float32 if dtype is None else dtype
+        self.device, self.dtype, self.training = _cuda(device), dtype, training
+        self._lib = _library()
+        self._shape = GroupNormShape(int(N), int(T), int(C_), int(groups), _choice(ACTIVATIONS, activation, "activation"), _dtype(dtype),
+                                     float(eps))
+        self._ref = C.byref(self._shape)
+        self.workspace = torch.empty(_bytes(self._lib.esrnn_group_norm_workspace_bytes, self._ref), dtype=torch.uint8, device=self.device)
+        self._size, self._channels, self._samples = torch.Size((N, T, C_)), torch.Size((C_,)), torch.Size((N,))
+        self.out = torch.empty(self._size, dtype=dtype, device=self.device)
+        self._forward_done = False
+        if training:
+            self.stats = torch.empty((N, groups, 2), dtype=torch.float32, device=self.device)
+            self.grad_x = torch.empty(self._size, dtype=dtype, device=self.device)
+            self.grad_scale, self.grad_shift = (torch.empty(C_, dtype=torch.float32, device=self.device) for _ in range(2))
+
+    def _given(self, x, scale, shift, lengths):
+        import torch
+        f = torch.float32
+        return (_check(x, "x", self._size, self.dtype, self.device), _check_optional(lengths, "lengths", self._samples, torch.int32, self.device),
+                _check(scale, "scale", self._channels, f, self.device), _check(shift, "shift", self._channels, f, self.device))
+
+    def forward(self, x, scale, shift, lengths=None, stream=None):
+        """out, zero past the lengths."""
+        _raise(self._lib.esrnn_group_norm_forward(
+            self._ref, *self._given(x, scale, shift, lengths), self.out.data_ptr(), self.stats.data_ptr() if self.training else None,
+            self.workspace.data_ptr(), _stream(stream, self.device)), "esrnn_group_norm_forward")
+        self._forward_done = True
+        return self.out
+
+    def backward(self, x, scale, shift, grad_out, lengths=None, stream=None):
+        """(grad_x, grad_scale, grad_shift) for the forward pass last run, which had the same x, scale, shift and lengths."""
+        if not self.training or not self._forward_done:
+            raise EsrnnError(4, "GroupNorm.backward")
+        _raise(self._lib.esrnn_group_norm_backward(
+            self._ref, *self._given(x, scale, shift, lengths), self.stats.data_ptr(),
+            _check(grad_out, "grad_out", self._size, self.dtype, self.device), self.grad_x.data_ptr(), self.grad_scale.data_ptr(),
+            self.grad_shift.data_ptr(), self.workspace.data_ptr(), _stream(stream, self.device)), "esrnn_group_norm_backward")
+        return self.grad_x, self.grad_scale, self.grad_shift
+
+
+class AdamW:
+    """One AdamW update of many tensors at once: params float32, grads float32, bfloat16 or float16 tensors of the same sizes whose
+    contents the caller renews in place, optionally copies (bfloat16 or float16) that get the updated parameters.  weight_decay:
+    one number, or one for each tensor.  clip_norm > 0 clips the gradient by its global norm, leaves the norm in grad_norm, and
+    changes nothing where the norm is not finite.
+
+    state_bits 32: m, v float32.  8: m and r = sqrt(v) float8_e4m3fn in units of m_scale, r_scale (float32, one for 256
+    elements), rounded at random with seed.  All flat, a tensor's elements from a multiple of 256 on (offsets), zero at the start.
+    The tensors are kept referenced; lr and the other hyper-parameters are plain attributes and may change between steps."""
+
+    def __init__(self, params: Sequence, grads: Sequence, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                 weight_decay=0.01, clip_norm: float = 0.0, state_bits: int = 32, seed: int = 0, copies: Optional[Sequence] = None):
+        import torch
+        self._handle = None
+        params, grads = list(params), list(grads)
+        copies = [None] * len(params) if copies is None else list(copies)
+        decays = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(params)
+        if not params or len({len(params), len(grads), len(copies), len(decays)}) != 1:
+            raise ValueError("params, grads, copies and weight decays have to be lists of the same length, at least one")
+        self.device = _cuda(params[0].device)
+        table = (AdamWTensor * len(params))()
+        self.offsets, at = [], 0
+        for i, (p, g, c, d) in enumerate(zip(params, grads, copies, decays)):
+            e = table[i]
+            e.param = _check(p, f"params[{i}]", p.shape, torch.float32, self.device)
+            e.grad, e.grad_dtype = _check(g, f"grads[{i}]", p.shape, g.dtype, self.device), _dtype(g.dtype)
+            if c is not None:
+                e.copy, e.copy_dtype = _check(c, f"copies[{i}]", p.shape, c.dtype, self.device), _dtype(c.dtype)
+            e.n, e.weight_decay = p.numel(), float(d)
+            self.offsets.append(at)
+            at += -(-p.numel() // ADAMW_BLOCK) * ADAMW_BLOCK
+        self._lib, self._tensors = _library(), (params, grads, copies)
+        handle = C.c_void_p()
+        _raise(self._lib.esrnn_adamw_create(table, len(params), int(state_bits), C.byref(handle)), "esrnn_adamw_create")
+        self._handle = handle
+        n = _bytes(self._lib.esrnn_adamw_state_elements, handle)
+        assert n == at
+        zeros = lambda size, dtype: torch.zeros(size, dtype=dtype, device=self.device)  # noqa: E731
+        self.v = self.r = self.m_scale = self.r_scale = None
+        if state_bits == 32:
+            self.m, self.v = zeros(n, torch.float32), zeros(n, torch.float32)
+        else:
+            self.m, self.r = (zeros(n, torch.uint8).view(torch.float8_e4m3fn) for _ in range(2))
+            self.m_scale, self.r_scale = zeros(n // ADAMW_BLOCK, torch.float32), zeros(n // ADAMW_BLOCK, torch.float32)
+        self.grad_norm = zeros(1, torch.float32)
+        self.workspace = torch.empty(_bytes(self._lib.esrnn_adamw_workspace_bytes, handle), dtype=torch.uint8, device=self.device)
+        self.lr, self.beta1, self.beta2, self.eps, self.clip_norm, self.seed = lr, beta1, beta2, eps, clip_norm, int(seed)
+        self._states = [None if t is None else t.data_ptr() for t in (self.m, self.v, self.r, self.m_scale, self.r_scale, self.grad_norm,
+                                                                      self.workspace)]
+        _raise(self._lib.esrnn_adamw_bind(handle, self._states[-1], _stream(None, self.device)), "esrnn_adamw_bind")
+
+    def step(self, step: int, stream=None) -> None:
+        """Update number `step`, from 1 on.  (The first one on another stream than the constructor's has to be ordered behind it.)"""
+        if self._handle is None:
+            raise EsrnnError(1, "AdamW.step after close")
+        opt = AdamWConfig(self.lr, self.beta1, self.beta2, self.eps, self.clip_norm, self.seed & 0xFFFFFFFF)
+        _raise(self._lib.esrnn_adamw_update(self._handle, C.byref(opt), int(step), *self._states, _stream(stream, self.device)),
+               "esrnn_adamw_update")
+
+    def close(self) -> None:
+        if self._handle is not None:
+            self._lib.esrnn_adamw_destroy(self._handle)
+            self._handle = None
+
+    def __del__(self):
+        self.close()

@@ -1,0 +1,294 @@
+"""AdamW over many tensors on the GPU against its formulas in 64 bits (numpy)."""
+import numpy as np
+import pytest
+
+from paper_1907_03329_amd import layers
+
+pytestmark = pytest.mark.gpu
+
+BLOCK = 256
+OPT = dict(lr=1e-2, beta1=0.9, beta2=0.99, eps=1e-8)
+SIZES = [1, 2, 3, 255, 256, 257, 2047, 2048, 2049, 5000, 70001, 64, 12]
+# One step in fp32: a parameter is off by a rounding of itself (2^-24) and by some 2^-22 of its change; moments by a few 2^-24 of the
+# terms they are made of.  Against the largest value of the array, 1e-6.
+ARITHMETIC = 1e-6
+
+
+def f32(x):
+    return np.asarray(x, dtype=np.float32).astype(np.float64)
+
+
+def rule(p, g, m, v, step, lr, beta1, beta2, eps, decay, factor=1.0):
+    """float64."""
+    g = g * factor
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * g * g
+    p = p * (1 - lr * decay) - lr * (m / (1 - beta1 ** step)) / (np.sqrt(v / (1 - beta2 ** step)) + eps)
+    return p, m, v
+
+
+def close(got, want, what="", tolerance=ARITHMETIC):
+    got = got.double().cpu().numpy().ravel()
+    assert np.abs(got - np.ravel(want)).max() <= tolerance * max(np.abs(want).max(), 1e-30), (what, np.abs(got - np.ravel(want)).max())
+
+
+def problem(rng, sizes, grad="float32", off=0, spread=1.0):
+    """Parameters and gradients as separate tensors, `off` elements behind a place that wide accesses like; float64 copies."""
+    import torch
+    params, grads, ref = [], [], []
+    for n in sizes:
+        p = torch.from_numpy(rng.normal(0, 0.5, n)).float()
+        g = torch.from_numpy(rng.normal(0, 0.1, n) * np.exp(rng.normal(0, spread, n))).to(getattr(torch, grad))
+        at = [torch.zeros(n + off, dtype=t.dtype, device="cuda")[off:] for t in (p, g)]
+        at[0].copy_(p)
+        at[1].copy_(g)
+        params.append(at[0])
+        grads.append(at[1])
+        ref.append((p.double().numpy(), g.double().numpy()))
+    return params, grads, ref
+
+
+def ranges(opt, sizes):
+    return [slice(o, o + n) for o, n in zip(opt.offsets, sizes)]
+
+
+@pytest.mark.parametrize("grad", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("off", [0, 1, 2, 4])
+@pytest.mark.parametrize("clip", [0.0, 0.5, 1e6])
+def test_three_steps(grad, off, clip):
+    import torch
+    rng = np.random.default_rng(off)
+    params, grads, ref = problem(rng, SIZES, grad, off)
+    copies = [torch.full((n,), float("nan"), dtype=torch.bfloat16 if i % 2 else torch.float16, device="cuda") if i % 3 else None
+              for i, n in enumerate(SIZES)]
+    decays = [0.1 * (i % 3) for i in range(len(SIZES))]
+    opt = layers.AdamW(params, grads, weight_decay=decays, clip_norm=clip, copies=copies, **OPT)
+    state = [(p, np.zeros_like(p), np.zeros_like(p)) for p, _ in ref]
+    for step in (1, 2, 3):
+        if step > 1:        # new gradients where the old ones were
+            for g, (p, old) in zip(grads, ref):
+                g.mul_(-0.5)
+            ref = [(p, g.double().cpu().numpy()) for g, (p, _) in zip(grads, ref)]
+        opt.step(step)
+        norm = np.sqrt(sum((g ** 2).sum() for _, g in ref))
+        factor = min(1.0, clip / (norm + 1e-6)) if clip > 0 else 1.0
+        state = [rule(p, g, m, v, step, decay=d, factor=factor, **OPT) for (p, m, v), (_, g), d in zip(state, ref, decays)]
+        if clip > 0:
+            assert abs(float(opt.grad_norm) - norm) <= 1e-6 * norm
+    for i, (p, r, (wp, wm, wv)) in enumerate(zip(params, ranges(opt, SIZES), state)):
+        close(p, wp, ("param", i))
+        close(opt.m[r], wm, ("m", i))
+        close(opt.v[r], wv, ("v", i))
+        if copies[i] is not None:
+            assert torch.equal(copies[i], p.to(copies[i].dtype))
+    inside = torch.zeros(opt.m.numel(), dtype=torch.bool, device="cuda")
+    for r in ranges(opt, SIZES):
+        inside[r] = True
+    assert not opt.m[~inside].any() and not opt.v[~inside].any()
+
+
+def test_large_steps_keep_the_bias_correction():
+    """1 - beta^step for beta near one and steps from 1 to a million."""
+    import torch
+    for step in (1, 2, 1000, 10 ** 6):
+        p, g = torch.ones(300, device="cuda"), torch.full((300,), 0.3, device="cuda")
+        opt = layers.AdamW([p], [g], lr=1e-2, beta1=0.9, beta2=0.9999, eps=1e-8, weight_decay=0.0)
+        opt.step(step)
+        want = rule(np.ones(300), f32(np.full(300, 0.3)), 0.0, 0.0, step, 1e-2, 0.9, 0.9999, 1e-8, 0.0)
+        close(1.0 - p, 1.0 - want[0], step, 1e-5)
+
+
+def random_words(place, seed, step):
+    mask = 0xFFFFFFFF
+    key = (seed * 0x9E3779B1 + step * 0x85EBCA77) & mask
+    w = place.astype(np.uint64)
+    w = (w & mask) ^ ((w >> np.uint64(32)) * np.uint64(0xC2B2AE35) & np.uint64(mask)) ^ np.uint64(key)
+    w = (w ^ (w >> np.uint64(16))) * np.uint64(0x7FEB352D) & np.uint64(mask)
+    w = (w ^ (w >> np.uint64(15))) * np.uint64(0x846CA68B) & np.uint64(mask)
+    return w ^ (w >> np.uint64(16))
+
+
+def quantised(x, bits16, never_zero):
+    """The two e4m3 neighbours of each magnitude in units of its block's scale, and which one the random bits choose (float64)."""
+    blocks = np.pad(np.abs(x), (0, -len(x) % BLOCK)).reshape(-1, BLOCK)
+    scale = f32(f32(blocks.max(1)) / np.float32(448.0))
+    y = np.abs(x) / np.repeat(np.where(scale > 0, scale, 1.0), BLOCK)[:len(x)]
+    ulp = np.exp2(np.floor(np.log2(np.maximum(y, 2.0 ** -6))) - 3)
+    low = np.floor(y / ulp) * ulp
+    q = np.floor(y / ulp + bits16 / 65536.0) * ulp
+    if never_zero:
+        q = np.where((q == 0) & (y > 0), 2.0 ** -9, q)
+    return q * np.sign(x), low, low + ulp, scale
+
+
+@pytest.mark.parametrize("off,grad", [(0, "float32"), (3, "bfloat16")])
+@pytest.mark.parametrize("clip", [0.0, 0.5])
+def test_moments_in_8_bits(off, grad, clip):
+    import torch
+    rng = np.random.default_rng(3 + off)
+    params, grads, ref = problem(rng, SIZES, grad, off, spread=2.0)
+    opt = layers.AdamW(params, grads, weight_decay=0.05, clip_norm=clip, state_bits=8, seed=77, **OPT)
+    norm = np.sqrt(sum((g ** 2).sum() for _, g in ref))
+    factor = min(1.0, clip / (norm + 1e-6)) if clip else 1.0
+    state = [(p, np.zeros_like(p), np.zeros_like(p)) for p, _ in ref]
+    for step in (1, 2, 3):
+        opt.step(step)
+        for i, ((p, m, v), (_, g), r) in enumerate(zip(state, ref, ranges(opt, SIZES))):
+            p, m, v = rule(p, g, m, v, step, decay=0.05, factor=factor, **OPT)
+            close(params[i], p, ("param", i, step))
+            w = random_words(np.arange(r.start, r.stop), 77, step)
+            got = []
+            for x, bits, codes, scales, never_zero in ((m, w >> np.uint64(16), opt.m, opt.m_scale, False),
+                                                       (np.sqrt(v), w & np.uint64(0xFFFF), opt.r, opt.r_scale, True)):
+                want, low, high, scale = quantised(x, bits.astype(np.float64), never_zero)
+                here = scales[r.start // BLOCK:-(-r.stop // BLOCK)].double().cpu().numpy()
+                assert np.abs(here - scale).max() <= 1e-6 * scale.max()
+                q = codes[r].float().double().cpu().numpy()
+                # one of the two neighbours, and the one that the random bits choose but where fp32 rounding tips the scale: a part in
+                # 1e5 of the elements (the bits decide at 2^-16 of a code, which fp32 places to 2^-20)
+                assert ((np.abs(np.abs(q) - low) <= 1e-12) | (np.abs(np.abs(q) - high) <= 1e-12) | (np.abs(np.abs(q) - 2.0 ** -9) < 1e-12)).mean() >= 1 - 1e-3
+                assert (np.abs(q - want) > 1e-12).sum() <= 1 + 1e-3 * len(q)
+                got.append(q * np.repeat(here, BLOCK)[:len(q)])
+            state[i] = (params[i].double().cpu().numpy(), got[0], got[1] ** 2)
+
+
+def test_rounding_keeps_the_mean():
+    """Moments of a constant gradient, many steps: the averages follow theirs, where rounding to nearest would stand still; the
+    standard error of the mean over 200 000 elements with a spacing of at most an eighth is below 1e-3."""
+    import torch
+    n = 200000
+    p, g = torch.zeros(n, device="cuda"), torch.full((n,), 1.0, device="cuda")
+    g[::256] = 4.0      # the largest of each block
+    opt = layers.AdamW([p], [g], state_bits=8, seed=5, weight_decay=0.0, lr=0.0, beta1=0.9, beta2=0.99, eps=1e-8)
+    others = torch.arange(n, device="cuda") % 256 != 0
+    for step in range(1, 61):
+        opt.step(step)
+    m = opt.m.float() * opt.m_scale.repeat_interleave(BLOCK)
+    r = opt.r.float() * opt.r_scale.repeat_interleave(BLOCK)
+    m, r = m[:n][others], r[:n][others]
+    assert abs(float(m.mean()) - (1 - 0.9 ** 60)) <= 5e-3
+    # the square root is rounded, so v = r^2 gains the variance of its rounding at every step: at most (1/16)^2 / 4 of it, of which
+    # 1 / (1 - beta2) steps are remembered, and it takes no part in less than that
+    assert 0.97 <= float((r.square().mean() / (1 - 0.99 ** 60)).sqrt()) <= 1.06
+
+
+def test_equal_steps_are_equal_and_seeds_matter():
+    import torch
+    results = []
+    for seed in (1, 1, 2):
+        rng = np.random.default_rng(9)
+        params, grads, _ = problem(rng, [3000, 77])
+        opt = layers.AdamW(params, grads, state_bits=8, seed=seed, **OPT)
+        for step in (1, 2):
+            opt.step(step)
+        results.append((opt.m.view(torch.uint8).clone(), opt.r.view(torch.uint8).clone(), params[0].clone()))
+    assert all(torch.equal(a, b) for a, b in zip(results[0], results[1]))
+    assert not torch.equal(results[0][0], results[2][0])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_gradient_that_is_not_finite(bits, bad):
+    import torch
+    rng = np.random.default_rng(10)
+    params, grads, _ = problem(rng, [3000, 500])
+    opt = layers.AdamW(params, grads, state_bits=bits, clip_norm=1.0, **OPT)
+    opt.step(1)
+    states = [t for t in (opt.m, opt.v, opt.r, opt.m_scale, opt.r_scale) if t is not None]
+    before = [t.view(torch.uint8).clone() for t in states + params]
+    grads[0][700] = bad
+    opt.step(2)             # with clipping: nothing changes
+    assert all(torch.equal(a, t.view(torch.uint8)) for a, t in zip(before, states + params))
+    assert not bool(torch.isfinite(opt.grad_norm))
+    opt.clip_norm = 0.0
+    opt.step(2)             # without: the element, in 8 bits later its block
+    grads[0][700] = 0.0
+    opt.step(3)
+    broken = ~torch.isfinite(params[0])
+    assert bool(broken[700]) and bool(torch.isfinite(params[1]).all())
+    assert int(broken.sum()) == (1 if bits == 32 else BLOCK)
+    assert bits == 32 or bool(broken[512:768].all())
+
+
+def test_gradients_that_are_zero():
+    """Nothing but the decay, and no division of zero by zero."""
+    import torch
+    for bits in (32, 8):
+        p, g = torch.ones(300, device="cuda"), torch.zeros(300, device="cuda")
+        opt = layers.AdamW([p], [g], state_bits=bits, lr=0.1, weight_decay=0.5, clip_norm=1.0)
+        opt.step(1)
+        close(p, np.full(300, 0.95))
+        assert float(opt.grad_norm) == 0.0
+
+
+def test_norm_of_very_large_gradients():
+    import torch
+    p, g = torch.zeros(1000, device="cuda"), torch.full((1000,), 1e25, device="cuda")
+    opt = layers.AdamW([p], [g], lr=0.1, weight_decay=0.0, clip_norm=1.0)
+    opt.step(1)
+    assert abs(float(opt.grad_norm) / (1e25 * 1000 ** 0.5) - 1) <= 1e-5
+    close(p, np.full(1000, -0.1), "", 1e-4)
+
+
+def test_many_tensors_streams_and_graphs():
+    """More tensors than one launch carries to the device; the same steps eagerly, on another stream and replayed."""
+    import torch
+    sizes = [1 + 37 * i % 700 for i in range(300)]
+    results = []
+    side = torch.cuda.Stream()
+    for how in ("eager", "stream", "graph"):
+        rng = np.random.default_rng(12)
+        params, grads, ref = problem(rng, sizes)
+        opt = layers.AdamW(params, grads, weight_decay=0.1, clip_norm=0.1, **OPT)
+        side.wait_stream(torch.cuda.current_stream())
+        if how == "graph":
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                opt.step(1)
+        for _ in range(3):
+            if how == "graph":
+                graph.replay()
+            else:
+                opt.step(1, stream=side if how == "stream" else None)
+            torch.cuda.synchronize()
+            assert torch.ones(5, device="cuda").sum() == 5
+        results.append([t.clone() for t in params] + [opt.m.clone(), opt.v.clone()])
+    assert all(torch.equal(a, b) for a, b in zip(results[0], results[1]))
+    assert all(torch.equal(a, b) for a, b in zip(results[0], results[2]))
+    factor = 0.1 / (np.sqrt(sum((g ** 2).sum() for _, g in ref)) + 1e-6)
+    for i in (0, 57, 299):
+        p, m, v = ref[i][0], 0.0, 0.0
+        for _ in range(3):
+            p, m, v = rule(p, ref[i][1], m, v, 1, decay=0.1, factor=factor, **OPT)
+        close(results[0][i], p, i, 3 * ARITHMETIC)
+
+
+def test_refusals():
+    import torch
+    from paper_1907_03329_amd.binding import EsrnnError
+    p, g = torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda")
+    for params, grads in (([], []), ([p], []), ([p.half()], [g]), ([p], [g[:4]]), ([p], [g.cpu()]), ([p], [g.double()]),
+                          ([torch.zeros(4, 4, device="cuda").t()], [torch.zeros(4, 4, device="cuda")])):
+        with pytest.raises(ValueError):
+            layers.AdamW(params, grads)
+    with pytest.raises(ValueError):
+        layers.AdamW([p], [g], weight_decay=[0.1, 0.2])
+    for kw in (dict(state_bits=4), dict(weight_decay=-1.0), dict(weight_decay=float("nan")), dict(copies=[torch.zeros(8, device="cuda")])):
+        with pytest.raises(EsrnnError):
+            layers.AdamW([p], [g], **kw)
+    with pytest.raises(EsrnnError):
+        layers.AdamW([p[:0]], [g[:0]])
+    opt = layers.AdamW([p], [g])
+    for step, kw in ((0, {}), (1, dict(beta1=1.0)), (1, dict(beta2=-0.1)), (1, dict(lr=float("nan"))), (1, dict(eps=-1.0)), (1, dict(clip_norm=float("nan")))):
+        before = {k: getattr(opt, k) for k in kw}
+        for k, v in kw.items():
+            setattr(opt, k, v)
+        with pytest.raises(EsrnnError) as e:
+            opt.step(step)
+        assert e.value.status == 2
+        for k, v in before.items():
+            setattr(opt, k, v)
+    opt.step(1)
+    opt.close()
+    with pytest.raises(EsrnnError):
+        opt.step(2)
