@@ -78,7 +78,7 @@ esrnn_status esrnn_recurrence_workspace_bytes(const esrnn_recurrence_shape *shap
     if (!recurrence_sizes(*shape)) return ESRNN_ERR_CONFIG;
     const RecurrencePlan p = recurrence_plan(*shape);
     // at least something to allocate
-    *bytes = p.segments > 1 ? (size_t)shape->B * p.segments * 2 * shape->C * sizeof(float) : 256;
+    *bytes = p.ahead ? p.words * sizeof(float) : 256;
     return ESRNN_OK;
 }
 

@@ -82,9 +82,13 @@ inline bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<u
 inline size_t element_bytes(int dtype) { return dtype == ESRNN_F32 ? 4 : 2; }
 
 // ---- gated linear recurrence (recurrence_kernels.hip) ----
-// Positions of a block, the blocks of a sequence, and how many neighbouring blocks a workgroup takes (a segment).
+// Waves of a workgroup, positions of a block, the blocks of a sequence; ahead: every block has a workgroup of its own, and its maps go
+// through `words` floats of the workspace, by whole groups of 2^log_group blocks too.
 struct RecurrencePlan {
-    int waves, block, blocks, per_segment, segments;
+    int waves, block, blocks;
+    bool ahead;
+    int log_group, groups;
+    size_t words;
 };
 RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s);
 struct RecurrenceForward {
@@ -92,7 +96,7 @@ struct RecurrenceForward {
     const int32_t *lengths;
     const float *initial;
     void *out;
-    float *last, *saved, *parts;
+    float *last, *saved, *words;
 };
 struct RecurrenceBackward {
     const void *x, *gate;
@@ -101,7 +105,7 @@ struct RecurrenceBackward {
     const void *grad_out;
     const float *grad_last;
     void *grad_x, *grad_gate;
-    float *grad_initial, *parts;
+    float *grad_initial, *words;
 };
 hipError_t launch_recurrence_forward(const esrnn_recurrence_shape &s, const RecurrenceForward &a, hipStream_t st);
 hipError_t launch_recurrence_backward(const esrnn_recurrence_shape &s, const RecurrenceBackward &a, hipStream_t st);

@@ -4,9 +4,12 @@
 // together is associative: a sequence is cut into pieces, every piece's map is computed at the same time, and the states between
 // the pieces follow.  Here a thread has kSteps neighbouring positions of four channels in registers, sixteen threads side by side a
 // row of 64 channels, so a wave has four pieces and a block of positions is 4 or 16 of them, put together by shuffles within a wave and
-// through LDS between the waves.  A workgroup takes the blocks of a segment one behind the other with the state in registers.
-// Sequences with few channels in all have several segments, each a workgroup: their maps come first (kMaps, reading x and
-// gate once more), then every workgroup puts together the maps before its own.
+// through LDS between the waves.
+//
+// Many sequences and channels: a workgroup takes all blocks of its 64 channels one behind the other, the state in registers.
+// Few: every block has a workgroup of its own (kAhead), which reads its positions once, hands its map on through memory, and puts together
+// the maps of the blocks before it, which are under way at the same time.  (As two launches, maps first and then x and gate once more, 8
+// sequences of 4096 positions and 2048 channels took 146 us forward and 198 us in reverse.)
 //
 // The reverse pass runs the same maps from the end: mu_t = a_t (d_t + mu_{t+1}), with d the gradient of out.  The states h_{t-1} that the
 // gradient of the gate needs are computed again, in fp32, from the state before the block that the forward pass leaves: reading
@@ -21,6 +24,8 @@ namespace {
 
 constexpr int kSteps = 8;       // positions of a thread
 constexpr int kTile = 64;       // channels of a workgroup
+// rows of 64 channels from which a workgroup takes a whole sequence
+constexpr int kLinesAlone = 1024;
 
 struct Args {
     const void *x, *gate, *grad_out;
@@ -29,8 +34,8 @@ struct Args {
     const int32_t *lengths;
     const float *initial, *saved_in, *grad_last;
     float *last, *saved, *grad_initial;
-    float *parts;               // [B][segments][2][C]: maps of the segments
-    int B, T, C, tiles, blocks, per_segment, segments;
+    float *words;               // kAhead: the ticket (256 bytes), then for each 64 channels of a sequence the maps of its blocks
+    int B, T, C, tiles, blocks, groups, log_group;      // and of their groups of 2^log_group blocks, [blocks + groups][2][64]
 };
 
 __device__ __forceinline__ f32x4 splat(float v) { return f32x4{v, v, v, v}; }
@@ -56,9 +61,9 @@ __device__ __forceinline__ f32x4 shift_down(f32x4 v, int lanes)
     return r;
 }
 
-// The maps of the pieces of a block, one of each thread, in order of time (or against it): what comes in at this thread's piece when
-// `in` comes in at the first, and what comes out of the last.  All threads of the workgroup; `lds` is not written again before
-// the next barrier but one.
+// The maps of the pieces of a block, one of each thread, in order of time (or against it: then the caller counts waves from the last one
+// as well): what comes in at this thread's piece when `carry` comes in at the first, and what comes out of the last.  All threads of the
+// workgroup; `lds` is not written again before the next barrier but one.
 template <int NW, bool kReverse>
 struct Pieces {
     f32x4 A, B;             // of the pieces of this wave before this thread's
@@ -101,8 +106,7 @@ struct Pieces {
         }
         f32x4 h = carry, mine = carry;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            const int w = kReverse ? NW - 1 - i : i;
+        for (int w = 0; w < NW; ++w) {
             if (w == wave) mine = h;
             h = lds[w][0][lane16] * h + lds[w][1][lane16];
         }
@@ -111,28 +115,110 @@ struct Pieces {
     }
 };
 
-// The state behind the segments first .. end - 1 (kReverse: before them, from the last to the first) that `in` enters: their maps are dealt to the
-// threads' rows in runs of neighbours and put together like the pieces of a block.
-template <int NW, bool kReverse, bool kAligned>
-__device__ __forceinline__ f32x4 through_segments(const float *parts, int C, int first, int end, f32x4 in, const Channels<kAligned, 16> &ch,
-                                                  f32x4 (*lds)[2][16], int wave, int row, int lane16)
+// Maps that pass from workgroup to workgroup.
+//
+// They are written through to memory and read past the caches, and every float tells by itself whether it is there: the words are
+// filled with kEmpty before the launch (no result has this pattern, one of the NaNs).  Which maps a block puts together, and how, depends on
+// its number alone: those of the whole groups before its own, then those of the blocks before it in its group; the last block of a group
+// hands on the group's map, and waits for no other group for that.  So results do not depend on who was first, a block waits for two
+// others one behind the other at most, and reads 2 sqrt(blocks) maps at most.
+// Every wait ends: blocks are taken by ticket, in the order in which they follow each other, whoever waits waits for lower tickets only, and
+// a block's own map waits for nobody.  (A wait that goes on for seconds all the same, because calls overlap on one workspace, is given
+// up, once for all this thread reads; its maps are NaN.)
+constexpr unsigned kEmpty = 0xffffffffu;
+constexpr int kMostLooks = 1 << 22, kMap = 128;     // floats of a map
+
+struct Map {
+    f32x4 A, B;
+    __device__ __forceinline__ Map after(const Map &o) const { return {A * o.A, A * o.B + B}; }
+};
+__device__ __forceinline__ bool there(f32x4 v)
 {
-    const int n = end - first, run = (n + 4 * NW - 1) / (4 * NW);
-    const int from = min((wave * 4 + row) * run, n), to = min(from + run, n);
-    f32x4 A = splat(1.0f), B = splat(0.0f);
-    for (int i = from; i < to; ++i) {
-        const float *p = parts + (size_t)(first + (kReverse ? to - 1 - (i - from) : i)) * 2 * C;
-        const f32x4 a = ch.load(p), b = ch.load(p + C);
-        B = a * B + b;
-        A = a * A;
-    }
-    const Pieces<NW, kReverse> pieces(A, B, row, lane16);
-    pieces.leave(lds, wave, row, lane16);
-    if (NW > 1) __syncthreads();
-    (void)pieces.enter(in, lds, wave, lane16);
-    if (NW > 1) __syncthreads();
-    return in;
+    const u32x4 u = __builtin_bit_cast(u32x4, v);
+    return u[0] != kEmpty && u[1] != kEmpty && u[2] != kEmpty && u[3] != kEmpty;
 }
+// The maps of a row of 64 channels: of its blocks, behind them of their groups.  Map i is at 4 i kMap bytes.
+struct Line {
+    buf_rsrc at;
+    int blocks;
+    bool lost = false;
+    __device__ __forceinline__ Line(float *words, int n_blocks, int n_groups) : at(make_rsrc(words, 4 * kMap * (n_blocks + n_groups))), blocks(n_blocks) {}
+
+    __device__ __forceinline__ Map look(int i) const
+    {
+        const unsigned lane_bytes = 4 * kMap * i + 16 * (threadIdx.x & 15);
+        return {__builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(at, lane_bytes, 0, kBufShared)),
+                __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(at, lane_bytes + 256, 0, kBufShared))};
+    }
+    // by the sixteen threads of one row
+    __device__ __forceinline__ void hand_on(int i, const Map &m) const
+    {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f32x4 v = half ? m.B : m.A;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = v[k] != v[k] ? __builtin_nanf("") : v[k];
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), at, 4 * kMap * i + 256 * half + 16 * (threadIdx.x & 15), 0, kBufShared);
+        }
+    }
+    // map i of this thread's row
+    __device__ __forceinline__ Map wait(int i)
+    {
+        asm volatile("" ::: "memory");
+        Map m = look(i);
+        for (int looks = lost ? kMostLooks : 0; !(there(m.A) && there(m.B)); ++looks) {
+            asm volatile("" ::: "memory");
+            if (looks == kMostLooks) {
+                lost = true;
+                break;
+            }
+            __builtin_amdgcn_s_sleep(1);
+            m = look(i);
+        }
+        return lost ? Map{splat(__builtin_nanf("")), splat(__builtin_nanf(""))} : m;
+    }
+    // n maps one behind the other, the first `groups_first` of them of groups, the others of blocks from `block` on: dealt to the rows of
+    // the workgroup in runs of neighbours, which are put together like the pieces of a block.  All threads; `lds` is the call's own.
+    template <int NW>
+    __device__ __forceinline__ Map put_together(int groups_first, int block, int n, f32x4 (*lds)[2][16], int wave, int row, int lane16)
+    {
+        const int run = (n + 4 * NW - 1) / (4 * NW), from = min((wave * 4 + row) * run, n), to = min(from + run, n);
+        Map m{splat(1.0f), splat(0.0f)};
+        for (int j = from; j < to; ++j)
+            m = wait(j < groups_first ? blocks + j : block + j - groups_first).after(m);
+        const Pieces<NW, false> pieces(m.A, m.B, row, lane16);
+        pieces.leave(lds, wave, row, lane16);
+        __syncthreads();
+        return whole<NW>(lds, lane16);
+    }
+    // the map of a whole block from what its waves have left
+    template <int NW>
+    static __device__ __forceinline__ Map whole(const f32x4 (*lds)[2][16], int lane16)
+    {
+        Map m{lds[0][0][lane16], lds[0][1][lane16]};
+#pragma unroll
+        for (int w = 1; w < NW; ++w) m = Map{lds[w][0][lane16], lds[w][1][lane16]}.after(m);
+        return m;
+    }
+    // The state that enters block k of the sequence, if `first` enters the first: hands on the block's map, and the group's.
+    template <int NW>
+    __device__ __forceinline__ f32x4 entering(int k, const Map &own, f32x4 first, int log_group, f32x4 (*lds)[NW][2][16], int wave, int row, int lane16)
+    {
+        const bool writes = wave == 0 && row == 0;
+        if (writes) hand_on(k, own);
+        const int group = k >> log_group, in_group = k & ((1 << log_group) - 1);
+        Map m{splat(1.0f), splat(0.0f)};
+        if (in_group == (1 << log_group) - 1) {
+            m = put_together<NW>(0, group << log_group, in_group, lds[0], wave, row, lane16);
+            if (writes) hand_on(blocks + group, own.after(m));
+            if (group > 0) m = m.after(put_together<NW>(group, 0, group, lds[1], wave, row, lane16));
+        } else if (k > 0) {
+            m = put_together<NW>(group, group << log_group, group + in_group, lds[0], wave, row, lane16);
+        }
+        // (NaN for all threads of the workgroup: what one of them could not wait for has gone through LDS)
+        return m.A * first + m.B;
+    }
+};
 
 template <int kKind>
 __device__ __forceinline__ void maps_of(f32x4 g, f32x4 x, bool inside, f32x4 &a, f32x4 &z, f32x4 &b)
@@ -166,30 +252,49 @@ __device__ __forceinline__ void store_state(float *p, f32x4 v, const Channels<kA
 }
 
 
-// kMaps: the map of every segment but the last, nothing else.
-template <class E, bool kAligned, int kKind, int NW, bool kMaps>
+// What a workgroup works on: a row of 64 channels of a sequence, and with kAhead one of its blocks, drawn by ticket: rows side by side, block for
+// block.
+struct Place {
+    int line, block;
+};
+template <bool kAhead>
+__device__ __forceinline__ Place draw_place(const Args &a)
+{
+    if (!kAhead) return {(int)blockIdx.x, 0};
+    __shared__ unsigned s_ticket;
+    if (threadIdx.x == 0) s_ticket = atomicAdd(reinterpret_cast<unsigned *>(a.words), 1u);
+    __syncthreads();
+    // (in a workspace that another call writes, a ticket is any number: every place has to be in the launch)
+    const unsigned ticket = min((unsigned)__builtin_amdgcn_readfirstlane((int)s_ticket), gridDim.x - 1), lines = (unsigned)(a.B * a.tiles);
+    return {(int)(ticket % lines), (int)(ticket / lines)};
+}
+__device__ __forceinline__ Line line_of(const Args &a, int line)
+{
+    return Line(a.words + 64 + (size_t)line * (a.blocks + a.groups) * kMap, a.blocks, a.groups);
+}
+
+template <class E, bool kAligned, int kKind, int NW, bool kAhead>
 __global__ void __launch_bounds__(64 * NW) recurrence_forward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
     __shared__ f32x4 lds[2][NW][2][16];
+    __shared__ f32x4 lds_ahead[kAhead ? 2 : 1][NW][2][16];
     const int lane16 = threadIdx.x & 15, row = (threadIdx.x >> 4) & 3, wave = threadIdx.x >> 6;
-    const int b = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, segment = blockIdx.y;
+    const Place place = draw_place<kAhead>(a);
+    const int b = place.line / a.tiles, tile = place.line % a.tiles;
     const Channels<kAligned, 16> ch(lane16, tile * kTile, a.C);
     const int length = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-    const int first = segment * a.per_segment, end = min(first + a.per_segment, a.blocks);
     const E *x = static_cast<const E *>(a.x) + b * a.xb, *gate = static_cast<const E *>(a.gate) + b * a.gb;
     E *out = static_cast<E *>(a.out) + b * a.ob;
-    float *parts = a.parts + (size_t)b * a.segments * 2 * a.C;
+    const bool writes = wave == 0 && row == 0;
 
-    f32x4 carry = splat(0.0f), decay = splat(1.0f);
-    if (!kMaps) {
-        if (a.initial) carry = load_state(a.initial + (size_t)b * a.C, ch);
-        if (segment > 0) carry = through_segments<NW, false>(parts, a.C, 0, segment, carry, ch, lds[0], wave, row, lane16);
-    }
-    for (int block = first; block < end; ++block) {
+    f32x4 carry = splat(0.0f);
+    if (a.initial) carry = load_state(a.initial + (size_t)b * a.C, ch);
+    if (length == 0 && place.block == 0 && writes && a.last) store_state(a.last + (size_t)b * a.C, carry, ch);
+    const int end = kAhead ? place.block + 1 : a.blocks;
+    for (int block = place.block; block < end; ++block) {
         const int t0 = block * kBlock + (wave * 4 + row) * kSteps;
         if (block * kBlock >= length) {     // nothing left of the sequence
-            if (kMaps) break;
             for (int i = 0; i < kSteps; ++i)
                 if (t0 + i < a.T) ch.store(out + (t0 + i) * a.ot, Vec4<E>{});
             continue;
@@ -210,108 +315,82 @@ __global__ void __launch_bounds__(64 * NW) recurrence_forward_kernel(Args a)
             A = as[i] * A;
         }
         const Pieces<NW, false> pieces(A, B, row, lane16);
-        auto &shared = lds[block & 1];
+        auto &shared = lds[kAhead ? 0 : block & 1];
         pieces.leave(shared, wave, row, lane16);
         if (NW > 1) __syncthreads();
-        if (!kMaps && a.saved && wave == 0 && row == 0)
-            store_state(a.saved + ((size_t)b * a.blocks + block) * a.C, carry, ch);
-        if (kMaps) {        // the product of all a as well: the map of zero, without what it adds
-            f32x4 factor = pieces.wave_A;
-            if (NW > 1) {
-                factor = splat(1.0f);
-                for (int w = 0; w < NW; ++w) factor = factor * shared[w][0][lane16];
-            }
-            decay = decay * factor;
-        }
+        if constexpr (kAhead)
+            carry = line_of(a, place.line).template entering<NW>(block, Line::whole<NW>(shared, lane16), carry, a.log_group, lds_ahead, wave, row, lane16);
+        if (a.saved && writes) store_state(a.saved + ((size_t)b * a.blocks + block) * a.C, carry, ch);
         f32x4 h = pieces.enter(carry, shared, wave, lane16);
-        if (kMaps) continue;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             h = as[i] * h + bs[i];
             if (t0 + i < a.T) ch.store(out + (t0 + i) * a.ot, from_f32<E>(t0 + i < length ? h : splat(0.0f)));
         }
-    }
-    if (wave != 0 || row != 0) return;
-    if (kMaps) {
-        store_state(parts + (size_t)segment * 2 * a.C, decay, ch);
-        store_state(parts + ((size_t)segment * 2 + 1) * a.C, carry, ch);
-    } else if (a.last && segment == a.segments - 1) {
-        store_state(a.last + (size_t)b * a.C, carry, ch);
+        if (block == (length - 1) / kBlock && writes && a.last) store_state(a.last + (size_t)b * a.C, carry, ch);
     }
 }
 
-// kMaps: the map of every segment but the first, against time.
-template <class E, bool kAligned, int kKind, int NW, bool kMaps>
-__global__ void __launch_bounds__(64 * NW) recurrence_backward_kernel(Args a)
+template <class E, bool kAligned, int kKind, int NW, bool kAhead>
+__global__ void __launch_bounds__(64 * NW, NW / 2) recurrence_backward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
     constexpr bool kSmooth = kKind == ESRNN_RECURRENCE_SMOOTH;
     __shared__ f32x4 lds[2][2][NW][2][16];
+    __shared__ f32x4 lds_ahead[kAhead ? 2 : 1][NW][2][16];
     const int lane16 = threadIdx.x & 15, row = (threadIdx.x >> 4) & 3, wave = threadIdx.x >> 6;
-    const int b = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, segment = blockIdx.y + (kMaps ? 1 : 0);
+    const Place place = draw_place<kAhead>(a);
+    const int b = place.line / a.tiles, tile = place.line % a.tiles;
     const Channels<kAligned, 16> ch(lane16, tile * kTile, a.C);
-    const int length = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-    const int first = segment * a.per_segment, end = min(first + a.per_segment, a.blocks);
+    const int length = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T, top = (length - 1) / kBlock;       // the last block with positions
     const E *x = static_cast<const E *>(a.x) + b * a.xb, *gate = static_cast<const E *>(a.gate) + b * a.gb;
     const E *grad_out = static_cast<const E *>(a.grad_out) + b * a.db;
     E *grad_x = static_cast<E *>(a.grad_x) + b * a.gxb, *grad_gate = static_cast<E *>(a.grad_gate) + b * a.ggb;
-    float *parts = a.parts + (size_t)b * a.segments * 2 * a.C;
+    const bool writes = wave == 0 && row == 0;
 
-    f32x4 carry = splat(0.0f), decay = splat(1.0f);
-    if (!kMaps) {
-        if (a.grad_last) carry = load_state(a.grad_last + (size_t)b * a.C, ch);
-        if (segment < a.segments - 1)
-            carry = through_segments<NW, true>(parts, a.C, segment + 1, a.segments, carry, ch, lds[0][0], wave, row, lane16);
-    }
-    for (int block = end - 1; block >= first; --block) {
+    f32x4 carry = splat(0.0f);
+    if (a.grad_last) carry = load_state(a.grad_last + (size_t)b * a.C, ch);
+    const int last = kAhead ? a.blocks - 1 - place.block : a.blocks - 1, first = kAhead ? last : 0;
+    for (int block = last; block >= first; --block) {
         const int t0 = block * kBlock + (wave * 4 + row) * kSteps;
         if (block * kBlock >= length) {
-            if (kMaps) continue;
             for (int i = 0; i < kSteps; ++i)
                 if (t0 + i < a.T) {
                     ch.store(grad_x + (t0 + i) * a.gxt, Vec4<E>{});
                     ch.store(grad_gate + (t0 + i) * a.ggt, Vec4<E>{});
                 }
+            if (block == 0 && writes && a.grad_initial) store_state(a.grad_initial + (size_t)b * a.C, carry, ch);
             continue;
         }
         Vec4<E> xs[kSteps], gs[kSteps], ds[kSteps];
-        f32x4 before;
-        if (!kMaps) before = load_state(a.saved_in + ((size_t)b * a.blocks + block) * a.C, ch);
+        f32x4 before = load_state(a.saved_in + ((size_t)b * a.blocks + block) * a.C, ch);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const long long t = min(t0 + i, length - 1);
             gs[i] = ch.load(gate + t * a.gt);
             ds[i] = ch.load(grad_out + t * a.dt);
-            if (!kMaps) xs[i] = ch.load(x + t * a.xt);
+            xs[i] = ch.load(x + t * a.xt);
         }
         f32x4 as[kSteps], zs[kSteps], A = splat(1.0f), B = splat(0.0f), M = splat(0.0f);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             f32x4 add;
-            maps_of<kKind>(to_f32<E>(gs[i]), kMaps ? splat(0.0f) : to_f32<E>(xs[i]), t0 + i < length, as[i], zs[i], add);
+            maps_of<kKind>(to_f32<E>(gs[i]), to_f32<E>(xs[i]), t0 + i < length, as[i], zs[i], add);
             B = as[i] * B + add;
             A = as[i] * A;
         }
 #pragma unroll
         for (int i = kSteps - 1; i >= 0; --i) M = as[i] * ((t0 + i < length ? to_f32<E>(ds[i]) : splat(0.0f)) + M);
         const Pieces<NW, true> back(A, M, row, lane16);
-        auto &shared = lds[block & 1];
-        back.leave(shared[1], wave, row, lane16);
-        if (kMaps) {
-            if (NW > 1) __syncthreads();
-            f32x4 factor = back.wave_A;
-            if (NW > 1) {
-                factor = splat(1.0f);
-                for (int w = NW - 1; w >= 0; --w) factor = factor * shared[1][w][0][lane16];
-            }
-            decay = decay * factor;
-            (void)back.enter(carry, shared[1], wave, lane16);
-            continue;
-        }
+        auto &shared = lds[kAhead ? 0 : block & 1];
+        // (the last wave first, as the maps against time follow each other)
+        back.leave(shared[1], NW - 1 - wave, row, lane16);
         const Pieces<NW, false> forth(A, B, row, lane16);
         forth.leave(shared[0], wave, row, lane16);
         if (NW > 1) __syncthreads();
-        f32x4 mu = back.enter(carry, shared[1], wave, lane16);
+        if constexpr (kAhead)
+            carry = line_of(a, place.line).template entering<NW>(top - block, Line::whole<NW>(shared[1], lane16), carry, a.log_group, lds_ahead, wave, row, lane16);
+        f32x4 mu = back.enter(carry, shared[1], NW - 1 - wave, lane16);
         f32x4 h = forth.enter(before, shared[0], wave, lane16);
         f32x4 hs[kSteps];       // the state before each position
 #pragma unroll
@@ -332,14 +411,15 @@ __global__ void __launch_bounds__(64 * NW) recurrence_backward_kernel(Args a)
                 ch.store(grad_gate + (t0 + i) * a.ggt, from_f32<E>(inside ? gg : splat(0.0f)));
             }
         }
+        if (block == 0 && writes && a.grad_initial) store_state(a.grad_initial + (size_t)b * a.C, carry, ch);
     }
-    if (wave != 0 || row != 0) return;
-    if (kMaps) {
-        store_state(parts + (size_t)segment * 2 * a.C, decay, ch);
-        store_state(parts + ((size_t)segment * 2 + 1) * a.C, carry, ch);
-    } else if (a.grad_initial && segment == 0) {
-        store_state(a.grad_initial + (size_t)b * a.C, carry, ch);
-    }
+}
+
+// Before a launch with kAhead: no ticket drawn, no map there.
+__global__ void __launch_bounds__(256) recurrence_words_kernel(u32x4 *words, long long n)
+{
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) words[i] = i < 16 ? u32x4{0, 0, 0, 0} : u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
 }
 
 // One position: a workgroup has 1024 neighbouring channels of a request.
@@ -388,7 +468,7 @@ Args args_of(const esrnn_recurrence_shape &s, const RecurrencePlan &p)
     r.gxb = s.grad_x_stride[0], r.gxt = s.grad_x_stride[1], r.ggb = s.grad_gate_stride[0], r.ggt = s.grad_gate_stride[1];
     r.B = s.B, r.T = s.T, r.C = s.C;
     r.tiles = (s.C + kTile - 1) / kTile;
-    r.blocks = p.blocks, r.per_segment = p.per_segment, r.segments = p.segments;
+    r.blocks = p.blocks, r.groups = p.groups, r.log_group = p.log_group;
     return r;
 }
 
@@ -401,38 +481,52 @@ bool groups_of_four(const void *p, const int64_t stride[2], int dtype)
 
 RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s)
 {
-    RecurrencePlan p;
+    RecurrencePlan p{};
     p.waves = s.T <= 64 ? 1 : 4;
     p.block = 4 * kSteps * p.waves;
     p.blocks = (s.T + p.block - 1) / p.block;
-    const long long rows = (long long)s.B * ((s.C + kTile - 1) / kTile);
-    const long long wanted = std::max<long long>(1, std::min<long long>(p.blocks, 1024 / rows));
-    p.per_segment = (int)((p.blocks + wanted - 1) / wanted);
-    p.segments = (p.blocks + p.per_segment - 1) / p.per_segment;
+    const long long lines = (long long)s.B * ((s.C + kTile - 1) / kTile);
+    p.ahead = p.waves == 4 && p.blocks > 1 && lines < kLinesAlone && lines * p.blocks <= (1 << 21);
+    if (p.ahead) {
+        for (p.log_group = 4; 1LL << 2 * p.log_group < p.blocks; ++p.log_group) {}
+        p.groups = p.blocks >> p.log_group;
+        p.words = 64 + (size_t)lines * (p.blocks + p.groups) * kMap;
+    }
     return p;
 }
+
+namespace {
+
+// f(kAhead) behind the clearing of the words
+template <class F>
+hipError_t with_words(const RecurrencePlan &p, float *words, hipStream_t st, F &&f)
+{
+    if (!p.ahead) return f(std::false_type{});
+    recurrence_words_kernel<<<(unsigned)((p.words / 4 + 255) / 256), 256, 0, st>>>(reinterpret_cast<u32x4 *>(words), (long long)(p.words / 4));
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? f(std::true_type{}) : e;
+}
+
+}  // namespace
 
 hipError_t launch_recurrence_forward(const esrnn_recurrence_shape &s, const RecurrenceForward &f, hipStream_t st)
 {
     const RecurrencePlan p = recurrence_plan(s);
     Args a = args_of(s, p);
-    a.x = f.x, a.gate = f.gate, a.out = f.out, a.lengths = f.lengths, a.initial = f.initial, a.last = f.last, a.saved = f.saved, a.parts = f.parts;
+    a.x = f.x, a.gate = f.gate, a.out = f.out, a.lengths = f.lengths, a.initial = f.initial, a.last = f.last, a.saved = f.saved, a.words = f.words;
     const bool aligned = s.C % 4 == 0 && groups_of_four(f.x, s.x_stride, s.dtype) && groups_of_four(f.gate, s.gate_stride, s.dtype) &&
                          groups_of_four(f.out, s.out_stride, s.dtype);
-    return with_element(s.dtype, [&](auto e) {
-        using E = decltype(e);
-        with_variant(aligned, s.kind, [&](auto al, auto kind) {
-            const unsigned rows = (unsigned)(s.B * a.tiles);
-            const dim3 maps(rows, a.segments - 1), all(rows, a.segments);
-            if (p.waves == 1) {
-                if (maps.y) recurrence_forward_kernel<E, al(), kind(), 1, true><<<maps, 64, 0, st>>>(a);
-                recurrence_forward_kernel<E, al(), kind(), 1, false><<<all, 64, 0, st>>>(a);
-            } else {
-                if (maps.y) recurrence_forward_kernel<E, al(), kind(), 4, true><<<maps, 256, 0, st>>>(a);
-                recurrence_forward_kernel<E, al(), kind(), 4, false><<<all, 256, 0, st>>>(a);
-            }
+    return with_words(p, f.words, st, [&](auto ahead) {
+        return with_element(s.dtype, [&](auto e) {
+            using E = decltype(e);
+            with_variant(aligned, s.kind, [&](auto al, auto kind) {
+                const unsigned lines = (unsigned)(s.B * a.tiles);
+                if constexpr (ahead()) recurrence_forward_kernel<E, al(), kind(), 4, true><<<lines * p.blocks, 256, 0, st>>>(a);
+                else if (p.waves == 1) recurrence_forward_kernel<E, al(), kind(), 1, false><<<lines, 64, 0, st>>>(a);
+                else recurrence_forward_kernel<E, al(), kind(), 4, false><<<lines, 256, 0, st>>>(a);
+            });
+            return hipGetLastError();
         });
-        return hipGetLastError();
     });
 }
 
@@ -441,24 +535,21 @@ hipError_t launch_recurrence_backward(const esrnn_recurrence_shape &s, const Rec
     const RecurrencePlan p = recurrence_plan(s);
     Args a = args_of(s, p);
     a.x = f.x, a.gate = f.gate, a.grad_out = f.grad_out, a.grad_x = f.grad_x, a.grad_gate = f.grad_gate, a.lengths = f.lengths;
-    a.saved_in = f.saved, a.grad_last = f.grad_last, a.grad_initial = f.grad_initial, a.parts = f.parts;
+    a.saved_in = f.saved, a.grad_last = f.grad_last, a.grad_initial = f.grad_initial, a.words = f.words;
     const bool aligned = s.C % 4 == 0 && groups_of_four(f.x, s.x_stride, s.dtype) && groups_of_four(f.gate, s.gate_stride, s.dtype) &&
                          groups_of_four(f.grad_out, s.grad_out_stride, s.dtype) && groups_of_four(f.grad_x, s.grad_x_stride, s.dtype) &&
                          groups_of_four(f.grad_gate, s.grad_gate_stride, s.dtype);
-    return with_element(s.dtype, [&](auto e) {
-        using E = decltype(e);
-        with_variant(aligned, s.kind, [&](auto al, auto kind) {
-            const unsigned rows = (unsigned)(s.B * a.tiles);
-            const dim3 maps(rows, a.segments - 1), all(rows, a.segments);
-            if (p.waves == 1) {
-                if (maps.y) recurrence_backward_kernel<E, al(), kind(), 1, true><<<maps, 64, 0, st>>>(a);
-                recurrence_backward_kernel<E, al(), kind(), 1, false><<<all, 64, 0, st>>>(a);
-            } else {
-                if (maps.y) recurrence_backward_kernel<E, al(), kind(), 4, true><<<maps, 256, 0, st>>>(a);
-                recurrence_backward_kernel<E, al(), kind(), 4, false><<<all, 256, 0, st>>>(a);
-            }
+    return with_words(p, f.words, st, [&](auto ahead) {
+        return with_element(s.dtype, [&](auto e) {
+            using E = decltype(e);
+            with_variant(aligned, s.kind, [&](auto al, auto kind) {
+                const unsigned lines = (unsigned)(s.B * a.tiles);
+                if constexpr (ahead()) recurrence_backward_kernel<E, al(), kind(), 4, true><<<lines * p.blocks, 256, 0, st>>>(a);
+                else if (p.waves == 1) recurrence_backward_kernel<E, al(), kind(), 1, false><<<lines, 64, 0, st>>>(a);
+                else recurrence_backward_kernel<E, al(), kind(), 4, false><<<lines, 256, 0, st>>>(a);
+            });
+            return hipGetLastError();
         });
-        return hipGetLastError();
     });
 }
 
