@@ -22,9 +22,9 @@ bool floats_aligned(const void *p) { return aligned_to(p, 4); }     // (of a nul
 
 bool recurrence_sizes(const esrnn_recurrence_shape &s)
 {
-    // workgroups along the first dimension of the grid: (sequence, tile of 64 channels)
+    // workgroups along the first dimension of the grid: (sequence, tile of channels)
     return s.B >= 1 && s.T >= 1 && s.C >= 1 && s.T <= (1 << 30) && s.C <= (1 << 24) &&
-           (int64_t)s.B * ((s.C + 63) / 64) <= (1 << 23) &&
+           (int64_t)s.B * ((s.C + 63) / 64) <= (1 << 22) &&
            (s.kind == ESRNN_RECURRENCE_SMOOTH || s.kind == ESRNN_RECURRENCE_DECAY) && element_type(s.dtype);
 }
 

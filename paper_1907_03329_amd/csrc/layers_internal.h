@@ -32,12 +32,16 @@ __device__ __forceinline__ Vec4<E> from_f32(f32x4 v)
     return __builtin_convertvector(v, Vec4<E>);
 }
 
-// A lane has four channels of a row of tiles of 4 W channels, W lanes side by side.  Aligned: neighbours, one wide access.  Else the
-// channels lane, lane + W, ..: every access of the W lanes is one run of neighbouring elements.
+// A lane has four channels of a row of tiles of 4 W channels, W lanes side by side.  Aligned: neighbours, one wide access; the last lane of a
+// row whose channels are no multiple of four has the last four of them, so that two lanes have the same channel (C >= 4).  Else
+// the channels lane, lane + W, ..: every access of the W lanes is one run of neighbouring elements.
 template <bool kAligned, int W>
 struct Channels {
-    int first, count;       // first channel of this lane, and how many exist from the tile's begin
-    __device__ __forceinline__ Channels(int lane, int begin, int C) : first(begin + (kAligned ? 4 * lane : lane)), count(C) {}
+    int first, count;       // first channel of this lane, and how many there are in all
+    __device__ __forceinline__ Channels(int lane, int begin, int C) : first(begin + (kAligned ? 4 * lane : lane)), count(C)
+    {
+        if (kAligned && first < C) first = min(first, C - 4);
+    }
     __device__ __forceinline__ int channel(int k) const { return first + (kAligned ? k : W * k); }
     __device__ __forceinline__ bool exists(int k) const { return channel(k) < count; }
     // a channel that can be read in the place of one that does not exist
@@ -67,15 +71,16 @@ struct Channels {
     }
 };
 
-// sigmoid(g) and sigmoid(-g), both to a few units in the last place: 1 - sigmoid would lose those of the small one
+// sigmoid(g) and sigmoid(-g), both to a few units in the last place (1 - sigmoid would lose those of the small one): with E = exp(-g),
+// 1 / (1 + E) and E / (1 + E).  Where E is infinite the first is zero and their product NaN, of which the minimum makes the 1 it has to be; a g
+// that is NaN stays one in the first.
 struct Sigmoids {
     float of, of_minus;
 };
 __device__ __forceinline__ Sigmoids sigmoids(float g)
 {
-    const float e = __builtin_amdgcn_exp2f(fabsf(g) * kSigmoidExponent);
-    const float large = fast_rcp(1.0f + e), small = e * large;
-    return g < 0.0f ? Sigmoids{small, large} : Sigmoids{large, small};
+    const float e = __builtin_amdgcn_exp2f(g * kSigmoidExponent), r = fast_rcp(1.0f + e);
+    return Sigmoids{r, fminf(e * r, 1.0f)};
 }
 
 inline bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
@@ -88,7 +93,7 @@ struct RecurrencePlan {
     int waves, block, blocks;
     bool ahead;
     int log_group, groups;
-    size_t words;
+    size_t tickets, words;
 };
 RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s);
 struct RecurrenceForward {

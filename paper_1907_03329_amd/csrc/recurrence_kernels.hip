@@ -25,7 +25,7 @@ namespace {
 constexpr int kSteps = 8;       // positions of a thread
 constexpr int kTile = 64;       // channels of a workgroup
 // rows of 64 channels from which a workgroup takes a whole sequence
-constexpr int kLinesAlone = 1024;
+constexpr int kLinesAlone = 256;
 
 struct Args {
     const void *x, *gate, *grad_out;
@@ -34,7 +34,7 @@ struct Args {
     const int32_t *lengths;
     const float *initial, *saved_in, *grad_last;
     float *last, *saved, *grad_initial;
-    float *words;               // kAhead: the ticket (256 bytes), then for each 64 channels of a sequence the maps of its blocks
+    float *words;               // kAhead: the tickets of the lines (64 channels of a sequence), then for each line the maps of its blocks
     int B, T, C, tiles, blocks, groups, log_group;      // and of their groups of 2^log_group blocks, [blocks + groups][2][64]
 };
 
@@ -68,7 +68,7 @@ template <int NW, bool kReverse>
 struct Pieces {
     f32x4 A, B;             // of the pieces of this wave before this thread's
     f32x4 wave_A, wave_B;   // of the whole wave
-    __device__ __forceinline__ Pieces(f32x4 a, f32x4 b, int row, int lane16)
+    __device__ __forceinline__ Pieces(f32x4 a, f32x4 b, int row, int lane)
     {
 #pragma unroll
         for (int off = 1; off < 4; off *= 2) {
@@ -79,7 +79,7 @@ struct Pieces {
                 a = a * pa;
             }
         }
-        const int end = (kReverse ? 0 : 48) + lane16;
+        const int end = (kReverse ? 0 : 48) + lane;
         wave_A = from_lane(a, end);
         wave_B = from_lane(b, end);
         A = kReverse ? shift_down(a, 16) : shift_up(a, 16);
@@ -89,15 +89,15 @@ struct Pieces {
             B = splat(0.0f);
         }
     }
-    __device__ __forceinline__ void leave(f32x4 (*lds)[2][16], int wave, int row, int lane16) const
+    __device__ __forceinline__ void leave(f32x4 (*lds)[2][16], int wave, int row, int lane) const
     {
         if (NW > 1 && row == 0) {
-            lds[wave][0][lane16] = wave_A;
-            lds[wave][1][lane16] = wave_B;
+            lds[wave][0][lane] = wave_A;
+            lds[wave][1][lane] = wave_B;
         }
     }
     // behind a barrier: `in` of this thread's piece; carry: in of the block, then out of it
-    __device__ __forceinline__ f32x4 enter(f32x4 &carry, const f32x4 (*lds)[2][16], int wave, int lane16) const
+    __device__ __forceinline__ f32x4 enter(f32x4 &carry, const f32x4 (*lds)[2][16], int wave, int lane) const
     {
         if (NW == 1) {
             const f32x4 in = A * carry + B;
@@ -105,10 +105,10 @@ struct Pieces {
             return in;
         }
         f32x4 h = carry, mine = carry;
-#pragma unroll
+#pragma unroll 2        // (all at once they would take the registers of the waves' maps)
         for (int w = 0; w < NW; ++w) {
             if (w == wave) mine = h;
-            h = lds[w][0][lane16] * h + lds[w][1][lane16];
+            h = lds[w][0][lane] * h + lds[w][1][lane];
         }
         carry = h;
         return A * mine + B;
@@ -122,11 +122,11 @@ struct Pieces {
 // its number alone: those of the whole groups before its own, then those of the blocks before it in its group; the last block of a group
 // hands on the group's map, and waits for no other group for that.  So results do not depend on who was first, a block waits for two
 // others one behind the other at most, and reads 2 sqrt(blocks) maps at most.
-// Every wait ends: blocks are taken by ticket, in the order in which they follow each other, whoever waits waits for lower tickets only, and
-// a block's own map waits for nobody.  (A wait that goes on for seconds all the same, because calls overlap on one workspace, is given
+// Every wait ends: the blocks of a line are taken by ticket, in the order in which they follow each other, whoever waits waits for lower
+// tickets of its line only, and a block's own map waits for nobody.  (A wait that goes on for seconds all the same, because calls overlap on one workspace, is given
 // up, once for all this thread reads; its maps are NaN.)
 constexpr unsigned kEmpty = 0xffffffffu;
-constexpr int kMostLooks = 1 << 22, kMap = 128;     // floats of a map
+constexpr int kMostLooks = 1 << 22, kMap = 128, kTicket = 64;       // floats of a map, and of a ticket's place
 
 struct Map {
     f32x4 A, B;
@@ -161,11 +161,9 @@ struct Line {
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), at, 4 * kMap * i + 256 * half + 16 * (threadIdx.x & 15), 0, kBufShared);
         }
     }
-    // map i of this thread's row
-    __device__ __forceinline__ Map wait(int i)
+    // map i, which `m` has been read from, once it is there
+    __device__ __forceinline__ Map wait(int i, Map m)
     {
-        asm volatile("" ::: "memory");
-        Map m = look(i);
         for (int looks = lost ? kMostLooks : 0; !(there(m.A) && there(m.B)); ++looks) {
             asm volatile("" ::: "memory");
             if (looks == kMostLooks) {
@@ -184,8 +182,14 @@ struct Line {
     {
         const int run = (n + 4 * NW - 1) / (4 * NW), from = min((wave * 4 + row) * run, n), to = min(from + run, n);
         Map m{splat(1.0f), splat(0.0f)};
-        for (int j = from; j < to; ++j)
-            m = wait(j < groups_first ? blocks + j : block + j - groups_first).after(m);
+        const auto index = [&](int j) { return j < groups_first ? blocks + j : block + j - groups_first; };
+        asm volatile("" ::: "memory");
+        for (int j = from; j < to; j += 2) {        // (two looks under way)
+            const int second = min(j + 1, to - 1);
+            const Map m0 = look(index(j)), m1 = look(index(second));
+            m = wait(index(j), m0).after(m);
+            if (j + 1 < to) m = wait(index(second), m1).after(m);
+        }
         const Pieces<NW, false> pieces(m.A, m.B, row, lane16);
         pieces.leave(lds, wave, row, lane16);
         __syncthreads();
@@ -220,19 +224,67 @@ struct Line {
     }
 };
 
+// a, z = 1 - a and b of four channels.  Where there is no position, a gate that keeps everything (kNoGate) and x = 0 make it the map that
+// changes nothing.
 template <int kKind>
-__device__ __forceinline__ void maps_of(f32x4 g, f32x4 x, bool inside, f32x4 &a, f32x4 &z, f32x4 &b)
+constexpr float kNoGate = kKind == ESRNN_RECURRENCE_SMOOTH ? -__builtin_inff() : __builtin_inff();
+template <int kKind>
+__device__ __forceinline__ void maps_of(f32x4 g, f32x4 x, f32x4 &a, f32x4 &z, f32x4 &b)
 {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const Sigmoids s = sigmoids(g[k]);
-        const float keep = kKind == ESRNN_RECURRENCE_SMOOTH ? s.of_minus : s.of;
-        const float take = kKind == ESRNN_RECURRENCE_SMOOTH ? s.of : s.of_minus;
-        a[k] = inside ? keep : 1.0f;
-        z[k] = inside ? take : 0.0f;
-        b[k] = inside ? (kKind == ESRNN_RECURRENCE_SMOOTH ? take * x[k] : x[k]) : 0.0f;
+        a[k] = kKind == ESRNN_RECURRENCE_SMOOTH ? s.of_minus : s.of;
+        z[k] = kKind == ESRNN_RECURRENCE_SMOOTH ? s.of : s.of_minus;
     }
+    b = kKind == ESRNN_RECURRENCE_SMOOTH ? z * x : x;
 }
+
+// The kSteps positions of this thread in one array: four channels of position i.  kFast: the block begins at a scalar base, the thread's place in
+// it never changes, position i is a scalar offset, and lanes without channels or positions lie outside the buffer, so that they
+// read zeros and write nothing: no address is left to compute on the vector ALU, whose cycles the maps need.  (For groups of four elements
+// that begin at a multiple of four bytes, and blocks that span less than 2 GiB.)
+template <class E, bool kFast>
+struct Positions;
+constexpr unsigned kOutside = 0x80000000u;
+
+template <class E>
+struct Positions<E, true> {
+    buf_rsrc rsrc;
+    unsigned at, step;
+    const Channels<true, 16> &ch;
+    // of one block: `base` is the block's first position, `first` this thread's in the block
+    __device__ __forceinline__ Positions(const E *base, long long stride, int first, const Channels<true, 16> &c)
+        : rsrc(make_rsrc(base, 0x7fffffff)), at(c.exists(0) ? (first * (unsigned)stride + c.first) * sizeof(E) : kOutside),
+          step((unsigned)stride * sizeof(E)), ch(c)
+    {
+    }
+    __device__ __forceinline__ Vec4<E> load(int i, bool there) const
+    {
+        const unsigned from = there ? at : kOutside;
+        if constexpr (sizeof(E) == 4) return __builtin_bit_cast(Vec4<E>, __builtin_amdgcn_raw_buffer_load_b128(rsrc, from, i * step, 0));
+        else return __builtin_bit_cast(Vec4<E>, __builtin_amdgcn_raw_buffer_load_b64(rsrc, from, i * step, 0));
+    }
+    __device__ __forceinline__ void store(int i, bool there, Vec4<E> v) const
+    {
+        const unsigned to = there ? at : kOutside;
+        // (four dwords: no scalar offset, see buf_store4)
+        if constexpr (sizeof(E) == 4) buf_store4(rsrc, to == kOutside ? kOutside : to + i * step, v);
+        else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), rsrc, to, i * step, 0);
+    }
+};
+template <class E>
+struct Positions<E, false> {
+    E *base;
+    long long stride;
+    const Channels<false, 16> &ch;
+    __device__ __forceinline__ Positions(const E *b, long long s, int first, const Channels<false, 16> &c) : base(const_cast<E *>(b) + first * s), stride(s), ch(c) {}
+    __device__ __forceinline__ Vec4<E> load(int i, bool there) const { return there ? ch.load(base + i * stride) : Vec4<E>{}; }
+    __device__ __forceinline__ void store(int i, bool there, Vec4<E> v) const
+    {
+        if (there) ch.store(base + i * stride, v);
+    }
+};
 
 // Channels of fp32 arrays [..][C] follow the dealing of the elements'.
 template <bool kAligned>
@@ -252,8 +304,9 @@ __device__ __forceinline__ void store_state(float *p, f32x4 v, const Channels<kA
 }
 
 
-// What a workgroup works on: a row of 64 channels of a sequence, and with kAhead one of its blocks, drawn by ticket: rows side by side, block for
-// block.
+// What a workgroup works on: a line (64 channels of a sequence), and with kAhead one of its blocks, drawn by ticket.  Every line has a ticket
+// of its own, in a cache line of its own: one for all of them is counted up once in 15 to 18 ns, which is what launches of thousands of
+// workgroups then took (131072 positions of 256 channels: 76 us forward).
 struct Place {
     int line, block;
 };
@@ -262,27 +315,27 @@ __device__ __forceinline__ Place draw_place(const Args &a)
 {
     if (!kAhead) return {(int)blockIdx.x, 0};
     __shared__ unsigned s_ticket;
-    if (threadIdx.x == 0) s_ticket = atomicAdd(reinterpret_cast<unsigned *>(a.words), 1u);
+    const unsigned line = blockIdx.x % (unsigned)(a.B * a.tiles);
+    if (threadIdx.x == 0) s_ticket = atomicAdd(reinterpret_cast<unsigned *>(a.words) + kTicket * line, 1u);
     __syncthreads();
     // (in a workspace that another call writes, a ticket is any number: every place has to be in the launch)
-    const unsigned ticket = min((unsigned)__builtin_amdgcn_readfirstlane((int)s_ticket), gridDim.x - 1), lines = (unsigned)(a.B * a.tiles);
-    return {(int)(ticket % lines), (int)(ticket / lines)};
+    return {(int)line, (int)min((unsigned)__builtin_amdgcn_readfirstlane((int)s_ticket), (unsigned)a.blocks - 1)};
 }
 __device__ __forceinline__ Line line_of(const Args &a, int line)
 {
-    return Line(a.words + 64 + (size_t)line * (a.blocks + a.groups) * kMap, a.blocks, a.groups);
+    return Line(a.words + kTicket * (size_t)(a.B * a.tiles) + (size_t)line * (a.blocks + a.groups) * kMap, a.blocks, a.groups);
 }
 
-template <class E, bool kAligned, int kKind, int NW, bool kAhead>
-__global__ void __launch_bounds__(64 * NW) recurrence_forward_kernel(Args a)
+template <class E, bool kFast, int kKind, int NW, bool kAhead>
+__global__ void __launch_bounds__(64 * NW, NW == 8 ? 2 : 4) recurrence_forward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
     __shared__ f32x4 lds[2][NW][2][16];
     __shared__ f32x4 lds_ahead[kAhead ? 2 : 1][NW][2][16];
-    const int lane16 = threadIdx.x & 15, row = (threadIdx.x >> 4) & 3, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 15, row = (threadIdx.x >> 4) & 3, wave = threadIdx.x >> 6;
     const Place place = draw_place<kAhead>(a);
-    const int b = place.line / a.tiles, tile = place.line % a.tiles;
-    const Channels<kAligned, 16> ch(lane16, tile * kTile, a.C);
+    const int b = place.line / a.tiles;
+    const Channels<kFast, 16> ch(lane, place.line % a.tiles * kTile, a.C);
     const int length = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
     const E *x = static_cast<const E *>(a.x) + b * a.xb, *gate = static_cast<const E *>(a.gate) + b * a.gb;
     E *out = static_cast<E *>(a.out) + b * a.ob;
@@ -292,56 +345,58 @@ __global__ void __launch_bounds__(64 * NW) recurrence_forward_kernel(Args a)
     if (a.initial) carry = load_state(a.initial + (size_t)b * a.C, ch);
     if (length == 0 && place.block == 0 && writes && a.last) store_state(a.last + (size_t)b * a.C, carry, ch);
     const int end = kAhead ? place.block + 1 : a.blocks;
+    const int first = (wave * 4 + row) * kSteps;
     for (int block = place.block; block < end; ++block) {
-        const int t0 = block * kBlock + (wave * 4 + row) * kSteps;
-        if (block * kBlock >= length) {     // nothing left of the sequence
-            for (int i = 0; i < kSteps; ++i)
-                if (t0 + i < a.T) ch.store(out + (t0 + i) * a.ot, Vec4<E>{});
+        const int begin = block * kBlock, left = length - begin - first, rest = a.T - begin - first;      // positions from this thread's first on
+        const Positions<E, kFast> to(out + begin * a.ot, a.ot, first, ch);
+        if (begin >= length) {     // nothing left of the sequence
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) to.store(i, i < rest, Vec4<E>{});
             continue;
         }
+        const Positions<E, kFast> of_x(x + begin * a.xt, a.xt, first, ch), of_gate(gate + begin * a.gt, a.gt, first, ch);
         Vec4<E> xs[kSteps], gs[kSteps];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const long long t = min(t0 + i, length - 1);
-            xs[i] = ch.load(x + t * a.xt);
-            gs[i] = ch.load(gate + t * a.gt);
+            xs[i] = of_x.load(i, i < left);
+            gs[i] = of_gate.load(i, i < left);
         }
         f32x4 as[kSteps], bs[kSteps], A = splat(1.0f), B = splat(0.0f);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             f32x4 z;
-            maps_of<kKind>(to_f32<E>(gs[i]), to_f32<E>(xs[i]), t0 + i < length, as[i], z, bs[i]);
+            maps_of<kKind>(to_f32<E>(i < left ? gs[i] : from_f32<E>(splat(kNoGate<kKind>))), to_f32<E>(xs[i]), as[i], z, bs[i]);
             B = as[i] * B + bs[i];
             A = as[i] * A;
         }
-        const Pieces<NW, false> pieces(A, B, row, lane16);
+        const Pieces<NW, false> pieces(A, B, row, lane);
         auto &shared = lds[kAhead ? 0 : block & 1];
-        pieces.leave(shared, wave, row, lane16);
+        pieces.leave(shared, wave, row, lane);
         if (NW > 1) __syncthreads();
         if constexpr (kAhead)
-            carry = line_of(a, place.line).template entering<NW>(block, Line::whole<NW>(shared, lane16), carry, a.log_group, lds_ahead, wave, row, lane16);
+            carry = line_of(a, place.line).template entering<NW>(block, Line::whole<NW>(shared, lane), carry, a.log_group, lds_ahead, wave, row, lane);
         if (a.saved && writes) store_state(a.saved + ((size_t)b * a.blocks + block) * a.C, carry, ch);
-        f32x4 h = pieces.enter(carry, shared, wave, lane16);
+        f32x4 h = pieces.enter(carry, shared, wave, lane);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             h = as[i] * h + bs[i];
-            if (t0 + i < a.T) ch.store(out + (t0 + i) * a.ot, from_f32<E>(t0 + i < length ? h : splat(0.0f)));
+            to.store(i, i < rest, i < left ? from_f32<E>(h) : Vec4<E>{});
         }
         if (block == (length - 1) / kBlock && writes && a.last) store_state(a.last + (size_t)b * a.C, carry, ch);
     }
 }
 
-template <class E, bool kAligned, int kKind, int NW, bool kAhead>
-__global__ void __launch_bounds__(64 * NW, NW / 2) recurrence_backward_kernel(Args a)
+template <class E, bool kFast, int kKind, int NW, bool kAhead>
+__global__ void __launch_bounds__(64 * NW, 2) recurrence_backward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
     constexpr bool kSmooth = kKind == ESRNN_RECURRENCE_SMOOTH;
     __shared__ f32x4 lds[2][2][NW][2][16];
     __shared__ f32x4 lds_ahead[kAhead ? 2 : 1][NW][2][16];
-    const int lane16 = threadIdx.x & 15, row = (threadIdx.x >> 4) & 3, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 15, row = (threadIdx.x >> 4) & 3, wave = threadIdx.x >> 6;
     const Place place = draw_place<kAhead>(a);
-    const int b = place.line / a.tiles, tile = place.line % a.tiles;
-    const Channels<kAligned, 16> ch(lane16, tile * kTile, a.C);
+    const int b = place.line / a.tiles;
+    const Channels<kFast, 16> ch(lane, place.line % a.tiles * kTile, a.C);
     const int length = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T, top = (length - 1) / kBlock;       // the last block with positions
     const E *x = static_cast<const E *>(a.x) + b * a.xb, *gate = static_cast<const E *>(a.gate) + b * a.gb;
     const E *grad_out = static_cast<const E *>(a.grad_out) + b * a.db;
@@ -350,76 +405,76 @@ __global__ void __launch_bounds__(64 * NW, NW / 2) recurrence_backward_kernel(Ar
 
     f32x4 carry = splat(0.0f);
     if (a.grad_last) carry = load_state(a.grad_last + (size_t)b * a.C, ch);
-    const int last = kAhead ? a.blocks - 1 - place.block : a.blocks - 1, first = kAhead ? last : 0;
-    for (int block = last; block >= first; --block) {
-        const int t0 = block * kBlock + (wave * 4 + row) * kSteps;
-        if (block * kBlock >= length) {
-            for (int i = 0; i < kSteps; ++i)
-                if (t0 + i < a.T) {
-                    ch.store(grad_x + (t0 + i) * a.gxt, Vec4<E>{});
-                    ch.store(grad_gate + (t0 + i) * a.ggt, Vec4<E>{});
-                }
+    const int last = kAhead ? a.blocks - 1 - place.block : a.blocks - 1, end = kAhead ? last : 0;
+    const int first = (wave * 4 + row) * kSteps;
+    for (int block = last; block >= end; --block) {
+        const int begin = block * kBlock, left = length - begin - first, rest = a.T - begin - first;
+        const Positions<E, kFast> to_x(grad_x + begin * a.gxt, a.gxt, first, ch), to_gate(grad_gate + begin * a.ggt, a.ggt, first, ch);
+        if (begin >= length) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                to_x.store(i, i < rest, Vec4<E>{});
+                to_gate.store(i, i < rest, Vec4<E>{});
+            }
             if (block == 0 && writes && a.grad_initial) store_state(a.grad_initial + (size_t)b * a.C, carry, ch);
             continue;
         }
+        const Positions<E, kFast> of_x(x + begin * a.xt, a.xt, first, ch), of_gate(gate + begin * a.gt, a.gt, first, ch),
+            of_out(grad_out + begin * a.dt, a.dt, first, ch);
         Vec4<E> xs[kSteps], gs[kSteps], ds[kSteps];
         f32x4 before = load_state(a.saved_in + ((size_t)b * a.blocks + block) * a.C, ch);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const long long t = min(t0 + i, length - 1);
-            gs[i] = ch.load(gate + t * a.gt);
-            ds[i] = ch.load(grad_out + t * a.dt);
-            xs[i] = ch.load(x + t * a.xt);
+            gs[i] = of_gate.load(i, i < left);
+            ds[i] = of_out.load(i, i < left);
+            xs[i] = of_x.load(i, i < left);
         }
         f32x4 as[kSteps], zs[kSteps], A = splat(1.0f), B = splat(0.0f), M = splat(0.0f);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             f32x4 add;
-            maps_of<kKind>(to_f32<E>(gs[i]), to_f32<E>(xs[i]), t0 + i < length, as[i], zs[i], add);
+            maps_of<kKind>(to_f32<E>(i < left ? gs[i] : from_f32<E>(splat(kNoGate<kKind>))), to_f32<E>(xs[i]), as[i], zs[i], add);
             B = as[i] * B + add;
             A = as[i] * A;
         }
 #pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) M = as[i] * ((t0 + i < length ? to_f32<E>(ds[i]) : splat(0.0f)) + M);
-        const Pieces<NW, true> back(A, M, row, lane16);
+        for (int i = kSteps - 1; i >= 0; --i) M = as[i] * (to_f32<E>(ds[i]) + M);
+        __builtin_amdgcn_sched_barrier(0);      // (or conversions move up from below, and with them registers)
+        const Pieces<NW, true> back(A, M, row, lane);
         auto &shared = lds[kAhead ? 0 : block & 1];
         // (the last wave first, as the maps against time follow each other)
-        back.leave(shared[1], NW - 1 - wave, row, lane16);
-        const Pieces<NW, false> forth(A, B, row, lane16);
-        forth.leave(shared[0], wave, row, lane16);
+        back.leave(shared[1], NW - 1 - wave, row, lane);
+        const Pieces<NW, false> forth(A, B, row, lane);
+        forth.leave(shared[0], wave, row, lane);
         if (NW > 1) __syncthreads();
         if constexpr (kAhead)
-            carry = line_of(a, place.line).template entering<NW>(top - block, Line::whole<NW>(shared[1], lane16), carry, a.log_group, lds_ahead, wave, row, lane16);
-        f32x4 mu = back.enter(carry, shared[1], NW - 1 - wave, lane16);
-        f32x4 h = forth.enter(before, shared[0], wave, lane16);
-        f32x4 hs[kSteps];       // the state before each position
+            carry = line_of(a, place.line).template entering<NW>(top - block, Line::whole<NW>(shared[1], lane), carry, a.log_group, lds_ahead, wave, row, lane);
+        f32x4 mu = back.enter(carry, shared[1], NW - 1 - wave, lane);
+        f32x4 h = forth.enter(before, shared[0], wave, lane);
+        f32x4 rate[kSteps];     // of the state that comes in, with the gate, but for a factor a
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            hs[i] = h;
             const f32x4 xi = to_f32<E>(xs[i]);
-            h = as[i] * h + (kSmooth ? (t0 + i < length ? zs[i] * xi : splat(0.0f)) : (t0 + i < length ? xi : splat(0.0f)));
+            rate[i] = zs[i] * (kSmooth ? xi - h : h);
+            h = as[i] * h + (kSmooth ? zs[i] * xi : xi);
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = kSteps - 1; i >= 0; --i) {
-            const bool inside = t0 + i < length;
-            const f32x4 lambda = (inside ? to_f32<E>(ds[i]) : splat(0.0f)) + mu;
+            const f32x4 lambda = to_f32<E>(ds[i]) + mu;
             mu = as[i] * lambda;
-            if (t0 + i < a.T) {
-                const f32x4 gx = kSmooth ? zs[i] * lambda : lambda;
-                const f32x4 gg = mu * zs[i] * (kSmooth ? to_f32<E>(xs[i]) - hs[i] : hs[i]);
-                ch.store(grad_x + (t0 + i) * a.gxt, from_f32<E>(inside ? gx : splat(0.0f)));
-                ch.store(grad_gate + (t0 + i) * a.ggt, from_f32<E>(inside ? gg : splat(0.0f)));
-            }
+            to_x.store(i, i < rest, i < left ? from_f32<E>(kSmooth ? zs[i] * lambda : lambda) : Vec4<E>{});
+            to_gate.store(i, i < rest, i < left ? from_f32<E>(mu * rate[i]) : Vec4<E>{});
         }
         if (block == 0 && writes && a.grad_initial) store_state(a.grad_initial + (size_t)b * a.C, carry, ch);
     }
 }
 
 // Before a launch with kAhead: no ticket drawn, no map there.
-__global__ void __launch_bounds__(256) recurrence_words_kernel(u32x4 *words, long long n)
+__global__ void __launch_bounds__(256) recurrence_words_kernel(u32x4 *words, long long tickets, long long n)
 {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) words[i] = i < 16 ? u32x4{0, 0, 0, 0} : u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
+    if (i < n) words[i] = i < tickets ? u32x4{0, 0, 0, 0} : u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
 }
 
 // One position: a workgroup has 1024 neighbouring channels of a request.
@@ -439,7 +494,7 @@ __global__ void __launch_bounds__(256) recurrence_step_kernel(RecurrenceStep a, 
     const f32x4 g = to_f32<E>(ch.load(static_cast<const E *>(a.gate) + i * a.gate_stride));
     float *state = a.state + (size_t)slot * a.C;
     f32x4 keep, take, add;
-    maps_of<kKind>(g, x, true, keep, take, add);
+    maps_of<kKind>(g, x, keep, take, add);
     const f32x4 h = keep * ch.load(state) + add;
     ch.store(state, h);
     ch.store(out, from_f32<E>(h));
@@ -476,21 +531,28 @@ bool groups_of_four(const void *p, const int64_t stride[2], int dtype)
 {
     return aligned_to(p, 4 * element_bytes(dtype)) && (stride[0] | stride[1]) % 4 == 0;
 }
+// What Positions takes to be fast: groups of four elements from a multiple of four bytes on, in blocks of less than 2 GiB.
+bool fast(const void *p, const int64_t stride[2], const esrnn_recurrence_shape &s, const RecurrencePlan &plan)
+{
+    const bool dwords = s.dtype == ESRNN_F32 || (aligned_to(p, 4) && (stride[0] | stride[1] | s.C) % 2 == 0);
+    return s.C >= 4 && dwords && plan.block * stride[1] + s.C < (int64_t(1) << 29);
+}
 
 }  // namespace
 
 RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s)
 {
     RecurrencePlan p{};
-    p.waves = s.T <= 64 ? 1 : 4;
+    const long long lines = (long long)s.B * ((s.C + kTile - 1) / kTile);
+    p.ahead = s.T > 128 && lines < kLinesAlone && lines * ((s.T + 127) / 128) <= (1 << 21);
+    p.waves = p.ahead ? 4 : s.T <= 32 ? 1 : s.T <= 128 ? 2 : s.T <= 256 ? 4 : 8;
     p.block = 4 * kSteps * p.waves;
     p.blocks = (s.T + p.block - 1) / p.block;
-    const long long lines = (long long)s.B * ((s.C + kTile - 1) / kTile);
-    p.ahead = p.waves == 4 && p.blocks > 1 && lines < kLinesAlone && lines * p.blocks <= (1 << 21);
     if (p.ahead) {
         for (p.log_group = 4; 1LL << 2 * p.log_group < p.blocks; ++p.log_group) {}
         p.groups = p.blocks >> p.log_group;
-        p.words = 64 + (size_t)lines * (p.blocks + p.groups) * kMap;
+        p.tickets = (size_t)lines * kTicket;
+        p.words = p.tickets + (size_t)lines * (p.blocks + p.groups) * kMap;
     }
     return p;
 }
@@ -502,7 +564,8 @@ template <class F>
 hipError_t with_words(const RecurrencePlan &p, float *words, hipStream_t st, F &&f)
 {
     if (!p.ahead) return f(std::false_type{});
-    recurrence_words_kernel<<<(unsigned)((p.words / 4 + 255) / 256), 256, 0, st>>>(reinterpret_cast<u32x4 *>(words), (long long)(p.words / 4));
+    recurrence_words_kernel<<<(unsigned)((p.words / 4 + 255) / 256), 256, 0, st>>>(reinterpret_cast<u32x4 *>(words), (long long)(p.tickets / 4),
+                                                                                   (long long)(p.words / 4));
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? f(std::true_type{}) : e;
 }
@@ -514,16 +577,22 @@ hipError_t launch_recurrence_forward(const esrnn_recurrence_shape &s, const Recu
     const RecurrencePlan p = recurrence_plan(s);
     Args a = args_of(s, p);
     a.x = f.x, a.gate = f.gate, a.out = f.out, a.lengths = f.lengths, a.initial = f.initial, a.last = f.last, a.saved = f.saved, a.words = f.words;
-    const bool aligned = s.C % 4 == 0 && groups_of_four(f.x, s.x_stride, s.dtype) && groups_of_four(f.gate, s.gate_stride, s.dtype) &&
-                         groups_of_four(f.out, s.out_stride, s.dtype);
+    const bool all_fast = fast(f.x, s.x_stride, s, p) && fast(f.gate, s.gate_stride, s, p) && fast(f.out, s.out_stride, s, p);
     return with_words(p, f.words, st, [&](auto ahead) {
         return with_element(s.dtype, [&](auto e) {
             using E = decltype(e);
-            with_variant(aligned, s.kind, [&](auto al, auto kind) {
+            with_variant(all_fast, s.kind, [&](auto al, auto kind) {
                 const unsigned lines = (unsigned)(s.B * a.tiles);
-                if constexpr (ahead()) recurrence_forward_kernel<E, al(), kind(), 4, true><<<lines * p.blocks, 256, 0, st>>>(a);
-                else if (p.waves == 1) recurrence_forward_kernel<E, al(), kind(), 1, false><<<lines, 64, 0, st>>>(a);
-                else recurrence_forward_kernel<E, al(), kind(), 4, false><<<lines, 256, 0, st>>>(a);
+                const auto launch = [&](auto waves) {
+                    recurrence_forward_kernel<E, al(), kind(), waves(), ahead()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
+                };
+                if constexpr (ahead()) launch(Int<4>{});
+                else switch (p.waves) {
+                case 1: return launch(Int<1>{});
+                case 2: return launch(Int<2>{});
+                case 4: return launch(Int<4>{});
+                default: return launch(Int<8>{});
+                }
             });
             return hipGetLastError();
         });
@@ -536,17 +605,23 @@ hipError_t launch_recurrence_backward(const esrnn_recurrence_shape &s, const Rec
     Args a = args_of(s, p);
     a.x = f.x, a.gate = f.gate, a.grad_out = f.grad_out, a.grad_x = f.grad_x, a.grad_gate = f.grad_gate, a.lengths = f.lengths;
     a.saved_in = f.saved, a.grad_last = f.grad_last, a.grad_initial = f.grad_initial, a.words = f.words;
-    const bool aligned = s.C % 4 == 0 && groups_of_four(f.x, s.x_stride, s.dtype) && groups_of_four(f.gate, s.gate_stride, s.dtype) &&
-                         groups_of_four(f.grad_out, s.grad_out_stride, s.dtype) && groups_of_four(f.grad_x, s.grad_x_stride, s.dtype) &&
-                         groups_of_four(f.grad_gate, s.grad_gate_stride, s.dtype);
+    const bool all_fast = fast(f.x, s.x_stride, s, p) && fast(f.gate, s.gate_stride, s, p) && fast(f.grad_out, s.grad_out_stride, s, p) &&
+                          fast(f.grad_x, s.grad_x_stride, s, p) && fast(f.grad_gate, s.grad_gate_stride, s, p);
     return with_words(p, f.words, st, [&](auto ahead) {
         return with_element(s.dtype, [&](auto e) {
             using E = decltype(e);
-            with_variant(aligned, s.kind, [&](auto al, auto kind) {
+            with_variant(all_fast, s.kind, [&](auto al, auto kind) {
                 const unsigned lines = (unsigned)(s.B * a.tiles);
-                if constexpr (ahead()) recurrence_backward_kernel<E, al(), kind(), 4, true><<<lines * p.blocks, 256, 0, st>>>(a);
-                else if (p.waves == 1) recurrence_backward_kernel<E, al(), kind(), 1, false><<<lines, 64, 0, st>>>(a);
-                else recurrence_backward_kernel<E, al(), kind(), 4, false><<<lines, 256, 0, st>>>(a);
+                const auto launch = [&](auto waves) {
+                    recurrence_backward_kernel<E, al(), kind(), waves(), ahead()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
+                };
+                if constexpr (ahead()) launch(Int<4>{});
+                else switch (p.waves) {
+                case 1: return launch(Int<1>{});
+                case 2: return launch(Int<2>{});
+                case 4: return launch(Int<4>{});
+                default: return launch(Int<8>{});
+                }
             });
             return hipGetLastError();
         });
