@@ -327,7 +327,7 @@ __device__ __forceinline__ Line line_of(const Args &a, int line)
 }
 
 template <class E, bool kFast, int kKind, int NW, bool kAhead>
-__global__ void __launch_bounds__(64 * NW, NW == 8 ? 2 : 4) recurrence_forward_kernel(Args a)
+__global__ void __launch_bounds__(64 * NW, NW == 8 ? 2 : kAhead ? 3 : 4) recurrence_forward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
     __shared__ f32x4 lds[2][NW][2][16];
