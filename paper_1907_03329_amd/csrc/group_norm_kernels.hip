@@ -32,6 +32,7 @@ struct Norm {
     float eps;
     int tile, tiles, log_w;     // channels of a workgroup, workgroups of a sample, log2 of the lanes side by side (sample way)
     int chunk, chunks;          // positions of a workgroup, workgroups along positions (stream way)
+    int wave_pairs;             // LDS of a wave (position way)
 };
 
 __device__ __forceinline__ int length_of(const Norm &a, int n) { return a.lengths ? min(max(a.lengths[n], 0), a.T) : a.T; }
@@ -272,80 +273,105 @@ __global__ void __launch_bounds__(NT) norm_sample_backward_kernel(Norm a)
 }
 
 // ---- position ----------------------------------------------------------------------------------------------------
-// T = 1.  A row of a sample's channels is 2^log_w lanes x J chunks of four channels; a wave has 64 >> log_w rows at once.  What a lane has to add
-// to a group goes through the wave's own part of LDS: as the sum of its four channels where groups consist of such fours (kQuads), else
-// channel by channel.  No other wave takes part, so nothing waits at a barrier.
-template <bool kAligned, bool kQuads, int J>
-struct Row {
-    static_assert(kAligned || !kQuads, "");
-    int C, D, G, log_w, lane, row;      // lane: within the row; row: of the wave's
-    float *entries, *sums;              // LDS of this wave: values to add up, sums of groups
+// T = 1.  Groups of one sample have nothing to do with each other, so a wave has a tile of whole groups, some 256 channels, of R samples at
+// once, or of R 64 / w where w < 64 lanes hold the tile's channels.  What a group adds up goes through the wave's own part of LDS: of
+// four channels together where groups consist of such fours (kQuads), else channel by channel.  A group wider than 256 channels
+// is a tile, in J chunks of 256, and is added up over the lanes.  No other wave takes part, so nothing waits at a barrier.
+struct Pair {
+    float a, b;
+};
+template <bool kAligned, bool kQuads, int J, int R>
+struct Tile {
+    static_assert(kAligned || !kQuads || J > 1, "");
+    static constexpr int kEach = kQuads ? 1 : 4;        // entries of a lane and chunk
+    int begin, count, D, groups, log_w, lane, row, rows;        // first channel, channels; row: of the wave's `rows` for each of R
+    Pair *entries, *sums;
+    int n, log_s, part, item_row, item_group;
 
-    __device__ __forceinline__ int channel(int j, int k) const
+    __device__ __forceinline__ Tile(const Norm &a, Pair *lds)
+        : begin(blockIdx.x % a.tiles * a.tile), count(min(a.tile, a.C - begin)), D(a.D), groups(count / a.D), log_w(a.log_w),
+          lane(threadIdx.x & ((1 << a.log_w) - 1)), row((threadIdx.x & 63) >> a.log_w), rows(64 >> a.log_w)
     {
-        return (j << (log_w + 2)) + (kAligned ? 4 * lane + k : lane + (k << log_w));
+        entries = lds + (threadIdx.x >> 6) * a.wave_pairs;
+        sums = entries + R * rows * row_entries();
+        n = kQuads ? D / 4 : D;
+        const int items = R * rows * groups;
+        for (log_s = 0; items << (log_s + 1) <= 64 && 1 << log_s < n; ++log_s) {}      // lanes that share a group
+        const int l = threadIdx.x & 63;
+        part = l & ((1 << log_s) - 1);
+        item_row = (l >> log_s) / groups;
+        item_group = (l >> log_s) - item_row * groups;
     }
-    __device__ __forceinline__ bool exists(int j, int k) const { return channel(j, k) < C; }
+    __device__ __forceinline__ int channel(int j, int k) const { return (j << (log_w + 2)) + (kAligned ? 4 * lane + k : lane + (k << log_w)); }
+    __device__ __forceinline__ bool exists(int j, int k) const { return channel(j, k) < count; }
     template <class E>
-    __device__ __forceinline__ Vec4<E> load(const E *p, int j) const
+    __device__ __forceinline__ Vec4<E> load(const E *p, int j) const        // p: channel 0 of the sample
     {
-        if constexpr (kAligned) return *reinterpret_cast<const Vec4<E> *>(p + min(channel(j, 0), C - 4));
+        if constexpr (kAligned) return *reinterpret_cast<const Vec4<E> *>(p + begin + min(channel(j, 0), count - 4));
         Vec4<E> v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = p[min(channel(j, k), C - 1)];
+        for (int k = 0; k < 4; ++k) v[k] = p[begin + min(channel(j, k), count - 1)];
         return v;
     }
     template <class E>
     __device__ __forceinline__ void store(E *p, int j, Vec4<E> v) const
     {
         if constexpr (kAligned) {
-            if (exists(j, 0)) *reinterpret_cast<Vec4<E> *>(p + channel(j, 0)) = v;
+            if (exists(j, 0)) *reinterpret_cast<Vec4<E> *>(p + begin + channel(j, 0)) = v;
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (exists(j, k)) p[channel(j, k)] = v[k];
+                if (exists(j, k)) p[begin + channel(j, k)] = v[k];
         }
     }
     __device__ __forceinline__ f32x4 parameters(const float *p, int j) const
     {
         f32x4 v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = p[min(channel(j, k), C - 1)];
+        for (int k = 0; k < 4; ++k) v[k] = p[begin + min(channel(j, k), count - 1)];
         return v;
     }
-    // Entries of a group lie side by side; a word of padding after 32 keeps lanes that read at the distance of a group off each
-    // other's banks.
-    __device__ static __forceinline__ int padded(int i) { return i + (i >> 5); }
-    __device__ __forceinline__ int row_entries() const { return padded((J << (log_w + (kQuads ? 0 : 2))) - 1) + 1; }
-    __device__ __forceinline__ int group(int j, int k) const { return min(channel(j, k), C - 1) / D; }
-
-    // v: what each channel adds.  Afterwards total(j, k) is its group's sum.
-    __device__ __forceinline__ void add_up(const f32x4 (&v)[J]) const
+    __device__ __forceinline__ int group(int j, int k) const { return min(channel(j, k), count - 1) / D; }
+    __device__ __forceinline__ f32x4 existing(f32x4 v, int j) const
     {
-        float *mine = entries + row * row_entries();
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            if (kQuads) mine[padded((j << log_w) + lane)] = (v[j][0] + v[j][1]) + (v[j][2] + v[j][3]);
-            else
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mine[padded(channel(j, k))] = v[j][k];
-        }
+        for (int k = 0; k < 4; ++k) v[k] = exists(j, k) ? v[k] : 0.0f;
+        return v;
+    }
+
+    // Entries of a group lie side by side; a place of padding after 16 keeps lanes that read at the distance of a group off each other's banks.
+    __device__ static __forceinline__ int padded(int i) { return i + (i >> 4); }
+    __device__ __forceinline__ int row_entries() const { return padded(J * kEach << log_w); }
+    __device__ __forceinline__ Pair &entry(int r, int j, int k) const
+    {
+        return entries[(r * rows + row) * row_entries() + padded(kQuads ? (j << log_w) + lane : channel(j, k))];
+    }
+    __device__ __forceinline__ Pair sum(int r, int g) const { return sums[(r * rows + row) * groups + g]; }
+    // f(entries of a group, this lane's first one, step between them, group's place in sums, whether this lane writes it) for every group of the
+    // wave; the lanes of a group follow each other, 2^log_s of them
+    template <class F>
+    __device__ __forceinline__ void for_groups(F &&f) const
+    {
         ordered();
-        const int items = G << (6 - log_w), n = kQuads ? D / 4 : D;
-        int log_s = 0;      // lanes that share a group
-        while (items << (log_s + 1) <= 64 && 1 << log_s < n) ++log_s;
-        const int wave_lane = threadIdx.x & 63, part = wave_lane & ((1 << log_s) - 1);
-        for (int item0 = 0; item0 < items; item0 += 64 >> log_s) {
-            const int item = item0 + (wave_lane >> log_s), r = item / G, g = item - r * G;
-            float sum = 0.0f;
-            if (item < items)
-                for (int i = part; i < n; i += 1 << log_s) sum += entries[r * row_entries() + padded(g * n + i)];
-            for (int off = 1; off < 1 << log_s; off *= 2) sum += __shfl_xor(sum, off, 64);
-            if (item < items && part == 0) sums[item] = sum;
+        int r = item_row, g = item_group;
+        for (int item = 0; item < R * rows * groups; item += 64 >> log_s) {
+            const bool there = r < R * rows;
+            const Pair *mine = entries + (there ? r : 0) * row_entries();
+            const int at = (there ? g : 0) * n;
+            f([&](int i) { return mine[padded(at + i)]; }, there, r * groups + g);
+            g += 64 >> log_s;
+            while (g >= groups) {
+                g -= groups;
+                ++r;
+            }
         }
         ordered();
     }
-    __device__ __forceinline__ float total(int g) const { return sums[row * G + g]; }
+    __device__ __forceinline__ float over_lanes(float v) const
+    {
+        for (int off = 1; off < 1 << log_s; off *= 2) v += __shfl_xor(v, off, 64);
+        return v;
+    }
     __device__ static __forceinline__ void ordered()
     {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -354,159 +380,201 @@ struct Row {
     }
 };
 
-// f32x4 of a value of each channel's group
-template <bool kAligned, bool kQuads, int J, class F>
-__device__ __forceinline__ f32x4 by_group(const int (&g)[J][kQuads ? 1 : 4], int j, F &&f)
-{
-    if constexpr (kQuads) return splat(f(g[j][0]));
-    else return f32x4{f(g[j][0]), f(g[j][1]), f(g[j][2]), f(g[j][3])};
-}
-
 extern __shared__ float s_dynamic[];
 
-template <bool kAligned, bool kQuads, int J>
-__device__ __forceinline__ Row<kAligned, kQuads, J> row_of(const Norm &a)
-{
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    Row<kAligned, kQuads, J> r{a.C, a.D, a.G, a.log_w, lane & ((1 << a.log_w) - 1), lane >> a.log_w, nullptr, nullptr};
-    r.entries = s_dynamic + wave * a.tile;      // (floats of a wave)
-    r.sums = r.entries + (64 >> a.log_w) * r.row_entries();
-    return r;
-}
-
-template <class E, bool kAligned, bool kQuads, int J, bool kSilu>
+template <class E, bool kAligned, bool kQuads, int J, int R, bool kSilu>
 __global__ void __launch_bounds__(256) norm_position_forward_kernel(Norm a)
 {
-    const auto row = row_of<kAligned, kQuads, J>(a);
-    const int rows = 64 >> a.log_w, wave = threadIdx.x >> 6, step = (int)gridDim.x * 4 * rows;
-    int g[J][kQuads ? 1 : 4];
+    constexpr int kEach = kQuads ? 1 : 4;
+    const Tile<kAligned, kQuads, J, R> tile(a, reinterpret_cast<Pair *>(s_dynamic));
+    int g[J][kEach];
     f32x4 scale[J], shift[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
 #pragma unroll
-        for (int k = 0; k < (kQuads ? 1 : 4); ++k) g[j][k] = row.group(j, k);
-        scale[j] = row.parameters(a.scale, j);
-        shift[j] = row.parameters(a.shift, j);
+        for (int k = 0; k < kEach; ++k) g[j][k] = tile.group(j, k);
+        scale[j] = tile.parameters(a.scale, j);
+        shift[j] = tile.parameters(a.shift, j);
     }
     const float inverse = 1.0f / (float)a.D;
+    const int stride = R * tile.rows, step = (int)(gridDim.x / a.tiles) * 4 * stride;
     const E *x = static_cast<const E *>(a.x);
-    Vec4<E> next[J];
-    int first = (blockIdx.x * 4 + wave) * rows;     // of this wave's samples (the same in all its lanes)
-    if (first < a.N)
+    for (int first = ((int)(blockIdx.x / a.tiles) * 4 + (int)(threadIdx.x >> 6)) * stride; first < a.N; first += step) {
+        Vec4<E> xs[R][J];
+        bool valid[R];
 #pragma unroll
-        for (int j = 0; j < J; ++j) next[j] = row.load(x + (size_t)min(first + row.row, a.N - 1) * a.C, j);
-    for (; first < a.N; first += step) {
-        const int n = min(first + row.row, a.N - 1);
-        const bool here = first + row.row < a.N, valid = length_of(a, n) > 0;
-        f32x4 v[J], part[J], mean[J], rstd[J];
+        for (int r = 0; r < R; ++r) {
+            const int n = min(first + r * tile.rows + tile.row, a.N - 1);
+            valid[r] = length_of(a, n) > 0;
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            v[j] = to_f32<E>(next[j]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) part[j][k] = valid && row.exists(j, k) ? v[j][k] : 0.0f;
+            for (int j = 0; j < J; ++j) xs[r][j] = tile.load(x + (size_t)n * a.C, j);
         }
-        if (first + step < a.N)
+        Pair only{0.0f, 0.0f};      // J > 1: mean and rstd of the one group
+        if constexpr (J > 1) {
+            f32x4 sum = splat(0.0f);
 #pragma unroll
-            for (int j = 0; j < J; ++j) next[j] = row.load(x + (size_t)min(first + step + row.row, a.N - 1) * a.C, j);
-        row.add_up(part);
+            for (int j = 0; j < J; ++j) sum += tile.existing(to_f32<E>(xs[0][j]), j);
+            only.a = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3])) * inverse;
+            sum = splat(0.0f);
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            mean[j] = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return row.total(i); }) * inverse;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float d = v[j][k] - mean[j][k];
-                part[j][k] = valid && row.exists(j, k) ? d * d : 0.0f;
+            for (int j = 0; j < J; ++j) {
+                const f32x4 d = tile.existing(to_f32<E>(xs[0][j]) - only.a, j);
+                sum += d * d;
             }
+            only.b = __builtin_amdgcn_rsqf(wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3])) * inverse + a.eps);
+            if (a.stats && (threadIdx.x & 63) == 0) reinterpret_cast<Pair *>(a.stats)[(size_t)first * a.G + tile.begin / a.D] = only;
         }
-        row.ordered();
-        row.add_up(part);
+        // four channels: their mean and the sum of squared differences to it; a channel by itself: its value
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            rstd[j] = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return 1.0f / sqrtf(row.total(i) * inverse + a.eps); });
-            if (!here) continue;
-            f32x4 y = (v[j] - mean[j]) * rstd[j] * scale[j] + shift[j];
+        for (int r = 0; r < R && J == 1; ++r)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = activate(y[k], kSilu);
-            row.store(static_cast<E *>(a.out) + (size_t)n * a.C, j, from_f32<E>(valid ? y : splat(0.0f)));
-            if (!a.stats) continue;
+            for (int j = 0; j < J; ++j) {
+                const f32x4 v = to_f32<E>(xs[r][j]);
+                if (kQuads) {
+                    const float mean = 0.25f * ((v[0] + v[1]) + (v[2] + v[3]));
+                    const f32x4 d = v - mean;
+                    tile.entry(r, j, 0) = Pair{mean, (d[0] * d[0] + d[1] * d[1]) + (d[2] * d[2] + d[3] * d[3])};
+                } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int c = row.channel(j, k);
-                if (c < a.C && c % a.D == 0) {
-                    float *s = a.stats + ((size_t)n * a.G + g[j][kQuads ? 0 : k]) * 2;
-                    s[0] = mean[j][k];
-                    s[1] = rstd[j][k];
+                    for (int k = 0; k < kEach; ++k) tile.entry(r, j, k) = Pair{v[k], 0.0f};
                 }
             }
+        if constexpr (J == 1) tile.for_groups([&](auto &&entry, bool there, int to) {
+            float sum = 0.0f, square = 0.0f;
+            for (int i = tile.part; i < tile.n; i += 1 << tile.log_s) sum += entry(i).a;
+            const float mean = tile.over_lanes(sum) * (kQuads ? 4.0f * inverse : inverse);
+            for (int i = tile.part; i < tile.n; i += 1 << tile.log_s) {
+                const Pair e = entry(i);
+                const float d = e.a - mean;
+                square += kQuads ? e.b + 4.0f * d * d : d * d;
+            }
+            const float rstd = __builtin_amdgcn_rsqf(tile.over_lanes(square) * inverse + a.eps);
+            if (there && tile.part == 0) tile.sums[to] = Pair{mean, rstd};
+        });
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int n = first + r * tile.rows + tile.row;
+            if (n >= a.N) continue;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const f32x4 v = to_f32<E>(xs[r][j]);
+                f32x4 y;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const Pair s = J > 1 ? only : tile.sum(r, g[j][kQuads ? 0 : k]);
+                    y[k] = activate((v[k] - s.a) * s.b * scale[j][k] + shift[j][k], kSilu);
+                }
+                tile.store(static_cast<E *>(a.out) + (size_t)n * a.C, j, valid[r] ? from_f32<E>(y) : Vec4<E>{});
+            }
         }
-        row.ordered();
+        if (a.stats && J == 1)
+            for (int i = threadIdx.x & 63; i < stride * tile.groups; i += 64) {
+                const int r = i / tile.groups;
+                if (first + r < a.N) reinterpret_cast<Pair *>(a.stats)[(size_t)(first + r) * a.G + tile.begin / a.D + i - r * tile.groups] = tile.sums[i];
+            }
+        tile.ordered();
     }
 }
 
-template <class E, bool kAligned, bool kQuads, int J, bool kSilu>
+template <class E, bool kAligned, bool kQuads, int J, int R, bool kSilu>
 __global__ void __launch_bounds__(256) norm_position_backward_kernel(Norm a)
 {
-    const auto row = row_of<kAligned, kQuads, J>(a);
-    const int rows = 64 >> a.log_w, wave = threadIdx.x >> 6, step = (int)gridDim.x * 4 * rows;
-    int g[J][kQuads ? 1 : 4];
+    constexpr int kEach = kQuads ? 1 : 4;
+    const Tile<kAligned, kQuads, J, R> tile(a, reinterpret_cast<Pair *>(s_dynamic));
+    int g[J][kEach];
     f32x4 scale[J], shift[J], p1[J], p2[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
 #pragma unroll
-        for (int k = 0; k < (kQuads ? 1 : 4); ++k) g[j][k] = row.group(j, k);
-        scale[j] = row.parameters(a.scale, j);
-        shift[j] = row.parameters(a.shift, j);
+        for (int k = 0; k < kEach; ++k) g[j][k] = tile.group(j, k);
+        scale[j] = tile.parameters(a.scale, j);
+        shift[j] = tile.parameters(a.shift, j);
         p1[j] = p2[j] = splat(0.0f);
     }
     const float inverse = 1.0f / (float)a.D;
+    const int stride = R * tile.rows, step = (int)(gridDim.x / a.tiles) * 4 * stride;
     const E *x = static_cast<const E *>(a.x), *grad_out = static_cast<const E *>(a.grad_out);
-    for (int first = (blockIdx.x * 4 + wave) * rows; first < a.N; first += step) {
-        const int n = min(first + row.row, a.N - 1);
-        const bool here = first + row.row < a.N, valid = length_of(a, n) > 0;
-        const size_t base = (size_t)n * a.C;
-        f32x4 xhat[J], du[J], part[J], s1[J], rstd[J];
-        Vec4<E> xs[J], ds[J];
+    for (int first = ((int)(blockIdx.x / a.tiles) * 4 + (int)(threadIdx.x >> 6)) * stride; first < a.N; first += step) {
+        Vec4<E> xs[R][J], ds[R][J];
+        Pair stats[R][J][kEach];        // (of four channels: of their group)
+        bool valid[R];
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            xs[j] = row.load(x + base, j);
-            ds[j] = row.load(grad_out + base, j);
-        }
+        for (int r = 0; r < R; ++r) {
+            const int at = first + r * tile.rows + tile.row, n = min(at, a.N - 1);
+            valid[r] = at < a.N && length_of(a, n) > 0;
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const float *stats = a.stats_in + (size_t)n * a.G * 2;
-            const f32x4 mean = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return stats[2 * i]; });
-            rstd[j] = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return stats[2 * i + 1]; });
-            xhat[j] = (to_f32<E>(xs[j]) - mean) * rstd[j];
-            du[j] = to_f32<E>(ds[j]);
+            for (int j = 0; j < J; ++j) {
+                xs[r][j] = tile.load(x + (size_t)n * a.C, j);
+                ds[r][j] = tile.load(grad_out + (size_t)n * a.C, j);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                du[j][k] *= slope(xhat[j][k] * scale[j][k] + shift[j][k], kSilu);
-                if (!(here && valid && row.exists(j, k))) du[j][k] = xhat[j][k] = 0.0f;
+                for (int k = 0; k < kEach; ++k)
+                    stats[r][j][k] = reinterpret_cast<const Pair *>(a.stats_in)[(size_t)n * a.G + tile.begin / a.D + g[j][k]];
             }
-            p1[j] += du[j];
-            p2[j] += du[j] * xhat[j];
-            {
+        }
+        f32x4 xhat[R][J], du[R][J];
+        Pair only{0.0f, 0.0f};
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const f32x4 v = to_f32<E>(xs[r][j]), d = to_f32<E>(ds[r][j]);
+                f32x4 own;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const Pair s = stats[r][j][kQuads ? 0 : k];
+                    xhat[r][j][k] = (v[k] - s.a) * s.b;
+                    du[r][j][k] = d[k] * slope(xhat[r][j][k] * scale[j][k] + shift[j][k], kSilu);
+                }
+                if (!valid[r]) xhat[r][j] = du[r][j] = splat(0.0f);
+                p1[j] += du[r][j];
+                p2[j] += du[r][j] * xhat[r][j];
+                {
 #pragma clang fp contract(off)
-                part[j] = scale[j] * du[j];
+                    own = scale[j] * du[r][j];      // (as in input_gradient)
+                }
+                const f32x4 along = own * xhat[r][j];
+                if (J > 1) {
+                    const f32x4 o = tile.existing(own, j), l = tile.existing(along, j);
+                    only.a += (o[0] + o[1]) + (o[2] + o[3]);
+                    only.b += (l[0] + l[1]) + (l[2] + l[3]);
+                } else if (kQuads) tile.entry(r, j, 0) = Pair{(own[0] + own[1]) + (own[2] + own[3]), (along[0] + along[1]) + (along[2] + along[3])};
+                else
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) tile.entry(r, j, k) = Pair{own[k], along[k]};
+            }
+        if (J > 1) only = Pair{wave_sum(only.a) * inverse, wave_sum(only.b) * inverse};
+        if constexpr (J == 1) tile.for_groups([&](auto &&entry, bool there, int to) {
+            Pair sum{0.0f, 0.0f};
+            for (int i = tile.part; i < tile.n; i += 1 << tile.log_s) {
+                const Pair e = entry(i);
+                sum.a += e.a;
+                sum.b += e.b;
+            }
+            sum.a = tile.over_lanes(sum.a) * inverse;
+            sum.b = tile.over_lanes(sum.b) * inverse;
+            if (there && tile.part == 0) tile.sums[to] = sum;
+        });
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int n = first + r * tile.rows + tile.row;
+            if (n >= a.N) continue;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                f32x4 s1, s2, rstd;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const Pair s = J > 1 ? only : tile.sum(r, g[j][kQuads ? 0 : k]);
+                    s1[k] = s.a;
+                    s2[k] = s.b;
+                    rstd[k] = stats[r][j][kQuads ? 0 : k].b;
+                }
+                const f32x4 gx = input_gradient(rstd, scale[j], du[r][j], s1, xhat[r][j], s2);
+                tile.store(static_cast<E *>(a.grad_x) + (size_t)n * a.C, j, valid[r] ? from_f32<E>(gx) : Vec4<E>{});
             }
         }
-        row.add_up(part);
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            s1[j] = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return row.total(i); }) * inverse;
-            part[j] = part[j] * xhat[j];
-        }
-        row.ordered();
-        row.add_up(part);
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const f32x4 s2 = by_group<kAligned, kQuads, J>(g, j, [&](int i) { return row.total(i); }) * inverse;
-            const f32x4 gx = input_gradient(rstd[j], scale[j], du[j], s1[j], xhat[j], s2);
-            if (here) row.store(static_cast<E *>(a.grad_x) + base, j, from_f32<E>(valid ? gx : splat(0.0f)));
-        }
-        row.ordered();
+        tile.ordered();
     }
-    // the wave's rows, then the waves one behind the other: parts [workgroups][2][C]
+    // the wave's rows, then the waves one behind the other: parts [workgroups of a tile][2][C]
     for (int off = 1 << a.log_w; off < 64; off *= 2)
 #pragma unroll
         for (int j = 0; j < J; ++j)
@@ -517,19 +585,23 @@ __global__ void __launch_bounds__(256) norm_position_backward_kernel(Norm a)
             }
     for (int w = 0; w < 4; ++w) {
         __syncthreads();
-        if (wave != w || row.row != 0) continue;
+        if ((int)(threadIdx.x >> 6) != w || tile.row != 0) continue;
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (row.exists(j, k)) {
-                    const int c = row.channel(j, k);
+                if (tile.exists(j, k)) {
+                    const int c = tile.channel(j, k);
                     s_dynamic[c] = w ? s_dynamic[c] + p1[j][k] : p1[j][k];
-                    s_dynamic[a.C + c] = w ? s_dynamic[a.C + c] + p2[j][k] : p2[j][k];
+                    s_dynamic[a.tile + c] = w ? s_dynamic[a.tile + c] + p2[j][k] : p2[j][k];
                 }
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < 2 * a.C; c += 256) a.parts[(size_t)blockIdx.x * 2 * a.C + c] = s_dynamic[c];
+    float *parts = a.parts + (size_t)(blockIdx.x / a.tiles) * 2 * a.C + tile.begin;
+    for (int c = threadIdx.x; c < tile.count; c += 256) {
+        parts[c] = s_dynamic[c];
+        parts[a.C + c] = s_dynamic[a.tile + c];
+    }
 }
 
 // Sums over `rows` rows of [rows][2][C]: a workgroup has 64 channels of one of the two and a run of rows, its waves every 16th of them.
@@ -811,9 +883,11 @@ struct Way {
     int threads, rows_each;     // sample: of a workgroup; positions a thread
     int tile, tiles, log_w, chunk, chunks;
     int pieces;                 // position: chunks of four channels a lane
-    int forward_groups, backward_groups;        // position: workgroups
+    int forward_groups, backward_groups;        // position: workgroups of a tile
     int part_rows;              // rows [2][C] of channel sums that the reverse pass leaves
 };
+
+constexpr int kMostPositionTile = 2048, kPositionRows = 4;      // channels of a group, samples at once (of groups up to 256)
 
 // Rows are added up in two launches from this many on: one alone reads them with 2 C / 64 workgroups.
 constexpr int kManyRows = 1024, kRuns = 64;
@@ -822,18 +896,25 @@ Way way_of(const esrnn_group_norm_shape &s)
 {
     Way w{};
     const int D = s.C / s.G;
-    if (s.T == 1) {
-        for (w.log_w = 0; w.log_w < 6 && 4 << w.log_w < s.C; ++w.log_w) {}
-        for (w.pieces = 1; w.pieces << (w.log_w + 2) < s.C && w.pieces < 16; w.pieces *= 2) {}
-        if (w.pieces <= (D % 4 ? 4 : 8)) {
-            w.kind = kPosition;
-            const int rows = 4 * (64 >> w.log_w);       // of a workgroup
-            const int64_t most = ((int64_t)s.N + rows - 1) / rows;
-            w.forward_groups = (int)std::min<int64_t>(most, 2048);
-            w.backward_groups = (int)std::min<int64_t>(most, 512);
-            w.part_rows = w.backward_groups;
-            return w;
-        }
+    if (s.T == 1 && D <= kMostPositionTile) {
+        // whole groups up to 256 channels, of which a few groups less may be whole groups of four channels
+        int groups = std::max(1, std::min(s.G, 256 / D));
+        for (int fewer = groups; fewer > std::max(1, groups - 4); --fewer)
+            if (fewer * D % 4 == 0) {
+                groups = fewer;
+                break;
+            }
+        w.kind = kPosition;
+        w.tile = groups * D;
+        w.tiles = (s.G + groups - 1) / groups;
+        for (w.log_w = 0; w.log_w < 6 && 4 << w.log_w < w.tile; ++w.log_w) {}
+        for (w.pieces = 1; w.pieces * 256 < w.tile; w.pieces *= 2) {}
+        const int rows = 4 * (w.pieces == 1 ? kPositionRows : 1) * (64 >> w.log_w);     // of a workgroup
+        const int64_t most = ((int64_t)s.N + rows - 1) / rows;
+        w.forward_groups = (int)std::min<int64_t>(most, std::max(1, 4096 / w.tiles));
+        w.backward_groups = (int)std::min<int64_t>(most, std::max(1, 2048 / w.tiles));
+        w.part_rows = w.backward_groups;
+        return w;
     }
     // sample: whole groups side by side up to 64 channels (a run of 128 bytes of bf16), as many positions as fit
     int groups = std::max(1, std::min(s.G, 64 / D));
@@ -882,48 +963,51 @@ void with_flags(bool aligned, bool silu, F &&f)
 }
 
 
-// LDS of a wave of the position way, in floats: entries of its rows, sums of their groups.
-int position_floats(const esrnn_group_norm_shape &s, const Way &w, bool quads)
+// LDS of a wave of the position way, in pairs: entries of its rows, sums of their groups (as Tile has them)
+int position_pairs(const esrnn_group_norm_shape &s, const Way &w, bool quads)
 {
-    const int rows = 64 >> w.log_w, entries = w.pieces << (w.log_w + (quads ? 0 : 2));
-    return rows * (entries + (entries - 1) / 32 + s.G);
+    if (w.pieces > 1) return 0;
+    const int rows = kPositionRows * (64 >> w.log_w), entries = (quads ? 1 : 4) << w.log_w;
+    return rows * (entries + entries / 16 + w.tile / (s.C / s.G));
 }
 
-// f(pieces, aligned, quads) for the instantiations that there are: groups that are no fours of channels have at most four pieces, unless
-// it is only the arrays' alignment that keeps the fours apart.
+// f(pieces, samples at once, aligned, quads)
 template <class F>
 void with_pieces(int pieces, bool aligned, bool quads, F &&f)
 {
-    const auto layout = [&](auto j) {
-        if (aligned && quads) f(j, std::true_type{}, std::true_type{});
-        else if (!aligned) f(j, std::false_type{}, std::false_type{});
-        else if constexpr (j() <= 4) f(j, std::true_type{}, std::false_type{});
+    const auto layout = [&](auto j, auto r) {
+        // (of one group in chunks there is nothing to tell apart)
+        if (aligned && (quads || j() > 1)) f(j, r, std::true_type{}, std::true_type{});
+        else if (aligned) f(j, r, std::true_type{}, std::bool_constant<(j() > 1)>{});
+        else f(j, r, std::false_type{}, std::bool_constant<(j() > 1)>{});
     };
+    using One = std::integral_constant<int, 1>;
     switch (pieces) {
-    case 1: return layout(std::integral_constant<int, 1>{});
-    case 2: return layout(std::integral_constant<int, 2>{});
-    case 4: return layout(std::integral_constant<int, 4>{});
-    default: return layout(std::integral_constant<int, 8>{});
+    case 1: return layout(One{}, std::integral_constant<int, kPositionRows>{});
+    case 2: return layout(std::integral_constant<int, 2>{}, One{});
+    case 4: return layout(std::integral_constant<int, 4>{}, One{});
+    default: return layout(std::integral_constant<int, 8>{}, One{});
     }
 }
 
 template <class E, bool kSilu>
 void position_forward(const esrnn_group_norm_shape &s, Norm a, const Way &w, bool aligned, hipStream_t st)
 {
-    const bool quads = aligned && a.D % 4 == 0;
-    a.tile = position_floats(s, w, quads);
-    with_pieces(w.pieces, aligned, quads, [&](auto j, auto al, auto q) {
-        norm_position_forward_kernel<E, al(), q(), j(), kSilu><<<w.forward_groups, 256, 16 * a.tile, st>>>(a);
+    const bool fours = aligned && w.tile % 4 == 0, quads = fours && a.D % 4 == 0;
+    a.wave_pairs = position_pairs(s, w, quads);
+    with_pieces(w.pieces, fours, quads, [&](auto j, auto r, auto al, auto q) {
+        norm_position_forward_kernel<E, al(), q(), j(), r(), kSilu><<<w.tiles * w.forward_groups, 256, 4 * sizeof(Pair) * a.wave_pairs, st>>>(a);
     });
 }
 
 template <class E, bool kSilu>
 void position_backward(const esrnn_group_norm_shape &s, Norm a, const Way &w, bool aligned, hipStream_t st)
 {
-    const bool quads = aligned && a.D % 4 == 0;
-    a.tile = position_floats(s, w, quads);
-    with_pieces(w.pieces, aligned, quads, [&](auto j, auto al, auto q) {
-        norm_position_backward_kernel<E, al(), q(), j(), kSilu><<<w.backward_groups, 256, std::max(16 * a.tile, 8 * a.C), st>>>(a);
+    const bool fours = aligned && w.tile % 4 == 0, quads = fours && a.D % 4 == 0;
+    a.wave_pairs = position_pairs(s, w, quads);
+    const size_t lds = std::max(4 * sizeof(Pair) * a.wave_pairs, 2 * sizeof(float) * a.tile);
+    with_pieces(w.pieces, fours, quads, [&](auto j, auto r, auto al, auto q) {
+        norm_position_backward_kernel<E, al(), q(), j(), r(), kSilu><<<w.tiles * w.backward_groups, 256, lds, st>>>(a);
     });
 }
 
