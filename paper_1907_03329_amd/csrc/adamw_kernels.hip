@@ -20,41 +20,46 @@ namespace {
 // 7 against 127): the upper 12 bits of the scaled magnitude, denormal or not, are the code
 constexpr float kMostE4m3 = 448.0f, kToCode = 0x1p-120f, kLeastScale = 0x1p-100f;
 
-template <class E>
-__device__ __forceinline__ f32x4 load_group(const void *base, long long at, int left, bool aligned)
+// N groups of four neighbours of this lane, 256 elements apart, of a tensor of n elements; `whole`: all of the wave's groups are in it (the same
+// in all lanes).  Pointers out of a table are told to be global memory.
+template <class E, int N>
+__device__ __forceinline__ void load_groups(const void *base, long long first, long long n, bool whole, f32x4 (&v)[N])
 {
-    const E *p = static_cast<const E *>(base) + at;
-    if (aligned && left >= 4) return to_f32<E>(*reinterpret_cast<const Vec4<E> *>(p));
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    typedef typename Loose<E>::Four Four;
+    const auto *p = (const __attribute__((address_space(1))) E *)base + first;
+    if (whole) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k < left) v[k] = (float)p[k];
-    return v;
-}
-template <class E>
-__device__ __forceinline__ void store_group(void *base, long long at, int left, bool aligned, f32x4 v)
-{
-    E *p = static_cast<E *>(base) + at;
-    const Vec4<E> r = from_f32<E>(v);
-    if (aligned && left >= 4) {
-        *reinterpret_cast<Vec4<E> *>(p) = r;
+        for (int j = 0; j < N; ++j) v[j] = to_f32<E>(*reinterpret_cast<const __attribute__((address_space(1))) Four *>(p + 256 * j));
         return;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k < left) p[k] = r[k];
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[j][k] = first + 256 * j + k < n ? (float)p[256 * j + k] : 0.0f;
 }
-__device__ __forceinline__ f32x4 load_grad(const AdamWEntry &e, long long at, int left)
+template <class E, int N>
+__device__ __forceinline__ void store_groups(void *base, long long first, long long n, bool whole, const f32x4 (&v)[N])
 {
-    if (e.grad_dtype == ESRNN_BF16) return load_group<__bf16>(e.grad, at, left, e.aligned);
-    if (e.grad_dtype == ESRNN_F16) return load_group<_Float16>(e.grad, at, left, e.aligned);
-    return load_group<float>(e.grad, at, left, e.aligned);
+    typedef typename Loose<E>::Four Four;
+    auto *p = (__attribute__((address_space(1))) E *)base + first;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const Vec4<E> r = from_f32<E>(v[j]);
+        if (whole) {
+            *reinterpret_cast<__attribute__((address_space(1))) Four *>(p + 256 * j) = r;
+            continue;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (first + 256 * j + k < n) p[256 * j + k] = r[k];
+    }
 }
-
-// the place of one group of four neighbours of this lane in its tensor
-__device__ __forceinline__ int elements_left(const AdamWEntry &e, long long at)
+template <int N>
+__device__ __forceinline__ void load_grad(const AdamWEntry &e, long long first, bool whole, f32x4 (&g)[N])
 {
-    return (int)min(max(e.n - at, 0LL), 4LL);
+    if (e.grad_dtype == ESRNN_BF16) load_groups<__bf16>(e.grad, first, e.n, whole, g);
+    else if (e.grad_dtype == ESRNN_F16) load_groups<_Float16>(e.grad, first, e.n, whole, g);
+    else load_groups<float>(e.grad, first, e.n, whole, g);
 }
 
 __global__ void __launch_bounds__(1024) adamw_norm_kernel(const AdamWEntry *__restrict__ entries, const int *__restrict__ owner, int chunks,
@@ -64,16 +69,21 @@ __global__ void __launch_bounds__(1024) adamw_norm_kernel(const AdamWEntry *__re
     __shared__ double s_wave[16];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     double acc = 0.0;       // (squares of fp32 numbers do not overflow)
-    for (int chunk = __builtin_amdgcn_readfirstlane(blockIdx.x * 16 + wave); chunk < chunks; chunk += gridDim.x * 16) {
-        const AdamWEntry e = entries[owner[chunk]];
-        const long long first = (long long)(chunk - e.first_chunk) * kAdamWChunk + 4 * lane;
+    const int step = gridDim.x * 16;
+    int chunk = __builtin_amdgcn_readfirstlane(blockIdx.x * 16 + wave);
+    // the next chunk's tensor is looked up while this one's elements are under way
+    AdamWEntry e = chunk < chunks ? entries[owner[chunk]] : AdamWEntry{};
+    while (chunk < chunks) {
+        const int next = chunk + step;
+        const long long first = (long long)(chunk - e.first_chunk) * kAdamWChunk;
         f32x4 g[kGroups];
-#pragma unroll
-        for (int j = 0; j < kGroups; ++j) g[j] = load_grad(e, first + 256 * j, elements_left(e, first + 256 * j));
+        load_grad(e, first + 4 * lane, first + kAdamWChunk <= e.n, g);
+        e = entries[owner[min(next, chunks - 1)]];
 #pragma unroll
         for (int j = 0; j < kGroups; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc += (double)g[j][k] * (double)g[j][k];
+        chunk = next;
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) acc += __shfl_xor(acc, off, 64);
@@ -137,17 +147,15 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
     const long long first = (long long)(chunk - e.first_chunk) * kAdamWChunk + wave * (256 * kGroups) + 4 * lane;
     const long long flat = e.flat + first;      // place in the moments
 
-    int left[kGroups];
+    const bool whole = first - 4 * lane + 256 * kGroups <= e.n;
     f32x4 p[kGroups], g[kGroups], m[kGroups], v[kGroups];
     unsigned m8[kGroups], r8[kGroups];
     float m_scale[kGroups], r_scale[kGroups];
+    load_groups<float>(e.param, first, e.n, whole, p);
+    load_grad(e, first, whole, g);
 #pragma unroll
     for (int j = 0; j < kGroups; ++j) {
-        const long long at = first + 256 * j;
-        left[j] = elements_left(e, at);
-        const bool block = at - 4 * lane < e.n;     // (uniform: the wave has a block here)
-        p[j] = load_group<float>(e.param, at, left[j], e.aligned);
-        g[j] = load_grad(e, at, left[j]);
+        const bool block = first - 4 * lane + 256 * j < e.n;        // (uniform: the wave has a block here)
         if (kBits == 32) {
             m[j] = v[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if (block) {
@@ -168,6 +176,7 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
     float scale = 1.0f;
     if (u.partial) {
         __shared__ double s_sum[4];
+        static_assert(kAdamWNormBlocks <= 256, "");
         double sum = (int)threadIdx.x < u.n_partial ? u.partial[threadIdx.x] : 0.0;
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
@@ -195,12 +204,6 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
         for (int k = 0; k < 4; ++k) {
             root[k] = sqrtf(v[j][k]);
             p[j][k] = keep * p[j][k] - u.rate * m[j][k] * fast_rcp(root[k] * u.root_correction + u.eps);
-        }
-        const long long at = first + 256 * j;
-        store_group<float>(e.param, at, left[j], e.aligned, p[j]);
-        if (e.copy) {
-            if (e.copy_dtype == ESRNN_BF16) store_group<__bf16>(e.copy, at, left[j], e.aligned, p[j]);
-            else store_group<_Float16>(e.copy, at, left[j], e.aligned, p[j]);
         }
         if (kBits == 32) {
             *reinterpret_cast<f32x4 *>(static_cast<float *>(u.m) + flat + 256 * j) = m[j];
@@ -231,6 +234,10 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
             u.r_scale[(flat + 256 * j) >> 8] = sr.scale;
         }
     }
+    store_groups<float>(e.param, first, e.n, whole, p);
+    if (!e.copy) return;
+    if (e.copy_dtype == ESRNN_BF16) store_groups<__bf16>(e.copy, first, e.n, whole, p);
+    else store_groups<_Float16>(e.copy, first, e.n, whole, p);
 }
 
 // The table comes to the device as arguments of launches: no copy from host memory that might still be read after the call.

@@ -96,7 +96,7 @@ struct TileChannels {
 // Sums over the workgroup's rows, and over the channels of each group.  NV values a channel.
 template <int NT, int NV, bool kAligned>
 struct TileSums {
-    // channel sums of each wave [slots][NV][tile], sums of groups [groups][NV]
+    // channel sums of each wave [slots][NV][tile], of the workgroup [NV][tile] (in the first slot's place), sums of groups [groups][NV]
     float *part, *group;
     int slots, tile, D;
     __device__ __forceinline__ void channels(f32x4 (&v)[NV], const TileChannels<kAligned> &ch, int log_w)
@@ -115,22 +115,29 @@ struct TileSums {
                 for (int k = 0; k < 4; ++k)
                     if (ch.exists(k)) part[(slot * NV + i) * tile + ch.at(k)] = v[i][k];
         __syncthreads();
+        for (int at = threadIdx.x; at < NV * tile; at += NT) {
+            float sum[4] = {part[at], 0.0f, 0.0f, 0.0f};
+            int s = 1;
+            for (; s + 4 <= slots; s += 4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += part[(s + i) * NV * tile + at];
+            for (; s < slots; ++s) sum[0] += part[s * NV * tile + at];
+            part[at] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        }
+        __syncthreads();
     }
+    __device__ __forceinline__ float channel(int i, int c) const { return part[i * tile + c]; }
     // behind channels(): a wave a group; weight: of a channel
     template <class W>
     __device__ __forceinline__ void groups(W &&weight)
     {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        int log_d = 0;
-        while ((1 << log_d) < D && log_d < 6) ++log_d;
-        const int c0 = lane & ((1 << log_d) - 1), s0 = lane >> log_d, s_step = 64 >> log_d;
         for (int g = wave; g * D < tile; g += NT / 64) {
             float sum[NV] = {};
-            for (int c = c0; c < D; c += 64) {
+            for (int c = lane; c < D; c += 64) {
                 const float f = weight(g * D + c);
-                for (int s = s0; s < slots; s += s_step)
 #pragma unroll
-                    for (int i = 0; i < NV; ++i) sum[i] += f * part[(s * NV + i) * tile + g * D + c];
+                for (int i = 0; i < NV; ++i) sum[i] += f * channel(i, g * D + c);
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -243,13 +250,8 @@ __global__ void __launch_bounds__(NT) norm_sample_backward_kernel(Norm a)
         }
     sums.channels(v, ch, a.log_w);
     for (int c = threadIdx.x; c < ch.count; c += NT) {      // sums of the sample, to be added up over the samples
-        float p1 = 0.0f, p2 = 0.0f;
-        for (int s = 0; s < sums.slots; ++s) {
-            p1 += part[(s * 2) * ch.count + c];
-            p2 += part[(s * 2 + 1) * ch.count + c];
-        }
-        a.parts[((size_t)n * 2) * a.C + ch.begin + c] = p1;
-        a.parts[((size_t)n * 2 + 1) * a.C + ch.begin + c] = p2;
+        a.parts[((size_t)n * 2) * a.C + ch.begin + c] = sums.channel(0, c);
+        a.parts[((size_t)n * 2 + 1) * a.C + ch.begin + c] = sums.channel(1, c);
     }
     sums.groups([&](int c) { return a.scale[ch.begin + c]; });
     const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
@@ -604,25 +606,236 @@ __global__ void __launch_bounds__(256) norm_position_backward_kernel(Norm a)
     }
 }
 
-// Sums over `rows` rows of [rows][2][C]: a workgroup has 64 channels of one of the two and a run of rows, its waves every 16th of them.
-// From workgroups of one run to [runs][2][C]; of a single run, to the gradients.
-__global__ void __launch_bounds__(1024) norm_sum_rows_kernel(const float *__restrict__ parts, int rows, int C, float *to_shift, float *to_scale)
-{
-    __shared__ float s_sum[16][64];
-    const int lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane, wave = threadIdx.x >> 6;
-    const int run = (rows + (int)gridDim.z - 1) / (int)gridDim.z, first = blockIdx.z * run, end = min(first + run, rows);
-    const float *p = parts + (size_t)blockIdx.y * C + min(c, C - 1);
-    float sum[4] = {};
-    for (int r = first + wave; r < end; r += 64)
+// Groups of more than 512 channels: a workgroup has one group of R samples, J chunks of 1024 channels, and adds up over its waves.
+template <bool kAligned, int J>
+struct WideRow {
+    int begin, count;
+    __device__ __forceinline__ int channel(int j, int k) const { return 1024 * j + (kAligned ? 4 * (int)threadIdx.x + k : (int)threadIdx.x + 256 * k); }
+    __device__ __forceinline__ bool exists(int j, int k) const { return channel(j, k) < count; }
+    template <class E>
+    __device__ __forceinline__ Vec4<E> load(const E *p, int j) const
+    {
+        if constexpr (kAligned) return *reinterpret_cast<const Vec4<E> *>(p + begin + min(channel(j, 0), count - 4));
+        Vec4<E> v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (r + 16 * i < end) sum[i] += p[(size_t)(r + 16 * i) * 2 * C];
-    s_sum[wave][lane] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        for (int k = 0; k < 4; ++k) v[k] = p[begin + min(channel(j, k), count - 1)];
+        return v;
+    }
+    template <class E>
+    __device__ __forceinline__ void store(E *p, int j, Vec4<E> v) const
+    {
+        if constexpr (kAligned) {
+            if (exists(j, 0)) *reinterpret_cast<Vec4<E> *>(p + begin + channel(j, 0)) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (exists(j, k)) p[begin + channel(j, k)] = v[k];
+        }
+    }
+    __device__ __forceinline__ f32x4 parameters(const float *p, int j) const
+    {
+        f32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = p[begin + min(channel(j, k), count - 1)];
+        return v;
+    }
+    __device__ __forceinline__ f32x4 existing(f32x4 v, int j) const
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = exists(j, k) ? v[k] : 0.0f;
+        return v;
+    }
+};
+// N sums over the workgroup at once; `shared`: [4][N], not written again before the next barrier but one
+template <int N>
+__device__ __forceinline__ void workgroup_sums(float (&v)[N], float (*shared)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = wave_sum(v[i]);
+        if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6][i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (shared[0][i] + shared[1][i]) + (shared[2][i] + shared[3][i]);
+}
+__device__ __forceinline__ float across(f32x4 v) { return (v[0] + v[1]) + (v[2] + v[3]); }
+
+template <class E, bool kAligned, int J, bool kSilu>
+__global__ void __launch_bounds__(256) norm_wide_forward_kernel(Norm a)
+{
+    constexpr int R = 4 / J;
+    __shared__ float s_sum[2][4][R];
+    const int g = blockIdx.x % a.G;
+    const WideRow<kAligned, J> row{g * a.D, a.D};
+    f32x4 scale[J], shift[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        scale[j] = row.parameters(a.scale, j);
+        shift[j] = row.parameters(a.shift, j);
+    }
+    const float inverse = 1.0f / (float)a.D;
+    const E *x = static_cast<const E *>(a.x);
+    for (int first = (int)(blockIdx.x / a.G) * R; first < a.N; first += (int)(gridDim.x / a.G) * R) {
+        f32x4 v[R][J];
+        float sum[R], square[R];
+        {
+            Vec4<E> xs[R][J];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int j = 0; j < J; ++j) xs[r][j] = row.load(x + (size_t)min(first + r, a.N - 1) * a.C, j);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                f32x4 all = splat(0.0f);
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    v[r][j] = to_f32<E>(xs[r][j]);
+                    all += row.existing(v[r][j], j);
+                }
+                sum[r] = across(all);
+            }
+        }
+        workgroup_sums(sum, s_sum[0]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            f32x4 all = splat(0.0f);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                v[r][j] -= sum[r] * inverse;
+                const f32x4 d = row.existing(v[r][j], j);
+                all += d * d;
+            }
+            square[r] = across(all);
+        }
+        workgroup_sums(square, s_sum[1]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int n = first + r;
+            if (n >= a.N) break;
+            const float rstd = __builtin_amdgcn_rsqf(square[r] * inverse + a.eps);
+            const bool valid = length_of(a, n) > 0;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                f32x4 y = v[r][j] * rstd * scale[j] + shift[j];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[k] = activate(y[k], kSilu);
+                row.store(static_cast<E *>(a.out) + (size_t)n * a.C, j, valid ? from_f32<E>(y) : Vec4<E>{});
+            }
+            if (a.stats && threadIdx.x == 0) reinterpret_cast<Pair *>(a.stats)[(size_t)n * a.G + g] = Pair{sum[r] * inverse, rstd};
+        }
+    }
+}
+
+template <class E, bool kAligned, int J, bool kSilu>
+__global__ void __launch_bounds__(256) norm_wide_backward_kernel(Norm a)
+{
+    constexpr int R = 4 / J;
+    __shared__ float s_sum[2][4][2 * R];
+    const int g = blockIdx.x % a.G;
+    const WideRow<kAligned, J> row{g * a.D, a.D};
+    f32x4 scale[J], shift[J], p1[J], p2[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        scale[j] = row.parameters(a.scale, j);
+        shift[j] = row.parameters(a.shift, j);
+        p1[j] = p2[j] = splat(0.0f);
+    }
+    const float inverse = 1.0f / (float)a.D;
+    const E *x = static_cast<const E *>(a.x), *grad_out = static_cast<const E *>(a.grad_out);
+    int turn = 0;
+    for (int first = (int)(blockIdx.x / a.G) * R; first < a.N; first += (int)(gridDim.x / a.G) * R) {
+        Vec4<E> xs[R][J], ds[R][J];
+        Pair stats[R];
+        f32x4 xhat[R][J], du[R][J];
+        float sum[2 * R];
+        bool valid[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int n = min(first + r, a.N - 1);
+            valid[r] = first + r < a.N && length_of(a, n) > 0;
+            stats[r] = reinterpret_cast<const Pair *>(a.stats_in)[(size_t)n * a.G + g];
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                xs[r][j] = row.load(x + (size_t)n * a.C, j);
+                ds[r][j] = row.load(grad_out + (size_t)n * a.C, j);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            f32x4 s1 = splat(0.0f), s2 = splat(0.0f);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                xhat[r][j] = (to_f32<E>(xs[r][j]) - stats[r].a) * stats[r].b;
+                du[r][j] = to_f32<E>(ds[r][j]);
+                f32x4 own;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    du[r][j][k] *= slope(xhat[r][j][k] * scale[j][k] + shift[j][k], kSilu);
+                    if (!(valid[r] && row.exists(j, k))) du[r][j][k] = xhat[r][j][k] = 0.0f;
+                }
+                p1[j] += du[r][j];
+                p2[j] += du[r][j] * xhat[r][j];
+                own = scale[j] * du[r][j];
+                s1 += own;
+                s2 += own * xhat[r][j];
+            }
+            sum[2 * r] = across(s1);
+            sum[2 * r + 1] = across(s2);
+        }
+        workgroup_sums(sum, s_sum[turn]);
+        turn ^= 1;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int n = first + r;
+            if (n >= a.N) break;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const f32x4 gx = input_gradient(splat(stats[r].b), scale[j], du[r][j], splat(sum[2 * r] * inverse), xhat[r][j], splat(sum[2 * r + 1] * inverse));
+                row.store(static_cast<E *>(a.grad_x) + (size_t)n * a.C, j, valid[r] ? from_f32<E>(gx) : Vec4<E>{});
+            }
+        }
+    }
+    float *parts = a.parts + (size_t)(blockIdx.x / a.G) * 2 * a.C + row.begin;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (row.exists(j, k)) {
+                parts[row.channel(j, k)] = p1[j][k];
+                parts[a.C + row.channel(j, k)] = p2[j][k];
+            }
+}
+
+// Sums of 64 channels over `rows` rows at a distance of 2 C, by a workgroup of NW waves, which take every NW-th row.
+template <int NW>
+__device__ __forceinline__ void sum_rows_of_tile(const float *__restrict__ parts, int rows, int C, int tile, float *__restrict__ to)
+{
+    __shared__ float s_sum[NW][64];
+    constexpr int kAtOnce = 8;
+    const int lane = threadIdx.x & 63, c = tile * 64 + lane, wave = threadIdx.x >> 6;
+    const float *p = parts + min(c, C - 1);
+    float sum[kAtOnce] = {};
+    int r = wave;
+    for (; r + (kAtOnce - 1) * NW < rows; r += kAtOnce * NW)
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) sum[i] += p[(size_t)(r + NW * i) * 2 * C];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+        if (r + NW * i < rows) sum[i] += p[(size_t)(r + NW * i) * 2 * C];
+    s_sum[wave][lane] = ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
     __syncthreads();
     if (wave != 0 || c >= C) return;
     float all = 0.0f;
-    for (int w = 0; w < 16; ++w) all += s_sum[w][lane];
-    (blockIdx.y ? to_scale : to_shift)[(size_t)blockIdx.z * 2 * C + c] = all;
+    for (int w = 0; w < NW; ++w) all += s_sum[w][lane];
+    to[c] = all;
+}
+// [rows][2][C], in gridDim.z runs: of several to [runs][2][C], of one to the gradients
+__global__ void __launch_bounds__(1024) norm_sum_rows_kernel(const float *__restrict__ parts, int rows, int C, float *to_shift, float *to_scale)
+{
+    const int run = (rows + (int)gridDim.z - 1) / (int)gridDim.z, first = min((int)blockIdx.z * run, rows);
+    sum_rows_of_tile<16>(parts + ((size_t)first * 2 + blockIdx.y) * C, min(run, rows - first), C, blockIdx.x,
+                         (blockIdx.y ? to_scale : to_shift) + (size_t)blockIdx.z * 2 * C);
 }
 
 // ---- stream ------------------------------------------------------------------------------------------------------
@@ -702,29 +915,52 @@ __device__ __forceinline__ int positions_in(const Norm &a, int chunk, int length
     return max(min(min((chunk + 1) * a.chunk, a.T), length) - chunk * a.chunk, 0);
 }
 
-// stats [N][G][2]: a wave a group
-__global__ void __launch_bounds__(64) norm_stats_kernel(Norm a)
+// f(chunk, channel of the group) for this thread's share of the entries of a group, by a workgroup of 256
+template <class F>
+__device__ __forceinline__ void for_entries(const Norm &a, F &&f)
 {
+    int chunk = threadIdx.x / a.D, c = threadIdx.x % a.D;
+    const int chunks_on = 256 / a.D, c_on = 256 % a.D;
+    while (chunk < a.chunks) {
+        f(chunk, c);
+        chunk += chunks_on;
+        c += c_on;
+        if (c >= a.D) {
+            c -= a.D;
+            ++chunk;
+        }
+    }
+}
+// sum over a workgroup of 256; `shared`: four words of the call's own
+__device__ __forceinline__ float workgroup_sum(float v, float *shared)
+{
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (shared[0] + shared[1]) + (shared[2] + shared[3]);
+}
+
+// stats [N][G][2]: a workgroup a group
+__global__ void __launch_bounds__(256) norm_stats_kernel(Norm a)
+{
+    __shared__ float s_sum[2][4];
     const int n = blockIdx.x / a.G, g = blockIdx.x % a.G, length = length_of(a, n);
     const float *p = a.parts + (size_t)n * a.chunks * 2 * a.C + g * a.D;
-    Moments all{0.0f, 0.0f, 0.0f};
-    const long long entries = (long long)a.chunks * a.D;
-    for (long long i = threadIdx.x; i < entries; i += 64) {
-        const int chunk = (int)(i / a.D), c = (int)(i % a.D);
-        all.add(Moments{(float)positions_in(a, chunk, length), p[(size_t)chunk * 2 * a.C + c], p[((size_t)chunk * 2 + 1) * a.C + c]});
-    }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        const Moments o{__shfl_xor(all.n, off, 64), __shfl_xor(all.mean, off, 64), __shfl_xor(all.square, off, 64)};
-        // (the same order on both sides of an exchange, for the same bits)
-        Moments lower = threadIdx.x & off ? o : all;
-        lower.add(threadIdx.x & off ? all : o);
-        all = lower;
-    }
+    // the mean first, then what lies off it: sums whose terms do not wait for each other
+    const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
+    float sum = 0.0f, square = 0.0f;
+    for_entries(a, [&](int chunk, int c) { sum += (float)positions_in(a, chunk, length) * p[(size_t)chunk * 2 * a.C + c]; });
+    const float mean = workgroup_sum(sum, s_sum[0]) * inverse;
+    for_entries(a, [&](int chunk, int c) {
+        const int here = positions_in(a, chunk, length);
+        const float d = p[(size_t)chunk * 2 * a.C + c] - mean;
+        if (here > 0) square += p[((size_t)chunk * 2 + 1) * a.C + c] + (float)here * d * d;
+    });
+    square = workgroup_sum(square, s_sum[1]);
     if (threadIdx.x == 0) {
         float *s = a.stats + (size_t)blockIdx.x * 2;
-        s[0] = all.mean;
-        s[1] = 1.0f / sqrtf((all.n > 0.0f ? all.square / all.n : 0.0f) + a.eps);
+        s[0] = mean;
+        s[1] = 1.0f / sqrtf(square * inverse + a.eps);
     }
 }
 
@@ -819,23 +1055,28 @@ __global__ void __launch_bounds__(256) norm_gradient_sums_kernel(Norm a)
     a.parts[(((size_t)n * a.chunks + chunk) * 2 + which) * a.C + tile * 64 + c] = sum;
 }
 
-// sums [N][G][2] behind parts: S1 / M and S2 / M, a wave a group
-__global__ void __launch_bounds__(64) norm_group_sums_kernel(Norm a)
+// sums [N][G][2] behind parts: S1 / M and S2 / M, a workgroup a group; in the same launch, by the first `channel_groups` workgroups, the
+// sums over all samples and chunks (where there is one run of them)
+__global__ void __launch_bounds__(256) norm_group_sums_kernel(Norm a, int channel_groups)
 {
-    const int n = blockIdx.x / a.G, g = blockIdx.x % a.G, length = length_of(a, n);
+    __shared__ float s_sum[2][4];
+    if ((int)blockIdx.x < channel_groups) {
+        const int tiles = channel_groups / 2, which = blockIdx.x / tiles;
+        sum_rows_of_tile<4>(a.parts + (size_t)which * a.C, a.N * a.chunks, a.C, blockIdx.x % tiles, which ? a.grad_scale : a.grad_shift);
+        return;
+    }
+    const int item = (int)blockIdx.x - channel_groups, n = item / a.G, g = item % a.G, length = length_of(a, n);
     const float *p = a.parts + (size_t)n * a.chunks * 2 * a.C + g * a.D, *scale = a.scale + g * a.D;
     float s1 = 0.0f, s2 = 0.0f;
-    const long long entries = (long long)a.chunks * a.D;
-    for (long long i = threadIdx.x; i < entries; i += 64) {
-        const int chunk = (int)(i / a.D), c = (int)(i % a.D);
+    for_entries(a, [&](int chunk, int c) {
         s1 += scale[c] * p[(size_t)chunk * 2 * a.C + c];
         s2 += scale[c] * p[((size_t)chunk * 2 + 1) * a.C + c];
-    }
-    s1 = wave_sum(s1);
-    s2 = wave_sum(s2);
+    });
+    s1 = workgroup_sum(s1, s_sum[0]);
+    s2 = workgroup_sum(s2, s_sum[1]);
     if (threadIdx.x == 0) {
         const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
-        float *s = a.parts + (size_t)a.N * a.chunks * 2 * a.C + (size_t)blockIdx.x * 2;
+        float *s = a.parts + (size_t)a.N * a.chunks * 2 * a.C + (size_t)item * 2;
         s[0] = s1 * inverse;
         s[1] = s2 * inverse;
     }
@@ -877,7 +1118,7 @@ __global__ void __launch_bounds__(256) norm_gradient_kernel(Norm a)
 }
 
 // ---- which way, and its sizes ------------------------------------------------------------------------------------
-enum Kind { kPosition, kSample, kStream };
+enum Kind { kPosition, kWide, kSample, kStream };
 struct Way {
     Kind kind;
     int threads, rows_each;     // sample: of a workgroup; positions a thread
@@ -887,7 +1128,7 @@ struct Way {
     int part_rows;              // rows [2][C] of channel sums that the reverse pass leaves
 };
 
-constexpr int kMostPositionTile = 2048, kPositionRows = 4;      // channels of a group, samples at once (of groups up to 256)
+constexpr int kMostPositionTile = 512, kPositionRows = 4;       // channels of a group, samples at once (of groups up to 256)
 
 // Rows are added up in two launches from this many on: one alone reads them with 2 C / 64 workgroups.
 constexpr int kManyRows = 1024, kRuns = 64;
@@ -896,6 +1137,16 @@ Way way_of(const esrnn_group_norm_shape &s)
 {
     Way w{};
     const int D = s.C / s.G;
+    if (s.T == 1 && D > kMostPositionTile && D <= 4096) {
+        w.kind = kWide;
+        w.tiles = s.G;
+        w.pieces = D <= 1024 ? 1 : D <= 2048 ? 2 : 4;
+        const int64_t most = ((int64_t)s.N * w.pieces + 3) / 4;
+        w.forward_groups = (int)std::min<int64_t>(most, std::max(1, 2048 / s.G));
+        w.backward_groups = (int)std::min<int64_t>(most, std::max(1, 1024 / s.G));
+        w.part_rows = w.backward_groups;
+        return w;
+    }
     if (s.T == 1 && D <= kMostPositionTile) {
         // whole groups up to 256 channels, of which a few groups less may be whole groups of four channels
         int groups = std::max(1, std::min(s.G, 256 / D));
@@ -916,23 +1167,28 @@ Way way_of(const esrnn_group_norm_shape &s)
         w.part_rows = w.backward_groups;
         return w;
     }
-    // sample: whole groups side by side up to 64 channels (a run of 128 bytes of bf16), as many positions as fit
-    int groups = std::max(1, std::min(s.G, 64 / D));
-    for (int fewer = groups; fewer > 1; --fewer)        // (whole groups of four channels, if a few groups less give them)
-        if (fewer * D % 4 == 0) {
-            groups = fewer;
+    // sample: whole groups side by side up to 64 channels (a run of 128 bytes of bf16), as many positions as fit; up to 32 channels only for few
+    // workgroups, where the launches of the stream way are what counts (2 samples of 1000 x 96 fp32, forward 11 against 15 us; 64 of
+    // 1024 x 512 bf16: 58 against 46)
+    constexpr int kSplits[5][3] = {{64, 256, 4}, {64, 256, 16}, {64, 1024, 4}, {64, 1024, 8}, {32, 1024, 8}};   // channels, threads, positions each
+    for (const auto &split : kSplits) {
+        if (split[0] < 64 && (int64_t)s.N * s.C > 256 * 32) break;
+        int groups = std::max(1, std::min(s.G, split[0] / D));
+        for (int fewer = groups; fewer > 1; --fewer)        // (whole groups of four channels, if a few groups less give them)
+            if (fewer * D % 4 == 0) {
+                groups = fewer;
+                break;
+            }
+        w.tile = groups * D;
+        for (w.log_w = 0; 4 << w.log_w < w.tile; ++w.log_w) {}
+        w.tiles = (s.G + groups - 1) / groups;
+        if (w.tile <= kMostTile && split[1] >> w.log_w >= 1 && (int64_t)s.N * w.tiles * split[1] <= (int64_t(1) << 31) &&
+            (int64_t)s.T <= (int64_t)(split[1] >> w.log_w) * split[2]) {
+            w.kind = kSample;
+            w.threads = split[1], w.rows_each = split[2];
             break;
         }
-    w.tile = groups * D;
-    for (w.log_w = 0; 4 << w.log_w < w.tile; ++w.log_w) {}
-    w.tiles = (s.G + groups - 1) / groups;
-    for (int threads : {256, 1024})
-        for (int rows : {4, 16})
-            if (w.kind != kSample && w.tile <= kMostTile && threads >> w.log_w >= 1 && (int64_t)s.N * w.tiles * threads <= (int64_t(1) << 31) &&
-                (int64_t)s.T <= (int64_t)(threads >> w.log_w) * rows) {
-                w.kind = kSample;
-                w.threads = threads, w.rows_each = rows;
-            }
+    }
     w.part_rows = s.N;
     if (w.kind == kSample) return w;
     w.kind = kStream;
@@ -984,9 +1240,7 @@ void with_pieces(int pieces, bool aligned, bool quads, F &&f)
     using One = std::integral_constant<int, 1>;
     switch (pieces) {
     case 1: return layout(One{}, std::integral_constant<int, kPositionRows>{});
-    case 2: return layout(std::integral_constant<int, 2>{}, One{});
-    case 4: return layout(std::integral_constant<int, 4>{}, One{});
-    default: return layout(std::integral_constant<int, 8>{}, One{});
+    default: return layout(std::integral_constant<int, 2>{}, One{});
     }
 }
 
@@ -1009,6 +1263,16 @@ void position_backward(const esrnn_group_norm_shape &s, Norm a, const Way &w, bo
     with_pieces(w.pieces, fours, quads, [&](auto j, auto r, auto al, auto q) {
         norm_position_backward_kernel<E, al(), q(), j(), r(), kSilu><<<w.tiles * w.backward_groups, 256, lds, st>>>(a);
     });
+}
+
+template <class F>
+void with_wide_pieces(int pieces, F &&f)
+{
+    switch (pieces) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    default: return f(std::integral_constant<int, 4>{});
+    }
 }
 
 // The sums over `rows` rows at parts; `more`: room for kRuns rows.
@@ -1041,7 +1305,7 @@ hipError_t launch_group_norm_forward(const esrnn_group_norm_shape &s, const Grou
     const Way w = way_of(s);
     Norm a = norm_of(s, f, w);
     const size_t group = 4 * element_bytes(s.dtype);
-    const bool aligned = s.C % 4 == 0 && aligned_to(f.x, group) && aligned_to(f.out, group);
+    const bool aligned = s.C % 4 == 0 && aligned_to(f.x, group) && aligned_to(f.out, group), fours = aligned && a.D % 4 == 0;
     return with_element(s.dtype, [&](auto e) {
         using E = decltype(e);
         with_flags(aligned && (w.kind != kSample || w.tile % 4 == 0), a.silu, [&](auto al, auto silu) {
@@ -1049,18 +1313,25 @@ hipError_t launch_group_norm_forward(const esrnn_group_norm_shape &s, const Grou
                 position_forward<E, silu()>(s, a, w, aligned, st);
                 return;
             }
+            if (w.kind == kWide) {
+                with_wide_pieces(w.pieces, [&](auto j) {
+                    if (fours) norm_wide_forward_kernel<E, true, j(), silu()><<<s.G * w.forward_groups, 256, 0, st>>>(a);
+                    else norm_wide_forward_kernel<E, false, j(), silu()><<<s.G * w.forward_groups, 256, 0, st>>>(a);
+                });
+                return;
+            }
             if (w.kind == kSample) {
                 const unsigned grid = (unsigned)(s.N * w.tiles);
                 if (w.threads == 256 && w.rows_each == 4) norm_sample_forward_kernel<E, al(), 256, 4, silu()><<<grid, 256, 0, st>>>(a);
                 else if (w.threads == 256) norm_sample_forward_kernel<E, al(), 256, 16, silu()><<<grid, 256, 0, st>>>(a);
                 else if (w.rows_each == 4) norm_sample_forward_kernel<E, al(), 1024, 4, silu()><<<grid, 1024, 0, st>>>(a);
-                else norm_sample_forward_kernel<E, al(), 1024, 16, silu()><<<grid, 1024, 0, st>>>(a);
+                else norm_sample_forward_kernel<E, al(), 1024, 8, silu()><<<grid, 1024, 0, st>>>(a);
                 return;
             }
             if (!a.stats) a.stats = a.parts + groups_at(s, w);
             const dim3 grid((unsigned)(s.N * w.tiles), w.chunks);
             norm_moments_kernel<E, al()><<<grid, 256, 0, st>>>(a);
-            norm_stats_kernel<<<(unsigned)(s.N * s.G), 64, 0, st>>>(a);
+            norm_stats_kernel<<<(unsigned)(s.N * s.G), 256, 0, st>>>(a);
             norm_apply_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
         });
         return hipGetLastError();
@@ -1073,6 +1344,7 @@ hipError_t launch_group_norm_backward(const esrnn_group_norm_shape &s, const Gro
     const Norm a = norm_of(s, f, w);
     const size_t group = 4 * element_bytes(s.dtype);
     const bool aligned = s.C % 4 == 0 && aligned_to(f.x, group) && aligned_to(f.grad_out, group) && aligned_to(f.grad_x, group);
+    const bool fours = aligned && a.D % 4 == 0;
     return with_element(s.dtype, [&](auto e) {
         using E = decltype(e);
         with_flags(aligned && (w.kind != kSample || w.tile % 4 == 0), a.silu, [&](auto al, auto silu) {
@@ -1082,19 +1354,28 @@ hipError_t launch_group_norm_backward(const esrnn_group_norm_shape &s, const Gro
                 sum_rows(a, w.part_rows, runs, st);
                 return;
             }
+            if (w.kind == kWide) {
+                with_wide_pieces(w.pieces, [&](auto j) {
+                    if (fours) norm_wide_backward_kernel<E, true, j(), silu()><<<s.G * w.backward_groups, 256, 0, st>>>(a);
+                    else norm_wide_backward_kernel<E, false, j(), silu()><<<s.G * w.backward_groups, 256, 0, st>>>(a);
+                });
+                sum_rows(a, w.part_rows, runs, st);
+                return;
+            }
             if (w.kind == kSample) {
                 const unsigned grid = (unsigned)(s.N * w.tiles);
                 if (w.threads == 256 && w.rows_each == 4) norm_sample_backward_kernel<E, al(), 256, 4, silu()><<<grid, 256, 0, st>>>(a);
                 else if (w.threads == 256) norm_sample_backward_kernel<E, al(), 256, 16, silu()><<<grid, 256, 0, st>>>(a);
                 else if (w.rows_each == 4) norm_sample_backward_kernel<E, al(), 1024, 4, silu()><<<grid, 1024, 0, st>>>(a);
-                else norm_sample_backward_kernel<E, al(), 1024, 16, silu()><<<grid, 1024, 0, st>>>(a);
+                else norm_sample_backward_kernel<E, al(), 1024, 8, silu()><<<grid, 1024, 0, st>>>(a);
                 sum_rows(a, w.part_rows, runs, st);
                 return;
             }
             const dim3 grid((unsigned)(s.N * w.tiles), w.chunks);
             norm_gradient_sums_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
-            norm_group_sums_kernel<<<(unsigned)(s.N * s.G), 64, 0, st>>>(a);
-            sum_rows(a, w.part_rows, runs, st);
+            const int channel_groups = w.part_rows < kManyRows ? 2 * ((s.C + 63) / 64) : 0;
+            norm_group_sums_kernel<<<(unsigned)(channel_groups + s.N * s.G), 256, 0, st>>>(a, channel_groups);
+            if (!channel_groups) sum_rows(a, w.part_rows, runs, st);
             norm_gradient_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
         });
         return hipGetLastError();

@@ -215,7 +215,6 @@ esrnn_status esrnn_adamw_create(const esrnn_adamw_tensor *tensors, int32_t count
             e.weight_decay = t.weight_decay;
             e.first_chunk = (int)chunks;
             e.grad_dtype = (unsigned char)t.grad_dtype, e.copy_dtype = (unsigned char)t.copy_dtype;
-            e.aligned = aligned_to(t.param, 16) && aligned_to(t.grad, 4 * element_bytes(t.grad_dtype)) && aligned_to(t.copy, 8);
             flat += (t.n + ESRNN_ADAMW_BLOCK - 1) / ESRNN_ADAMW_BLOCK * ESRNN_ADAMW_BLOCK;
             chunks += (t.n + kAdamWChunk - 1) / kAdamWChunk;
             if (chunks > (1 << 23)) st = ESRNN_ERR_CONFIG;      // (workgroups of a launch; 1.7e10 elements)

@@ -9,6 +9,11 @@ namespace esrnn {
 
 template <class E>
 using Vec4 = E __attribute__((ext_vector_type(4)));
+// the same at the alignment of one element: the hardware's global accesses ask for no more
+template <class E>
+struct Loose {
+    typedef E Four __attribute__((ext_vector_type(4), aligned(sizeof(E))));
+};
 
 // f(element type tag) for the element type of a call (checked before)
 template <class F>
@@ -87,10 +92,10 @@ inline bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<u
 inline size_t element_bytes(int dtype) { return dtype == ESRNN_F32 ? 4 : 2; }
 
 // ---- gated linear recurrence (recurrence_kernels.hip) ----
-// Waves of a workgroup, positions of a block, the blocks of a sequence; ahead: every block has a workgroup of its own, and its maps go
+// Waves of a workgroup, positions of a thread and of a block, the blocks of a sequence; ahead: every block has a workgroup of its own, and its maps go
 // through `words` floats of the workspace, by whole groups of 2^log_group blocks too.
 struct RecurrencePlan {
-    int waves, block, blocks;
+    int waves, steps, block, blocks;
     bool ahead;
     int log_group, groups;
     size_t tickets, words;
@@ -133,7 +138,7 @@ struct AdamWEntry {
     long long n, flat;          // elements; where the tensor begins in the moments
     float weight_decay;
     int first_chunk;
-    unsigned char grad_dtype, copy_dtype, aligned;      // aligned: every group of four elements is at a multiple of its size
+    unsigned char grad_dtype, copy_dtype;
 };
 struct AdamWUpdate {
     const AdamWEntry *entries;

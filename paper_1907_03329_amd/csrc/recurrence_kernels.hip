@@ -22,7 +22,6 @@ namespace esrnn {
 
 namespace {
 
-constexpr int kSteps = 8;       // positions of a thread
 constexpr int kTile = 64;       // channels of a workgroup
 // rows of 64 channels from which a workgroup takes a whole sequence
 constexpr int kLinesAlone = 256;
@@ -326,7 +325,7 @@ __device__ __forceinline__ Line line_of(const Args &a, int line)
     return Line(a.words + kTicket * (size_t)(a.B * a.tiles) + (size_t)line * (a.blocks + a.groups) * kMap, a.blocks, a.groups);
 }
 
-template <class E, bool kFast, int kKind, int NW, bool kAhead>
+template <class E, bool kFast, int kKind, int kSteps, int NW, bool kAhead>
 __global__ void __launch_bounds__(64 * NW, NW == 8 ? 2 : kAhead ? 3 : 4) recurrence_forward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
@@ -386,7 +385,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 ? 2 : kAhead ? 3 : 4) recurre
     }
 }
 
-template <class E, bool kFast, int kKind, int NW, bool kAhead>
+template <class E, bool kFast, int kKind, int kSteps, int NW, bool kAhead>
 __global__ void __launch_bounds__(64 * NW, 2) recurrence_backward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
@@ -546,7 +545,8 @@ RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s)
     const long long lines = (long long)s.B * ((s.C + kTile - 1) / kTile);
     p.ahead = s.T > 128 && lines < kLinesAlone && lines * ((s.T + 127) / 128) <= (1 << 21);
     p.waves = p.ahead ? 4 : s.T <= 32 ? 1 : s.T <= 128 ? 2 : s.T <= 256 ? 4 : 8;
-    p.block = 4 * kSteps * p.waves;
+    p.steps = s.T <= 8 ? 2 : 8;
+    p.block = 4 * p.steps * p.waves;
     p.blocks = (s.T + p.block - 1) / p.block;
     if (p.ahead) {
         for (p.log_group = 4; 1LL << 2 * p.log_group < p.blocks; ++p.log_group) {}
@@ -583,15 +583,16 @@ hipError_t launch_recurrence_forward(const esrnn_recurrence_shape &s, const Recu
             using E = decltype(e);
             with_variant(all_fast, s.kind, [&](auto al, auto kind) {
                 const unsigned lines = (unsigned)(s.B * a.tiles);
-                const auto launch = [&](auto waves) {
-                    recurrence_forward_kernel<E, al(), kind(), waves(), ahead()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
+                const auto launch = [&](auto steps, auto waves) {
+                    recurrence_forward_kernel<E, al(), kind(), steps(), waves(), ahead()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
                 };
-                if constexpr (ahead()) launch(Int<4>{});
+                if constexpr (ahead()) launch(Int<8>{}, Int<4>{});
+                else if (p.steps == 2) launch(Int<2>{}, Int<1>{});
                 else switch (p.waves) {
-                case 1: return launch(Int<1>{});
-                case 2: return launch(Int<2>{});
-                case 4: return launch(Int<4>{});
-                default: return launch(Int<8>{});
+                case 1: return launch(Int<8>{}, Int<1>{});
+                case 2: return launch(Int<8>{}, Int<2>{});
+                case 4: return launch(Int<8>{}, Int<4>{});
+                default: return launch(Int<8>{}, Int<8>{});
                 }
             });
             return hipGetLastError();
@@ -612,15 +613,16 @@ hipError_t launch_recurrence_backward(const esrnn_recurrence_shape &s, const Rec
             using E = decltype(e);
             with_variant(all_fast, s.kind, [&](auto al, auto kind) {
                 const unsigned lines = (unsigned)(s.B * a.tiles);
-                const auto launch = [&](auto waves) {
-                    recurrence_backward_kernel<E, al(), kind(), waves(), ahead()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
+                const auto launch = [&](auto steps, auto waves) {
+                    recurrence_backward_kernel<E, al(), kind(), steps(), waves(), ahead()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
                 };
-                if constexpr (ahead()) launch(Int<4>{});
+                if constexpr (ahead()) launch(Int<8>{}, Int<4>{});
+                else if (p.steps == 2) launch(Int<2>{}, Int<1>{});
                 else switch (p.waves) {
-                case 1: return launch(Int<1>{});
-                case 2: return launch(Int<2>{});
-                case 4: return launch(Int<4>{});
-                default: return launch(Int<8>{});
+                case 1: return launch(Int<8>{}, Int<1>{});
+                case 2: return launch(Int<8>{}, Int<2>{});
+                case 4: return launch(Int<8>{}, Int<4>{});
+                default: return launch(Int<8>{}, Int<8>{});
                 }
             });
             return hipGetLastError();
