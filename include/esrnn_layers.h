@@ -144,8 +144,9 @@ esrnn_status esrnn_adamw_destroy(esrnn_adamw *h);
 /* Elements of each flat moment array: a multiple of ESRNN_ADAMW_BLOCK. */
 esrnn_status esrnn_adamw_state_elements(const esrnn_adamw *h, size_t *n);
 esrnn_status esrnn_adamw_workspace_bytes(const esrnn_adamw *h, size_t *bytes);
-/* Writes the list of tensors into the workspace.  Once, before the first update with this workspace, and ordered before it. */
-esrnn_status esrnn_adamw_bind(const esrnn_adamw *h, void *workspace, void *stream);
+/* Writes the list of tensors into the workspace.  Once, ordered before the first update, which returns ESRNN_ERR_ORDER without it or with
+ * another workspace than the last one bound; nothing else may write to the workspace from then on. */
+esrnn_status esrnn_adamw_bind(esrnn_adamw *h, void *workspace, void *stream);
 /* step counts from 1.  Moments are zero before the first step: 32 bits m, v; 8 bits m, r, m_scale, r_scale (v NULL), else
  * r and the scales NULL.  norm: one float or NULL; written if clip_norm > 0. */
 esrnn_status esrnn_adamw_update(const esrnn_adamw *h, const esrnn_adamw_config *opt, int32_t step, void *m, float *v, void *r,

@@ -60,6 +60,7 @@ struct esrnn_adamw {
     AdamWEntry *entry;
     int count, state_bits, chunks;
     int64_t elements;           // of a flat moment array
+    const void *bound;          // the workspace that has the table, or null
 };
 
 namespace {
@@ -199,6 +200,7 @@ esrnn_status esrnn_adamw_create(const esrnn_adamw_tensor *tensors, int32_t count
         return ESRNN_ERR_HIP;
     }
     h->entry = entry;
+    h->bound = nullptr;
     esrnn_status st = ESRNN_OK;
     int64_t flat = 0, chunks = 0;
     for (int32_t i = 0; i < count && st == ESRNN_OK; ++i) {
@@ -252,13 +254,14 @@ esrnn_status esrnn_adamw_workspace_bytes(const esrnn_adamw *h, size_t *bytes)
     return ESRNN_OK;
 }
 
-esrnn_status esrnn_adamw_bind(const esrnn_adamw *h, void *workspace, void *stream)
+esrnn_status esrnn_adamw_bind(esrnn_adamw *h, void *workspace, void *stream)
 {
     if (!h || !workspace) return ESRNN_ERR_NULL;
     if (!aligned_to(workspace, 256)) return ESRNN_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
     ESRNN_TRY(launch_adamw_bind(h->entry, h->count, reinterpret_cast<AdamWEntry *>(ws + adamw_entries_at()),
                                 reinterpret_cast<int *>(ws + adamw_owner_at(*h)), h->chunks, static_cast<hipStream_t>(stream)));
+    h->bound = workspace;
     return ESRNN_OK;
 }
 
@@ -275,7 +278,7 @@ esrnn_status esrnn_adamw_update(const esrnn_adamw *h, const esrnn_adamw_config *
     if (!aligned_to(m, h->state_bits == 32 ? 16 : 4) || !aligned_to(v, 16) || !aligned_to(r, 4) || !floats_aligned(m_scale) ||
         !floats_aligned(r_scale) || !floats_aligned(norm))
         return ESRNN_ERR_CONFIG;
-    if (!aligned_to(workspace, 256)) return ESRNN_ERR_WORKSPACE;
+    if (workspace != h->bound) return ESRNN_ERR_ORDER;
     char *ws = static_cast<char *>(workspace);
     AdamWUpdate u{};
     u.entries = reinterpret_cast<const AdamWEntry *>(ws + adamw_entries_at());

@@ -326,7 +326,7 @@ __device__ __forceinline__ Line line_of(const Args &a, int line)
 }
 
 template <class E, bool kFast, int kKind, int kSteps, int NW, bool kAhead>
-__global__ void __launch_bounds__(64 * NW, NW == 8 ? 2 : kAhead ? 3 : 4) recurrence_forward_kernel(Args a)
+__global__ void __launch_bounds__(64 * NW, NW == 8 || !kFast ? 2 : kAhead ? 3 : 4) recurrence_forward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
     __shared__ f32x4 lds[2][NW][2][16];
@@ -544,7 +544,7 @@ RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s)
     RecurrencePlan p{};
     const long long lines = (long long)s.B * ((s.C + kTile - 1) / kTile);
     p.ahead = s.T > 128 && lines < kLinesAlone && lines * ((s.T + 127) / 128) <= (1 << 21);
-    p.waves = p.ahead ? 4 : s.T <= 32 ? 1 : s.T <= 128 ? 2 : s.T <= 256 ? 4 : 8;
+    p.waves = p.ahead ? 4 : s.T <= 32 ? 1 : s.T <= 64 || (s.T <= 128 && lines >= 1024) ? 2 : s.T <= 256 ? 4 : 8;
     p.steps = s.T <= 8 ? 2 : 8;
     p.block = 4 * p.steps * p.waves;
     p.blocks = (s.T + p.block - 1) / p.block;
