@@ -1,6 +1,6 @@
 // AdamW over many tensors at once (include/esrnn_layers.h).
 //
-// All tensors are one list of chunks of kChunk elements, a workgroup each, so that a list of any length is one launch (two with
+// All tensors are one list of chunks of 2048 elements (of 1024 in short lists), a workgroup each, so that a list of any length is one launch (two with
 // clipping: sums of squares in a fixed order first, which every workgroup of the update adds up in the same order).  A chunk finds its
 // tensor through a table in the workspace.  A wave has whole blocks of 256 elements, four neighbours a lane: the block of an 8-bit
 // moment's scale is one wave's, and its largest magnitude takes six steps within the wave.
@@ -37,22 +37,20 @@ __device__ __forceinline__ void load_groups(const void *base, long long first, l
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[j][k] = first + 256 * j + k < n ? (float)p[256 * j + k] : 0.0f;
 }
-template <class E, int N>
-__device__ __forceinline__ void store_groups(void *base, long long first, long long n, bool whole, const f32x4 (&v)[N])
+// one of them
+template <class E>
+__device__ __forceinline__ void store_group(void *base, long long at, long long n, bool whole, f32x4 v)
 {
     typedef typename Loose<E>::Four Four;
-    auto *p = (__attribute__((address_space(1))) E *)base + first;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const Vec4<E> r = from_f32<E>(v[j]);
-        if (whole) {
-            *reinterpret_cast<__attribute__((address_space(1))) Four *>(p + 256 * j) = r;
-            continue;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (first + 256 * j + k < n) p[256 * j + k] = r[k];
+    auto *p = (__attribute__((address_space(1))) E *)base + at;
+    const Vec4<E> r = from_f32<E>(v);
+    if (whole) {
+        *reinterpret_cast<__attribute__((address_space(1))) Four *>(p) = r;
+        return;
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (at + k < n) p[k] = r[k];
 }
 template <int N>
 __device__ __forceinline__ void load_grad(const AdamWEntry &e, long long first, bool whole, f32x4 (&g)[N])
@@ -62,10 +60,11 @@ __device__ __forceinline__ void load_grad(const AdamWEntry &e, long long first, 
     else load_groups<float>(e.grad, first, e.n, whole, g);
 }
 
+template <int kChunk>
 __global__ void __launch_bounds__(1024) adamw_norm_kernel(const AdamWEntry *__restrict__ entries, const int *__restrict__ owner, int chunks,
                                                           double *__restrict__ partial)
 {
-    constexpr int kGroups = kAdamWChunk / 256;
+    constexpr int kGroups = kChunk / 256;
     __shared__ double s_wave[16];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     double acc = 0.0;       // (squares of fp32 numbers do not overflow)
@@ -75,9 +74,9 @@ __global__ void __launch_bounds__(1024) adamw_norm_kernel(const AdamWEntry *__re
     AdamWEntry e = chunk < chunks ? entries[owner[chunk]] : AdamWEntry{};
     while (chunk < chunks) {
         const int next = chunk + step;
-        const long long first = (long long)(chunk - e.first_chunk) * kAdamWChunk;
+        const long long first = (long long)(chunk - e.first_chunk) * kChunk;
         f32x4 g[kGroups];
-        load_grad(e, first + 4 * lane, first + kAdamWChunk <= e.n, g);
+        load_grad(e, first + 4 * lane, first + kChunk <= e.n, g);
         e = entries[owner[min(next, chunks - 1)]];
 #pragma unroll
         for (int j = 0; j < kGroups; ++j)
@@ -138,13 +137,13 @@ __device__ __forceinline__ void moments(f32x4 &m, f32x4 &v, f32x4 g, const AdamW
 }
 
 // kBits: of the moments.
-template <int kBits>
+template <int kBits, int kChunk>
 __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
 {
-    constexpr int kGroups = kAdamWChunk / 1024;
+    constexpr int kGroups = kChunk / 1024;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, chunk = blockIdx.x;
     const AdamWEntry e = u.entries[u.owner[chunk]];
-    const long long first = (long long)(chunk - e.first_chunk) * kAdamWChunk + wave * (256 * kGroups) + 4 * lane;
+    const long long first = (long long)(chunk - e.first_chunk) * kChunk + wave * (256 * kGroups) + 4 * lane;
     const long long flat = e.flat + first;      // place in the moments
 
     const bool whole = first - 4 * lane + 256 * kGroups <= e.n;
@@ -205,6 +204,11 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
             root[k] = sqrtf(v[j][k]);
             p[j][k] = keep * p[j][k] - u.rate * m[j][k] * fast_rcp(root[k] * u.root_correction + u.eps);
         }
+        store_group<float>(e.param, first + 256 * j, e.n, whole, p[j]);
+        if (e.copy) {
+            if (e.copy_dtype == ESRNN_BF16) store_group<__bf16>(e.copy, first + 256 * j, e.n, whole, p[j]);
+            else store_group<_Float16>(e.copy, first + 256 * j, e.n, whole, p[j]);
+        }
         if (kBits == 32) {
             *reinterpret_cast<f32x4 *>(static_cast<float *>(u.m) + flat + 256 * j) = m[j];
             *reinterpret_cast<f32x4 *>(u.v + flat + 256 * j) = v[j];
@@ -234,10 +238,6 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
             u.r_scale[(flat + 256 * j) >> 8] = sr.scale;
         }
     }
-    store_groups<float>(e.param, first, e.n, whole, p);
-    if (!e.copy) return;
-    if (e.copy_dtype == ESRNN_BF16) store_groups<__bf16>(e.copy, first, e.n, whole, p);
-    else store_groups<_Float16>(e.copy, first, e.n, whole, p);
 }
 
 // The table comes to the device as arguments of launches: no copy from host memory that might still be read after the call.
@@ -277,18 +277,29 @@ hipError_t launch_adamw_bind(const AdamWEntry *host, int count, AdamWEntry *entr
     return hipGetLastError();
 }
 
-hipError_t launch_adamw_update(AdamWUpdate u, int chunks, double *partial, int state_bits, hipStream_t st)
+namespace {
+
+template <int kChunk>
+hipError_t launch_update(AdamWUpdate u, int chunks, double *partial, int state_bits, hipStream_t st)
 {
     if (u.clip_norm > 0.0f) {
         u.partial = partial;
         u.n_partial = std::min((chunks + 15) / 16, kAdamWNormBlocks);
-        adamw_norm_kernel<<<u.n_partial, 1024, 0, st>>>(u.entries, u.owner, chunks, partial);
+        adamw_norm_kernel<kChunk><<<u.n_partial, 1024, 0, st>>>(u.entries, u.owner, chunks, partial);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (state_bits == 32) adamw_update_kernel<32><<<chunks, 256, 0, st>>>(u);
-    else adamw_update_kernel<8><<<chunks, 256, 0, st>>>(u);
+    if (state_bits == 32) adamw_update_kernel<32, kChunk><<<chunks, 256, 0, st>>>(u);
+    else adamw_update_kernel<8, kChunk><<<chunks, 256, 0, st>>>(u);
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_adamw_update(const AdamWUpdate &u, int chunk, int chunks, double *partial, int state_bits, hipStream_t st)
+{
+    return chunk == kAdamWChunk ? launch_update<kAdamWChunk>(u, chunks, partial, state_bits, st)
+                                : launch_update<kAdamWSmallChunk>(u, chunks, partial, state_bits, st);
 }
 
 }  // namespace esrnn

@@ -58,7 +58,7 @@ bool group_norm_sizes(const esrnn_group_norm_shape &s)
 
 struct esrnn_adamw {
     AdamWEntry *entry;
-    int count, state_bits, chunks;
+    int count, state_bits, chunk, chunks;       // elements of a chunk, chunks
     int64_t elements;           // of a flat moment array
     const void *bound;          // the workspace that has the table, or null
 };
@@ -215,7 +215,6 @@ esrnn_status esrnn_adamw_create(const esrnn_adamw_tensor *tensors, int32_t count
             e = AdamWEntry{};
             e.param = t.param, e.grad = t.grad, e.copy = t.copy, e.n = t.n, e.flat = flat;
             e.weight_decay = t.weight_decay;
-            e.first_chunk = (int)chunks;
             e.grad_dtype = (unsigned char)t.grad_dtype, e.copy_dtype = (unsigned char)t.copy_dtype;
             flat += (t.n + ESRNN_ADAMW_BLOCK - 1) / ESRNN_ADAMW_BLOCK * ESRNN_ADAMW_BLOCK;
             chunks += (t.n + kAdamWChunk - 1) / kAdamWChunk;
@@ -226,6 +225,12 @@ esrnn_status esrnn_adamw_create(const esrnn_adamw_tensor *tensors, int32_t count
         delete[] entry;
         delete h;
         return st;
+    }
+    h->chunk = chunks <= kAdamWFewChunks ? kAdamWSmallChunk : kAdamWChunk;
+    chunks = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        entry[i].first_chunk = (int)chunks;
+        chunks += (entry[i].n + h->chunk - 1) / h->chunk;
     }
     h->count = count, h->state_bits = state_bits, h->chunks = (int)chunks, h->elements = flat;
     *out = h;
@@ -289,7 +294,7 @@ esrnn_status esrnn_adamw_update(const esrnn_adamw *h, const esrnn_adamw_config *
     u.root_correction = (float)(1.0 / std::sqrt(1.0 - std::pow(opt->beta2, (double)step)));
     u.key = opt->seed * 0x9E3779B1u + (uint32_t)step * 0x85EBCA77u;
     u.m = m, u.v = v, u.r = r, u.m_scale = m_scale, u.r_scale = r_scale, u.norm = norm;
-    ESRNN_TRY(launch_adamw_update(u, h->chunks, reinterpret_cast<double *>(ws), h->state_bits, static_cast<hipStream_t>(stream)));
+    ESRNN_TRY(launch_adamw_update(u, h->chunk, h->chunks, reinterpret_cast<double *>(ws), h->state_bits, static_cast<hipStream_t>(stream)));
     return ESRNN_OK;
 }
 

@@ -87,6 +87,29 @@ def test_three_steps(grad, off, clip):
     assert not opt.m[~inside].any() and not opt.v[~inside].any()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad,off", [("float32", 0), ("bfloat16", 1)])
+def test_long_lists(bits, grad, off):
+    """(larger chunks; the last of a tensor is not whole)"""
+    import torch
+    rng = np.random.default_rng(21)
+    sizes = [1500001, 77, 700003, 2048 * 3, 1]
+    params, grads, ref = problem(rng, sizes, grad, off)
+    opt = layers.AdamW(params, grads, weight_decay=0.1, clip_norm=3.0, state_bits=bits, seed=4, **OPT)
+    opt.step(1)
+    factor = min(1.0, 3.0 / (np.sqrt(sum((g ** 2).sum() for _, g in ref)) + 1e-6))
+    for i, (r, (p, g)) in enumerate(zip(ranges(opt, sizes), ref)):
+        wp, wm, wv = rule(p, g, 0.0, 0.0, 1, decay=0.1, factor=factor, **OPT)
+        close(params[i], wp, i)
+        if bits == 32:
+            close(opt.m[r], wm, ("m", i))
+            close(opt.v[r], wv, ("v", i))
+        else:       # within the spacing of e4m3, an eighth, and of its smallest codes
+            scale = opt.m_scale.repeat_interleave(BLOCK)[r].double().cpu().numpy()
+            q = opt.m[r].float().double().cpu().numpy()
+            assert (np.abs(q * scale - wm) <= np.abs(wm) / 8 + 2.0 ** -9 * scale * 1.001).all()
+
+
 def test_large_steps_keep_the_bias_correction():
     """1 - beta^step for beta near one and steps from 1 to a million."""
     import torch
