@@ -103,12 +103,24 @@ __device__ __forceinline__ int wave_max_bits(int v)
     return v;
 }
 
-__device__ __forceinline__ unsigned random_word(unsigned long long place, unsigned key)
+// of a place's lower word, and the key with what its upper word adds
+__device__ __forceinline__ unsigned key_of(long long place, unsigned key) { return (unsigned)(place >> 32) * 0xC2B2AE35u ^ key; }
+__device__ __forceinline__ unsigned random_word(unsigned place, unsigned key)
 {
-    unsigned w = (unsigned)place ^ (unsigned)(place >> 32) * 0xC2B2AE35u ^ key;
+    unsigned w = place ^ key;
     w = (w ^ w >> 16) * 0x7FEB352Du;
     w = (w ^ w >> 15) * 0x846CA68Bu;
     return w ^ w >> 16;
+}
+
+// sqrt, correctly rounded for numbers that are no denormals (and to a unit in the last place for those): the hardware's root is off by one
+// unit at most, and which of the three it has to be shows in the sign of x - root (root +- a unit).  Zero, infinity and NaN stay.
+__device__ __forceinline__ float root_of(float x)
+{
+    const float s = __builtin_amdgcn_sqrtf(x);
+    const float below = __builtin_bit_cast(float, __builtin_bit_cast(int, s) - 1), above = __builtin_bit_cast(float, __builtin_bit_cast(int, s) + 1);
+    const float down = __builtin_fmaf(-below, s, x), up = __builtin_fmaf(-above, s, x);
+    return up > 0.0f ? above : down <= 0.0f ? below : s;
 }
 
 struct Scale {
@@ -121,12 +133,10 @@ __device__ __forceinline__ Scale scale_of(int most_bits)
     if (most_bits >= 0x7f800000) return {__builtin_nanf(""), 0.0f, false};
     return scale > kLeastScale ? Scale{scale, 1.0f / scale, true} : Scale{0.0f, 0.0f, true};
 }
+// a magnitude as the float whose upper 12 bits are its code, rounded down
+__device__ __forceinline__ unsigned scaled(float magnitude, const Scale &s) { return __builtin_bit_cast(unsigned, magnitude * s.inverse * kToCode); }
 // 16 random bits behind the three of the code's mantissa, of the 20 that are cut off: up with the probability of what is cut off
-__device__ __forceinline__ unsigned code_of(float magnitude, const Scale &s, unsigned bits16)
-{
-    const unsigned y = __builtin_bit_cast(unsigned, magnitude * s.inverse * kToCode);
-    return (y + (bits16 << 4)) >> 20;
-}
+__device__ __forceinline__ unsigned code_of(unsigned y, unsigned bits16) { return (y + (bits16 << 4)) >> 20; }
 
 // Every operation rounded by itself, as an elementwise program rounds them: which of two codes a moment takes hangs on its last bits.
 __device__ __forceinline__ void moments(f32x4 &m, f32x4 &v, f32x4 g, const AdamWUpdate &u)
@@ -201,7 +211,7 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
         moments(m[j], v[j], g[j] * scale, u);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            root[k] = sqrtf(v[j][k]);
+            root[k] = root_of(v[j][k]);
             p[j][k] = keep * p[j][k] - u.rate * m[j][k] * fast_rcp(root[k] * u.root_correction + u.eps);
         }
         store_group<float>(e.param, first + 256 * j, e.n, whole, p[j]);
@@ -222,15 +232,17 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
         }
         const Scale sm = scale_of(wave_max_bits(most_m)), sr = scale_of(wave_max_bits(most_r));
         unsigned m_codes = 0, r_codes = 0;
+        const unsigned place = (unsigned)(flat + 256 * j), key = key_of(flat + 256 * j, u.key);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const unsigned w = random_word((unsigned long long)(flat + 256 * j + k), u.key);
-            const unsigned mc = code_of(fabsf(m[j][k]), sm, w >> 16) | (m[j][k] < 0.0f ? 0x80u : 0u);
-            const float y = root[k] * sr.inverse * kToCode;
-            const unsigned rc = max(code_of(root[k], sr, w & 0xffffu), y > 0.0f ? 1u : 0u);
-            m_codes |= (sm.finite ? mc : 0x7fu) << 8 * k;
-            r_codes |= (sr.finite ? rc : 0x7fu) << 8 * k;
+            const unsigned w = random_word(place + k, key);      // (a multiple of four: no carry into the upper word)
+            const float mk = m[j][k];       // (a bit cast of the vector's element itself is one of its first element)
+            const unsigned ym = scaled(fabsf(mk), sm), yr = scaled(root[k], sr), sign = __builtin_bit_cast(unsigned, mk) >> 24 & 0x80u;
+            m_codes |= (code_of(ym, w >> 16) | sign) << 8 * k;
+            r_codes |= max(code_of(yr, w & 0xffffu), min(yr, 1u)) << 8 * k;
         }
+        if (!sm.finite) m_codes = 0x7f7f7f7fu;
+        if (!sr.finite) r_codes = 0x7f7f7f7fu;
         reinterpret_cast<unsigned *>(u.m)[(flat + 256 * j) >> 2] = m_codes;
         reinterpret_cast<unsigned *>(u.r)[(flat + 256 * j) >> 2] = r_codes;
         if (lane == 0) {
