@@ -37,6 +37,24 @@ __device__ __forceinline__ Vec4<E> from_f32(f32x4 v)
     return __builtin_convertvector(v, Vec4<E>);
 }
 
+// Groups of four elements at a scalar base and a lane's offset in bytes, at multiples of four bytes: no address is left to compute on the vector
+// ALU.  A lane at kOutside reads zeros and writes nothing; a base reaches over less than 2 GiB.
+constexpr unsigned kOutside = 0x80000000u;
+__device__ __forceinline__ buf_rsrc make_base(const void *p) { return make_rsrc(p, 0x7fffffff); }
+template <class E>
+__device__ __forceinline__ Vec4<E> load_four(buf_rsrc base, unsigned lane_bytes, unsigned scalar_bytes = 0)
+{
+    if constexpr (sizeof(E) == 4) return __builtin_bit_cast(Vec4<E>, __builtin_amdgcn_raw_buffer_load_b128(base, lane_bytes, scalar_bytes, 0));
+    else return __builtin_bit_cast(Vec4<E>, __builtin_amdgcn_raw_buffer_load_b64(base, lane_bytes, scalar_bytes, 0));
+}
+// (four dwords: no scalar offset, see buf_store4)
+template <class E>
+__device__ __forceinline__ void store_four(buf_rsrc base, unsigned lane_bytes, Vec4<E> v)
+{
+    if constexpr (sizeof(E) == 4) buf_store4(base, lane_bytes, v);
+    else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), base, lane_bytes, 0, 0);
+}
+
 // A lane has four channels of a row of tiles of 4 W channels, W lanes side by side.  Aligned: neighbours, one wide access; the last lane of a
 // row whose channels are no multiple of four has the last four of them, so that two lanes have the same channel (C >= 4).  Else
 // the channels lane, lane + W, ..: every access of the W lanes is one run of neighbouring elements.

@@ -245,7 +245,6 @@ __device__ __forceinline__ void maps_of(f32x4 g, f32x4 x, f32x4 &a, f32x4 &z, f3
 // that begin at a multiple of four bytes, and blocks that span less than 2 GiB.)
 template <class E, bool kFast>
 struct Positions;
-constexpr unsigned kOutside = 0x80000000u;
 
 template <class E>
 struct Positions<E, true> {
@@ -254,15 +253,13 @@ struct Positions<E, true> {
     const Channels<true, 16> &ch;
     // of one block: `base` is the block's first position, `first` this thread's in the block
     __device__ __forceinline__ Positions(const E *base, long long stride, int first, const Channels<true, 16> &c)
-        : rsrc(make_rsrc(base, 0x7fffffff)), at(c.exists(0) ? (first * (unsigned)stride + c.first) * sizeof(E) : kOutside),
+        : rsrc(make_base(base)), at(c.exists(0) ? (first * (unsigned)stride + c.first) * sizeof(E) : kOutside),
           step((unsigned)stride * sizeof(E)), ch(c)
     {
     }
     __device__ __forceinline__ Vec4<E> load(int i, bool there) const
     {
-        const unsigned from = there ? at : kOutside;
-        if constexpr (sizeof(E) == 4) return __builtin_bit_cast(Vec4<E>, __builtin_amdgcn_raw_buffer_load_b128(rsrc, from, i * step, 0));
-        else return __builtin_bit_cast(Vec4<E>, __builtin_amdgcn_raw_buffer_load_b64(rsrc, from, i * step, 0));
+        return load_four<E>(rsrc, there ? at : kOutside, i * step);
     }
     __device__ __forceinline__ void store(int i, bool there, Vec4<E> v) const
     {
