@@ -5,12 +5,19 @@
 //             S1 = sum over the group's channels of scale P1, S2 of scale P2;  grad_x = rstd (scale du - (S1 + xhat S2) / M),
 //             M the elements of the group that exist
 //
-// Three ways, by size alone, all with sums in fp32 and variances from differences to a mean (of the group where the data stay on
-// chip, else of a thread's rows, put together pairwise by count: sums of squares would lose the variance of data far from zero):
-//   sample   a workgroup holds all positions of some groups of a sample in registers: x is read once, one launch
-//   position T = 1: a wave has one or several samples with all their channels; sums over a group pass through the wave's own LDS
-//   stream   anything: sums per channel and chunk of positions, sums per group (and of the gradients over samples), the result; three launches,
-//            x read twice, the second time from the last-level cache where it fits
+// Four ways, by size alone, all with sums in fp32 and variances from differences to a mean (of the group where the data stay on
+// chip, else of a thread's rows, put together pairwise by count: sums of squares would lose the variance of data far from zero); out and grad_x are
+// rounded once, to nearest, as they are stored:
+//   sample   a workgroup holds all positions of some groups of a sample in registers: x is read once, one launch.  16 x 72 x 40 fp32: 6.9 us with its
+//            launch, of which the call on the host is 5.5.
+//   position T = 1: a wave has one or several samples with all their channels; sums over a group pass through the wave's own LDS.
+//            16384 x 2048 bf16 in 16 groups: forward 30 us, 4.5 TB/s, reverse 45 us, 4.5 TB/s; the vector ALU is busy for all (forward) and 86 % of
+//            the cycles, with the sigmoid, its derivative and the conversions of 16 bits.
+//   wide     T = 1, groups of more than 512 channels: a workgroup has a group.  16384 x 2048 bf16 in one group: 28 and 59 us (a wave for each: 68, 245).
+//   stream   anything else: sums per channel and chunk of positions, sums per group (and of the gradients over samples), the result; three launches,
+//            x read twice, the second time from the last-level cache where it fits.  6 ragged samples of up to 16384 positions of 256 channels, bf16:
+//            forward 11 + 5 + 18 us, reverse 22 + 6 + 27, where 25 M elements at most are 50 MB an array.  Memory and last-level cache are the bound,
+//            and the vector ALU near it (68 to 79 % of the cycles).
 #include <algorithm>
 
 #include "layers_internal.h"
@@ -150,12 +157,13 @@ struct TileSums {
     }
 };
 
-constexpr int kMostTile = 1024;     // channels of a workgroup of the sample way
+// channels of a workgroup of the sample way
+constexpr int most_tile(int threads) { return threads * 4 < 1024 ? threads * 4 : 1024; }
 
 template <class E, bool kAligned, int NT, int K, bool kSilu>
 __global__ void __launch_bounds__(NT) norm_sample_forward_kernel(Norm a)
 {
-    __shared__ float part[NT / 64 * 256], group[kMostTile];
+    __shared__ float part[NT / 64 * 256], group[most_tile(NT)];
     const int n = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, rows = NT >> a.log_w, row = (int)threadIdx.x >> a.log_w;
     const TileChannels<kAligned> ch{tile * a.tile, min(a.tile, a.C - tile * a.tile), 1 << a.log_w, (int)threadIdx.x & ((1 << a.log_w) - 1)};
     const int length = length_of(a, n);
@@ -212,7 +220,7 @@ __global__ void __launch_bounds__(NT) norm_sample_forward_kernel(Norm a)
 template <class E, bool kAligned, int NT, int K, bool kSilu>
 __global__ void __launch_bounds__(NT) norm_sample_backward_kernel(Norm a)
 {
-    __shared__ float part[NT / 64 * 256 * 2], group[kMostTile * 2];
+    __shared__ float part[NT / 64 * 256 * 2], group[most_tile(NT) * 2];
     const int n = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, rows = NT >> a.log_w, row = (int)threadIdx.x >> a.log_w;
     const TileChannels<kAligned> ch{tile * a.tile, min(a.tile, a.C - tile * a.tile), 1 << a.log_w, (int)threadIdx.x & ((1 << a.log_w) - 1)};
     const int length = length_of(a, n);
@@ -1135,7 +1143,8 @@ struct Way {
 
 constexpr int kMostPositionTile = 512, kPositionRows = 4;       // channels of a group, samples at once (of groups up to 256)
 
-// Rows are added up in two launches from this many on: one alone reads them with 2 C / 64 workgroups.
+// Rows are added up in two launches, the first in kRuns runs, from this many on: one alone reads them with 2 C / 64 workgroups (reverse pass of
+// 8000 x 16 x 128 bf16 62 us, with one launch 81; 2048 x 16 x 64 fp32 20 against 22).
 constexpr int kManyRows = 1024, kRuns = 64;
 
 Way way_of(const esrnn_group_norm_shape &s)
@@ -1143,6 +1152,7 @@ Way way_of(const esrnn_group_norm_shape &s)
     Way w{};
     const int D = s.C / s.G;
     if (s.T == 1 && D > kMostPositionTile && D <= 4096) {
+        // (a wave for each group needs more registers than it has beyond 512 channels: figures above)
         w.kind = kWide;
         w.tiles = s.G;
         w.pieces = D <= 1024 ? 1 : D <= 2048 ? 2 : 4;
@@ -1173,10 +1183,14 @@ Way way_of(const esrnn_group_norm_shape &s)
         w.part_rows = w.backward_groups;
         return w;
     }
-    // sample: whole groups side by side up to 64 channels (a run of 128 bytes of bf16), as many positions as fit; up to 32 channels only for few
-    // workgroups, where the launches of the stream way are what counts (2 samples of 1000 x 96 fp32, forward 11 against 15 us; 64 of
-    // 1024 x 512 bf16: 58 against 46)
-    constexpr int kSplits[5][3] = {{64, 256, 4}, {64, 256, 16}, {64, 1024, 4}, {64, 1024, 8}, {32, 1024, 8}};   // channels, threads, positions each
+    // sample: whole groups side by side up to 64 channels (a run of 128 bytes of bf16), as many positions as fit.  Against the stream way, forward and
+    // reverse: 512 x 72 x 64 fp32 10 and 13 us against 16 and 20, 64 x 512 x 512 bf16 26 and 42 against 26 and 42.
+    // A wave by itself waits at no barrier, but has all groups of the tile to add up: up to 16 positions, from 2048 workgroups on (4096 x 16 x 64 fp32 15
+    // and 25 us, with 256 threads 22 and 38; 2048 12 and 18 against 13 and 22; 1024 10 and 16 against 9 and 13; 3000 x 4 x 256 bf16 17 and 25
+    // against 44 and 50).
+    // Up to 32 channels only for few workgroups, where the launches of the stream way are what counts (2 samples of 1000 x 96 fp32, forward 11
+    // against 15 us; 64 of 1024 x 512 bf16: 58 against 46).
+    constexpr int kSplits[6][3] = {{64, 64, 4}, {64, 256, 4}, {64, 256, 16}, {64, 1024, 4}, {64, 1024, 8}, {32, 1024, 8}};   // channels, threads, positions each
     for (const auto &split : kSplits) {
         if (split[0] < 64 && (int64_t)s.N * s.C > 256 * 32) break;
         int groups = std::max(1, std::min(s.G, split[0] / D));
@@ -1188,7 +1202,8 @@ Way way_of(const esrnn_group_norm_shape &s)
         w.tile = groups * D;
         for (w.log_w = 0; 4 << w.log_w < w.tile; ++w.log_w) {}
         w.tiles = (s.G + groups - 1) / groups;
-        if (w.tile <= kMostTile && split[1] >> w.log_w >= 1 && (int64_t)s.N * w.tiles * split[1] <= (int64_t(1) << 31) &&
+        if (split[1] == 64 && (int64_t)s.N * w.tiles < 2048) continue;
+        if (w.tile <= most_tile(split[1]) && split[1] >> w.log_w >= 1 && (int64_t)s.N * w.tiles * split[1] <= (int64_t(1) << 31) &&
             (int64_t)s.T <= (int64_t)(split[1] >> w.log_w) * split[2]) {
             w.kind = kSample;
             w.threads = split[1], w.rows_each = split[2];
@@ -1198,6 +1213,7 @@ Way way_of(const esrnn_group_norm_shape &s)
     w.part_rows = s.N;
     if (w.kind == kSample) return w;
     w.kind = kStream;
+    // some 2048 workgroups (1024 to 8192 make no difference), of 128 positions at least
     w.tiles = (s.C + 63) / 64;
     const int64_t columns = (int64_t)s.N * w.tiles;
     int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((s.T + 127) / 128, 2048 / columns));
@@ -1328,7 +1344,8 @@ hipError_t launch_group_norm_forward(const esrnn_group_norm_shape &s, const Grou
             }
             if (w.kind == kSample) {
                 const unsigned grid = (unsigned)(s.N * w.tiles);
-                if (w.threads == 256 && w.rows_each == 4) norm_sample_forward_kernel<E, al(), 256, 4, silu()><<<grid, 256, 0, st>>>(a);
+                if (w.threads == 64) norm_sample_forward_kernel<E, al(), 64, 4, silu()><<<grid, 64, 0, st>>>(a);
+                else if (w.threads == 256 && w.rows_each == 4) norm_sample_forward_kernel<E, al(), 256, 4, silu()><<<grid, 256, 0, st>>>(a);
                 else if (w.threads == 256) norm_sample_forward_kernel<E, al(), 256, 16, silu()><<<grid, 256, 0, st>>>(a);
                 else if (w.rows_each == 4) norm_sample_forward_kernel<E, al(), 1024, 4, silu()><<<grid, 1024, 0, st>>>(a);
                 else norm_sample_forward_kernel<E, al(), 1024, 8, silu()><<<grid, 1024, 0, st>>>(a);
@@ -1370,7 +1387,8 @@ hipError_t launch_group_norm_backward(const esrnn_group_norm_shape &s, const Gro
             }
             if (w.kind == kSample) {
                 const unsigned grid = (unsigned)(s.N * w.tiles);
-                if (w.threads == 256 && w.rows_each == 4) norm_sample_backward_kernel<E, al(), 256, 4, silu()><<<grid, 256, 0, st>>>(a);
+                if (w.threads == 64) norm_sample_backward_kernel<E, al(), 64, 4, silu()><<<grid, 64, 0, st>>>(a);
+                else if (w.threads == 256 && w.rows_each == 4) norm_sample_backward_kernel<E, al(), 256, 4, silu()><<<grid, 256, 0, st>>>(a);
                 else if (w.threads == 256) norm_sample_backward_kernel<E, al(), 256, 16, silu()><<<grid, 256, 0, st>>>(a);
                 else if (w.rows_each == 4) norm_sample_backward_kernel<E, al(), 1024, 4, silu()><<<grid, 1024, 0, st>>>(a);
                 else norm_sample_backward_kernel<E, al(), 1024, 8, silu()><<<grid, 1024, 0, st>>>(a);

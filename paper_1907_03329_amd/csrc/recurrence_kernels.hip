@@ -8,12 +8,16 @@
 //
 // Many sequences and channels: a workgroup takes all blocks of its 64 channels one behind the other, the state in registers.
 // Few: every block has a workgroup of its own (kAhead), which reads its positions once, hands its map on through memory, and puts together
-// the maps of the blocks before it, which are under way at the same time.  (As two launches, maps first and then x and gate once more, 8
-// sequences of 4096 positions and 2048 channels took 146 us forward and 198 us in reverse.)
+// the maps of the blocks before it, which are under way at the same time.
 //
 // The reverse pass runs the same maps from the end: mu_t = a_t (d_t + mu_{t+1}), with d the gradient of out.  The states h_{t-1} that the
 // gradient of the gate needs are computed again, in fp32, from the state before the block that the forward pass leaves: reading
 // out instead would be one array more, and rounded to its element type.
+//
+// Every array is read once and written once, 3 arrays forward and 5 in reverse, so memory is the bound: in bf16, 8 sequences of 4096 positions
+// and 2048 channels take 96 us forward and 160 us in reverse, 4.2 TB/s both (a copy reaches 5.1); 64 x 501 x 240 elements, 17 and 26 us;
+// one sequence of 131072 positions of 256 channels, 56 and 102 us behind 5 us each that clear the words below, 3.6 and 3.3 TB/s.  The
+// vector ALU is busy for 40 % of the cycles.  Maps, states and their sums are fp32; out and the gradients are rounded once, to nearest, as they are stored.
 #include <algorithm>
 
 #include "layers_internal.h"
@@ -22,8 +26,10 @@ namespace esrnn {
 
 namespace {
 
-constexpr int kTile = 64;       // channels of a workgroup
-// rows of 64 channels from which a workgroup takes a whole sequence
+constexpr int kTile = 64;       // channels of a workgroup: 128 bytes of 16 bits, a whole cache line (16 channels were slower in every shape)
+// Lines (64 channels of a sequence) from which a workgroup takes a whole sequence.  Alone against ahead, bf16, forward and reverse: 8 x 4096 x 2048
+// (256 lines) 96 and 160 us against 107 and 180, 16 x 2048 x 1024 (256) 42 and 84 against 45 and 96; 4 x 8192 x 512 (32) 107 and 199 against
+// 29 and 45.
 constexpr int kLinesAlone = 256;
 
 struct Args {
@@ -242,7 +248,8 @@ __device__ __forceinline__ void maps_of(f32x4 g, f32x4 x, f32x4 &a, f32x4 &z, f3
 // The kSteps positions of this thread in one array: four channels of position i.  kFast: the block begins at a scalar base, the thread's place in
 // it never changes, position i is a scalar offset, and lanes without channels or positions lie outside the buffer, so that they
 // read zeros and write nothing: no address is left to compute on the vector ALU, whose cycles the maps need.  (For groups of four elements
-// that begin at a multiple of four bytes, and blocks that span less than 2 GiB.)
+// that begin at a multiple of four bytes, and blocks that span less than 2 GiB.  8 x 4096 x 2048 bf16: 96 and 160 us; with 64-bit
+// addresses for each access 119 and 174, 864 vector instructions a block in the place of 598.)
 template <class E, bool kFast>
 struct Positions;
 
@@ -473,7 +480,9 @@ __global__ void __launch_bounds__(256) recurrence_words_kernel(u32x4 *words, lon
     if (i < n) words[i] = i < tickets ? u32x4{0, 0, 0, 0} : u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
 }
 
-// One position: a workgroup has 1024 neighbouring channels of a request.
+// One position: a workgroup has 1024 neighbouring channels of a request.  Reads x, gate and the state, writes out and the state, nothing waits for
+// anything else: 1024 requests of 2048 channels in bf16 are 29 MB, 5.8 us at the rate of a copy, and the call takes 7.1 us, 6.3 of which the host
+// needs to make it; 7 requests of 240 channels take the same.
 template <class E, bool kAligned, int kKind>
 __global__ void __launch_bounds__(256) recurrence_step_kernel(RecurrenceStep a, int tiles)
 {
@@ -540,7 +549,12 @@ RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s)
 {
     RecurrencePlan p{};
     const long long lines = (long long)s.B * ((s.C + kTile - 1) / kTile);
+    // (2^21 blocks: their maps are 1 GiB)
     p.ahead = s.T > 128 && lines < kLinesAlone && lines * ((s.T + 127) / 128) <= (1 << 21);
+    // The block is the sequence where that is short; in long ones 8 waves have more bytes on their way, but short ones leave them idle.  Forward and
+    // reverse, bf16: 16 lines of 72 positions 5.8 us forward with 2 waves, 4.7 with 4; 2048 x 100 x 64 (2048 lines) 18 and 31 with 2, 18 and 34 with 4,
+    // 25 and 62 with 8; 64 x 501 x 240 16 and 26 with 4, 16 and 32 with 8 (ahead); 128 x 512 x 1024 86 and 160 with 8, 95 and 154 with 4.
+    // A thread has 8 positions, or 2 where 4 threads hold the sequence with that: 4096 x 8 x 512 40 and 87 us with 8, 19 and 30 with 2.
     p.waves = p.ahead ? 4 : s.T <= 32 ? 1 : s.T <= 64 || (s.T <= 128 && lines >= 1024) ? 2 : s.T <= 256 ? 4 : 8;
     p.steps = s.T <= 8 ? 2 : 8;
     p.block = 4 * p.steps * p.waves;

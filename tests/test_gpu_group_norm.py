@@ -111,6 +111,13 @@ def test_every_position_by_itself(N, C, G, dtype):
     check(N, 1, C, G, dtype=dtype, act="none", lengths=(np.arange(N) % 3 > 0).astype(int), seed=N + 1)
 
 
+@pytest.mark.parametrize("N,T,C,G", [(2050, 5, 60, 3), (2048, 16, 64, 64), (700, 16, 200, 8), (2100, 2, 37, 1), (600, 4, 1000, 4), (600, 3, 1026, 6)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_many_short_samples(N, T, C, G, dtype):
+    check(N, T, C, G, dtype=dtype, seed=C)
+    check(N, T, C, G, dtype=dtype, act="none", lengths="ragged", seed=C + 1)
+
+
 @pytest.mark.parametrize("T,C,G", [(50, 40, 4), (700, 96, 8), (2500, 64, 2), (9, 37, 1)])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_ragged_lengths_with_garbage_behind_them(T, C, G, dtype):

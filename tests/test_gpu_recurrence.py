@@ -253,6 +253,27 @@ def test_equal_calls_are_equal_and_streams_and_graphs_do_not_matter():
         assert all(torch.equal(a, b) for a, b in zip(results, eager))
 
 
+def test_two_layers_on_two_streams_at_once():
+    """Their launches overlap, and each has its own workspace."""
+    import torch
+    made = [check(2, 6000, 128, dtype="bfloat16", kind=kind, initial=True, seed=31 + i) for i, kind in enumerate(("smooth", "decay"))]
+    made = [(layer, (x, g, d, lens, h0.cuda(), dl.cuda()), results) for layer, (x, g, d, lens, h0, dl), results in made]
+    want = [[t.clone() for t in results] for _, _, results in made]
+    streams = [torch.cuda.Stream() for _ in made]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for _, _, results in made:
+            for t in results:
+                t.zero_()
+        torch.cuda.synchronize()
+        for (layer, (x, g, d, lens, h0, dl), _), stream in zip(made, streams):
+            layer.forward(x, g, lengths=lens, initial=h0, stream=stream)
+            layer.backward(x, g, d, lengths=lens, grad_last=dl, stream=stream)
+        torch.cuda.synchronize()
+        for (_, _, results), w in zip(made, want):
+            assert all(torch.equal(a, b) for a, b in zip(results, w))
+
+
 def test_gradients_into_the_halves_of_one_array():
     import torch
     rng = np.random.default_rng(13)
