@@ -149,7 +149,7 @@ hipError_t launch_recurrence_step(int kind, int dtype, const RecurrenceStep &a, 
 
 // ---- AdamW over many tensors (adamw_kernels.hip) ----
 // Elements of a workgroup: 2048, or 1024 in lists of up to 512 chunks, that do not fill the chip (40 tensors of 3000 elements, norm and update:
-// 5.0 + 4.5 us with 2048, 3.7 + 3.7 with 1024; 72 M elements, update alone: 360, 373 with 4096).
+// 5.0 + 4.5 us with 2048, 3.7 + 3.7 with 1024; 73 M elements, update alone: 360, 373 with 4096).
 constexpr int kAdamWChunk = 2048, kAdamWSmallChunk = 1024, kAdamWFewChunks = 512, kAdamWNormBlocks = 256, kAdamWEntriesAtOnce = 56;
 struct AdamWEntry {
     float *param;
