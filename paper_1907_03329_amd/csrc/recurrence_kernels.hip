@@ -15,7 +15,8 @@
 // out instead would be one array more, and rounded to its element type.
 //
 // Every array is read once and written once, 3 arrays forward and 5 in reverse, so memory is the bound: in bf16, 8 sequences of 4096 positions
-// and 2048 channels take 96 us forward and 160 us in reverse, 4.2 TB/s both (a copy reaches 5.1); 64 x 501 x 240 elements, 17 and 26 us;
+// and 2048 channels take 96 us forward and 160 us in reverse, 4.2 TB/s both (a copy reaches 5.1); 501 ragged sequences of up to 240 positions of 50 channels,
+// fp32, 17 and 26 us;
 // one sequence of 131072 positions of 256 channels, 56 and 102 us behind 5 us each that clear the words below, 3.6 and 3.3 TB/s.  The
 // vector ALU is busy for 40 % of the cycles.  Maps, states and their sums are fp32; out and the gradients are rounded once, to nearest, as they are stored.
 #include <algorithm>
@@ -28,9 +29,9 @@ namespace {
 
 constexpr int kTile = 64;       // channels of a workgroup: 128 bytes of 16 bits, a whole cache line (16 channels were slower in every shape)
 // Lines (64 channels of a sequence) from which a workgroup takes a whole sequence.  Alone against ahead, bf16, forward and reverse: 8 x 4096 x 2048
-// (256 lines) 96 and 160 us against 107 and 180, 16 x 2048 x 1024 (256) 42 and 84 against 45 and 96; 4 x 8192 x 512 (32) 107 and 199 against
-// 29 and 45.
-constexpr int kLinesAlone = 256;
+// (256 lines) 96 and 160 us against 107 and 180, 240 lines of 2048 positions 39 and 73 against 41 and 79, of 512 12 and 20 against 15 and 24; 192 of
+// 2048 37 and 60 against 35 and 55, of 512 11 and 18 against 12 and 21; 128 of 2048 35 and 51 against 27 and 40, 32 30 and 48 against 11 and 14.
+constexpr int kLinesAlone = 192;
 
 struct Args {
     const void *x, *gate, *grad_out;
@@ -245,21 +246,84 @@ __device__ __forceinline__ void maps_of(f32x4 g, f32x4 x, f32x4 &a, f32x4 &z, f3
     b = kKind == ESRNN_RECURRENCE_SMOOTH ? z * x : x;
 }
 
+// How a call's channels are read, by the least aligned of its arrays:
+//   kFast         groups of four elements at multiples of four bytes, blocks of less than 2 GiB: from scalar bases (Positions)
+//   kFour alone   at least four channels: groups of four at the alignment of one element, 64-bit addresses
+//   neither       one by one
+// Scalar bases leave fewer registers to addresses, which workgroups of one or two waves need: 2048 x 100 x 64 bf16 forward 16 us with kFast, 19.5 with
+// kFour alone, 4096 x 30 x 64 9.9 and 10.7; 8 x 4096 x 2048 95 and 160 us forward and reverse with either.  kFour alone against one by one: 8 x 4096 x
+// 2047 136 and 232 us against 168 and 256, 18 x 108288 x 33 203 and 319 against 244 and 407.
+enum Access { kOneByOne, kByFours, kByFoursFast };
+
+// Four neighbouring channels of a line for each of sixteen lanes; the last lane with channels has the last four there are, so that two lanes may
+// have the same channel.  kFour: C is 4 at least.
+template <bool kFour>
+struct LineChannels {
+    int first, count;
+    __device__ __forceinline__ LineChannels(int lane, int begin, int C) : first(begin + 4 * lane), count(C)
+    {
+        if (kFour && first < C) first = min(first, C - 4);
+    }
+    __device__ __forceinline__ int channel(int k) const { return first + k; }
+    __device__ __forceinline__ bool exists(int k) const { return channel(k) < count; }
+    // a channel that can be read in the place of one that does not exist
+    __device__ __forceinline__ int readable(int k) const { return kFour ? min(first, count - 4) + k : min(first + k, count - 1); }
+    // (at the alignment of one element, which the hardware's global accesses allow)
+    template <class E>
+    __device__ __forceinline__ Vec4<E> load(const E *row) const
+    {
+        if constexpr (kFour) return *reinterpret_cast<const typename Loose<E>::Four *>(row + readable(0));
+        Vec4<E> v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = row[readable(k)];
+        return v;
+    }
+    template <class E>
+    __device__ __forceinline__ void store(E *row, Vec4<E> v) const
+    {
+        if constexpr (kFour) {
+            if (exists(0)) *reinterpret_cast<typename Loose<E>::Four *>(row + first) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (exists(k)) row[channel(k)] = v[k];
+        }
+    }
+};
+
 // The kSteps positions of this thread in one array: four channels of position i.  kFast: the block begins at a scalar base, the thread's place in
 // it never changes, position i is a scalar offset, and lanes without channels or positions lie outside the buffer, so that they
-// read zeros and write nothing: no address is left to compute on the vector ALU, whose cycles the maps need.  (For groups of four elements
-// that begin at a multiple of four bytes, and blocks that span less than 2 GiB.  8 x 4096 x 2048 bf16: 96 and 160 us; with 64-bit
-// addresses for each access 119 and 174, 864 vector instructions a block in the place of 598.)
-template <class E, bool kFast>
-struct Positions;
-
+// read zeros and write nothing: no address is left to compute on the vector ALU, whose cycles the maps need.
+template <class E, bool kFast, bool kFour>
+struct Positions {
+    E *base, *mine;         // of the block, and of this thread's first position
+    long long stride;
+    const LineChannels<kFour> &ch;
+    __device__ __forceinline__ Positions(const E *b, long long s, int first, const LineChannels<kFour> &c)
+        : base(const_cast<E *>(b)), mine(base + first * s), stride(s), ch(c)
+    {
+    }
+    // What is not there is read from the block's first position, which is, and masked out.  (A mask that the compiler does not see through: of a
+    // selection it makes a branch around the load, and then every load is waited for by itself.)
+    __device__ __forceinline__ Vec4<E> load(int i, bool there) const
+    {
+        using Bits = unsigned __attribute__((ext_vector_type(sizeof(E))));
+        unsigned mask = there ? 0xffffffffu : 0u;
+        asm("" : "+v"(mask));
+        return __builtin_bit_cast(Vec4<E>, __builtin_bit_cast(Bits, ch.load(there ? mine + i * stride : base)) & mask);
+    }
+    __device__ __forceinline__ void store(int i, bool there, Vec4<E> v) const
+    {
+        if (there) ch.store(mine + i * stride, v);
+    }
+};
 template <class E>
-struct Positions<E, true> {
+struct Positions<E, true, true> {
     buf_rsrc rsrc;
     unsigned at, step;
-    const Channels<true, 16> &ch;
+    const LineChannels<true> &ch;
     // of one block: `base` is the block's first position, `first` this thread's in the block
-    __device__ __forceinline__ Positions(const E *base, long long stride, int first, const Channels<true, 16> &c)
+    __device__ __forceinline__ Positions(const E *base, long long stride, int first, const LineChannels<true> &c)
         : rsrc(make_base(base)), at(c.exists(0) ? (first * (unsigned)stride + c.first) * sizeof(E) : kOutside),
           step((unsigned)stride * sizeof(E)), ch(c)
     {
@@ -276,30 +340,17 @@ struct Positions<E, true> {
         else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), rsrc, to, i * step, 0);
     }
 };
-template <class E>
-struct Positions<E, false> {
-    E *base;
-    long long stride;
-    const Channels<false, 16> &ch;
-    __device__ __forceinline__ Positions(const E *b, long long s, int first, const Channels<false, 16> &c) : base(const_cast<E *>(b) + first * s), stride(s), ch(c) {}
-    __device__ __forceinline__ Vec4<E> load(int i, bool there) const { return there ? ch.load(base + i * stride) : Vec4<E>{}; }
-    __device__ __forceinline__ void store(int i, bool there, Vec4<E> v) const
-    {
-        if (there) ch.store(base + i * stride, v);
-    }
-};
-
 // Channels of fp32 arrays [..][C] follow the dealing of the elements'.
-template <bool kAligned>
-__device__ __forceinline__ f32x4 load_state(const float *p, const Channels<kAligned, 16> &ch)
+template <bool kFour>
+__device__ __forceinline__ f32x4 load_state(const float *p, const LineChannels<kFour> &ch)
 {
     f32x4 v;
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = p[ch.readable(k)];
     return v;
 }
-template <bool kAligned>
-__device__ __forceinline__ void store_state(float *p, f32x4 v, const Channels<kAligned, 16> &ch)
+template <bool kFour>
+__device__ __forceinline__ void store_state(float *p, f32x4 v, const LineChannels<kFour> &ch)
 {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -329,8 +380,8 @@ __device__ __forceinline__ Line line_of(const Args &a, int line)
     return Line(a.words + kTicket * (size_t)(a.B * a.tiles) + (size_t)line * (a.blocks + a.groups) * kMap, a.blocks, a.groups);
 }
 
-template <class E, bool kFast, int kKind, int kSteps, int NW, bool kAhead>
-__global__ void __launch_bounds__(64 * NW, NW == 8 || !kFast ? 2 : kAhead ? 3 : 4) recurrence_forward_kernel(Args a)
+template <class E, bool kFast, int kKind, int kSteps, int NW, bool kAhead, bool kFour>
+__global__ void __launch_bounds__(64 * NW, !kFour && NW < 8 ? 1 : NW == 8 || !kFast ? 2 : kAhead ? 3 : 4) recurrence_forward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
     __shared__ f32x4 lds[2][NW][2][16];
@@ -338,7 +389,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || !kFast ? 2 : kAhead ? 3 : 
     const int lane = threadIdx.x & 15, row = (threadIdx.x >> 4) & 3, wave = threadIdx.x >> 6;
     const Place place = draw_place<kAhead>(a);
     const int b = place.line / a.tiles;
-    const Channels<kFast, 16> ch(lane, place.line % a.tiles * kTile, a.C);
+    const LineChannels<kFour> ch(lane, place.line % a.tiles * kTile, a.C);
     const int length = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
     const E *x = static_cast<const E *>(a.x) + b * a.xb, *gate = static_cast<const E *>(a.gate) + b * a.gb;
     E *out = static_cast<E *>(a.out) + b * a.ob;
@@ -351,13 +402,13 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || !kFast ? 2 : kAhead ? 3 : 
     const int first = (wave * 4 + row) * kSteps;
     for (int block = place.block; block < end; ++block) {
         const int begin = block * kBlock, left = length - begin - first, rest = a.T - begin - first;      // positions from this thread's first on
-        const Positions<E, kFast> to(out + begin * a.ot, a.ot, first, ch);
+        const Positions<E, kFast, kFour> to(out + begin * a.ot, a.ot, first, ch);
         if (begin >= length) {     // nothing left of the sequence
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) to.store(i, i < rest, Vec4<E>{});
             continue;
         }
-        const Positions<E, kFast> of_x(x + begin * a.xt, a.xt, first, ch), of_gate(gate + begin * a.gt, a.gt, first, ch);
+        const Positions<E, kFast, kFour> of_x(x + begin * a.xt, a.xt, first, ch), of_gate(gate + begin * a.gt, a.gt, first, ch);
         Vec4<E> xs[kSteps], gs[kSteps];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
@@ -389,7 +440,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || !kFast ? 2 : kAhead ? 3 : 
     }
 }
 
-template <class E, bool kFast, int kKind, int kSteps, int NW, bool kAhead>
+template <class E, bool kFast, int kKind, int kSteps, int NW, bool kAhead, bool kFour>
 __global__ void __launch_bounds__(64 * NW, 2) recurrence_backward_kernel(Args a)
 {
     constexpr int kBlock = 4 * kSteps * NW;
@@ -399,7 +450,7 @@ __global__ void __launch_bounds__(64 * NW, 2) recurrence_backward_kernel(Args a)
     const int lane = threadIdx.x & 15, row = (threadIdx.x >> 4) & 3, wave = threadIdx.x >> 6;
     const Place place = draw_place<kAhead>(a);
     const int b = place.line / a.tiles;
-    const Channels<kFast, 16> ch(lane, place.line % a.tiles * kTile, a.C);
+    const LineChannels<kFour> ch(lane, place.line % a.tiles * kTile, a.C);
     const int length = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T, top = (length - 1) / kBlock;       // the last block with positions
     const E *x = static_cast<const E *>(a.x) + b * a.xb, *gate = static_cast<const E *>(a.gate) + b * a.gb;
     const E *grad_out = static_cast<const E *>(a.grad_out) + b * a.db;
@@ -412,7 +463,7 @@ __global__ void __launch_bounds__(64 * NW, 2) recurrence_backward_kernel(Args a)
     const int first = (wave * 4 + row) * kSteps;
     for (int block = last; block >= end; --block) {
         const int begin = block * kBlock, left = length - begin - first, rest = a.T - begin - first;
-        const Positions<E, kFast> to_x(grad_x + begin * a.gxt, a.gxt, first, ch), to_gate(grad_gate + begin * a.ggt, a.ggt, first, ch);
+        const Positions<E, kFast, kFour> to_x(grad_x + begin * a.gxt, a.gxt, first, ch), to_gate(grad_gate + begin * a.ggt, a.ggt, first, ch);
         if (begin >= length) {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
@@ -422,7 +473,7 @@ __global__ void __launch_bounds__(64 * NW, 2) recurrence_backward_kernel(Args a)
             if (block == 0 && writes && a.grad_initial) store_state(a.grad_initial + (size_t)b * a.C, carry, ch);
             continue;
         }
-        const Positions<E, kFast> of_x(x + begin * a.xt, a.xt, first, ch), of_gate(gate + begin * a.gt, a.gt, first, ch),
+        const Positions<E, kFast, kFour> of_x(x + begin * a.xt, a.xt, first, ch), of_gate(gate + begin * a.gt, a.gt, first, ch),
             of_out(grad_out + begin * a.dt, a.dt, first, ch);
         Vec4<E> xs[kSteps], gs[kSteps], ds[kSteps];
         f32x4 before = load_state(a.saved_in + ((size_t)b * a.blocks + block) * a.C, ch);
@@ -509,14 +560,21 @@ template <int v>
 using Int = std::integral_constant<int, v>;
 
 template <class F>
-void with_variant(bool aligned, int kind, F &&f)
+void with_kind(int kind, F &&f)
 {
-    const auto of_kind = [&](auto al) {
-        if (kind == ESRNN_RECURRENCE_SMOOTH) f(al, Int<ESRNN_RECURRENCE_SMOOTH>{});
-        else f(al, Int<ESRNN_RECURRENCE_DECAY>{});
-    };
-    if (aligned) of_kind(std::true_type{});
-    else of_kind(std::false_type{});
+    if (kind == ESRNN_RECURRENCE_SMOOTH) f(Int<ESRNN_RECURRENCE_SMOOTH>{});
+    else f(Int<ESRNN_RECURRENCE_DECAY>{});
+}
+template <class F>
+void with_access(Access access, int kind, F &&f)
+{
+    with_kind(kind, [&](auto k) {
+        switch (access) {
+        case kOneByOne: return f(std::false_type{}, std::false_type{}, k);
+        case kByFours: return f(std::false_type{}, std::true_type{}, k);
+        default: return f(std::true_type{}, std::true_type{}, k);
+        }
+    });
 }
 
 Args args_of(const esrnn_recurrence_shape &s, const RecurrencePlan &p)
@@ -536,11 +594,10 @@ bool groups_of_four(const void *p, const int64_t stride[2], int dtype)
 {
     return aligned_to(p, 4 * element_bytes(dtype)) && (stride[0] | stride[1]) % 4 == 0;
 }
-// What Positions takes to be fast: groups of four elements from a multiple of four bytes on, in blocks of less than 2 GiB.
-bool fast(const void *p, const int64_t stride[2], const esrnn_recurrence_shape &s, const RecurrencePlan &plan)
+Access access_of(const void *p, const int64_t stride[2], const esrnn_recurrence_shape &s, const RecurrencePlan &plan)
 {
     const bool dwords = s.dtype == ESRNN_F32 || (aligned_to(p, 4) && (stride[0] | stride[1] | s.C) % 2 == 0);
-    return s.C >= 4 && dwords && plan.block * stride[1] + s.C < (int64_t(1) << 29);
+    return s.C < 4 ? kOneByOne : dwords && plan.block * stride[1] + s.C < (int64_t(1) << 29) ? kByFoursFast : kByFours;
 }
 
 }  // namespace
@@ -549,11 +606,12 @@ RecurrencePlan recurrence_plan(const esrnn_recurrence_shape &s)
 {
     RecurrencePlan p{};
     const long long lines = (long long)s.B * ((s.C + kTile - 1) / kTile);
-    // (2^21 blocks: their maps are 1 GiB)
-    p.ahead = s.T > 128 && lines < kLinesAlone && lines * ((s.T + 127) / 128) <= (1 << 21);
+    // Ahead from 257 positions on: up to 256 the second block costs less than clearing the words (32 lines of 256 positions 7 and 10 us against 8
+    // and 10, of 512 9 and 14 against 8 and 10).  2^21 blocks: their maps are 1 GiB.
+    p.ahead = s.T > 256 && lines < kLinesAlone && lines * ((s.T + 127) / 128) <= (1 << 21);
     // The block is the sequence where that is short; in long ones 8 waves have more bytes on their way, but short ones leave them idle.  Forward and
     // reverse, bf16: 16 lines of 72 positions 5.8 us forward with 2 waves, 4.7 with 4; 2048 x 100 x 64 (2048 lines) 18 and 31 with 2, 18 and 34 with 4,
-    // 25 and 62 with 8; 64 x 501 x 240 16 and 26 with 4, 16 and 32 with 8 (ahead); 128 x 512 x 1024 86 and 160 with 8, 95 and 154 with 4.
+    // 25 and 62 with 8; 501 x 240 x 50 fp32 16 and 26 with 4, 16 and 32 with 8; 128 x 512 x 1024 86 and 160 with 8, 95 and 154 with 4.
     // A thread has 8 positions, or 2 where 4 threads hold the sequence with that: 4096 x 8 x 512 40 and 87 us with 8, 19 and 30 with 2.
     p.waves = p.ahead ? 4 : s.T <= 32 ? 1 : s.T <= 64 || (s.T <= 128 && lines >= 1024) ? 2 : s.T <= 256 ? 4 : 8;
     p.steps = s.T <= 8 ? 2 : 8;
@@ -588,14 +646,14 @@ hipError_t launch_recurrence_forward(const esrnn_recurrence_shape &s, const Recu
     const RecurrencePlan p = recurrence_plan(s);
     Args a = args_of(s, p);
     a.x = f.x, a.gate = f.gate, a.out = f.out, a.lengths = f.lengths, a.initial = f.initial, a.last = f.last, a.saved = f.saved, a.words = f.words;
-    const bool all_fast = fast(f.x, s.x_stride, s, p) && fast(f.gate, s.gate_stride, s, p) && fast(f.out, s.out_stride, s, p);
+    const Access access = std::min({access_of(f.x, s.x_stride, s, p), access_of(f.gate, s.gate_stride, s, p), access_of(f.out, s.out_stride, s, p)});
     return with_words(p, f.words, st, [&](auto ahead) {
         return with_element(s.dtype, [&](auto e) {
             using E = decltype(e);
-            with_variant(all_fast, s.kind, [&](auto al, auto kind) {
+            with_access(access, s.kind, [&](auto fast, auto four, auto kind) {
                 const unsigned lines = (unsigned)(s.B * a.tiles);
                 const auto launch = [&](auto steps, auto waves) {
-                    recurrence_forward_kernel<E, al(), kind(), steps(), waves(), ahead()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
+                    recurrence_forward_kernel<E, fast(), kind(), steps(), waves(), ahead(), four()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
                 };
                 if constexpr (ahead()) launch(Int<8>{}, Int<4>{});
                 else if (p.steps == 2) launch(Int<2>{}, Int<1>{});
@@ -617,15 +675,15 @@ hipError_t launch_recurrence_backward(const esrnn_recurrence_shape &s, const Rec
     Args a = args_of(s, p);
     a.x = f.x, a.gate = f.gate, a.grad_out = f.grad_out, a.grad_x = f.grad_x, a.grad_gate = f.grad_gate, a.lengths = f.lengths;
     a.saved_in = f.saved, a.grad_last = f.grad_last, a.grad_initial = f.grad_initial, a.words = f.words;
-    const bool all_fast = fast(f.x, s.x_stride, s, p) && fast(f.gate, s.gate_stride, s, p) && fast(f.grad_out, s.grad_out_stride, s, p) &&
-                          fast(f.grad_x, s.grad_x_stride, s, p) && fast(f.grad_gate, s.grad_gate_stride, s, p);
+    const Access access = std::min({access_of(f.x, s.x_stride, s, p), access_of(f.gate, s.gate_stride, s, p), access_of(f.grad_out, s.grad_out_stride, s, p),
+                                    access_of(f.grad_x, s.grad_x_stride, s, p), access_of(f.grad_gate, s.grad_gate_stride, s, p)});
     return with_words(p, f.words, st, [&](auto ahead) {
         return with_element(s.dtype, [&](auto e) {
             using E = decltype(e);
-            with_variant(all_fast, s.kind, [&](auto al, auto kind) {
+            with_access(access, s.kind, [&](auto fast, auto four, auto kind) {
                 const unsigned lines = (unsigned)(s.B * a.tiles);
                 const auto launch = [&](auto steps, auto waves) {
-                    recurrence_backward_kernel<E, al(), kind(), steps(), waves(), ahead()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
+                    recurrence_backward_kernel<E, fast(), kind(), steps(), waves(), ahead(), four()><<<ahead() ? lines * p.blocks : lines, 64 * waves(), 0, st>>>(a);
                 };
                 if constexpr (ahead()) launch(Int<8>{}, Int<4>{});
                 else if (p.steps == 2) launch(Int<2>{}, Int<1>{});
@@ -649,8 +707,9 @@ hipError_t launch_recurrence_step(int kind, int dtype, const RecurrenceStep &a, 
     const int tiles = (a.C + 1023) / 1024;
     return with_element(dtype, [&](auto e) {
         using E = decltype(e);
-        with_variant(aligned, kind, [&](auto al, auto k) {
-            recurrence_step_kernel<E, al(), k()><<<(unsigned)(a.rows * tiles), 256, 0, st>>>(a, tiles);
+        with_kind(kind, [&](auto k) {
+            if (aligned) recurrence_step_kernel<E, true, k()><<<(unsigned)(a.rows * tiles), 256, 0, st>>>(a, tiles);
+            else recurrence_step_kernel<E, false, k()><<<(unsigned)(a.rows * tiles), 256, 0, st>>>(a, tiles);
         });
         return hipGetLastError();
     });

@@ -253,6 +253,13 @@ def test_equal_calls_are_equal_and_streams_and_graphs_do_not_matter():
         assert all(torch.equal(a, b) for a, b in zip(results, eager))
 
 
+@pytest.mark.parametrize("B,T,C", [(1, 1300, 37), (2, 700, 3), (3, 400, 1), (70, 300, 133), (200, 257, 5), (195, 256, 2), (5, 255, 67)])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_odd_channels_over_several_blocks(B, T, C, dtype):
+    check(B, T, C, dtype=dtype, kind="smooth", lengths="ragged", initial=True, seed=C)
+    check(B, T, C, dtype=dtype, kind="decay", time_major=True, seed=C + 1)
+
+
 def test_two_layers_on_two_streams_at_once():
     """Their launches overlap, and each has its own workspace."""
     import torch
