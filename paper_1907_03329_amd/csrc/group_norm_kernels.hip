@@ -1177,8 +1177,8 @@ Way way_of(const esrnn_group_norm_shape &s)
         for (w.pieces = 1; w.pieces * 256 < w.tile; w.pieces *= 2) {}
         const int rows = 4 * (w.pieces == 1 ? kPositionRows : 1) * (64 >> w.log_w);     // of a workgroup
         const int64_t most = ((int64_t)s.N + rows - 1) / rows;
-        // (16384 x 2048 bf16, forward with 1024, 2048, 3072, 4096 workgroups: 34, 32, 30, 31 us; reverse with 512, 1024, 2048: 54, 45, 47)
-        w.forward_groups = (int)std::min<int64_t>(most, std::max(1, 3072 / w.tiles));
+        // (16384 x 2048 bf16, forward with 1024, 2048, 3000, 4096 workgroups: 34, 32, 30, 31 us; reverse with 512, 1024, 2048: 54, 45, 47)
+        w.forward_groups = (int)std::min<int64_t>(most, std::max(1, 3000 / w.tiles));
         w.backward_groups = (int)std::min<int64_t>(most, std::max(1, 1024 / w.tiles));
         w.part_rows = w.backward_groups;
         return w;
