@@ -44,12 +44,14 @@ struct Norm {
 
 __device__ __forceinline__ int length_of(const Norm &a, int n) { return a.lengths ? min(max(a.lengths[n], 0), a.T) : a.T; }
 
-__device__ __forceinline__ float activate(float u, int silu) { return silu ? u * sigmoids(u).of : u; }
+// (zero where exp(-u) is above 2^126, u < -87.3)
+__device__ __forceinline__ float sigmoid_of(float u) { return fast_rcp(1.0f + __builtin_amdgcn_exp2f(u * kSigmoidExponent)); }
+__device__ __forceinline__ float activate(float u, int silu) { return silu ? u * sigmoid_of(u) : u; }
 // derivative of u s, s = sigmoid(u): s + u s (1 - s).  (Of 1 - s only as much counts as the sum has room for.)
 __device__ __forceinline__ float slope(float u, int silu)
 {
     if (!silu) return 1.0f;
-    const float s = fast_rcp(1.0f + __builtin_amdgcn_exp2f(u * kSigmoidExponent));
+    const float s = sigmoid_of(u);
     return u * s * (1.0f - s) + s;
 }
 

@@ -94,16 +94,18 @@ struct Channels {
     }
 };
 
-// sigmoid(g) and sigmoid(-g), both to a few units in the last place (1 - sigmoid would lose those of the small one): with E = exp(-g),
-// 1 / (1 + E) and E / (1 + E).  Where E is infinite the first is zero and their product NaN, of which the minimum makes the 1 it has to be; a g
-// that is NaN stays one in the first.
+// sigmoid(g) and sigmoid(-g) (1 - sigmoid would lose the digits of the small one): with E = exp(-g), 1 / (1 + E) and E / (1 + E).  The hardware's
+// reciprocal gives no denormals: where 1 + E is above 2^126 (g < -87.3) it is zero, which is what the first is then taken to be; in the second 2^-126
+// stands in its place, so that the product is 1 or more, up to infinity, and the minimum makes the 1 it has to be.  (The minimum that keeps a NaN:
+// a gate that is NaN makes both of them NaN.)  The larger of the two is off by about a unit in the last place, 2^-24 of it; the smaller one by
+// some |g| / 3 more, as the exponent is one rounded product: 10 at |g| = 30.  Infinite gates give exactly 0 and 1.
 struct Sigmoids {
     float of, of_minus;
 };
 __device__ __forceinline__ Sigmoids sigmoids(float g)
 {
     const float e = __builtin_amdgcn_exp2f(g * kSigmoidExponent), r = fast_rcp(1.0f + e);
-    return Sigmoids{r, fminf(e * r, 1.0f)};
+    return Sigmoids{r, __builtin_elementwise_minimum(e * fmaxf(r, 0x1p-126f), 1.0f)};
 }
 
 inline bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
