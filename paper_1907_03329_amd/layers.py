@@ -2,7 +2,7 @@
 activation, AdamW over many tensors.
 
 Argument marshalling only, as in binding.py: the classes own the buffers of a layer, every call runs in the library's
-kernels on the current stream (or the one given), and a failed call raises EsrnnError.  There is no fallback.
+kernels on the current stream of the tensors' device (or the one given), and a failed call raises EsrnnError.  There is no fallback.
 Tensors that a call names have to live until the stream has run it, as with any work of torch on that stream.
 """
 from __future__ import annotations
@@ -92,9 +92,18 @@ def _raise(status, what):
         raise EsrnnError(status, what)
 
 
+# (torch.cuda.current_stream() builds an object around this number: 1.9 us of a call of 8)
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _stream(stream, device) -> int:
-    # (torch.cuda.current_stream() builds an object around this number: 1.9 us of a call of 8)
-    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+    """The stream given, which has to be one of `device`, or that device's current one.  The library launches on the current device: the callers
+    below make `device` that first."""
+    if stream is None:
+        return _raw_stream(device.index)
+    if stream.device != device:
+        raise ValueError(f"the stream is one of {stream.device}, the tensors are on {device}")
+    return stream.cuda_stream
 
 
 def _bytes(fn, *args) -> int:
@@ -169,6 +178,9 @@ class GatedRecurrence:
 
     def forward(self, x, gate, lengths=None, initial=None, stream=None):
         """(out, last): all states in the element type, zero past the lengths, and the last one of every sequence in float32."""
+        if _current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self.forward(x, gate, lengths, initial, stream)
         s = self._shape
         x_ptr, gate_ptr = self._elements(x, "x", s.x_stride), self._elements(gate, "gate", s.gate_stride)
         _raise(self._lib.esrnn_recurrence_forward(
@@ -181,6 +193,9 @@ class GatedRecurrence:
 
     def backward(self, x, gate, grad_out, lengths=None, grad_last=None, grad_x=None, grad_gate=None, stream=None):
         """(grad_x, grad_gate, grad_initial) for the forward pass last run, which had the same x, gate and lengths."""
+        if _current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self.backward(x, gate, grad_out, lengths, grad_last, grad_x, grad_gate, stream)
         if not self.training or not self._forward_done:
             raise EsrnnError(4, "GatedRecurrence.backward")
         grad_x = self.grad_x if grad_x is None else grad_x
@@ -203,6 +218,9 @@ def recurrence_step(x, gate, state, out, slots=None, kind: str = "smooth", strea
     shape, dtype, device = x.shape, x.dtype, x.device
     if len(shape) != 2 or state.dim() != 2 or device.type != "cuda":
         raise ValueError("x has to be [rows, C] and state [pool, C] on a GPU")
+    if _current_device() != device.index:
+        with torch.cuda.device(device):
+            return recurrence_step(x, gate, state, out, slots, kind, stream)
     rows, channels = shape
     (x_stride, x_channel), (gate_stride, gate_channel), (out_stride, out_channel) = x.stride(), gate.stride(), out.stride()
     if channels != 1 and not x_channel == gate_channel == out_channel == 1:
@@ -249,6 +267,9 @@ class GroupNorm:
 
     def forward(self, x, scale, shift, lengths=None, stream=None):
         """out, zero past the lengths."""
+        if _current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self.forward(x, scale, shift, lengths, stream)
         _raise(self._lib.esrnn_group_norm_forward(
             self._ref, *self._given(x, scale, shift, lengths), self._out_ptr, self._stats_ptr, self._workspace_ptr,
             _stream(stream, self.device)), "esrnn_group_norm_forward")
@@ -257,6 +278,9 @@ class GroupNorm:
 
     def backward(self, x, scale, shift, grad_out, lengths=None, stream=None):
         """(grad_x, grad_scale, grad_shift) for the forward pass last run, which had the same x, scale, shift and lengths."""
+        if _current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self.backward(x, scale, shift, grad_out, lengths, stream)
         if not self.training or not self._forward_done:
             raise EsrnnError(4, "GroupNorm.backward")
         _raise(self._lib.esrnn_group_norm_backward(
@@ -314,10 +338,14 @@ class AdamW:
         self.lr, self.beta1, self.beta2, self.eps, self.clip_norm, self.seed = lr, beta1, beta2, eps, clip_norm, int(seed)
         self._states = [None if t is None else t.data_ptr() for t in (self.m, self.v, self.r, self.m_scale, self.r_scale, self.grad_norm,
                                                                       self.workspace)]
-        _raise(self._lib.esrnn_adamw_bind(handle, self._states[-1], _stream(None, self.device)), "esrnn_adamw_bind")
+        with torch.cuda.device(self.device):
+            _raise(self._lib.esrnn_adamw_bind(handle, self._states[-1], _stream(None, self.device)), "esrnn_adamw_bind")
 
     def step(self, step: int, stream=None) -> None:
         """Update number `step`, from 1 on.  (The first one on another stream than the constructor's has to be ordered behind it.)"""
+        if _current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self.step(step, stream)
         if self._handle is None:
             raise EsrnnError(1, "AdamW.step after close")
         opt = AdamWConfig(self.lr, self.beta1, self.beta2, self.eps, self.clip_norm, self.seed & 0xFFFFFFFF)
