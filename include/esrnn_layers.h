@@ -34,7 +34,8 @@ typedef enum { ESRNN_F32 = 0, ESRNN_BF16 = 1, ESRNN_F16 = 2 } esrnn_dtype;
  *       (exponential smoothing, Section 3.1 Eq. (1), with a coefficient of its own at every position)
  *   ESRNN_RECURRENCE_DECAY    h_t = a_t h_{t-1} + x_t,            a = sigmoid(gate)
  * Strides are in elements, of a sequence and of a position; channels are contiguous.  Any order of B and T, gaps, and
- * x and gate as parts of one array are fine; a written array must not overlap itself or another.
+ * x and gate as parts of one array are fine; a written array must not overlap itself or another (last initial, say, or grad_x x): refused where
+ * arrays begin at one place or have the same strides.
  */
 typedef enum { ESRNN_RECURRENCE_SMOOTH = 0, ESRNN_RECURRENCE_DECAY = 1 } esrnn_recurrence_kind;
 

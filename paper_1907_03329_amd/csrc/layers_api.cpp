@@ -1,6 +1,7 @@
 // C ABI of the layer operators (include/esrnn_layers.h): argument checks and the launches of each call.
 #include <cmath>
 #include <new>
+#include <utility>
 
 #include "layers_internal.h"
 
@@ -41,6 +42,32 @@ bool writable_strides(const esrnn_recurrence_shape &s, const int64_t st[2])
     const bool sequences_inside = (s.B == 1 || st[0] >= s.C) && (s.T == 1 || st[1] >= (s.B == 1 ? 0 : (int64_t)(s.B - 1) * st[0]) + s.C);
     return positions_inside || sequences_inside;
 }
+
+// Whether an array that is written shares elements with another one of its type, as far as strides show it: arrays that begin at one place, or
+// have the same strides and lie within each other's reach.  (Those with strides of their own that reach into each other are taken to be the caller's design.)
+bool rows_overlap(const esrnn_recurrence_shape &s, const void *written, const int64_t written_stride[2], const void *other, const int64_t other_stride[2])
+{
+    if (written == other) return true;
+    const int64_t e = (int64_t)element_bytes(s.dtype), row = s.C * e;
+    const auto reach = [&](const int64_t st[2]) { return ((s.B - 1) * st[0] + (s.T - 1) * st[1]) * e + row; };
+    const int64_t apart = reinterpret_cast<intptr_t>(other) - reinterpret_cast<intptr_t>(written);
+    if (apart >= reach(written_stride) || -apart >= reach(other_stride)) return false;
+    if ((s.B > 1 && written_stride[0] != other_stride[0]) || (s.T > 1 && written_stride[1] != other_stride[1])) return false;
+    // Rows of the one are those of the other, moved.  Strides of a written array nest: all rows of the inner dimension lie within one step of the
+    // outer one, so only the two nearest steps of each can bring two rows together.
+    int64_t count[2] = {s.B, s.T}, step[2] = {s.B > 1 ? written_stride[0] * e : 0, s.T > 1 ? written_stride[1] * e : 0};
+    if (step[0] < step[1]) std::swap(count[0], count[1]), std::swap(step[0], step[1]);
+    for (int i = 0; i < 2; ++i) {
+        const int64_t outer = step[0] ? (apart < 0 ? -(-apart / step[0]) - 1 : apart / step[0]) + i : 0, rest = apart - outer * step[0];
+        for (int j = 0; j < 2; ++j) {
+            const int64_t inner = step[1] ? (rest < 0 ? -(-rest / step[1]) - 1 : rest / step[1]) + j : 0, left = rest - inner * step[1];
+            if (outer > -count[0] && outer < count[0] && inner > -count[1] && inner < count[1] && left > -row && left < row) return true;
+        }
+    }
+    return false;
+}
+// of fp32 arrays of n and m elements, either of which may be null
+bool floats_overlap(const float *a, size_t n, const float *b, size_t m) { return a && b && a < b + m && b < a + n; }
 
 }  // namespace
 
@@ -102,6 +129,11 @@ esrnn_status esrnn_recurrence_forward(const esrnn_recurrence_shape *shape, const
         !floats_aligned(initial) || !floats_aligned(last) || !floats_aligned(saved))
         return ESRNN_ERR_CONFIG;
     if (!aligned_to(workspace, 256)) return ESRNN_ERR_WORKSPACE;
+    const size_t states = (size_t)s.B * s.C, kept = states * recurrence_plan(s).blocks;
+    const float *left = static_cast<const float *>(saved);
+    if (rows_overlap(s, out, s.out_stride, x, s.x_stride) || rows_overlap(s, out, s.out_stride, gate, s.gate_stride) ||
+        floats_overlap(last, states, initial, states) || floats_overlap(left, kept, initial, states) || floats_overlap(left, kept, last, states))
+        return ESRNN_ERR_CONFIG;
     const RecurrenceForward f{x, gate, lengths, initial, out, last, static_cast<float *>(saved), static_cast<float *>(workspace)};
     ESRNN_TRY(launch_recurrence_forward(s, f, static_cast<hipStream_t>(stream)));
     return ESRNN_OK;
@@ -121,6 +153,16 @@ esrnn_status esrnn_recurrence_backward(const esrnn_recurrence_shape *shape, cons
         !floats_aligned(grad_last) || !floats_aligned(grad_initial))
         return ESRNN_ERR_CONFIG;
     if (!aligned_to(workspace, 256)) return ESRNN_ERR_WORKSPACE;
+    const size_t states = (size_t)s.B * s.C, kept = states * recurrence_plan(s).blocks;
+    if (rows_overlap(s, grad_x, s.grad_x_stride, grad_gate, s.grad_gate_stride) || floats_overlap(grad_initial, states, grad_last, states) ||
+        floats_overlap(grad_initial, states, static_cast<const float *>(saved), kept))
+        return ESRNN_ERR_CONFIG;
+    const struct {
+        const void *p;
+        const int64_t *stride;
+    } read[3] = {{x, s.x_stride}, {gate, s.gate_stride}, {grad_out, s.grad_out_stride}};
+    for (const auto &r : read)
+        if (rows_overlap(s, grad_x, s.grad_x_stride, r.p, r.stride) || rows_overlap(s, grad_gate, s.grad_gate_stride, r.p, r.stride)) return ESRNN_ERR_CONFIG;
     const RecurrenceBackward f{x, gate, lengths, static_cast<const float *>(saved), grad_out, grad_last, grad_x, grad_gate, grad_initial,
                                static_cast<float *>(workspace)};
     ESRNN_TRY(launch_recurrence_backward(s, f, static_cast<hipStream_t>(stream)));

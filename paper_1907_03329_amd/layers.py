@@ -139,7 +139,8 @@ class GatedRecurrence:
     Tensors are [B, T, C], with time_major [T, B, C]; x, gate, grad_out (and grad_x, grad_gate, where the caller gives them) may
     be strided in any way that keeps channels next to each other, as the two halves of one projection's result do.
     lengths: int32 [B], positions that exist; initial, grad_last: float32 [B, C] or None (zero).
-    Owns out, last, the gradients and what the reverse pass needs, all overwritten by the next call."""
+    Owns out, last, the gradients and what the reverse pass needs, all overwritten by the next call; last may be that call's initial, and
+    grad_initial the next reverse pass's grad_last (they are copied before)."""
 
     def __init__(self, B: int, T: int, C_: int, kind: str = "smooth", dtype=None, time_major: bool = False,
                  training: bool = True, device="cuda"):
@@ -158,7 +159,7 @@ class GatedRecurrence:
         self.last = torch.empty(self._rows, dtype=torch.float32, device=self.device)
         self._out_ptr, self._last_ptr, self._workspace_ptr = self.out.data_ptr(), self.last.data_ptr(), self.workspace.data_ptr()
         self._elements(self.out, "out", s.out_stride)
-        self._forward_done, self._saved_ptr = False, None
+        self._forward_done, self._saved_ptr, self._carried = False, None, None
         if training:
             self.saved = torch.empty(saved // 4, dtype=torch.float32, device=self.device)
             self.grad_x, self.grad_gate = (torch.empty(self._size, dtype=dtype, device=self.device) for _ in range(2))
@@ -176,6 +177,19 @@ class GatedRecurrence:
     def _lengths(self, lengths):
         return _check_optional(lengths, "lengths", self._rows[:1], torch.int32, self.device)
 
+    def _states(self, t, name, own, stream):
+        """The address of states that a call reads: of a copy, if they are the layer's `own` that the call overwrites."""
+        if t is None:
+            return None
+        at = _check(t, name, self._rows, torch.float32, self.device)
+        if at != own:
+            return at
+        if self._carried is None:
+            self._carried = torch.empty_like(t)
+        with torch.cuda.stream(stream):     # (None: the current one)
+            self._carried.copy_(t)
+        return self._carried.data_ptr()
+
     def forward(self, x, gate, lengths=None, initial=None, stream=None):
         """(out, last): all states in the element type, zero past the lengths, and the last one of every sequence in float32."""
         if _current_device() != self.device.index:
@@ -185,7 +199,7 @@ class GatedRecurrence:
         x_ptr, gate_ptr = self._elements(x, "x", s.x_stride), self._elements(gate, "gate", s.gate_stride)
         _raise(self._lib.esrnn_recurrence_forward(
             self._ref, x_ptr, gate_ptr, self._lengths(lengths),
-            _check_optional(initial, "initial", self._rows, torch.float32, self.device), self._out_ptr, self._last_ptr,
+            self._states(initial, "initial", self._last_ptr, stream), self._out_ptr, self._last_ptr,
             self._saved_ptr, self._workspace_ptr, _stream(stream, self.device)),
             "esrnn_recurrence_forward")
         self._forward_done = True
@@ -207,7 +221,7 @@ class GatedRecurrence:
         gg_ptr = self._elements(grad_gate, "grad_gate", s.grad_gate_stride)
         _raise(self._lib.esrnn_recurrence_backward(
             self._ref, x_ptr, gate_ptr, self._lengths(lengths), self._saved_ptr, d_ptr,
-            _check_optional(grad_last, "grad_last", self._rows, torch.float32, self.device), gx_ptr, gg_ptr,
+            self._states(grad_last, "grad_last", self._grad_initial_ptr, stream), gx_ptr, gg_ptr,
             self._grad_initial_ptr, self._workspace_ptr, _stream(stream, self.device)), "esrnn_recurrence_backward")
         return grad_x, grad_gate, self.grad_initial
 
