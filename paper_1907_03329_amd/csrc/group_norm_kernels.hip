@@ -955,27 +955,34 @@ __device__ __forceinline__ float workgroup_sum(float v, float *shared)
     return (shared[0] + shared[1]) + (shared[2] + shared[3]);
 }
 
+// Workgroups of the sums over groups, one a group up to this many: a launch has to have fewer than 2^32 threads.
+constexpr int kMostGroupWorkgroups = 1 << 22;
+unsigned group_workgroups(const esrnn_group_norm_shape &s) { return (unsigned)std::min<int64_t>((int64_t)s.N * s.G, kMostGroupWorkgroups); }
+
 // stats [N][G][2]: a workgroup a group
 __global__ void __launch_bounds__(256) norm_stats_kernel(Norm a)
 {
+    // (two places in turn: a barrier lies between the reads of one and its next writes)
     __shared__ float s_sum[2][4];
-    const int n = blockIdx.x / a.G, g = blockIdx.x % a.G, length = length_of(a, n);
-    const float *p = a.parts + (size_t)n * a.chunks * 2 * a.C + g * a.D;
-    // the mean first, then what lies off it: sums whose terms do not wait for each other
-    const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
-    float sum = 0.0f, square = 0.0f;
-    for_entries(a, [&](int chunk, int c) { sum += (float)positions_in(a, chunk, length) * p[(size_t)chunk * 2 * a.C + c]; });
-    const float mean = workgroup_sum(sum, s_sum[0]) * inverse;
-    for_entries(a, [&](int chunk, int c) {
-        const int here = positions_in(a, chunk, length);
-        const float d = p[(size_t)chunk * 2 * a.C + c] - mean;
-        if (here > 0) square += p[((size_t)chunk * 2 + 1) * a.C + c] + (float)here * d * d;
-    });
-    square = workgroup_sum(square, s_sum[1]);
-    if (threadIdx.x == 0) {
-        float *s = a.stats + (size_t)blockIdx.x * 2;
-        s[0] = mean;
-        s[1] = 1.0f / sqrtf(square * inverse + a.eps);
+    for (int item = blockIdx.x; item < a.N * a.G; item += gridDim.x) {
+        const int n = item / a.G, g = item % a.G, length = length_of(a, n);
+        const float *p = a.parts + (size_t)n * a.chunks * 2 * a.C + g * a.D;
+        // the mean first, then what lies off it: sums whose terms do not wait for each other
+        const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
+        float sum = 0.0f, square = 0.0f;
+        for_entries(a, [&](int chunk, int c) { sum += (float)positions_in(a, chunk, length) * p[(size_t)chunk * 2 * a.C + c]; });
+        const float mean = workgroup_sum(sum, s_sum[0]) * inverse;
+        for_entries(a, [&](int chunk, int c) {
+            const int here = positions_in(a, chunk, length);
+            const float d = p[(size_t)chunk * 2 * a.C + c] - mean;
+            if (here > 0) square += p[((size_t)chunk * 2 + 1) * a.C + c] + (float)here * d * d;
+        });
+        square = workgroup_sum(square, s_sum[1]);
+        if (threadIdx.x == 0) {
+            float *s = a.stats + (size_t)item * 2;
+            s[0] = mean;
+            s[1] = 1.0f / sqrtf(square * inverse + a.eps);
+        }
     }
 }
 
@@ -1080,20 +1087,22 @@ __global__ void __launch_bounds__(256) norm_group_sums_kernel(Norm a, int channe
         sum_rows_of_tile<4>(a.parts + (size_t)which * a.C, a.N * a.chunks, a.C, blockIdx.x % tiles, which ? a.grad_scale : a.grad_shift);
         return;
     }
-    const int item = (int)blockIdx.x - channel_groups, n = item / a.G, g = item % a.G, length = length_of(a, n);
-    const float *p = a.parts + (size_t)n * a.chunks * 2 * a.C + g * a.D, *scale = a.scale + g * a.D;
-    float s1 = 0.0f, s2 = 0.0f;
-    for_entries(a, [&](int chunk, int c) {
-        s1 += scale[c] * p[(size_t)chunk * 2 * a.C + c];
-        s2 += scale[c] * p[((size_t)chunk * 2 + 1) * a.C + c];
-    });
-    s1 = workgroup_sum(s1, s_sum[0]);
-    s2 = workgroup_sum(s2, s_sum[1]);
-    if (threadIdx.x == 0) {
-        const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
-        float *s = a.parts + (size_t)a.N * a.chunks * 2 * a.C + (size_t)item * 2;
-        s[0] = s1 * inverse;
-        s[1] = s2 * inverse;
+    for (int item = (int)blockIdx.x - channel_groups; item < a.N * a.G; item += (int)gridDim.x - channel_groups) {
+        const int n = item / a.G, g = item % a.G, length = length_of(a, n);
+        const float *p = a.parts + (size_t)n * a.chunks * 2 * a.C + g * a.D, *scale = a.scale + g * a.D;
+        float s1 = 0.0f, s2 = 0.0f;
+        for_entries(a, [&](int chunk, int c) {
+            s1 += scale[c] * p[(size_t)chunk * 2 * a.C + c];
+            s2 += scale[c] * p[((size_t)chunk * 2 + 1) * a.C + c];
+        });
+        s1 = workgroup_sum(s1, s_sum[0]);
+        s2 = workgroup_sum(s2, s_sum[1]);
+        if (threadIdx.x == 0) {
+            const float inverse = length > 0 ? 1.0f / ((float)length * (float)a.D) : 0.0f;
+            float *s = a.parts + (size_t)a.N * a.chunks * 2 * a.C + (size_t)item * 2;
+            s[0] = s1 * inverse;
+            s[1] = s2 * inverse;
+        }
     }
 }
 
@@ -1356,7 +1365,7 @@ hipError_t launch_group_norm_forward(const esrnn_group_norm_shape &s, const Grou
             if (!a.stats) a.stats = a.parts + groups_at(s, w);
             const dim3 grid((unsigned)(s.N * w.tiles), w.chunks);
             norm_moments_kernel<E, al()><<<grid, 256, 0, st>>>(a);
-            norm_stats_kernel<<<(unsigned)(s.N * s.G), 256, 0, st>>>(a);
+            norm_stats_kernel<<<group_workgroups(s), 256, 0, st>>>(a);
             norm_apply_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
         });
         return hipGetLastError();
@@ -1400,7 +1409,7 @@ hipError_t launch_group_norm_backward(const esrnn_group_norm_shape &s, const Gro
             const dim3 grid((unsigned)(s.N * w.tiles), w.chunks);
             norm_gradient_sums_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
             const int channel_groups = w.part_rows < kManyRows ? 2 * ((s.C + 63) / 64) : 0;
-            norm_group_sums_kernel<<<(unsigned)(channel_groups + s.N * s.G), 256, 0, st>>>(a, channel_groups);
+            norm_group_sums_kernel<<<channel_groups + group_workgroups(s), 256, 0, st>>>(a, channel_groups);
             if (!channel_groups) sum_rows(a, w.part_rows, runs, st);
             norm_gradient_kernel<E, al(), silu()><<<grid, 256, 0, st>>>(a);
         });
