@@ -1152,7 +1152,9 @@ struct Way {
     int part_rows;              // rows [2][C] of channel sums that the reverse pass leaves
 };
 
-constexpr int kMostPositionTile = 512, kPositionRows = 4;       // channels of a group, samples at once (of groups up to 256)
+// Channels of a group: of a wave; of a workgroup (four chunks of 1024: the widest that was built, beyond it the stream way takes single positions
+// too, with one of its sixteen rows of threads at work); samples at once (of groups up to 256).
+constexpr int kMostPositionTile = 512, kMostWideTile = 4096, kPositionRows = 4;
 
 // Rows are added up in two launches, the first in kRuns runs, from this many on: one alone reads them with 2 C / 64 workgroups (reverse pass of
 // 8000 x 16 x 128 bf16 62 us, with one launch 81; 2048 x 16 x 64 fp32 20 against 22).
@@ -1162,7 +1164,7 @@ Way way_of(const esrnn_group_norm_shape &s)
 {
     Way w{};
     const int D = s.C / s.G;
-    if (s.T == 1 && D > kMostPositionTile && D <= 4096) {
+    if (s.T == 1 && D > kMostPositionTile && D <= kMostWideTile) {
         // (a wave for each group needs more registers than it has beyond 512 channels: figures above)
         w.kind = kWide;
         w.tiles = s.G;
@@ -1326,6 +1328,8 @@ size_t groups_at(const esrnn_group_norm_shape &s, const Way &w) { return (size_t
 size_t runs_at(const esrnn_group_norm_shape &s, const Way &w) { return groups_at(s, w) + (w.kind == kStream ? (size_t)s.N * s.G * 2 : 0); }
 
 }  // namespace
+
+bool group_norm_single_positions(const esrnn_group_norm_shape &s) { return s.T == 1 && s.C / s.G <= kMostWideTile; }
 
 size_t group_norm_workspace_floats(const esrnn_group_norm_shape &s)
 {

@@ -75,9 +75,13 @@ namespace {
 
 bool group_norm_sizes(const esrnn_group_norm_shape &s)
 {
-    return s.N >= 1 && s.T >= 1 && s.C >= 1 && s.G >= 1 && s.C <= (1 << 20) && s.T <= (1 << 30) && s.C % s.G == 0 &&
-           (int64_t)s.N * s.T <= (int64_t(1) << 31) && (int64_t)s.N * ((s.C + 63) / 64) <= (1 << 22) && (int64_t)s.N * s.G <= (1 << 25) &&
-           (s.activation == ESRNN_NORM_NONE || s.activation == ESRNN_NORM_SILU) && element_type(s.dtype) && s.eps > 0.0f &&
+    if (!(s.N >= 1 && s.T >= 1 && s.C >= 1 && s.G >= 1 && s.C <= (1 << 20) && s.T <= (1 << 30) && s.C % s.G == 0)) return false;
+    // single positions by some thousand workgroups, whatever N is: offsets of samples are 64 bits, their numbers 32
+    // anything else by a workgroup or more for (sample, tile of channels)
+    const bool fits = group_norm_single_positions(s) ? s.N <= (1 << 30) && s.C <= kMostElements / s.N
+                                                     : (int64_t)s.N * s.T <= (int64_t(1) << 31) &&
+                                                           (int64_t)s.N * ((s.C + 63) / 64) <= (1 << 22) && (int64_t)s.N * s.G <= (1 << 25);
+    return fits && (s.activation == ESRNN_NORM_NONE || s.activation == ESRNN_NORM_SILU) && element_type(s.dtype) && s.eps > 0.0f &&
            s.eps < __builtin_inff();
 }
 

@@ -187,6 +187,8 @@ struct GroupNormArgs {
     float *stats, *grad_scale, *grad_shift;
     float *parts;               // the workspace
 };
+// Whether every position is normalised by itself, by kernels of their own (T = 1 and groups that they hold).
+bool group_norm_single_positions(const esrnn_group_norm_shape &s);
 size_t group_norm_workspace_floats(const esrnn_group_norm_shape &s);
 hipError_t launch_group_norm_forward(const esrnn_group_norm_shape &s, const GroupNormArgs &a, hipStream_t st);
 hipError_t launch_group_norm_backward(const esrnn_group_norm_shape &s, const GroupNormArgs &a, hipStream_t st);

@@ -58,3 +58,40 @@ def test_more_groups_than_a_launch_has_workgroups():
     assert not out[0].any() and not gx[0].any()
     for t in (out, gx):     # zero behind the lengths
         assert not any(t[k:k + (1 << 15), 2:].any() for k in range(0, N - 1 - (1 << 15), 1 << 15))
+
+
+@pytest.mark.parametrize("N,C,G", [(131072, 4096, 32), ((1 << 23) + 5, 64, 16), (600001, 8192, 2)])
+def test_many_positions_by_themselves(N, C, G):
+    """More samples times channels than the way for long samples takes, more than 2^25 groups, offsets beyond 2^32 elements in wide groups."""
+    import torch
+    free, _ = torch.cuda.mem_get_info()
+    if free < 10 * N * C + (16 << 30):
+        pytest.skip("needs more device memory")
+    generator = torch.Generator(device="cuda").manual_seed(C)
+    x, d = (torch.empty((N, 1, C), dtype=torch.bfloat16, device="cuda").normal_(generator=generator) for _ in range(2))
+    scale, shift = torch.linspace(0.5, 1.5, C, device="cuda"), torch.linspace(-1.0, 1.0, C, device="cuda")
+    lengths = (torch.arange(N, device="cuda") % 7 > 0).int()
+    layer = layers.GroupNorm(N, 1, C, G, activation="silu", eps=EPS, dtype=torch.bfloat16)
+    for t in (layer.out, layer.stats, layer.grad_x):
+        t.fill_(float("nan"))
+    out = layer.forward(x, scale, shift, lengths=lengths)
+    gx, gs, gb = layer.backward(x, scale, shift, d, lengths=lengths)
+    sums, tolerance = torch.zeros(4, C, dtype=torch.float64, device="cuda"), ROUNDING["bfloat16"] + ARITHMETIC
+    rows = (1 << 26) // C
+    for first in range(0, N, rows):
+        at = slice(first, min(first + rows, N))
+        v, exists = x[at, 0].double().unflatten(1, (G, C // G)), lengths[at].double()[:, None]
+        mean, var = v.mean(2, keepdim=True), v.var(2, unbiased=False, keepdim=True)
+        rstd = 1.0 / (var + EPS).sqrt()
+        xhat = ((v - mean) * rstd).flatten(1)
+        u = xhat * scale + shift
+        p = torch.sigmoid(u)
+        du = d[at, 0].double() * (p + u * p * (1 - p)) * exists
+        g, xg = (du * scale).unflatten(1, (G, C // G)), xhat.unflatten(1, (G, C // G))
+        dx = (rstd * (g - g.mean(2, keepdim=True) - xg * (g * xg).mean(2, keepdim=True))).flatten(1)
+        for got, want in ((out, u * p * exists), (gx, dx)):
+            assert float((got[at, 0].double() - want).abs().max()) <= tolerance * float(want.abs().max()), first
+        along = du * xhat
+        sums += torch.stack([along.sum(0), along.abs().sum(0), du.sum(0), du.abs().sum(0)])
+    assert float((gs.double() - sums[0]).abs().max()) <= ARITHMETIC * float(sums[1].max())
+    assert float((gb.double() - sums[2]).abs().max()) <= ARITHMETIC * float(sums[3].max())
