@@ -32,6 +32,15 @@ def windows(y: np.ndarray, lengths: np.ndarray):
     return contiguous(features), contiguous(diff[:, LAGS:LAGS + P]), np.maximum(lengths - 1 - LAGS, 0).astype(np.int32)
 
 
+def following(features, targets, lengths):
+    """Features [B, LAGS] of the position behind the last one of each series: the last one's, moved on by its target, which is the last log
+    difference that there is."""
+    if int(lengths.min()) < 1:
+        raise ValueError(f"series of fewer than {LAGS + 2} observations have no position to go on from")
+    b, last = torch.arange(len(features), device=features.device), lengths.long() - 1
+    return torch.cat([features[b, last, 1:], targets[b, last, None].to(features.dtype)], 1)
+
+
 class Forecaster:
     """Parameters, buffers and steps of the network for batches of B series of P positions."""
 
@@ -137,8 +146,7 @@ def main(argv=None):
     ms = (time.perf_counter() - began) / max(1, args.steps - 1) * 1e3
     spread = float((targets[exists.view(-1, P) > 0]).square().mean())
     net.predict(features, lengths, exists)
-    ends = torch.stack([features[b, n - 1] for b, n in enumerate(lengths.tolist())])
-    ahead = net.forecast(ends, net.last.clone(), cfg.H)
+    ahead = net.forecast(following(features, targets, lengths), net.last.clone(), cfg.H)
     print(f"{args.workload}, {args.batch} series, {P} positions, {args.channels} channels, {args.dtype}, moments in {args.bits} bits: "
           f"mean squared error {first:.5f} -> {float(loss):.5f} (mean square of the targets {spread:.5f}), {ms:.3f} ms a step; "
           f"forecasts {tuple(ahead.shape)}, finite: {bool(ahead.isfinite().all())}")
