@@ -128,6 +128,8 @@ def main(argv=None):
     ap.add_argument("--dtype", choices=("f32", "bf16", "f16"), default="bf16")
     ap.add_argument("--bits", type=int, choices=(32, 8), default=8)
     args = ap.parse_args(argv)
+    if args.steps < 1:
+        ap.error("--steps has to be at least 1")
     dtype = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[args.dtype]
     cfg = synth.CONFIGS[args.workload].with_(B=args.batch)
     given = synth.make_inputs(cfg, seed=0, ragged=True)
@@ -137,7 +139,8 @@ def main(argv=None):
     features, targets, lengths, exists = (torch.from_numpy(t).cuda() for t in (features, targets, lengths, exists))
     features = features.to(dtype)
     net = Forecaster(args.batch, P, args.channels, dtype=dtype, state_bits=args.bits)
-    first = float(net.train_step(features, targets, lengths, exists))
+    loss = net.train_step(features, targets, lengths, exists)
+    first = float(loss)
     torch.cuda.synchronize()
     began = time.perf_counter()
     for _ in range(args.steps - 1):
