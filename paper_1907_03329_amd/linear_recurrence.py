@@ -86,7 +86,7 @@ class Forecaster:
         g, z = self.grads, self._z.view(-1, C)
         torch.sum(d, dim=0, out=g["b_out"])
         g["w_out"].copy_(z.float().t() @ d)       # (products over all positions in 32 bits)
-        grad_z = (d @ self.params["w_out"].t()).to(self.dtype)
+        grad_z = (d @ self.weights["w_out"].float().t()).to(self.dtype)     # (of the weights that the forward pass had)
         states, scale, shift = self.recurrence.out.view(-1, 1, C), self.params["scale"], self.params["shift"]
         grad_states, grad_scale, grad_shift = self.norm.backward(states, scale, shift, grad_z.view(-1, 1, C), lengths=exists)
         g["scale"].copy_(grad_scale)
