@@ -82,21 +82,22 @@ class Forecaster:
         count = mask.sum().clamp_min(1.0)
         error = (self.predict(features, lengths, exists) - targets) * mask
         loss = (error * error).sum() / count
-        d = (2.0 / count * error).view(-1, 1)
+        # Gradients of the sum, not of the mean, until they are in 32 bits: a position's share of a large batch is too small for fp16.
+        d, share = (2.0 * error).view(-1, 1), 1.0 / count
         g, z = self.grads, self._z.view(-1, C)
-        torch.sum(d, dim=0, out=g["b_out"])
-        g["w_out"].copy_(z.float().t() @ d)       # (products over all positions in 32 bits)
+        torch.mul(d.sum(0), share, out=g["b_out"])
+        torch.mul(z.float().t() @ d, share, out=g["w_out"])       # (products over all positions in 32 bits)
         grad_z = (d @ self.weights["w_out"].float().t()).to(self.dtype)     # (of the weights that the forward pass had)
         states, scale, shift = self.recurrence.out.view(-1, 1, C), self.params["scale"], self.params["shift"]
         grad_states, grad_scale, grad_shift = self.norm.backward(states, scale, shift, grad_z.view(-1, 1, C), lengths=exists)
-        g["scale"].copy_(grad_scale)
-        g["shift"].copy_(grad_shift)
+        torch.mul(grad_scale, share, out=g["scale"])
+        torch.mul(grad_shift, share, out=g["shift"])
         self.recurrence.backward(self._both[..., :C], self._both[..., C:], grad_states.view(B, P, C), lengths=lengths,
                                  grad_x=self.grad_both[..., :C], grad_gate=self.grad_both[..., C:])
         flat = self.grad_both.view(-1, 2 * C)
         flat = flat.float()
-        g["w_in"].copy_(features.view(-1, LAGS).float().t() @ flat)
-        torch.sum(flat, dim=0, out=g["b_in"])
+        torch.mul(features.view(-1, LAGS).float().t() @ flat, share, out=g["w_in"])
+        torch.mul(flat.sum(0), share, out=g["b_in"])
         self.steps += 1
         self.optimiser.step(self.steps)
         return loss
