@@ -141,8 +141,8 @@ __device__ __forceinline__ Scale scale_of(int most_bits)
     if (most_bits >= 0x7f800000) return {__builtin_nanf(""), 0.0f, false};
     return scale > kLeastScale ? Scale{scale, 1.0f / scale, true} : Scale{0.0f, 0.0f, true};
 }
-// a magnitude as the float whose upper 12 bits are its code, rounded down
-__device__ __forceinline__ unsigned scaled(float magnitude, const Scale &s) { return __builtin_bit_cast(unsigned, magnitude * s.inverse * kToCode); }
+// a magnitude in units of the scale (not zero unless magnitude or scale are) as the float whose upper 12 bits are its code, rounded down
+__device__ __forceinline__ unsigned scaled(float units) { return __builtin_bit_cast(unsigned, units * kToCode); }
 // 16 random bits behind the three of the code's mantissa, of the 20 that are cut off: up with the probability of what is cut off
 __device__ __forceinline__ unsigned code_of(unsigned y, unsigned bits16) { return (y + (bits16 << 4)) >> 20; }
 
@@ -245,9 +245,11 @@ __global__ void __launch_bounds__(256) adamw_update_kernel(AdamWUpdate u)
         for (int k = 0; k < 4; ++k) {
             const unsigned w = random_word(place + k, key);      // (a multiple of four: no carry into the upper word)
             const float mk = m[j][k];       // (a bit cast of the vector's element itself is one of its first element)
-            const unsigned ym = scaled(fabsf(mk), sm), yr = scaled(root[k], sr), sign = __builtin_bit_cast(unsigned, mk) >> 24 & 0x80u;
+            const float units = root[k] * sr.inverse;
+            const unsigned ym = scaled(fabsf(mk) * sm.inverse), yr = scaled(units), sign = __builtin_bit_cast(unsigned, mk) >> 24 & 0x80u;
             m_codes |= (code_of(ym, w >> 16) | sign) << 8 * k;
-            r_codes |= max(code_of(yr, w & 0xffffu), min(yr, 1u)) << 8 * k;
+            // (at least one for any root: `yr` itself may be too small for a float)
+            r_codes |= max(code_of(yr, w & 0xffffu), min(__builtin_bit_cast(unsigned, units), 1u)) << 8 * k;
         }
         if (!sm.finite) m_codes = 0x7f7f7f7fu;
         if (!sr.finite) r_codes = 0x7f7f7f7fu;
