@@ -26,3 +26,20 @@ def test_a_small_root_beside_a_large_one_keeps_the_smallest_code(small):
     g.zero_()
     opt.step(200)
     assert bool((opt.r.view(torch.uint8) > 0).all()) and float((p - before).abs().max()) <= 1e-2
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-37, 1e-38, 1e-40, 1e-44, 1e-50, 1e-300])
+def test_eps_that_is_no_normal_number(bits, eps):
+    """Gradients of zero: nothing but the decay, as 0 / eps is 0 for any eps; others: as with eps of 1e-30."""
+    import torch
+    results = []
+    for e in (eps, 1e-30):
+        p, g = torch.ones(512, device="cuda"), torch.zeros(512, device="cuda")
+        g[:100] = torch.linspace(1e-12, 1.0, 100)
+        opt = layers.AdamW([p], [g], state_bits=bits, lr=0.1, weight_decay=0.5, eps=e)
+        for step in (1, 2):
+            opt.step(step)
+        results.append(p)
+    assert bool((results[0][100:] - 0.95 ** 2).abs().max() <= 1e-6)
+    assert torch.equal(results[0], results[1])
