@@ -95,3 +95,23 @@ def test_many_positions_by_themselves(N, C, G):
         sums += torch.stack([along.sum(0), along.abs().sum(0), du.sum(0), du.abs().sum(0)])
     assert float((gs.double() - sums[0]).abs().max()) <= ARITHMETIC * float(sums[1].max())
     assert float((gb.double() - sums[2]).abs().max()) <= ARITHMETIC * float(sums[3].max())
+
+
+@pytest.mark.parametrize("N,T,C,G", [(9, 1, 32, 4), (9, 1, 37, 1), (5, 1, 1024, 2), (5, 1, 2048, 1), (2, 40, 32, 4), (1, 3000, 32, 4)])
+@pytest.mark.parametrize("eps", [1e-5, 1e-30, 1e-37, 1e-39, 1e-43])
+def test_constant_groups_with_a_small_eps(N, T, C, G, eps):
+    """No variance, so everything hangs on eps alone, which may be less than the smallest normal number."""
+    import torch
+    x = torch.full((N, T, C), 2.0, device="cuda")
+    scale, shift = torch.linspace(0.5, 1.5, C, device="cuda"), torch.linspace(-1.0, 1.0, C, device="cuda")
+    d = torch.randn(N, T, C, device="cuda", generator=torch.Generator(device="cuda").manual_seed(C))
+    layer = layers.GroupNorm(N, T, C, G, activation="none", eps=eps)
+    out = layer.forward(x, scale, shift)
+    assert torch.equal(out, shift.expand_as(out))
+    rstd = 1.0 / np.sqrt(np.float64(np.float32(eps)))
+    assert float((layer.stats[..., 1].double() / rstd - 1).abs().max()) <= 1e-6
+    gx, gs, gb = layer.backward(x, scale, shift, d)
+    g = (d.double() * scale.double()).view(N, T, G, C // G)
+    want = (rstd * (g - g.mean((1, 3), keepdim=True))).view(N, T, C)
+    assert float((gx.double() - want).abs().max()) <= ARITHMETIC * float(want.abs().max())
+    assert not gs.any() and float((gb.double() - d.double().sum((0, 1))).abs().max()) <= ARITHMETIC * float(d.double().abs().sum((0, 1)).max())
