@@ -1,0 +1,46 @@
+"""Gated linear recurrence on the GPU, element by element: small results are right by their own size, not only beside the largest of the array."""
+import numpy as np
+import pytest
+
+from paper_1907_03329_amd import layers
+from tests.test_gpu_recurrence import ROUNDING, definition
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("kind", ["smooth", "decay"])
+@pytest.mark.parametrize("T", [50, 600])
+def test_every_element_has_its_own_digits(dtype, kind, T):
+    """A gate of its own for each channel, from -40 to 40 and a little beside it from position to position.
+
+    Every result is a sum of products; run over magnitudes, the same recursions give the size S of what is added up.  A coefficient is off by 2 units
+    of 2^-24, a small one by |g| / 3 <= 14 more, and a term has at most T of them, each with two roundings: an element is off by (4 T + 64) 2^-24 S at
+    most, and by its rounding; what is below the normal numbers of its type may be lost."""
+    import torch
+    rng = np.random.default_rng(T)
+    gate = np.arange(-40.0, 41.0)
+    C, dt = len(gate), getattr(torch, dtype)
+    to = lambda v: torch.from_numpy(v).to(dt)  # noqa: E731
+    x, d = to(rng.normal(size=(1, T, C))), to(rng.normal(size=(1, T, C)))
+    g = to(gate + rng.uniform(-0.5, 0.5, (1, T, C)))
+    h0, dl = (torch.from_numpy(rng.normal(size=(1, C))).float() for _ in range(2))
+    layer = layers.GatedRecurrence(1, T, C, kind=kind, dtype=dt)
+    out, last = layer.forward(x.cuda(), g.cuda(), initial=h0.cuda())
+    gx, gg, gi = layer.backward(x.cuda(), g.cuda(), d.cuda(), grad_last=dl.cuda())
+    f = lambda t: t.double().numpy()  # noqa: E731
+    n = np.array([T])
+    want = definition(kind, f(x), f(g), f(h0), n, f(d), f(dl))
+    size = list(definition(kind, np.abs(f(x)), f(g), np.abs(f(h0)), n, np.abs(f(d)), np.abs(f(dl))))
+    # (its difference x - h is one of magnitudes there, where it has to be their sum)
+    z, rest = 1.0 / (1.0 + np.exp(-f(g))), 1.0 / (1.0 + np.exp(f(g)))
+    before = np.concatenate([np.abs(f(h0))[:, None], size[0][:, :-1]], 1)
+    if kind == "smooth":
+        lam = size[2] / z
+        size[3] = lam * (np.abs(f(x)) + before) * z * rest
+    for name, got, w, s, of in zip(("out", "last", "grad_x", "grad_gate", "grad_initial"), (out, last, gx, gg, gi), want, size,
+                                   (dtype, "float32", dtype, dtype, "float32")):
+        smallest = {"float32": 2.0 ** -126, "bfloat16": 2.0 ** -126, "float16": 2.0 ** -24}[of]
+        bound = ROUNDING[of] * np.abs(w) + (4 * T + 64) * 2.0 ** -24 * s + smallest
+        off = np.abs(got.double().cpu().numpy() - w) / bound
+        assert off.max() <= 1.0, (name, kind, dtype, off.max(), np.unravel_index(off.argmax(), off.shape))
