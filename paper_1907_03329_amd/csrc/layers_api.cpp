@@ -336,9 +336,11 @@ esrnn_status esrnn_adamw_update(const esrnn_adamw *h, const esrnn_adamw_config *
     AdamWUpdate u{};
     u.entries = reinterpret_cast<const AdamWEntry *>(ws + adamw_entries_at());
     u.owner = reinterpret_cast<const int *>(ws + adamw_owner_at(*h));
-    u.lr = (float)opt->lr, u.clip_norm = (float)opt->clip_norm;
-    // at least the smallest normal number, unless zero: the hardware's reciprocal of a smaller one is infinite, and zero times that NaN where a
-    // gradient has always been zero (roots that are not zero are above 2^-75, and the sum with them is the same)
+    u.lr = (float)opt->lr;
+    // Both at least the smallest normal number, unless they are zero.  Clipping to less than that stays clipping; and of eps the hardware's reciprocal is infinite
+    // where it is smaller, and zero times that NaN where a gradient has always been zero (roots that are not zero are above 2^-75, and the sum with
+    // them is the same).
+    u.clip_norm = opt->clip_norm > 0.0 ? std::max((float)opt->clip_norm, std::numeric_limits<float>::min()) : 0.0f;
     u.eps = opt->eps > 0.0 ? std::max((float)opt->eps, std::numeric_limits<float>::min()) : 0.0f;
     u.beta1 = (float)opt->beta1, u.new1 = (float)(1.0 - opt->beta1), u.beta2 = (float)opt->beta2, u.new2 = (float)(1.0 - opt->beta2);
     u.rate = (float)(opt->lr / (1.0 - std::pow(opt->beta1, (double)step)));

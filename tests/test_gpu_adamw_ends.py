@@ -43,3 +43,14 @@ def test_eps_that_is_no_normal_number(bits, eps):
         results.append(p)
     assert bool((results[0][100:] - 0.95 ** 2).abs().max() <= 1e-6)
     assert torch.equal(results[0], results[1])
+
+
+@pytest.mark.parametrize("clip", [1e-30, 1e-37, 1e-44, 1e-46, 1e-200])
+def test_clipping_to_almost_nothing(clip):
+    """A norm of 2 clipped to less than any number of fp32: the moments of a gradient of almost nothing, and a step of almost nothing of them."""
+    import torch
+    p, g = torch.ones(400, device="cuda"), torch.full((400,), 0.1, device="cuda")
+    opt = layers.AdamW([p], [g], lr=0.1, weight_decay=0.0, clip_norm=clip, eps=1e-8)
+    opt.step(1)
+    assert abs(float(opt.grad_norm) - 2.0) <= 1e-5
+    assert float(opt.m.abs().max()) <= 1e-31 and float((p - 1.0).abs().max()) <= 1e-6
