@@ -97,10 +97,8 @@ _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cud
 
 
 def _stream(stream, device) -> int:
-    """The stream given, which has to be one of `device`, or that device's current one.  The library launches on the current device: the callers
-    below make `device` that first."""
-    if stream is None:
-        return _raw_stream(device.index)
+    """The stream that a caller gives, which has to be one of `device` (else it is the device's current one).  The library launches on the current
+    device: the callers below make `device` that first."""
     if stream.device != device:
         raise ValueError(f"the stream is one of {stream.device}, the tensors are on {device}")
     return stream.cuda_stream
@@ -146,6 +144,7 @@ class GatedRecurrence:
                  training: bool = True, device="cuda"):
         dtype = torch.float32 if dtype is None else dtype
         self.device, self.dtype, self.time_major, self.training = _cuda(device), dtype, time_major, training
+        self._index = self.device.index
         self._lib = _library()
         s = RecurrenceShape()
         s.B, s.T, s.C, s.kind, s.dtype = int(B), int(T), int(C_), _choice(KINDS, kind, "kind"), _dtype(dtype)
@@ -192,7 +191,7 @@ class GatedRecurrence:
 
     def forward(self, x, gate, lengths=None, initial=None, stream=None):
         """(out, last): all states in the element type, zero past the lengths, and the last one of every sequence in float32."""
-        if _current_device() != self.device.index:
+        if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.forward(x, gate, lengths, initial, stream)
         s = self._shape
@@ -200,14 +199,14 @@ class GatedRecurrence:
         _raise(self._lib.esrnn_recurrence_forward(
             self._ref, x_ptr, gate_ptr, self._lengths(lengths),
             self._states(initial, "initial", self._last_ptr, stream), self._out_ptr, self._last_ptr,
-            self._saved_ptr, self._workspace_ptr, _stream(stream, self.device)),
-            "esrnn_recurrence_forward")
+            self._saved_ptr, self._workspace_ptr,
+            _raw_stream(self._index) if stream is None else _stream(stream, self.device)), "esrnn_recurrence_forward")
         self._forward_done = True
         return self.out, self.last
 
     def backward(self, x, gate, grad_out, lengths=None, grad_last=None, grad_x=None, grad_gate=None, stream=None):
         """(grad_x, grad_gate, grad_initial) for the forward pass last run, which had the same x, gate and lengths."""
-        if _current_device() != self.device.index:
+        if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.backward(x, gate, grad_out, lengths, grad_last, grad_x, grad_gate, stream)
         if not self.training or not self._forward_done:
@@ -222,7 +221,8 @@ class GatedRecurrence:
         _raise(self._lib.esrnn_recurrence_backward(
             self._ref, x_ptr, gate_ptr, self._lengths(lengths), self._saved_ptr, d_ptr,
             self._states(grad_last, "grad_last", self._grad_initial_ptr, stream), gx_ptr, gg_ptr,
-            self._grad_initial_ptr, self._workspace_ptr, _stream(stream, self.device)), "esrnn_recurrence_backward")
+            self._grad_initial_ptr, self._workspace_ptr,
+            _raw_stream(self._index) if stream is None else _stream(stream, self.device)), "esrnn_recurrence_backward")
         return grad_x, grad_gate, self.grad_initial
 
 
@@ -232,7 +232,8 @@ def recurrence_step(x, gate, state, out, slots=None, kind: str = "smooth", strea
     shape, dtype, device = x.shape, x.dtype, x.device
     if len(shape) != 2 or state.dim() != 2 or device.type != "cuda":
         raise ValueError("x has to be [rows, C] and state [pool, C] on a GPU")
-    if _current_device() != device.index:
+    index = device.index
+    if _current_device() != index:
         with torch.cuda.device(device):
             return recurrence_step(x, gate, state, out, slots, kind, stream)
     rows, channels = shape
@@ -244,7 +245,7 @@ def recurrence_step(x, gate, state, out, slots=None, kind: str = "smooth", strea
         _choice(KINDS, kind, "kind"), _dtype(dtype), rows, pool, channels, x.data_ptr(), x_stride,
         _check(gate, "gate", shape, dtype, device, dense=False), gate_stride, _check_optional(slots, "slots", shape[:1], torch.int32, device),
         _check(state, "state", (pool, channels), torch.float32, device), _check(out, "out", shape, dtype, device, dense=False), out_stride,
-        _stream(stream, device))
+        _raw_stream(index) if stream is None else _stream(stream, device))
     if status != ESRNN_OK:
         raise EsrnnError(status, "esrnn_recurrence_step")
 
@@ -258,6 +259,7 @@ class GroupNorm:
                  training: bool = True, device="cuda"):
         dtype = torch.float32 if dtype is None else dtype
         self.device, self.dtype, self.training = _cuda(device), dtype, training
+        self._index = self.device.index
         self._lib = _library()
         self._shape = GroupNormShape(int(N), int(T), int(C_), int(groups), _choice(ACTIVATIONS, activation, "activation"), _dtype(dtype),
                                      float(eps))
@@ -281,18 +283,18 @@ class GroupNorm:
 
     def forward(self, x, scale, shift, lengths=None, stream=None):
         """out, zero past the lengths."""
-        if _current_device() != self.device.index:
+        if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.forward(x, scale, shift, lengths, stream)
         _raise(self._lib.esrnn_group_norm_forward(
             self._ref, *self._given(x, scale, shift, lengths), self._out_ptr, self._stats_ptr, self._workspace_ptr,
-            _stream(stream, self.device)), "esrnn_group_norm_forward")
+            _raw_stream(self._index) if stream is None else _stream(stream, self.device)), "esrnn_group_norm_forward")
         self._forward_done = True
         return self.out
 
     def backward(self, x, scale, shift, grad_out, lengths=None, stream=None):
         """(grad_x, grad_scale, grad_shift) for the forward pass last run, which had the same x, scale, shift and lengths."""
-        if _current_device() != self.device.index:
+        if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.backward(x, scale, shift, grad_out, lengths, stream)
         if not self.training or not self._forward_done:
@@ -300,7 +302,7 @@ class GroupNorm:
         _raise(self._lib.esrnn_group_norm_backward(
             self._ref, *self._given(x, scale, shift, lengths), self._stats_ptr,
             _check(grad_out, "grad_out", self._size, self.dtype, self.device), *self._grads, self._workspace_ptr,
-            _stream(stream, self.device)), "esrnn_group_norm_backward")
+            _raw_stream(self._index) if stream is None else _stream(stream, self.device)), "esrnn_group_norm_backward")
         return self.grad_x, self.grad_scale, self.grad_shift
 
 
@@ -323,6 +325,7 @@ class AdamW:
         if not params or len({len(params), len(grads), len(copies), len(decays)}) != 1:
             raise ValueError("params, grads, copies and weight decays have to be lists of the same length, at least one")
         self.device = _cuda(params[0].device)
+        self._index = self.device.index
         table = (AdamWTensor * len(params))()
         self.offsets, at = [], 0
         for i, (p, g, c, d) in enumerate(zip(params, grads, copies, decays)):
@@ -353,18 +356,19 @@ class AdamW:
         self._states = [None if t is None else t.data_ptr() for t in (self.m, self.v, self.r, self.m_scale, self.r_scale, self.grad_norm,
                                                                       self.workspace)]
         with torch.cuda.device(self.device):
-            _raise(self._lib.esrnn_adamw_bind(handle, self._states[-1], _stream(None, self.device)), "esrnn_adamw_bind")
+            _raise(self._lib.esrnn_adamw_bind(handle, self._states[-1], _raw_stream(self._index)), "esrnn_adamw_bind")
 
     def step(self, step: int, stream=None) -> None:
         """Update number `step`, from 1 on.  (The first one on another stream than the constructor's has to be ordered behind it.)"""
-        if _current_device() != self.device.index:
+        if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.step(step, stream)
         if self._handle is None:
             raise EsrnnError(1, "AdamW.step after close")
         opt = AdamWConfig(self.lr, self.beta1, self.beta2, self.eps, self.clip_norm, self.seed & 0xFFFFFFFF)
-        _raise(self._lib.esrnn_adamw_update(self._handle, C.byref(opt), int(step), *self._states, _stream(stream, self.device)),
-               "esrnn_adamw_update")
+        _raise(self._lib.esrnn_adamw_update(
+            self._handle, C.byref(opt), int(step), *self._states,
+            _raw_stream(self._index) if stream is None else _stream(stream, self.device)), "esrnn_adamw_update")
 
     def close(self) -> None:
         if self._handle is not None:
