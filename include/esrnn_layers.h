@@ -111,14 +111,19 @@ esrnn_status esrnn_group_norm_backward(const esrnn_group_norm_shape *shape, cons
  *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2
  *   p <- p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
  * With clip_norm > 0, a gradient whose norm is not finite changes nothing at all; the norm is left where `norm` says.
- * Without, such a gradient makes its own elements NaN (in 8 bits: the moments of its block of 256).
+ * Without, such a gradient makes its own elements NaN (in 8 bits: the moments of its block of 256, and that a gradient beyond 1e19 does too, whose
+ * square is infinite in fp32).  An eps of zero gives 0 / 0 where a gradient has always been zero.
  *
  * Moments live in flat arrays over all tensors; a tensor's elements begin at a multiple of ESRNN_ADAMW_BLOCK, in list order.
  *   32 bits: m, v fp32.   8 bits: m and r = sqrt(v) in OCP e4m3 (one byte), in units of one fp32 scale for each
  *   block of ESRNN_ADAMW_BLOCK elements (its largest magnitude / 448).  They are rounded up or down at random with the mean kept: to
  *   nearest, a moving average would stand still as soon as its step is less than half a code.  The 16 + 16 random bits are a hash of
  *   seed, step and the element's place, so a repeated call repeats its result.  A root that is not zero keeps at least
- *   the smallest code.  The step itself uses the moments before they are rounded.
+ *   the smallest code (a block whose largest is below 2^-91 is zero).  The step itself uses the moments before they are rounded.
+ *
+ * `step` is an argument of the call: an update captured into a graph has the step number of its capture in every replay (and all of `opt`), in
+ * both bias corrections and, with 8-bit moments, in the random bits, so that every element is rounded with the same bits each time and the mean is not kept.
+ * Updates belong outside a graph that is replayed from step to step (or, with 32 bits, into one captured so late that the corrections are 1).
  */
 #define ESRNN_ADAMW_BLOCK 256
 
@@ -139,7 +144,8 @@ typedef struct {
 
 typedef struct esrnn_adamw esrnn_adamw;
 
-/* `tensors`: HOST array of `count` tensors, copied; its pointers are not dereferenced on the host.  state_bits: 32 or 8. */
+/* `tensors`: HOST array of `count` tensors, copied; its pointers are not dereferenced on the host, and no two written arrays may overlap.  state_bits:
+ * 32 or 8.  Gradients are read at these addresses at every step; gradients at others need a new handle, bound again. */
 esrnn_status esrnn_adamw_create(const esrnn_adamw_tensor *tensors, int32_t count, int32_t state_bits, esrnn_adamw **out);
 esrnn_status esrnn_adamw_destroy(esrnn_adamw *h);
 /* Elements of each flat moment array: a multiple of ESRNN_ADAMW_BLOCK. */

@@ -11,9 +11,10 @@
 //   sample   a workgroup holds all positions of some groups of a sample in registers: x is read once, one launch.  16 x 72 x 40 fp32: 6.9 us with its
 //            launch, of which the call on the host is 5.5.
 //   position T = 1: a wave has one or several samples with all their channels; sums over a group pass through the wave's own LDS.
-//            16384 x 2048 bf16 in 16 groups: forward 30 us, 4.5 TB/s, reverse 45 us, 4.5 TB/s; the vector ALU is busy for all (forward) and 86 % of
-//            the cycles, with the sigmoid, its derivative and the conversions of 16 bits.
-//   wide     T = 1, groups of more than 512 channels: a workgroup has a group.  16384 x 2048 bf16 in one group: 28 and 59 us (a wave for each: 68, 245).
+//            16384 x 2048 bf16 in 16 groups: forward 30 us among other passes, 4.5 TB/s, reverse 46 us with the sums over samples (under the profiler 32
+//            and 44 + 5); the vector ALU is busy for all (forward) and 86 % of the cycles, with the sigmoid, its derivative and the conversions of 16 bits.
+//   wide     T = 1, groups of 513 to 4096 channels: a workgroup has a group.  16384 x 2048 bf16 in one group: 27 and 60 us, the latter for bytes that
+//            a copy moves in 40, and why has not been measured (a wave for each group: 68, 245).
 //   stream   anything else: sums per channel and chunk of positions, sums per group (and of the gradients over samples), the result; three launches,
 //            x read twice, the second time from the last-level cache where it fits.  6 ragged samples of up to 16384 positions of 256 channels, bf16:
 //            forward 11 + 5 + 18 us, reverse 22 + 6 + 27, where 25 M elements at most are 50 MB an array.  Memory and last-level cache are the bound,
@@ -1160,8 +1161,9 @@ struct Way {
     int part_rows;              // rows [2][C] of channel sums that the reverse pass leaves
 };
 
-// Channels of a group: of a wave; of a workgroup (four chunks of 1024: the widest that was built, beyond it the stream way takes single positions
-// too, with one of its sixteen rows of threads at work); samples at once (of groups up to 256).
+// Channels of a group: of a wave; of a workgroup (four chunks of 1024 is the widest that was built, not a bound that was found: beyond it the stream way takes
+// single positions too, with one of its sixteen rows of threads at work and workgroups of few bytes: 8192 x 8192 bf16 in one group 2.9 and 5.9 ms for bytes
+// that a copy moves in 53 and 79 us); samples at once (of groups up to 256).
 constexpr int kMostPositionTile = 512, kMostWideTile = 4096, kPositionRows = 4;
 
 // Rows are added up in two launches, the first in kRuns runs, from this many on: one alone reads them with 2 C / 64 workgroups (reverse pass of
@@ -1198,7 +1200,8 @@ Way way_of(const esrnn_group_norm_shape &s)
         for (w.pieces = 1; w.pieces * 256 < w.tile; w.pieces *= 2) {}
         const int rows = 4 * (w.pieces == 1 ? kPositionRows : 1) * (64 >> w.log_w);     // of a workgroup
         const int64_t most = ((int64_t)s.N + rows - 1) / rows;
-        // (16384 x 2048 bf16, forward with 1024, 2048, 3000, 4096 workgroups: 34, 32, 30, 31 us; reverse with 512, 1024, 2048: 54, 45, 47)
+        // (16384 x 2048 bf16, the one size that they were tried at: forward with 1024, 2048, 3000, 4096 workgroups 34, 32, 30, 31 us; reverse with
+        // 512, 1024, 2048 54, 45, 47)
         w.forward_groups = (int)std::min<int64_t>(most, std::max(1, 3000 / w.tiles));
         w.backward_groups = (int)std::min<int64_t>(most, std::max(1, 1024 / w.tiles));
         w.part_rows = w.backward_groups;

@@ -97,8 +97,8 @@ struct Channels {
 // sigmoid(g) and sigmoid(-g) (1 - sigmoid would lose the digits of the small one): with E = exp(-g), 1 / (1 + E) and E / (1 + E).  The hardware's
 // reciprocal gives no denormals: where 1 + E is above 2^126 (g < -87.3) it is zero, which is what the first is then taken to be; in the second 2^-126
 // stands in its place, so that the product is 1 or more, up to infinity, and the minimum makes the 1 it has to be.  (The minimum that keeps a NaN:
-// a gate that is NaN makes both of them NaN.)  The larger of the two is off by about a unit in the last place, 2^-24 of it; the smaller one by
-// some |g| / 3 more, as the exponent is one rounded product: 10 at |g| = 30.  Infinite gates give exactly 0 and 1.
+// a gate that is NaN makes both of them NaN.)  The larger of the two is off by about a unit in the last place; the smaller one by up to |g| units of 2^-24
+// more, as the exponent is one rounded product: 29 at |g| = 30.  Infinite gates give exactly 0 and 1.
 struct Sigmoids {
     float of, of_minus;
 };

@@ -15,10 +15,9 @@
 // out instead would be one array more, and rounded to its element type.
 //
 // Every array is read once and written once, 3 arrays forward and 5 in reverse, so memory is the bound: in bf16, 8 sequences of 4096 positions
-// and 2048 channels take 96 us forward and 160 us in reverse, 4.2 TB/s both (a copy reaches 5.1); 501 ragged sequences of up to 240 positions of 50 channels,
-// fp32, 17 and 26 us;
-// one sequence of 131072 positions of 256 channels, 56 and 102 us behind 5 us each that clear the words below, 3.6 and 3.3 TB/s.  The
-// vector ALU is busy for 40 % of the cycles.  Maps, states and their sums are fp32; out and the gradients are rounded once, to nearest, as they are stored.
+// and 2048 channels take 95 us forward and 162 us in reverse among other passes, 4.2 TB/s both (a copy reaches 5.1), and 102 and 165 us as single dispatches under
+// the profiler.  Under the profiler too: 501 ragged sequences of up to 240 positions of 50 channels, fp32, 17 and 26 us; one sequence of 131072 positions of
+// 256 channels 69 and 102 us behind 5 us each that clear the words below, 2.9 and 3.3 TB/s.  The vector ALU is busy for 40 % of the cycles.  Maps, states and their sums are fp32; out and the gradients are rounded once, to nearest, as they are stored.
 #include <algorithm>
 
 #include "layers_internal.h"
@@ -27,7 +26,9 @@ namespace esrnn {
 
 namespace {
 
-constexpr int kTile = 64;       // channels of a workgroup: 128 bytes of 16 bits, a whole cache line (16 channels were slower in every shape)
+// Channels of a workgroup: 128 bytes of 16 bits, a whole cache line.  Lines of fewer leave lanes idle: 64 x 16384 x 16 bf16 takes 74 and 134 us for bytes
+// that a copy moves in 20 and 33, 18 x 108288 x 33 192 and 316 for 76 and 126.
+constexpr int kTile = 64;
 // Lines (64 channels of a sequence) from which a workgroup takes a whole sequence.  Alone against ahead, bf16, forward and reverse: 8 x 4096 x 2048
 // (256 lines) 96 and 160 us against 107 and 180, 240 lines of 2048 positions 39 and 73 against 41 and 79, of 512 12 and 20 against 15 and 24; 192 of
 // 2048 37 and 60 against 35 and 55, of 512 11 and 18 against 12 and 21; 128 of 2048 35 and 51 against 27 and 40, 32 30 and 48 against 11 and 14.
@@ -127,7 +128,7 @@ struct Pieces {
 // filled with kEmpty before the launch (no result has this pattern, one of the NaNs).  Which maps a block puts together, and how, depends on
 // its number alone: those of the whole groups before its own, then those of the blocks before it in its group; the last block of a group
 // hands on the group's map, and waits for no other group for that.  So results do not depend on who was first, a block waits for two
-// others one behind the other at most, and reads 2 sqrt(blocks) maps at most.
+// others one behind the other at most, and reads some 3 sqrt(blocks) maps at most: sqrt(blocks) of groups, 2 sqrt(blocks) of blocks (up to 256 blocks, 31).
 // Every wait ends: the blocks of a line are taken by ticket, in the order in which they follow each other, whoever waits waits for lower
 // tickets of its line only, and a block's own map waits for nobody.  (A wait that goes on for seconds all the same, because calls overlap on one workspace, is given
 // up, once for all this thread reads; its maps are NaN.)
@@ -252,7 +253,7 @@ __device__ __forceinline__ void maps_of(f32x4 g, f32x4 x, f32x4 &a, f32x4 &z, f3
 //   neither       one by one
 // Scalar bases leave fewer registers to addresses, which workgroups of one or two waves need: 2048 x 100 x 64 bf16 forward 16 us with kFast, 19.5 with
 // kFour alone, 4096 x 30 x 64 9.9 and 10.7; 8 x 4096 x 2048 95 and 160 us forward and reverse with either.  kFour alone against one by one: 8 x 4096 x
-// 2047 136 and 232 us against 168 and 256, 18 x 108288 x 33 203 and 319 against 244 and 407.
+// 2047 135 and 232 us against 168 and 256, 18 x 108288 x 33 192 and 316 against 244 and 407.
 enum Access { kOneByOne, kByFours, kByFoursFast };
 
 // Four neighbouring channels of a line for each of sixteen lanes; the last lane with channels has the last four there are, so that two lanes may

@@ -314,7 +314,11 @@ class AdamW:
 
     state_bits 32: m, v float32.  8: m and r = sqrt(v) float8_e4m3fn in units of m_scale, r_scale (float32, one for 256
     elements), rounded at random with seed.  All flat, a tensor's elements from a multiple of 256 on (offsets), zero at the start.
-    The tensors are kept referenced; lr and the other hyper-parameters are plain attributes and may change between steps."""
+    The tensors are kept referenced; lr and the other hyper-parameters are plain attributes and may change between steps.  Another list of tensors is
+    another AdamW: its table takes 0.1 ms for 24 tensors, 0.7 ms for 400, and its moments begin at zero.
+
+    A step captured into a graph keeps its number: replays repeat its bias correction and, with 8-bit moments, its random bits, which then no
+    longer keep the mean.  Leave step() out of graphs that are replayed from step to step."""
 
     def __init__(self, params: Sequence, grads: Sequence, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                  weight_decay=0.01, clip_norm: float = 0.0, state_bits: int = 32, seed: int = 0, copies: Optional[Sequence] = None):

@@ -15,7 +15,7 @@ def test_every_element_has_its_own_digits(dtype, kind, T):
     """A gate of its own for each channel, from -40 to 40 and a little beside it from position to position.
 
     Every result is a sum of products; run over magnitudes, the same recursions give the size S of what is added up.  A coefficient is off by 2 units
-    of 2^-24, a small one by |g| / 3 <= 14 more, and a term has at most T of them, each with two roundings: an element is off by (4 T + 64) 2^-24 S at
+    of 2^-24, a small one by |g| <= 41 more (the product of such coefficients is itself small), and a term has at most T of them, each with two roundings: an element is off by (4 T + 64) 2^-24 S at
     most, and by its rounding; what is below the normal numbers of its type may be lost."""
     import torch
     rng = np.random.default_rng(T)
