@@ -8,8 +8,8 @@
 // fp32 moments: memory is the bound.  73 M elements with bf16 gradients and a bf16 copy, 28 bytes each, take 360 us, 5.7 TB/s; the norm reads the
 // gradients once more, 2 bytes each, in 57 us, behind the write-back of what the program before it left in the caches (25 us by itself).
 // 8-bit moments: the same elements without a copy, 14 bytes each, take 190 us among other passes (178 to 215 as single dispatches), 5.4 TB/s, and the vector ALU
-// is as near its bound, with some 80 instructions an element: roots rounded correctly, 32 random bits, two codes.  40 tensors of some 3000 elements: launches, 3.7 us for each of
-// the two kernels.
+// is as near its bound, with some 80 instructions an element: roots rounded correctly, 32 random bits, two codes.  40 tensors of some 3000 elements:
+// launches, 3.7 us for each of the two kernels.
 //
 // The moments are fp32; 8 bits are a choice of the caller's: m and r = sqrt(v), which has half of v's range, as e4m3 with a scale for 256
 // neighbours, rounded up with the probability of what is cut off, so that small changes are not lost over many steps.

@@ -17,7 +17,8 @@
 // Every array is read once and written once, 3 arrays forward and 5 in reverse, so memory is the bound: in bf16, 8 sequences of 4096 positions
 // and 2048 channels take 95 us forward and 162 us in reverse among other passes, 4.2 TB/s both (a copy reaches 5.1), and 102 and 165 us as single dispatches under
 // the profiler.  Under the profiler too: 501 ragged sequences of up to 240 positions of 50 channels, fp32, 17 and 26 us; one sequence of 131072 positions of
-// 256 channels 69 and 102 us behind 5 us each that clear the words below, 2.9 and 3.3 TB/s.  The vector ALU is busy for 40 % of the cycles.  Maps, states and their sums are fp32; out and the gradients are rounded once, to nearest, as they are stored.
+// 256 channels 69 and 102 us behind 5 us each that clear the words below, 2.9 and 3.3 TB/s.  The vector ALU is busy for 40 % of the cycles.  Maps, states and
+// their sums are fp32; out and the gradients are rounded once, to nearest, as they are stored.
 #include <algorithm>
 
 #include "layers_internal.h"
