@@ -2,7 +2,7 @@
 
 hipcc cross-compiles without a GPU.  Each source is compiled to an object in
 parallel, then linked into one shared library that exports the C ABI of
-include/esrnn.h.
+include/.
 """
 from __future__ import annotations
 
@@ -20,7 +20,9 @@ SOURCES = ["esrnn_api.cpp", "plan.cpp", "es_kernels.hip", "lstm_kernels.hip", "l
            "lstm_forward_kernels.hip", "lstm_forward_residual_kernels.hip", "lstm_narrow_kernels.hip", "lstm_narrow_fwd_residual_kernels.hip", "lstm_narrow_bwd_kernels.hip", "lstm_narrow_bwd_split_kernels.hip", "lstm_together_kernels.hip",
            "lstm_together_wide_kernels.hip", "lstm_together_forecast_kernels.hip", "lstm_together_reverse_kernels.hip", "head_kernels.hip", "opt_kernels.hip",
            "static_scratch.hip", "probe_kernels.hip",
-           "layers_api.cpp", "recurrence_kernels.hip", "adamw_kernels.hip", "group_norm_kernels.hip"]
+           "layers_api.cpp", "recurrence_kernels.hip", "adamw_kernels.hip", "group_norm_kernels.hip",
+           "state_space_api.cpp", "convolution_kernels.hip", "selective_forward_kernels.hip", "selective_backward_kernels.hip", "selective_step_kernels.hip",
+           "block_norm_kernels.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,344 @@
+// Block norm: gate, norm behind a block, residual, norm before the next block, for every row by itself (include/esrnn_state_space.h).
+//
+// A row is held in registers by L lanes of a wave, or by one or several whole waves, whose sums go through LDS; a workgroup takes rows one behind
+// the other, so that a lane's weights are read once, and so that the gradients of the weights add up in its registers.  Forward, with act = silu(gate):
+//   v = y act | y,  r1 = 1 / sqrt(mean v^2 + eps),  p = v r1 post,  e = p act | p,  s = residual + scale e,  r2 = 1 / sqrt(mean s^2 + eps),  out = s r2 pre.
+// Reverse, with that = s r2, vhat = v r1 and the gradients D of out and S of sum:
+//   ds = S + r2 (D pre - that mean(D pre that)),  de = ds scale,  dp = de act | de,  dv = r1 (dp post - vhat mean(dp post vhat)),  dy = dv act | dv,
+//   dgate = silu'(gate) (dv y | de p),  dpre = sum D that,  dscale = sum ds e,  dpost = sum dp vhat.
+// The reverse pass computes s again from the residual, in fp32, rather than read the rounded sum.
+#include <algorithm>
+
+#include "state_space_internal.h"
+
+namespace esrnn {
+
+namespace {
+
+constexpr int kMostWorkgroups = 1024;
+
+struct Args {
+    BlockNormArgs a;
+    long long y, gate, residual, sum, out, grad_out, grad_sum, grad_y, grad_gate, grad_residual;       // strides of a row
+    int rows, C, before, after;         // where the gate is
+    float eps, inverse;                 // 1 / C
+};
+
+// How a row is held: L lanes of each of NW waves, M groups of four neighbouring channels a lane; RW rows of a workgroup at a time.
+template <int L_, int NW_, int M_>
+struct Layout {
+    static constexpr int L = L_, NW = NW_, M = M_, kThreads = NW > 1 ? 64 * NW : 256, RW = kThreads / (L * NW), kChannels = 4 * M * L * NW;
+};
+
+// Sums over the lanes of a row, the same in all of them.  `slot`: two sums that follow each other have different ones.
+template <class Y>
+__device__ __forceinline__ float row_sum(float v, float (*lds)[8], int slot)
+{
+#pragma unroll
+    for (int off = Y::L / 2; off > 0; off /= 2) v += __shfl_xor(v, off, 64);
+    if constexpr (Y::NW > 1) {
+        if ((threadIdx.x & 63) == 0) lds[slot][threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < Y::NW; ++w) v += lds[slot][w];
+    }
+    return v;
+}
+
+// A lane's channels: group m begins at 4 (m T + lane), T the lanes of a row.
+template <class Y, class E>
+__device__ __forceinline__ void load_row(const void *base, long long at, int lane, int C, f32x4 (&v)[Y::M])
+{
+    const E *row = static_cast<const E *>(base) + at;
+#pragma unroll
+    for (int m = 0; m < Y::M; ++m) {
+        const Neighbours<E, 4> ch{4 * (m * Y::L * Y::NW + lane), C};
+        v[m] = to_f32<E>(ch.load(row));
+    }
+}
+template <class Y, class E>
+__device__ __forceinline__ void store_row(void *base, long long at, int lane, int C, const f32x4 (&v)[Y::M])
+{
+    E *row = static_cast<E *>(base) + at;
+#pragma unroll
+    for (int m = 0; m < Y::M; ++m) {
+        const Neighbours<E, 4> ch{4 * (m * Y::L * Y::NW + lane), C};
+        ch.store(row, from_f32<E>(v[m]));
+    }
+}
+// Weights of a lane's channels, ones where there are none: in registers, or read for every row where a lane has too many channels for that.
+template <class Y>
+struct Weights {
+    static constexpr bool kKept = Y::M <= 2;
+    const float *from;
+    int lane, C;
+    f32x4 kept[kKept ? Y::M : 1];
+    __device__ __forceinline__ f32x4 read(int m) const
+    {
+        if (!from) return f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+        return Neighbours<float, 4>{4 * (m * Y::L * Y::NW + lane), C}.load(from);
+    }
+    __device__ __forceinline__ Weights(const float *w, int lane_, int C_) : from(w), lane(lane_), C(C_)
+    {
+        if constexpr (kKept)
+#pragma unroll
+            for (int m = 0; m < Y::M; ++m) kept[m] = read(m);
+    }
+    __device__ __forceinline__ f32x4 operator[](int m) const
+    {
+        if constexpr (kKept) return kept[m];
+        return read(m);
+    }
+};
+template <class Y>
+__device__ __forceinline__ float squares(const f32x4 (&v)[Y::M])
+{
+    f32x4 s = {};
+#pragma unroll
+    for (int m = 0; m < Y::M; ++m) s += v[m] * v[m];
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+template <class Y>
+__device__ __forceinline__ float products(const f32x4 (&v)[Y::M], const f32x4 (&u)[Y::M])
+{
+    f32x4 s = {};
+#pragma unroll
+    for (int m = 0; m < Y::M; ++m) s += v[m] * u[m];
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+// 1 / sqrt(mean + eps): a square root and a division, each rounded once
+__device__ __forceinline__ float inverse_root(float sum, const Args &p) { return 1.0f / sqrtf(fmaf(sum, p.inverse, p.eps)); }
+
+template <class E, class R, class Y>
+__global__ void __launch_bounds__(Y::kThreads) block_norm_forward_kernel(Args p)
+{
+    __shared__ float s_sums[4][8];
+    const int lane = threadIdx.x % (Y::L * Y::NW), in_group = threadIdx.x / (Y::L * Y::NW);
+    const Weights<Y> post(p.a.post_weight, lane, p.C), scale(p.a.scale, lane, p.C), pre(p.a.pre_weight, lane, p.C);
+    int turn = 0;
+    for (int first = blockIdx.x * Y::RW; first < p.rows; first += gridDim.x * Y::RW, turn ^= 2) {
+        const long long row = min(first + in_group, p.rows - 1);
+        const bool mine = first + in_group < p.rows, exists = !p.a.exists || p.a.exists[row] != 0;
+        f32x4 v[Y::M], act[Y::M], s[Y::M] = {};
+        load_row<Y, E>(p.a.y, row * p.y, lane, p.C, v);
+        if (p.a.gate) load_row<Y, E>(p.a.gate, row * p.gate, lane, p.C, act);
+        if (p.a.residual) load_row<Y, R>(p.a.residual, row * p.residual, lane, p.C, s);
+        if (!exists)        // (whatever lies there)
+#pragma unroll
+            for (int m = 0; m < Y::M; ++m) v[m] = act[m] = s[m] = f32x4{};
+        if (p.a.gate) {
+#pragma unroll
+            for (int m = 0; m < Y::M; ++m)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) act[m][k] = silu(act[m][k]).of;
+        }
+        if (p.before)
+#pragma unroll
+            for (int m = 0; m < Y::M; ++m) v[m] *= act[m];
+        float r1 = 1.0f, r2 = 1.0f;
+        if (p.a.post_weight) {
+            r1 = inverse_root(row_sum<Y>(squares<Y>(v), s_sums, turn), p);
+#pragma unroll
+            for (int m = 0; m < Y::M; ++m) v[m] = v[m] * r1 * post[m];
+        }
+        if (p.after)
+#pragma unroll
+            for (int m = 0; m < Y::M; ++m) v[m] *= act[m];
+#pragma unroll
+        for (int m = 0; m < Y::M; ++m) s[m] += scale[m] * v[m];
+        if (p.a.residual && mine) store_row<Y, R>(p.a.sum, row * p.sum, lane, p.C, s);
+        if (p.a.pre_weight) {
+            r2 = inverse_root(row_sum<Y>(squares<Y>(s), s_sums, turn + 1), p);
+#pragma unroll
+            for (int m = 0; m < Y::M; ++m) s[m] = s[m] * r2 * pre[m];
+        }
+        if (p.a.out && mine) store_row<Y, E>(p.a.out, row * p.out, lane, p.C, s);
+        if (p.a.stats && mine && lane == 0) {
+            p.a.stats[2 * row] = r1;
+            p.a.stats[2 * row + 1] = r2;
+        }
+    }
+}
+
+template <class E, class R, class Y>
+__global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p)
+{
+    constexpr int M = Y::M;
+    __shared__ float s_sums[4][8];
+    __shared__ __attribute__((aligned(16))) float s_parts[Y::RW > 1 ? Y::RW : 1][Y::RW > 1 ? Y::kChannels : 1];
+    const int lane = threadIdx.x % (Y::L * Y::NW), in_group = threadIdx.x / (Y::L * Y::NW);
+    const Weights<Y> post(p.a.post_weight, lane, p.C), scale(p.a.scale, lane, p.C), pre(p.a.pre_weight, lane, p.C);
+    f32x4 dpost[M] = {}, dscale[M] = {}, dpre[M] = {};
+    int turn = 0;
+    for (int first = blockIdx.x * Y::RW; first < p.rows; first += gridDim.x * Y::RW, turn ^= 2) {
+        const long long row = min(first + in_group, p.rows - 1);
+        const bool mine = first + in_group < p.rows, exists = mine && (!p.a.exists || p.a.exists[row] != 0);
+        f32x4 y[M], gate[M] = {}, s[M] = {}, d[M] = {}, ds[M] = {};
+        load_row<Y, E>(p.a.y, row * p.y, lane, p.C, y);
+        if (p.a.gate) load_row<Y, E>(p.a.gate, row * p.gate, lane, p.C, gate);
+        if (p.a.residual) load_row<Y, R>(p.a.residual, row * p.residual, lane, p.C, s);
+        if (p.a.grad_out) load_row<Y, E>(p.a.grad_out, row * p.grad_out, lane, p.C, d);
+        if (p.a.grad_sum) load_row<Y, R>(p.a.grad_sum, row * p.grad_sum, lane, p.C, ds);
+        const float r1 = exists ? p.a.stats_in[2 * row] : 0.0f, r2 = exists ? p.a.stats_in[2 * row + 1] : 0.0f;
+        if (!exists)
+#pragma unroll
+            for (int m = 0; m < M; ++m) y[m] = gate[m] = s[m] = d[m] = ds[m] = f32x4{};
+        f32x4 act[M], slope[M], vhat[M], e[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const Silu g = silu(gate[m][k]);
+                act[m][k] = g.of, slope[m][k] = g.slope;
+            }
+            vhat[m] = (p.before ? y[m] * act[m] : y[m]) * r1;
+            e[m] = vhat[m] * post[m];       // p, for now
+            s[m] += scale[m] * (p.after ? e[m] * act[m] : e[m]);
+        }
+        if (p.a.pre_weight) {
+            f32x4 weighted[M];
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                s[m] *= r2;                 // that
+                dpre[m] += d[m] * s[m];
+                weighted[m] = d[m] * pre[m];
+            }
+            const float mean = row_sum<Y>(products<Y>(weighted, s), s_sums, turn) * p.inverse;
+#pragma unroll
+            for (int m = 0; m < M; ++m) ds[m] += r2 * (weighted[m] - s[m] * mean);
+        } else if (!p.a.residual) {
+#pragma unroll
+            for (int m = 0; m < M; ++m) ds[m] = d[m];
+        }
+        if (p.a.grad_residual && mine) store_row<Y, R>(p.a.grad_residual, row * p.grad_residual, lane, p.C, ds);
+        f32x4 dgate[M], weighted[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const f32x4 of_e = p.after ? e[m] * act[m] : e[m];
+            dscale[m] += ds[m] * of_e;
+            const f32x4 de = ds[m] * scale[m];
+            dgate[m] = de * e[m];
+            const f32x4 dp = p.after ? de * act[m] : de;
+            dpost[m] += dp * vhat[m];
+            weighted[m] = dp * post[m];
+        }
+        if (p.a.post_weight) {
+            const float mean = row_sum<Y>(products<Y>(weighted, vhat), s_sums, turn + 1) * p.inverse;
+#pragma unroll
+            for (int m = 0; m < M; ++m) weighted[m] = r1 * (weighted[m] - vhat[m] * mean);
+        }
+        if (p.before)
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                dgate[m] = weighted[m] * y[m];
+                weighted[m] *= act[m];
+            }
+        if (mine) {
+            store_row<Y, E>(p.a.grad_y, row * p.grad_y, lane, p.C, weighted);
+            if (p.a.grad_gate) {
+#pragma unroll
+                for (int m = 0; m < M; ++m) dgate[m] *= slope[m];
+                store_row<Y, E>(p.a.grad_gate, row * p.grad_gate, lane, p.C, dgate);
+            }
+        }
+    }
+    // the workgroup's sums, rows of [3][C]
+#pragma unroll
+    for (int which = 0; which < 3; ++which) {
+        const f32x4 *sum = which == 0 ? dpost : which == 1 ? dscale : dpre;
+        float *to = p.a.parts + ((size_t)blockIdx.x * 3 + which) * p.C;
+        if constexpr (Y::RW > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int m = 0; m < M; ++m) *reinterpret_cast<f32x4 *>(&s_parts[in_group][4 * (m * Y::L + lane)]) = sum[m];
+            __syncthreads();
+            for (int c = threadIdx.x; c < p.C; c += Y::kThreads) {
+                float v = 0.0f;
+                for (int r = 0; r < Y::RW; ++r) v += s_parts[r][c];
+                to[c] = v;
+            }
+        } else {
+            store_row<Y, float>(to, 0, lane, p.C, *reinterpret_cast<const f32x4(*)[M]>(sum));
+        }
+    }
+}
+
+__global__ void __launch_bounds__(1024) block_norm_sum_kernel(const float *__restrict__ parts, int rows, int C, float *grad_post, float *grad_scale, float *grad_pre)
+{
+    sum_columns(parts, rows, 3ll * C, (long long)blockIdx.x * 64, [&](long long col, float v) {
+        float *to = col < C ? grad_post : col < 2ll * C ? grad_scale : grad_pre;
+        if (to) to[col % C] = v;
+    });
+}
+
+Args arguments(const esrnn_block_norm_shape &s, const BlockNormArgs &a)
+{
+    Args p{};
+    p.a = a;
+    p.y = s.y_stride, p.gate = s.gate_stride, p.residual = s.residual_stride, p.sum = s.sum_stride, p.out = s.out_stride;
+    p.grad_out = s.grad_out_stride, p.grad_sum = s.grad_sum_stride, p.grad_y = s.grad_y_stride, p.grad_gate = s.grad_gate_stride;
+    p.grad_residual = s.grad_residual_stride;
+    p.rows = s.rows, p.C = s.C, p.before = s.gate == ESRNN_GATE_BEFORE, p.after = s.gate == ESRNN_GATE_AFTER;
+    p.eps = s.eps, p.inverse = 1.0f / s.C;
+    return p;
+}
+
+template <class F>
+hipError_t with_layout(int C, F &&f)
+{
+    if (C <= 64) return f(Layout<16, 1, 1>{});
+    if (C <= 256) return f(Layout<64, 1, 1>{});
+    if (C <= 512) return f(Layout<64, 1, 2>{});
+    if (C <= 1024) return f(Layout<64, 2, 2>{});
+    if (C <= 2048) return f(Layout<64, 4, 2>{});
+    if (C <= 4096) return f(Layout<64, 8, 2>{});
+    return f(Layout<64, 8, 4>{});
+}
+template <class F>
+hipError_t with_types(const esrnn_block_norm_shape &s, F &&f)
+{
+    return with_element(s.dtype, [&](auto e) {
+        if (s.stream_dtype == s.dtype) return f(e, e);
+        return f(e, float{});
+    });
+}
+int workgroups(int rows, int at_a_time) { return (int)std::min<long long>(((long long)rows + at_a_time - 1) / at_a_time, kMostWorkgroups); }
+
+}  // namespace
+
+size_t block_norm_workspace_floats(const esrnn_block_norm_shape &s)
+{
+    return (size_t)std::min(s.rows, kMostWorkgroups) * 3 * s.C;
+}
+
+hipError_t launch_block_norm_forward(const esrnn_block_norm_shape &s, const BlockNormArgs &a, hipStream_t st)
+{
+    const Args p = arguments(s, a);
+    return with_types(s, [&](auto e, auto r) {
+        return with_layout(s.C, [&](auto y) {
+            typedef decltype(y) Y;
+            block_norm_forward_kernel<decltype(e), decltype(r), Y><<<dim3(workgroups(s.rows, Y::RW)), Y::kThreads, 0, st>>>(p);
+            return hipGetLastError();
+        });
+    });
+}
+
+hipError_t launch_block_norm_backward(const esrnn_block_norm_shape &s, const BlockNormArgs &a, hipStream_t st)
+{
+    const Args p = arguments(s, a);
+    int rows = 0;
+    const hipError_t failed = with_types(s, [&](auto e, auto r) {
+        return with_layout(s.C, [&](auto y) {
+            typedef decltype(y) Y;
+            rows = workgroups(s.rows, Y::RW);
+            block_norm_backward_kernel<decltype(e), decltype(r), Y><<<dim3(rows), Y::kThreads, 0, st>>>(p);
+            return hipGetLastError();
+        });
+    });
+    if (failed != hipSuccess || !(a.grad_post_weight || a.grad_scale || a.grad_pre_weight)) return failed;
+    block_norm_sum_kernel<<<dim3((3 * s.C + 63) / 64), 1024, 0, st>>>(a.parts, rows, s.C, a.grad_post_weight, a.grad_scale, a.grad_pre_weight);
+    return hipGetLastError();
+}
+
+}  // namespace esrnn

@@ -1,0 +1,315 @@
+// Selective scan over whole sequences, reverse pass (include/esrnn_state_space.h; selective_scan.h has the way it is cut up).
+//
+// With lambda_t the gradient of h_t and mu_t = a_t lambda_t that of what a_t multiplies, from the end:
+//   lambda_t = g_t c_t + mu_{t+1}        (g: gradient of out; behind the last position: that of the last state)
+//   grad c_t = sum over channels of g_t h_t,   grad b_t = sum over channels of lambda_t d_t x_t
+//   grad x_t = d_t sum_n lambda_t b_t + D g_t,  grad d_t = sum_n mu_t h_{t-1} A + x_t sum_n lambda_t b_t,  grad delta_t = grad d_t softplus'
+//   grad A = sum_t mu_t h_{t-1} d_t,  grad D = sum_t g_t x_t,  grad bias = sum_t grad delta_t,  grad initial = mu at the first position.
+// The states h are computed again, piece by piece, from the one before each piece that the forward pass has left; for a piece they stay in
+// registers, half of a lane's states at a time.  Sums over channels go through the lanes of a wave, where every addition also halves how many
+// values a lane has left, and then over tiles, in a second launch; those over positions through lanes and segments, in the same.
+#include <algorithm>
+
+#include "selective_scan.h"
+
+namespace esrnn {
+
+namespace {
+
+typedef unsigned u32pair __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ unsigned bits_of(float v) { return __builtin_bit_cast(unsigned, v); }
+__device__ __forceinline__ float float_of(unsigned v) { return __builtin_bit_cast(float, v); }
+
+// Sums over the halves of the wave of two values: the lower half gets that of a, the upper half that of b.
+__device__ __forceinline__ float fold_halves(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(bits_of(a), bits_of(b), false, false);
+    return float_of(r[0]) + float_of(r[1]);
+}
+// The same over neighbouring rows of 16 lanes: even rows a, odd rows b.
+__device__ __forceinline__ float fold_rows(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(bits_of(a), bits_of(b), false, false);
+    return float_of(r[0]) + float_of(r[1]);
+}
+// Within a row, over lanes kCtrl apart: `odd` lanes get the sum of b, others that of a.
+template <int kCtrl>
+__device__ __forceinline__ float fold(float a, float b, bool odd)
+{
+    const float keep = odd ? b : a, send = odd ? a : b;
+    return keep + float_of(__builtin_amdgcn_update_dpp(0, bits_of(send), kCtrl, 0xf, 0xf, true));
+}
+constexpr int kRowRotate8 = 0x128, kRowHalfMirror = 0x141, kQuadOther2 = 0x4e, kQuadOther1 = 0xb1;      // lanes i and i ^ 8, 7 - i, i ^ 2, i ^ 1
+
+// mu behind the last position of a segment, of the sequence's last segment with positions: the gradient of the last state.
+template <int NP, int SL>
+__device__ __forceinline__ void arriving(const Scan &k, const ScanPlace &at, size_t own, const float (&A)[NP], float (&mu)[NP])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) mu[n] = 0.0f;
+    if (k.a.grad_last) load_own<NP>(k.a.grad_last + own, at.slice, k.N, at.lane_mask, mu);
+    for (int s = max(at.length - 1, 0) / (k.span * kPiece); s > at.segment; --s) {
+        const float *map = map_of<NP, SL>(k, at, s);
+        float local[NP];
+        load_states<NP>(map, local);
+        const float sum = map[64 * NP + lane];
+#pragma unroll
+        for (int n = 0; n < NP; ++n) mu[n] = fmaf(__builtin_amdgcn_exp2f(sum * A[n]), mu[n], local[n]);
+    }
+}
+
+// The maps of all segments but the first, against time.
+template <class E, class BC, int NP, int SL>
+__global__ void __launch_bounds__(64 * SL) selective_back_maps_kernel(Scan k)
+{
+    ScanPlace at(k, k.segments - 1);
+    ++at.segment;
+    const int lane = threadIdx.x & 63;
+    const int begin = at.segment * k.span * kPiece, end = min(min(begin + k.span * kPiece, k.T), at.length);
+    if (begin >= end) return;
+    const E *delta = static_cast<const E *>(k.a.delta) + at.b * k.db, *grad = static_cast<const E *>(k.a.grad_out) + at.b * k.gb;
+    const BC *c = static_cast<const BC *>(k.c) + at.b * k.cb + at.group * k.group + NP * at.slice;
+    float A[NP], mu[NP];
+    load_own<NP>(k.a.A + (size_t)at.channel * k.N, at.slice, k.N, at.lane_mask, A);
+#pragma unroll
+    for (int n = 0; n < NP; ++n) A[n] *= kLog2e, mu[n] = 0.0f;
+    const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f;
+    float sum = 0.0f;
+    Column<E> ds, gs, next_ds, next_gs;
+    const int top = begin + (end - 1 - begin) / kPiece * kPiece;
+    ds.request(delta, k.dt, top, at.length, at.channel);
+    gs.request(grad, k.gt, top, at.length, at.channel);
+    for (int t0 = top; t0 >= begin; t0 -= kPiece) {
+        next_ds.request(delta, k.dt, max(t0 - kPiece, 0), at.length, at.channel);
+        next_gs.request(grad, k.gt, max(t0 - kPiece, 0), at.length, at.channel);
+        const int t = fresh(t0), left = at.length - 1 - t;
+        const BC *c0 = c + t * k.ct;
+#pragma unroll
+        for (int i = kPiece - 1; i >= 0; --i) {
+            const unsigned mask = i <= left ? at.lane_mask : 0u;
+            const float d = masked(step_size(ds.v[i], bias, k.softplus).of, mask), g = masked((float)gs.v[i], mask);
+            float cs[NP];
+            load_shared<BC, NP>(c0, k.ct, i, left, cs);
+            sum += d;
+#pragma unroll
+            for (int n = 0; n < NP; ++n) mu[n] = __builtin_amdgcn_exp2f(d * A[n]) * fmaf(cs[n], g, mu[n]);
+        }
+        ds = next_ds, gs = next_gs;
+    }
+    float *map = map_of<NP, SL>(k, at, at.segment);
+    store_states<NP>(map, mu);
+    map[64 * NP + lane] = sum;
+}
+
+template <class E, class BC, int NP, int SL>
+__global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_kernel(Scan k)
+{
+    constexpr int kPart = 4, kPadded = NP * SL;     // (states at a time: theirs at nine positions and their decays at eight take 68 registers)
+    __shared__ float s_sums[SL > 1 ? 2 : 1][SL > 1 ? SL : 1][2 * kPiece][64];
+    const ScanPlace at(k, k.segments);
+    const int lane = threadIdx.x & 63;
+    const int begin = at.segment * k.span * kPiece, end = min(begin + k.span * kPiece, k.T);
+    const E *x = static_cast<const E *>(k.a.x) + at.b * k.xb, *delta = static_cast<const E *>(k.a.delta) + at.b * k.db;
+    const E *grad = static_cast<const E *>(k.a.grad_out) + at.b * k.gb;
+    E *grad_x = static_cast<E *>(k.a.grad_x) + at.b * k.gxb, *grad_delta = static_cast<E *>(k.a.grad_delta) + at.b * k.gdb;
+    const BC *b = static_cast<const BC *>(k.b) + at.b * k.bb + at.group * k.group + NP * at.slice;
+    const BC *c = static_cast<const BC *>(k.c) + at.b * k.cb + at.group * k.group + NP * at.slice;
+    const size_t own = ((size_t)at.b * k.C + at.channel) * k.N;
+
+    float A[NP], mu[NP], dA[NP], dD = 0.0f, dbias = 0.0f;
+    load_own<NP>(k.a.A + (size_t)at.channel * k.N, at.slice, k.N, at.lane_mask, A);
+#pragma unroll
+    for (int n = 0; n < NP; ++n) A[n] *= kLog2e, dA[n] = 0.0f;
+    const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
+    if (begin < at.length || begin == 0) arriving<NP, SL>(k, at, own, A, mu);
+
+    // which of the values a lane has after all additions: one of four neighbouring positions, b or c, one of four states (every other quad the same)
+    const int row = lane / 16, part_step = lane & 3, part_state = (row & 1) * 2 + (lane >> 3 & 1);
+    const bool bit3 = lane & 8, bit1 = lane & 2, bit0 = lane & 1, part_lane = !(lane & 4);
+    // rows of [2][padded] for every position and group
+    const float *parts = k.part_rows + (((size_t)(at.tile % k.tiles) * k.B + at.b) * k.pieces * kPiece * k.G + at.group) * (2 * kPadded) + NP * at.slice;
+    const unsigned part_position = (unsigned)k.G * (2 * kPadded);
+    const unsigned part_at = part_lane ? 4 * (part_step * part_position + (row >> 1) * kPadded + part_state) : kOutside;
+
+    int turn = 0;
+    const int last = min(end, at.length);
+    if (begin < last) {
+        const int top = begin + (last - 1 - begin) / kPiece * kPiece;
+        for (int t0 = top; t0 >= begin; t0 -= kPiece, turn ^= 1) {
+            Column<E> xs, ds, gs;
+            xs.request(x, k.xt, t0, at.length, at.channel);
+            ds.request(delta, k.dt, t0, at.length, at.channel);
+            gs.request(grad, k.gt, t0, at.length, at.channel);
+            const int t = fresh(t0), left = at.length - 1 - t;
+            const float *saved = saved_of<NP, SL>(k, at, t / kPiece);
+            const BC *b0 = b + t * k.bt, *c0 = c + t * k.ct;
+            const buf_rsrc to_parts = make_base(parts + (size_t)t * part_position);
+            float d[kPiece], slope[kPiece], xi[kPiece], g[kPiece], through[kPiece], rate[kPiece];   // through: sum lambda b; rate: sum mu h_{t-1} A log2(e)
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) {
+                const unsigned mask = i <= left ? at.lane_mask : 0u;
+                const Softplus s = step_size(ds.v[i], bias, k.softplus);
+                d[i] = masked(s.of, mask), slope[i] = masked(s.slope, mask), xi[i] = masked((float)xs.v[i], mask), g[i] = masked((float)gs.v[i], mask);
+                through[i] = rate[i] = 0.0f;
+            }
+#pragma unroll
+            for (int n0 = 0; n0 < NP; n0 += kPart) {
+                // (or the parts' registers add up, and the loads of all of them become one)
+                __builtin_amdgcn_sched_barrier(0);
+                const int part = fresh(n0);
+                const BC *b_part = b0 + part, *c_part = c0 + part;
+                float h[kPiece + 1][kPart], decay[kPiece][kPart];
+                const f32x4 before = *reinterpret_cast<const f32x4 *>(saved + 64 * n0 + 4 * lane);
+#pragma unroll
+                for (int n = 0; n < kPart; ++n) h[0][n] = before[n];
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) {
+                    float bs[kPart];
+                    load_shared<BC, kPart>(b_part, k.bt, i, left, bs);
+                    const float u = d[i] * xi[i];
+#pragma unroll
+                    for (int n = 0; n < kPart; ++n) {
+                        decay[i][n] = __builtin_amdgcn_exp2f(d[i] * A[n0 + n]);
+                        h[i + 1][n] = fmaf(decay[i][n], h[i][n], u * bs[n]);
+                    }
+                }
+                float quad[4];
+#pragma unroll
+                for (int i = kPiece - 1; i >= 0; --i) {
+                    float bs[kPart], cs[kPart], of_b[kPart], of_c[kPart];
+                    load_shared<BC, kPart>(b_part, k.bt, i, left, bs);
+                    load_shared<BC, kPart>(c_part, k.ct, i, left, cs);
+                    const float u = d[i] * xi[i];
+#pragma unroll
+                    for (int n = 0; n < kPart; ++n) {
+                        const float lambda = fmaf(cs[n], g[i], mu[n0 + n]);
+                        of_c[n] = g[i] * h[i + 1][n];
+                        of_b[n] = u * lambda;
+                        through[i] = fmaf(bs[n], lambda, through[i]);
+                        mu[n0 + n] = decay[i][n] * lambda;
+                        const float m = mu[n0 + n] * h[i][n];
+                        rate[i] = fmaf(m, A[n0 + n], rate[i]);
+                        dA[n0 + n] = fmaf(m, d[i], dA[n0 + n]);
+                    }
+                    // eight values over 64 lanes: lower half of the wave b, upper half c; then the states; then both quads of eight lanes alike
+                    float w[kPart];
+#pragma unroll
+                    for (int n = 0; n < kPart; ++n) w[n] = fold_halves(of_b[n], of_c[n]);
+                    const float p = fold<kRowRotate8>(fold_rows(w[0], w[2]), fold_rows(w[1], w[3]), bit3);
+                    quad[i & 3] = p + float_of(__builtin_amdgcn_update_dpp(0, bits_of(p), kRowHalfMirror, 0xf, 0xf, true));
+                    if ((i & 3) == 0) {     // four positions: one value a lane
+                        const float even = fold<kQuadOther2>(quad[0], quad[2], bit1), odd = fold<kQuadOther2>(quad[1], quad[3], bit1);
+                        buf_store(to_parts, part_at, 4 * (i * part_position + n0), fold<kQuadOther1>(even, odd, bit0));
+                    }
+                }
+            }
+            complete(through);
+            complete(rate);
+            if constexpr (SL > 1) {
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) s_sums[turn][at.slice][i][lane] = through[i], s_sums[turn][at.slice][kPiece + i][lane] = rate[i];
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i)
+                    if (i % SL == at.slice) {
+                        through[i] = rate[i] = 0.0f;
+#pragma unroll
+                        for (int s = 0; s < SL; ++s) through[i] += s_sums[turn][s][i][lane], rate[i] += s_sums[turn][s][kPiece + i][lane];
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) {
+                if (i % SL != at.slice || t + i >= end) continue;
+                const float to_x = fmaf(d[i], through[i], D * g[i]), to_delta = fmaf(rate[i], kLn2, xi[i] * through[i]) * slope[i];
+                dbias += to_delta;
+                dD = fmaf(g[i], xi[i], dD);
+                if (at.lane_mask) {
+                    (grad_x + (t + i) * k.gxt)[at.channel] = (E)to_x;
+                    (grad_delta + (t + i) * k.gdt)[at.channel] = (E)to_delta;
+                }
+            }
+        }
+    }
+    if (at.segment == 0 && k.a.grad_initial) store_own<NP>(k.a.grad_initial + own, at.slice, k.N, at.lane_mask, mu);
+    for (int t = max(begin, (at.length + kPiece - 1) / kPiece * kPiece); t < end; ++t)
+        if (t % SL == at.slice && at.lane_mask) {
+            (grad_x + t * k.gxt)[at.channel] = (E)0.0f;
+            (grad_delta + t * k.gdt)[at.channel] = (E)0.0f;
+        }
+    float *sums = k.part_sums + ((((size_t)at.b * k.segments + at.segment) * (k.G * k.tiles) + at.tile) * SL + at.slice) * ((NP + 2) * 64);
+#pragma unroll
+    for (int n = 0; n < NP; ++n) sums[64 * n + lane] = dA[n];
+    sums[64 * NP + lane] = dD;
+    sums[64 * (NP + 1) + lane] = dbias;
+}
+
+// The sums over segments of the gradients of A, D and bias (the first workgroups; rows of [tile][slice][states + 2][64]) and those over tiles of the
+// gradients of b and c (the others; [tile][position][group][2][padded]).
+template <class E>
+__global__ void __launch_bounds__(1024) selective_sum_kernel(Scan k, int states, int slices, long long first_rows, E *grad_b, E *grad_c, long long gbb,
+                                                             long long gbt, long long gcb, long long gct)
+{
+    if (blockIdx.x < first_rows) {
+        const int wave = (states + 2) * 64;
+        sum_columns(k.part_sums, (long long)k.B * k.segments, (long long)k.G * k.tiles * slices * wave, (long long)blockIdx.x * 64, [&](long long col, float v) {
+            const int lane = col % 64, n = (int)(col / 64) % (states + 2), slice = (int)(col / wave) % slices, tile = (int)(col / wave / slices);
+            const int in_group = tile % k.tiles * 64 + lane, channel = tile / k.tiles * k.group_channels + in_group;
+            if (in_group >= k.group_channels) return;
+            if (n < states) {
+                if (slice * states + n < k.N) k.a.grad_A[(size_t)channel * k.N + slice * states + n] = v;
+            } else if (float *to = n == states ? k.a.grad_D : k.a.grad_bias) {
+                // every slice has its share of the positions
+                if (slice == 0) {
+                    for (int s = 1; s < slices; ++s)
+                        for (long long r = 0; r < (long long)k.B * k.segments; ++r) v += k.part_sums[(r * k.G * k.tiles * slices + tile * slices + s) * wave + n * 64 + lane];
+                    to[channel] = v;
+                }
+            }
+        });
+        return;
+    }
+    const int padded = states * slices, width = k.G * 2 * padded;
+    // (whole pieces of every sequence)
+    const long long i = (blockIdx.x - first_rows) * 1024 + threadIdx.x, length_of = (long long)k.pieces * kPiece, positions = k.B * length_of;
+    if (i >= positions * width) return;
+    const long long position = i / width;
+    const int within = (int)(i % width), n = within % padded, group = within / (2 * padded), b = (int)(position / length_of), t = (int)(position % length_of);
+    const bool is_c = within / padded & 1;
+    if (n >= k.N || t >= k.T) return;
+    const int length = k.a.lengths ? min(max(k.a.lengths[b], 0), k.T) : k.T;
+    float v = 0.0f;
+    if (t < length)
+        for (int q = 0; q < k.tiles; ++q) v += k.part_rows[q * positions * width + i];
+    E *to = is_c ? grad_c + b * gcb + t * gct : grad_b + b * gbb + t * gbt;
+    to[(long long)group * k.N + n] = (E)v;
+}
+
+}  // namespace
+
+hipError_t launch_selective_backward(const esrnn_selective_shape &s, const SelectiveArgs &a, hipStream_t st)
+{
+    SelectivePlan p = selective_plan(s, true);
+    const Scan k = scan_arguments(s, a, p);
+    if (const hipError_t e = launch_selective_widen(s, a, p, k, st); e != hipSuccess) return e;
+    const unsigned lines = (unsigned)(s.B * s.G * p.tiles);
+    const hipError_t failed = with_scan(s, p, [&](auto e, auto bc, auto states, auto slices) {
+        typedef decltype(e) E;
+        typedef decltype(bc) BC;
+        constexpr int NP = decltype(states)::value, SL = decltype(slices)::value;
+        if (p.segments > 1) selective_back_maps_kernel<E, BC, NP, SL><<<dim3(lines * (p.segments - 1)), 64 * SL, 0, st>>>(k);
+        selective_backward_kernel<E, BC, NP, SL><<<dim3(lines * p.segments), 64 * SL, 0, st>>>(k);
+        return hipGetLastError();
+    });
+    if (failed != hipSuccess) return failed;
+    const long long columns = (long long)s.G * p.tiles * p.slices * (p.states + 2), rows = ((long long)s.B * p.pieces * kPiece * s.G * 2 * p.padded + 1023) / 1024;
+    return with_element(s.dtype, [&](auto e) {
+        typedef decltype(e) E;
+        selective_sum_kernel<E><<<dim3((unsigned)(columns + rows)), 1024, 0, st>>>(k, p.states, p.slices, columns, static_cast<E *>(a.grad_b), static_cast<E *>(a.grad_c),
+                                                                              s.grad_b_stride[0], s.grad_b_stride[1], s.grad_c_stride[0], s.grad_c_stride[1]);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace esrnn

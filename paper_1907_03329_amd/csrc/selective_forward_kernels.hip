@@ -1,0 +1,222 @@
+// Selective scan over whole sequences, forward (include/esrnn_state_space.h; selective_scan.h has the way it is cut up).
+#include <algorithm>
+
+#include "selective_scan.h"
+
+namespace esrnn {
+
+namespace {
+
+constexpr int kThreadsOfRows = 256;
+
+// kMaps: the map of a segment, which needs neither c nor the output.
+template <class E, class BC, int NP, int SL, bool kMaps>
+__global__ void __launch_bounds__(64 * SL) selective_forward_kernel(Scan k)
+{
+    __shared__ float s_y[SL > 1 && !kMaps ? 2 : 1][SL > 1 && !kMaps ? SL : 1][kPiece][64];
+    const int segments = kMaps ? k.segments - 1 : k.segments;       // (nothing follows the last one)
+    const ScanPlace at(k, segments);
+    const int lane = threadIdx.x & 63;
+    const int begin = at.segment * k.span * kPiece, end = min(begin + k.span * kPiece, k.T);
+    const E *x = static_cast<const E *>(k.a.x) + at.b * k.xb, *delta = static_cast<const E *>(k.a.delta) + at.b * k.db;
+    E *out = static_cast<E *>(k.a.out) + at.b * k.ob;
+    const BC *b = static_cast<const BC *>(k.b) + at.b * k.bb + at.group * k.group + NP * at.slice;
+    const BC *c = static_cast<const BC *>(k.c) + at.b * k.cb + at.group * k.group + NP * at.slice;
+    const size_t own = ((size_t)at.b * k.C + at.channel) * k.N;
+
+    float A[NP], h[NP];
+    load_own<NP>(k.a.A + (size_t)at.channel * k.N, at.slice, k.N, at.lane_mask, A);
+#pragma unroll
+    for (int n = 0; n < NP; ++n) A[n] *= kLog2e, h[n] = 0.0f;
+    const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
+    if (!kMaps && k.a.initial && (begin < at.length || begin == 0)) load_own<NP>(k.a.initial + own, at.slice, k.N, at.lane_mask, h);
+    if (!kMaps && begin < at.length) {
+        for (int s = 0; s < at.segment; ++s) {
+            const float *map = map_of<NP, SL>(k, at, s);
+            float local[NP];
+            load_states<NP>(map, local);
+            const float sum = map[64 * NP + lane];
+#pragma unroll
+            for (int n = 0; n < NP; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(sum * A[n]), h[n], local[n]);
+        }
+    }
+    float sum = 0.0f;
+    Column<E> xs, ds, next_xs, next_ds;
+    if (begin < at.length) {
+        xs.request(x, k.xt, begin, at.length, at.channel);
+        ds.request(delta, k.dt, begin, at.length, at.channel);
+    }
+    int turn = 0;
+    for (int t0 = begin; t0 < min(end, at.length); t0 += kPiece, turn ^= 1) {
+        next_xs.request(x, k.xt, t0 + kPiece, at.length, at.channel);
+        next_ds.request(delta, k.dt, t0 + kPiece, at.length, at.channel);
+        if (!kMaps && k.a.saved) store_states<NP>(saved_of<NP, SL>(k, at, t0 / kPiece), h);
+        float y[kPiece];
+        const int t = fresh(t0), left = at.length - 1 - t;
+        const BC *b0 = b + t * k.bt, *c0 = c + t * k.ct;
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+            const unsigned mask = i <= left ? at.lane_mask : 0u;
+            const float d = masked(step_size(ds.v[i], bias, k.softplus).of, mask), xi = masked((float)xs.v[i], mask), u = d * xi;
+            float bs[NP], cs[NP];
+            load_shared<BC, NP>(b0, k.bt, i, left, bs);
+            if (kMaps) {
+                sum += d;
+            } else {
+                load_shared<BC, NP>(c0, k.ct, i, left, cs);
+            }
+            float part[4] = {at.slice == 0 ? D * xi : 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int n = 0; n < NP; ++n) {
+                h[n] = fmaf(__builtin_amdgcn_exp2f(d * A[n]), h[n], u * bs[n]);
+                if (!kMaps) part[n & 3] = fmaf(cs[n], h[n], part[n & 3]);
+            }
+            y[i] = (part[0] + part[1]) + (part[2] + part[3]);
+        }
+        if constexpr (!kMaps) {
+            complete(y);
+            if constexpr (SL > 1) {
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) s_y[turn][at.slice][i][lane] = y[i];
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i)
+                    if (i % SL == at.slice) {
+                        y[i] = 0.0f;
+#pragma unroll
+                        for (int s = 0; s < SL; ++s) y[i] += s_y[turn][s][i][lane];
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i)
+                if (t + i < end && i % SL == at.slice && at.lane_mask) (out + (t + i) * k.ot)[at.channel] = (E)(i <= left ? y[i] : 0.0f);
+        }
+        xs = next_xs, ds = next_ds;
+    }
+    if constexpr (kMaps) {
+        float *map = map_of<NP, SL>(k, at, at.segment);
+        store_states<NP>(map, h);
+        map[64 * NP + lane] = sum;
+    } else {
+        // positions past the length, from the first piece that has none of the sequence on
+        for (int t = max(begin, (at.length + kPiece - 1) / kPiece * kPiece); t < end; ++t)
+            if (t % SL == at.slice && at.lane_mask) (out + t * k.ot)[at.channel] = (E)0.0f;
+        const int last_segment = max(at.length - 1, 0) / (k.span * kPiece);
+        if (k.a.last && at.segment == last_segment) store_own<NP>(k.a.last + own, at.slice, k.N, at.lane_mask, h);
+    }
+}
+
+// b and c in rows of `padded` fp32 states, zeros behind the N there are: [2][B][T][G][padded].
+template <class E>
+__global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E *b, const E *c, long long bb, long long bt, long long cb, long long ct, int B,
+                                                                         int T, int G, int N, int padded, float *rows)
+{
+    const long long half = (long long)B * T * G * padded, i = (long long)blockIdx.x * kThreadsOfRows + threadIdx.x;
+    if (i >= 2 * half) return;
+    const bool second = i >= half;
+    long long rest = second ? i - half : i;
+    const int n = rest % padded;
+    rest /= padded;
+    const int g = rest % G;
+    rest /= G;
+    const int t = rest % T, s = rest / T;
+    const E *from = second ? c + s * cb + t * ct : b + s * bb + t * bt;
+    rows[i] = n < N ? (float)from[(long long)g * N + n] : 0.0f;
+}
+
+}  // namespace
+
+SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse)
+{
+    SelectivePlan p{};
+    p.states = s.N <= 4 ? 4 : s.N <= 8 ? 8 : 16;
+    p.slices = s.N <= 16 ? 1 : s.N <= 32 ? 2 : 4;
+    p.padded = p.states * p.slices;
+    p.tiles = (s.C / s.G + 63) / 64;
+    p.pieces = (s.T + kPiece - 1) / kPiece;
+    const long long lines = (long long)s.B * s.G * p.tiles * p.slices;
+    const long long wanted = std::min<long long>((2048 + lines - 1) / lines, 64);
+    p.segments = (int)std::max<long long>(1, std::min<long long>(wanted, (p.pieces + 1) / 2));
+    p.span = (p.pieces + p.segments - 1) / p.segments;
+    p.segments = (p.pieces + p.span - 1) / p.span;
+    const size_t tiles = (size_t)s.G * p.tiles;
+    p.maps = p.segments > 1 ? (size_t)s.B * p.segments * tiles * p.slices * (p.states + 1) * 64 : 0;
+    p.rows = 2 * (size_t)s.B * s.T * s.G * p.padded;
+    if (reverse) {
+        p.part_rows = (size_t)p.tiles * s.B * p.pieces * kPiece * s.G * 2 * p.padded;
+        p.part_sums = (size_t)s.B * p.segments * tiles * p.slices * (p.states + 2) * 64;
+    }
+    return p;
+}
+
+size_t selective_workspace_floats(const esrnn_selective_shape &s, bool reverse)
+{
+    const SelectivePlan p = selective_plan(s, reverse);
+    return 64 + p.maps + p.rows + p.part_rows + p.part_sums;
+}
+size_t selective_saved_floats(const esrnn_selective_shape &s)
+{
+    const SelectivePlan p = selective_plan(s, false);
+    return (size_t)s.B * p.pieces * s.G * p.tiles * p.padded * 64;
+}
+
+// Rows of b and c that the kernels read as they are: whole groups of states, at multiples of four bytes.  (fp16 is no upper half of a float.)
+static bool shared_as_given(const esrnn_selective_shape &s, const SelectivePlan &p, const void *row, const int64_t stride[2])
+{
+    if (s.N != p.padded || s.dtype == ESRNN_F16) return false;
+    return s.dtype == ESRNN_F32 || (aligned_to(row, 4) && stride[0] % 2 == 0 && stride[1] % 2 == 0);
+}
+
+Scan scan_arguments(const esrnn_selective_shape &s, const SelectiveArgs &a, SelectivePlan &p)
+{
+    Scan k{};
+    k.a = a;
+    k.xb = s.x_stride[0], k.xt = s.x_stride[1], k.db = s.delta_stride[0], k.dt = s.delta_stride[1], k.ob = s.out_stride[0], k.ot = s.out_stride[1];
+    k.gb = s.grad_out_stride[0], k.gt = s.grad_out_stride[1], k.gxb = s.grad_x_stride[0], k.gxt = s.grad_x_stride[1];
+    k.gdb = s.grad_delta_stride[0], k.gdt = s.grad_delta_stride[1];
+    k.B = s.B, k.T = s.T, k.C = s.C, k.N = s.N, k.G = s.G, k.softplus = s.delta_kind == ESRNN_DELTA_SOFTPLUS;
+    k.group_channels = s.C / s.G, k.tiles = p.tiles, k.pieces = p.pieces, k.segments = p.segments, k.span = p.span;
+    k.maps = a.workspace;
+    float *rows = a.workspace + p.maps;
+    k.part_rows = rows + p.rows, k.part_sums = k.part_rows + p.part_rows;
+    p.widened = !(shared_as_given(s, p, a.b, s.b_stride) && shared_as_given(s, p, a.c, s.c_stride));
+    if (p.widened) {
+        const long long position = (long long)s.G * p.padded, sequence = s.T * position;
+        k.b = rows, k.c = rows + s.B * sequence;
+        k.bb = k.cb = sequence, k.bt = k.ct = position, k.group = p.padded;
+    } else {
+        k.b = a.b, k.c = a.c;
+        k.bb = s.b_stride[0], k.bt = s.b_stride[1], k.cb = s.c_stride[0], k.ct = s.c_stride[1], k.group = s.N;
+    }
+    return k;
+}
+
+hipError_t launch_selective_widen(const esrnn_selective_shape &s, const SelectiveArgs &a, const SelectivePlan &p, const Scan &k, hipStream_t st)
+{
+    if (!p.widened) return hipSuccess;
+    return with_element(s.dtype, [&](auto e) {
+        typedef decltype(e) E;
+        selective_widen_kernel<E><<<dim3((unsigned)((p.rows + kThreadsOfRows - 1) / kThreadsOfRows)), kThreadsOfRows, 0, st>>>(
+            static_cast<const E *>(a.b), static_cast<const E *>(a.c), s.b_stride[0], s.b_stride[1], s.c_stride[0], s.c_stride[1], s.B, s.T, s.G, s.N,
+            p.padded, const_cast<float *>(static_cast<const float *>(k.b)));
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_selective_forward(const esrnn_selective_shape &s, const SelectiveArgs &a, hipStream_t st)
+{
+    SelectivePlan p = selective_plan(s, false);
+    const Scan k = scan_arguments(s, a, p);
+    if (const hipError_t e = launch_selective_widen(s, a, p, k, st); e != hipSuccess) return e;
+    const unsigned lines = (unsigned)(s.B * s.G * p.tiles);
+    return with_scan(s, p, [&](auto e, auto bc, auto states, auto slices) {
+        typedef decltype(e) E;
+        typedef decltype(bc) BC;
+        constexpr int NP = decltype(states)::value, SL = decltype(slices)::value;
+        if (p.segments > 1) selective_forward_kernel<E, BC, NP, SL, true><<<dim3(lines * (p.segments - 1)), 64 * SL, 0, st>>>(k);
+        selective_forward_kernel<E, BC, NP, SL, false><<<dim3(lines * p.segments), 64 * SL, 0, st>>>(k);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace esrnn

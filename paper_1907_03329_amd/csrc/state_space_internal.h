@@ -1,0 +1,190 @@
+// What the operators of a selective state space layer (include/esrnn_state_space.h) share: channels of a lane, sums over rows of partial
+// results, the softplus, and the launch functions that state_space_api.cpp calls.
+#pragma once
+
+#include "esrnn_state_space.h"
+#include "layers_internal.h"
+
+namespace esrnn {
+
+// V neighbouring channels of a lane from `first` on, of `count` in all: one access of 16 bytes at the alignment of one element where all of them
+// exist, one by one in the last lane of a row that they do not fill.
+template <class E, int V>
+struct Neighbours {
+    typedef E LooseValues __attribute__((ext_vector_type(V), aligned(sizeof(E))));
+    typedef E Values __attribute__((ext_vector_type(V)));
+    typedef unsigned Bits __attribute__((ext_vector_type(V * sizeof(E) / 4)));
+    typedef float Floats __attribute__((ext_vector_type(V)));
+    int first, count;
+    __device__ __forceinline__ bool some() const { return first < count; }
+    __device__ __forceinline__ bool all() const { return first + V <= count; }
+    // zeros where there are no channels
+    __device__ __forceinline__ Values load(const E *row) const
+    {
+        Values v = {};
+        if (all()) {
+            v = *reinterpret_cast<const LooseValues *>(row + first);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (first + k < count) v[k] = row[first + k];
+        }
+        return v;
+    }
+    __device__ __forceinline__ void store(E *row, Values v) const
+    {
+        if (all()) {
+            *reinterpret_cast<LooseValues *>(row + first) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (first + k < count) row[first + k] = v[k];
+        }
+    }
+    static __device__ __forceinline__ Floats widen(Values v) { return __builtin_convertvector(v, Floats); }
+    static __device__ __forceinline__ Values round(Floats v) { return __builtin_convertvector(v, Values); }
+};
+
+// The same where kWide says that there are V channels at least: then the last lane with channels has the last V there are, so that two lanes may
+// have the same channel, compute the same and write the same.  Else one by one, and the last channel in the place of those that do not exist.
+template <class E, int V, bool kWide>
+struct Overlapping {
+    typedef Neighbours<E, V> N;
+    int first, count;
+    __device__ __forceinline__ Overlapping(int begin, int C) : first(kWide && begin < C ? min(begin, C - V) : begin), count(C) {}
+    __device__ __forceinline__ bool some() const { return first < count; }
+    __device__ __forceinline__ int channel(int k) const { return kWide ? min(first, count - V) + k : min(first + k, count - 1); }
+    __device__ __forceinline__ typename N::Values load(const E *row) const
+    {
+        typename N::Values v;
+        if constexpr (kWide) {
+            v = *reinterpret_cast<const typename N::LooseValues *>(row + channel(0));
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = row[channel(k)];
+        }
+        return v;
+    }
+    // (by lanes with channels)
+    __device__ __forceinline__ void store(E *row, typename N::Values v) const
+    {
+        if constexpr (kWide) {
+            *reinterpret_cast<typename N::LooseValues *>(row + first) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (first + k < count) row[first + k] = v[k];
+        }
+    }
+};
+
+// Sums of `rows` rows of `cols` partial results, in a fixed order, for 64 columns from `first` on: by a workgroup of 1024 threads, sixteen rows at a
+// time; store(column, sum) by the threads of the first row.
+template <class F>
+__device__ __forceinline__ void sum_columns(const float *__restrict__ parts, long long rows, long long cols, long long first, F &&store)
+{
+    __shared__ float s_sum[16][64];
+    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
+    const long long col = first + lane;
+    float v[4] = {};
+    if (col < cols) {
+        long long r = row;
+        for (; r + 48 < rows; r += 64)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] += parts[(r + 16 * k) * cols + col];
+        for (; r < rows; r += 16) v[0] += parts[r * cols + col];
+    }
+    s_sum[row][lane] = (v[0] + v[1]) + (v[2] + v[3]);
+    __syncthreads();
+#pragma unroll
+    for (int half = 8; half > 0; half /= 2) {
+        if (row < half) s_sum[row][lane] += s_sum[row + half][lane];
+        __syncthreads();
+    }
+    if (row == 0 && col < cols) store(col, s_sum[0][lane]);
+}
+
+// softplus(v) = max(v, 0) + log(1 + exp(-|v|)) and its derivative sigmoid(v).  log(1 + e) = 2 atanh(e / (2 + e)): the argument is at most 1/3, and
+// seven terms of the series leave 2^-26 of it, at small e too, where the logarithm of 1 + e would have lost e's digits.  exp(-|v|) is zero
+// below 2^-126.
+struct Softplus {
+    float of, slope;
+};
+__device__ __forceinline__ Softplus softplus(float v)
+{
+    const float e = __builtin_amdgcn_exp2f(fabsf(v) * kSigmoidExponent), r = fast_rcp(1.0f + e);
+    const float s = e * fast_rcp(2.0f + e), z = s * s;
+    float p = 1.0f / 13.0f;
+    p = fmaf(p, z, 1.0f / 11.0f);
+    p = fmaf(p, z, 1.0f / 9.0f);
+    p = fmaf(p, z, 1.0f / 7.0f);
+    p = fmaf(p, z, 1.0f / 5.0f);
+    p = fmaf(p, z, 1.0f / 3.0f);
+    p = fmaf(p, z, 1.0f);
+    const float s2 = s + s;
+    return {fmaf(p, s2, fmaxf(v, 0.0f)), v < 0.0f ? e * r : r};
+}
+
+// u sigmoid(u) and its derivative, p (1 + u (1 - p)).  An infinite u gives -0 and 0, or itself and 1, not the product of zero and infinity.
+struct Silu {
+    float of, slope;
+};
+__device__ __forceinline__ Silu silu(float u)
+{
+    const Sigmoids s = sigmoids(u);
+    const float of = s.of == 0.0f ? -0.0f : u * s.of;
+    return {of, fmaf(fminf(of, 0x1p127f), s.of_minus, s.of)};
+}
+
+// ---- short causal convolution (convolution_kernels.hip) ----
+struct ConvolutionArgs {
+    const void *x, *grad_out, *initial;
+    const int32_t *lengths;
+    const float *weight, *bias, *grad_last;
+    void *out, *last, *grad_x;
+    float *grad_weight, *grad_bias, *grad_initial;
+    float *parts;               // the workspace: (K + 1) sums of every channel for every workgroup
+};
+size_t convolution_workspace_floats(const esrnn_convolution_shape &s);
+hipError_t launch_convolution_forward(const esrnn_convolution_shape &s, const ConvolutionArgs &a, hipStream_t st);
+hipError_t launch_convolution_backward(const esrnn_convolution_shape &s, const ConvolutionArgs &a, hipStream_t st);
+hipError_t launch_convolution_step(const esrnn_convolution_step_shape &s, const void *x, const float *weight, const float *bias, const int32_t *slots,
+                                   void *state, void *out, hipStream_t st);
+
+// ---- selective scan (selective_forward_kernels.hip, selective_backward_kernels.hip, selective_step_kernels.hip) ----
+struct SelectiveArgs {
+    const void *x, *delta, *b, *c, *grad_out;
+    const float *A, *D, *bias, *initial, *grad_last;
+    const int32_t *lengths;
+    void *out, *grad_x, *grad_delta, *grad_b, *grad_c;
+    float *last, *saved, *grad_A, *grad_D, *grad_bias, *grad_initial;
+    float *workspace;
+};
+size_t selective_workspace_floats(const esrnn_selective_shape &s, bool reverse);
+size_t selective_saved_floats(const esrnn_selective_shape &s);
+hipError_t launch_selective_forward(const esrnn_selective_shape &s, const SelectiveArgs &a, hipStream_t st);
+hipError_t launch_selective_backward(const esrnn_selective_shape &s, const SelectiveArgs &a, hipStream_t st);
+struct SelectiveStep {
+    const void *x, *delta, *b, *c;
+    const float *A, *D, *bias;
+    const int32_t *slots;
+    float *state;
+    void *out;
+};
+hipError_t launch_selective_step(const esrnn_selective_step_shape &s, const SelectiveStep &a, hipStream_t st);
+
+// ---- block norm (block_norm_kernels.hip) ----
+struct BlockNormArgs {
+    const void *y, *gate, *residual, *grad_out, *grad_sum;
+    const int32_t *exists;
+    const float *post_weight, *scale, *pre_weight, *stats_in;
+    void *sum, *out, *grad_y, *grad_gate, *grad_residual;
+    float *stats, *grad_post_weight, *grad_scale, *grad_pre_weight;
+    float *parts;               // the workspace: three sums of every channel for every workgroup
+};
+constexpr int kBlockNormMostChannels = 8192;
+size_t block_norm_workspace_floats(const esrnn_block_norm_shape &s);
+hipError_t launch_block_norm_forward(const esrnn_block_norm_shape &s, const BlockNormArgs &a, hipStream_t st);
+hipError_t launch_block_norm_backward(const esrnn_block_norm_shape &s, const BlockNormArgs &a, hipStream_t st);
+
+}  // namespace esrnn
