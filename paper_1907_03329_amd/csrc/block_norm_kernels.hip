@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
 
 __global__ void __launch_bounds__(1024) block_norm_sum_kernel(const float *__restrict__ parts, int rows, int C, float *grad_post, float *grad_scale, float *grad_pre)
 {
-    sum_columns(parts, rows, 3ll * C, (long long)blockIdx.x * 64, [&](long long col, float v) {
+    sum_columns<kSumColumns>(parts, rows, 3ll * C, (long long)blockIdx.x * kSumColumns, [&](long long col, float v) {
         float *to = col < C ? grad_post : col < 2ll * C ? grad_scale : grad_pre;
         if (to) to[col % C] = v;
     });
@@ -337,7 +337,7 @@ hipError_t launch_block_norm_backward(const esrnn_block_norm_shape &s, const Blo
         });
     });
     if (failed != hipSuccess || !(a.grad_post_weight || a.grad_scale || a.grad_pre_weight)) return failed;
-    block_norm_sum_kernel<<<dim3((3 * s.C + 63) / 64), 1024, 0, st>>>(a.parts, rows, s.C, a.grad_post_weight, a.grad_scale, a.grad_pre_weight);
+    block_norm_sum_kernel<<<dim3((3 * s.C + kSumColumns - 1) / kSumColumns), 1024, 0, st>>>(a.parts, rows, s.C, a.grad_post_weight, a.grad_scale, a.grad_pre_weight);
     return hipGetLastError();
 }
 

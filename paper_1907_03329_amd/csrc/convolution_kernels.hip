@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kThreads) convolution_backward_kernel(Args p)
 __global__ void __launch_bounds__(1024) convolution_sum_kernel(const float *__restrict__ parts, long long rows, int tiles, int K, int C, float *grad_weight,
                                                                float *grad_bias)
 {
-    sum_columns(parts, rows, (long long)tiles * (K + 1) * kTile, (long long)blockIdx.x * 64, [&](long long col, float v) {
+    sum_columns<kSumColumns>(parts, rows, (long long)tiles * (K + 1) * kTile, (long long)blockIdx.x * kSumColumns, [&](long long col, float v) {
         const int j = (int)(col / kTile) % (K + 1), c = (int)(col / ((K + 1) * kTile)) * kTile + (int)(col % kTile);
         if (c >= C) return;
         if (j < K) grad_weight[(long long)c * K + j] = v;
@@ -369,7 +369,7 @@ hipError_t launch_convolution_backward(const esrnn_convolution_shape &s, const C
         return hipGetLastError();
     });
     if (failed != hipSuccess) return failed;
-    convolution_sum_kernel<<<dim3(p.tiles * (s.K + 1)), 1024, 0, st>>>(a.parts, (long long)p.B * p.blocks, p.tiles, s.K, s.C, a.grad_weight, a.grad_bias);
+    convolution_sum_kernel<<<dim3(p.tiles * (s.K + 1) * (kTile / kSumColumns)), 1024, 0, st>>>(a.parts, (long long)p.B * p.blocks, p.tiles, s.K, s.C, a.grad_weight, a.grad_bias);
     return hipGetLastError();
 }
 

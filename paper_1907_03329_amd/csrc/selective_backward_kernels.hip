@@ -6,8 +6,8 @@
 //   grad x_t = d_t sum_n lambda_t b_t + D g_t,  grad d_t = sum_n mu_t h_{t-1} A + x_t sum_n lambda_t b_t,  grad delta_t = grad d_t softplus'
 //   grad A = sum_t mu_t h_{t-1} d_t,  grad D = sum_t g_t x_t,  grad bias = sum_t grad delta_t,  grad initial = mu at the first position.
 // The states h are computed again, piece by piece, from the one before each piece that the forward pass has left; for a piece they stay in
-// registers, half of a lane's states at a time.  Sums over channels go through the lanes of a wave, where every addition also halves how many
-// values a lane has left, and then over tiles, in a second launch; those over positions through lanes and segments, in the same.
+// registers, four of a lane's states at a time.  Sums over channels go through LDS within a wave and over tiles in a second launch; those over positions
+// stay in a lane and go over segments in the same.
 #include <algorithm>
 
 #include "selective_scan.h"
@@ -16,31 +16,28 @@ namespace esrnn {
 
 namespace {
 
-typedef unsigned u32pair __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ unsigned bits_of(float v) { return __builtin_bit_cast(unsigned, v); }
-__device__ __forceinline__ float float_of(unsigned v) { return __builtin_bit_cast(float, v); }
-
-// Sums over the halves of the wave of two values: the lower half gets that of a, the upper half that of b.
-__device__ __forceinline__ float fold_halves(float a, float b)
+// Sums over the lanes of a wave go through LDS: a lane leaves its four values for b and four for c at each of eight positions; then a lane has one of
+// eight positions, b or c, and adds up every fourth lane's, four states at a time, and the four lanes of a quad put their sums together, a state each.
+// That is 8.6 vector instructions for a position's eight values where exchanges between lanes alone, each of which halves the lanes and the values, take
+// 18; the vector ALU is the bound here and LDS is not.  Rows are 64 lanes x 16 bytes and 64 bytes more, so that the sixteen lanes of a read have all banks.
+constexpr int kSumRow = 64 * 4 + 16;
+// Sums of the quad's lanes, the first value in the lane 0, ..
+__device__ __forceinline__ float exchanged(float keep, float send, std::integral_constant<int, 2>)
 {
-    const auto r = __builtin_amdgcn_permlane32_swap(bits_of(a), bits_of(b), false, false);
-    return float_of(r[0]) + float_of(r[1]);
+    return keep + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, send), 0x4e, 0xf, 0xf, true));     // lane ^ 2
 }
-// The same over neighbouring rows of 16 lanes: even rows a, odd rows b.
-__device__ __forceinline__ float fold_rows(float a, float b)
+__device__ __forceinline__ float exchanged(float keep, float send, std::integral_constant<int, 1>)
 {
-    const auto r = __builtin_amdgcn_permlane16_swap(bits_of(a), bits_of(b), false, false);
-    return float_of(r[0]) + float_of(r[1]);
+    return keep + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, send), 0xb1, 0xf, 0xf, true));     // lane ^ 1
 }
-// Within a row, over lanes kCtrl apart: `odd` lanes get the sum of b, others that of a.
-template <int kCtrl>
-__device__ __forceinline__ float fold(float a, float b, bool odd)
+__device__ __forceinline__ float sum_of_quad(f32x4 v)
 {
-    const float keep = odd ? b : a, send = odd ? a : b;
-    return keep + float_of(__builtin_amdgcn_update_dpp(0, bits_of(send), kCtrl, 0xf, 0xf, true));
+    const bool upper = threadIdx.x & 2, odd = threadIdx.x & 1;
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 1> one;
+    const float p = exchanged(upper ? v[2] : v[0], upper ? v[0] : v[2], two), q = exchanged(upper ? v[3] : v[1], upper ? v[1] : v[3], two);
+    return exchanged(odd ? q : p, odd ? p : q, one);
 }
-constexpr int kRowRotate8 = 0x128, kRowHalfMirror = 0x141, kQuadOther2 = 0x4e, kQuadOther1 = 0xb1;      // lanes i and i ^ 8, 7 - i, i ^ 2, i ^ 1
 
 // mu behind the last position of a segment, of the sequence's last segment with positions: the gradient of the last state.
 template <int NP, int SL>
@@ -49,6 +46,7 @@ __device__ __forceinline__ void arriving(const Scan &k, const ScanPlace &at, siz
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int n = 0; n < NP; ++n) mu[n] = 0.0f;
+    if (k.carried) return load_states<NP>(map_of<NP, SL>(k, at, at.segment), mu);
     if (k.a.grad_last) load_own<NP>(k.a.grad_last + own, at.slice, k.N, at.lane_mask, mu);
     for (int s = max(at.length - 1, 0) / (k.span * kPiece); s > at.segment; --s) {
         const float *map = map_of<NP, SL>(k, at, s);
@@ -88,7 +86,7 @@ __global__ void __launch_bounds__(64 * SL) selective_back_maps_kernel(Scan k)
         const BC *c0 = c + t * k.ct;
 #pragma unroll
         for (int i = kPiece - 1; i >= 0; --i) {
-            const unsigned mask = i <= left ? at.lane_mask : 0u;
+            const unsigned mask = i <= left ? 0xffffffffu : 0u;
             const float d = masked(step_size(ds.v[i], bias, k.softplus).of, mask), g = masked((float)gs.v[i], mask);
             float cs[NP];
             load_shared<BC, NP>(c0, k.ct, i, left, cs);
@@ -108,6 +106,7 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
 {
     constexpr int kPart = 4, kPadded = NP * SL;     // (states at a time: theirs at nine positions and their decays at eight take 68 registers)
     __shared__ float s_sums[SL > 1 ? 2 : 1][SL > 1 ? SL : 1][2 * kPiece][64];
+    __shared__ __attribute__((aligned(16))) float s_shared[SL][2 * kPiece][kSumRow];
     const ScanPlace at(k, k.segments);
     const int lane = threadIdx.x & 63;
     const int begin = at.segment * k.span * kPiece, end = min(begin + k.span * kPiece, k.T);
@@ -125,13 +124,12 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
     const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
     if (begin < at.length || begin == 0) arriving<NP, SL>(k, at, own, A, mu);
 
-    // which of the values a lane has after all additions: one of four neighbouring positions, b or c, one of four states (every other quad the same)
-    const int row = lane / 16, part_step = lane & 3, part_state = (row & 1) * 2 + (lane >> 3 & 1);
-    const bool bit3 = lane & 8, bit1 = lane & 2, bit0 = lane & 1, part_lane = !(lane & 4);
-    // rows of [2][padded] for every position and group
+    // what a lane has after all additions: position lane / 8, b or c, state lane % 4; rows of [2][padded] for every position and group
     const float *parts = k.part_rows + (((size_t)(at.tile % k.tiles) * k.B + at.b) * k.pieces * kPiece * k.G + at.group) * (2 * kPadded) + NP * at.slice;
     const unsigned part_position = (unsigned)k.G * (2 * kPadded);
-    const unsigned part_at = part_lane ? 4 * (part_step * part_position + (row >> 1) * kPadded + part_state) : kOutside;
+    const unsigned part_at = 4 * ((lane >> 3) * part_position + (lane >> 2 & 1) * kPadded + (lane & 3));
+    float(*shared)[kSumRow] = s_shared[at.slice];
+    const float *shared_read = &shared[lane >> 2][4 * (lane & 3)];
 
     int turn = 0;
     const int last = min(end, at.length);
@@ -149,9 +147,10 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
             float d[kPiece], slope[kPiece], xi[kPiece], g[kPiece], through[kPiece], rate[kPiece];   // through: sum lambda b; rate: sum mu h_{t-1} A log2(e)
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) {
-                const unsigned mask = i <= left ? at.lane_mask : 0u;
+                const unsigned mask = i <= left ? 0xffffffffu : 0u;
                 const Softplus s = step_size(ds.v[i], bias, k.softplus);
-                d[i] = masked(s.of, mask), slope[i] = masked(s.slope, mask), xi[i] = masked((float)xs.v[i], mask), g[i] = masked((float)gs.v[i], mask);
+                d[i] = masked(masked(s.of, at.lane_mask), mask), g[i] = masked(masked((float)gs.v[i], at.lane_mask), mask);
+                slope[i] = masked(s.slope, mask), xi[i] = (float)xs.v[i];
                 through[i] = rate[i] = 0.0f;
             }
 #pragma unroll
@@ -175,7 +174,6 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
                         h[i + 1][n] = fmaf(decay[i][n], h[i][n], u * bs[n]);
                     }
                 }
-                float quad[4];
 #pragma unroll
                 for (int i = kPiece - 1; i >= 0; --i) {
                     float bs[kPart], cs[kPart], of_b[kPart], of_c[kPart];
@@ -193,20 +191,17 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
                         rate[i] = fmaf(m, A[n0 + n], rate[i]);
                         dA[n0 + n] = fmaf(m, d[i], dA[n0 + n]);
                     }
-                    // eight values over 64 lanes: lower half of the wave b, upper half c; then the states; then both quads of eight lanes alike
-                    float w[kPart];
-#pragma unroll
-                    for (int n = 0; n < kPart; ++n) w[n] = fold_halves(of_b[n], of_c[n]);
-                    const float p = fold<kRowRotate8>(fold_rows(w[0], w[2]), fold_rows(w[1], w[3]), bit3);
-                    quad[i & 3] = p + float_of(__builtin_amdgcn_update_dpp(0, bits_of(p), kRowHalfMirror, 0xf, 0xf, true));
-                    if ((i & 3) == 0) {     // four positions: one value a lane
-                        const float even = fold<kQuadOther2>(quad[0], quad[2], bit1), odd = fold<kQuadOther2>(quad[1], quad[3], bit1);
-                        buf_store(to_parts, part_at, 4 * (i * part_position + n0), fold<kQuadOther1>(even, odd, bit0));
-                    }
+                    *reinterpret_cast<f32x4 *>(&shared[2 * i][4 * lane]) = f32x4{of_b[0], of_b[1], of_b[2], of_b[3]};
+                    *reinterpret_cast<f32x4 *>(&shared[2 * i + 1][4 * lane]) = f32x4{of_c[0], of_c[1], of_c[2], of_c[3]};
                 }
+                f32x4 sum[2] = {*reinterpret_cast<const f32x4 *>(shared_read), *reinterpret_cast<const f32x4 *>(shared_read + 16)};
+#pragma unroll
+                for (int c = 2; c < 16; ++c) sum[c & 1] += *reinterpret_cast<const f32x4 *>(shared_read + 16 * c);
+                buf_store(to_parts, part_at, 4 * n0, sum_of_quad(sum[0] + sum[1]));
+                complete(through);
+                complete(rate);
+                complete(dA, n0, kPart);
             }
-            complete(through);
-            complete(rate);
             if constexpr (SL > 1) {
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i) s_sums[turn][at.slice][i][lane] = through[i], s_sums[turn][at.slice][kPiece + i][lane] = rate[i];
@@ -247,13 +242,15 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
 
 // The sums over segments of the gradients of A, D and bias (the first workgroups; rows of [tile][slice][states + 2][64]) and those over tiles of the
 // gradients of b and c (the others; [tile][position][group][2][padded]).
+constexpr int kSumElements = 4096;      // of a workgroup, about: whole positions
 template <class E>
-__global__ void __launch_bounds__(1024) selective_sum_kernel(Scan k, int states, int slices, long long first_rows, E *grad_b, E *grad_c, long long gbb,
-                                                             long long gbt, long long gcb, long long gct)
+__global__ void __launch_bounds__(1024) selective_sum_kernel(Scan k, int states, int slices, unsigned first_rows, int positions, E *grad_b, E *grad_c,
+                                                             long long gbb, long long gbt, long long gcb, long long gct)
 {
     if (blockIdx.x < first_rows) {
         const int wave = (states + 2) * 64;
-        sum_columns(k.part_sums, (long long)k.B * k.segments, (long long)k.G * k.tiles * slices * wave, (long long)blockIdx.x * 64, [&](long long col, float v) {
+        const long long cols = (long long)k.G * k.tiles * slices * wave, rows = (long long)k.B * k.segments;
+        sum_columns<kSumColumns>(k.part_sums, rows, cols, (long long)blockIdx.x * kSumColumns, [&](long long col, float v) {
             const int lane = col % 64, n = (int)(col / 64) % (states + 2), slice = (int)(col / wave) % slices, tile = (int)(col / wave / slices);
             const int in_group = tile % k.tiles * 64 + lane, channel = tile / k.tiles * k.group_channels + in_group;
             if (in_group >= k.group_channels) return;
@@ -263,27 +260,27 @@ __global__ void __launch_bounds__(1024) selective_sum_kernel(Scan k, int states,
                 // every slice has its share of the positions
                 if (slice == 0) {
                     for (int s = 1; s < slices; ++s)
-                        for (long long r = 0; r < (long long)k.B * k.segments; ++r) v += k.part_sums[(r * k.G * k.tiles * slices + tile * slices + s) * wave + n * 64 + lane];
+                        for (long long r = 0; r < rows; ++r) v += k.part_sums[r * cols + col + s * wave];
                     to[channel] = v;
                 }
             }
         });
         return;
     }
-    const int padded = states * slices, width = k.G * 2 * padded;
-    // (whole pieces of every sequence)
-    const long long i = (blockIdx.x - first_rows) * 1024 + threadIdx.x, length_of = (long long)k.pieces * kPiece, positions = k.B * length_of;
-    if (i >= positions * width) return;
-    const long long position = i / width;
-    const int within = (int)(i % width), n = within % padded, group = within / (2 * padded), b = (int)(position / length_of), t = (int)(position % length_of);
-    const bool is_c = within / padded & 1;
-    if (n >= k.N || t >= k.T) return;
+    const unsigned padded = states * slices, width = k.G * 2 * padded, place = blockIdx.x - first_rows;
+    const int whole = k.pieces * kPiece, runs = (k.T + positions - 1) / positions, b = place / (unsigned)runs, t0 = place % (unsigned)runs * positions;
     const int length = k.a.lengths ? min(max(k.a.lengths[b], 0), k.T) : k.T;
-    float v = 0.0f;
-    if (t < length)
-        for (int q = 0; q < k.tiles; ++q) v += k.part_rows[q * positions * width + i];
-    E *to = is_c ? grad_c + b * gcb + t * gct : grad_b + b * gbb + t * gbt;
-    to[(long long)group * k.N + n] = (E)v;
+    const size_t tile_apart = (size_t)k.B * whole * width;
+    const float *from = k.part_rows + ((size_t)b * whole + t0) * width;
+    grad_b += b * gbb, grad_c += b * gcb;
+    for (unsigned i = threadIdx.x; i < min(positions, k.T - t0) * width; i += 1024) {
+        const unsigned t = t0 + i / width, within = i % width, n = within % padded, group = within / (2 * padded);
+        if (n >= (unsigned)k.N) continue;
+        float v = 0.0f;
+        if (t < (unsigned)length)
+            for (int q = 0; q < k.tiles; ++q) v += from[q * tile_apart + i];
+        (within / padded & 1 ? grad_c + t * gct : grad_b + t * gbt)[group * k.N + n] = (E)v;
+    }
 }
 
 }  // namespace
@@ -298,16 +295,21 @@ hipError_t launch_selective_backward(const esrnn_selective_shape &s, const Selec
         typedef decltype(e) E;
         typedef decltype(bc) BC;
         constexpr int NP = decltype(states)::value, SL = decltype(slices)::value;
-        if (p.segments > 1) selective_back_maps_kernel<E, BC, NP, SL><<<dim3(lines * (p.segments - 1)), 64 * SL, 0, st>>>(k);
+        if (p.segments > 1) {
+            selective_back_maps_kernel<E, BC, NP, SL><<<dim3(lines * (p.segments - 1)), 64 * SL, 0, st>>>(k);
+            if (const hipError_t stopped = launch_selective_carry(s, p, k, true, st); stopped != hipSuccess) return stopped;
+        }
         selective_backward_kernel<E, BC, NP, SL><<<dim3(lines * p.segments), 64 * SL, 0, st>>>(k);
         return hipGetLastError();
     });
     if (failed != hipSuccess) return failed;
-    const long long columns = (long long)s.G * p.tiles * p.slices * (p.states + 2), rows = ((long long)s.B * p.pieces * kPiece * s.G * 2 * p.padded + 1023) / 1024;
+    const unsigned columns = (unsigned)(s.G * p.tiles * p.slices * (p.states + 2) * (64 / kSumColumns));
+    const int positions = std::max(1, kSumElements / (s.G * 2 * p.padded));
+    const unsigned runs = (unsigned)s.B * ((s.T + positions - 1) / positions);
     return with_element(s.dtype, [&](auto e) {
         typedef decltype(e) E;
-        selective_sum_kernel<E><<<dim3((unsigned)(columns + rows)), 1024, 0, st>>>(k, p.states, p.slices, columns, static_cast<E *>(a.grad_b), static_cast<E *>(a.grad_c),
-                                                                              s.grad_b_stride[0], s.grad_b_stride[1], s.grad_c_stride[0], s.grad_c_stride[1]);
+        selective_sum_kernel<E><<<dim3(columns + runs), 1024, 0, st>>>(k, p.states, p.slices, columns, positions, static_cast<E *>(a.grad_b), static_cast<E *>(a.grad_c),
+                                                                       s.grad_b_stride[0], s.grad_b_stride[1], s.grad_c_stride[0], s.grad_c_stride[1]);
         return hipGetLastError();
     });
 }

@@ -1,5 +1,6 @@
 // Selective scan over whole sequences, forward (include/esrnn_state_space.h; selective_scan.h has the way it is cut up).
 #include <algorithm>
+#include <cmath>
 
 #include "selective_scan.h"
 
@@ -29,8 +30,10 @@ __global__ void __launch_bounds__(64 * SL) selective_forward_kernel(Scan k)
 #pragma unroll
     for (int n = 0; n < NP; ++n) A[n] *= kLog2e, h[n] = 0.0f;
     const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
-    if (!kMaps && k.a.initial && (begin < at.length || begin == 0)) load_own<NP>(k.a.initial + own, at.slice, k.N, at.lane_mask, h);
-    if (!kMaps && begin < at.length) {
+    if (!kMaps && k.carried && at.segment > 0) {
+        if (begin < at.length) load_states<NP>(map_of<NP, SL>(k, at, at.segment), h);
+    } else if (!kMaps && (begin < at.length || begin == 0)) {
+        if (k.a.initial) load_own<NP>(k.a.initial + own, at.slice, k.N, at.lane_mask, h);
         for (int s = 0; s < at.segment; ++s) {
             const float *map = map_of<NP, SL>(k, at, s);
             float local[NP];
@@ -56,8 +59,7 @@ __global__ void __launch_bounds__(64 * SL) selective_forward_kernel(Scan k)
         const BC *b0 = b + t * k.bt, *c0 = c + t * k.ct;
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) {
-            const unsigned mask = i <= left ? at.lane_mask : 0u;
-            const float d = masked(step_size(ds.v[i], bias, k.softplus).of, mask), xi = masked((float)xs.v[i], mask), u = d * xi;
+            const float d = masked(step_size(ds.v[i], bias, k.softplus).of, i <= left ? 0xffffffffu : 0u), xi = (float)xs.v[i], u = d * xi;
             float bs[NP], cs[NP];
             load_shared<BC, NP>(b0, k.bt, i, left, bs);
             if (kMaps) {
@@ -106,6 +108,85 @@ __global__ void __launch_bounds__(64 * SL) selective_forward_kernel(Scan k)
     }
 }
 
+// A wave has a run of neighbouring segments, in their order or against it, and four states of 64 channels: first the run's own map, then, behind those
+// of the runs before it, what enters each of its segments.
+constexpr int kRuns = 16;
+template <int NP, int SL>
+__global__ void __launch_bounds__(64 * kRuns) selective_carry_kernel(Scan k, int reverse)
+{
+    __shared__ __attribute__((aligned(16))) f32x4 s_local[kRuns][64];
+    __shared__ float s_sum[kRuns][64];
+    const int lane = threadIdx.x & 63, run = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int quad = blockIdx.x % (NP / 4), slice = blockIdx.x / (NP / 4) % SL;
+    const unsigned line = blockIdx.x / (NP / 4 * SL);
+    const int tiles = k.G * k.tiles, tile = line % tiles, b = line / tiles;
+    const int in_group = tile % k.tiles * 64 + lane, channel = tile / k.tiles * k.group_channels + min(in_group, k.group_channels - 1);
+    const unsigned lane_mask = in_group < k.group_channels ? 0xffffffffu : 0u;
+    const int length = k.a.lengths ? min(max(__builtin_amdgcn_readfirstlane(k.a.lengths[b]), 0), k.T) : k.T;
+    const int last_segment = max(length - 1, 0) / (k.span * kPiece);
+    const int each = (k.segments + kRuns - 1) / kRuns, from = min(run * each, k.segments), to = min(from + each, k.segments);
+    // the place of number p, and whether it has a map: none comes in behind the last segment with positions, or from the last of all in their order
+    const auto segment = [&](int p) { return reverse ? k.segments - 1 - p : p; };
+    const auto has_map = [&](int p) { return p < k.segments - 1 && segment(p) <= last_segment; };
+    const auto place = [&](int p) { return k.maps + ((((size_t)b * k.segments + segment(p)) * tiles + tile) * SL + slice) * kMapFloats<NP>; };
+    float A[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int n = NP * slice + 4 * quad + r;
+        A[r] = masked(k.a.A[(size_t)channel * k.N + min(n, k.N - 1)], n < k.N ? lane_mask : 0u) * kLog2e;
+    }
+    const auto apply = [&](f32x4 h, f32x4 local, float sum) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) h[r] = fmaf(__builtin_amdgcn_exp2f(sum * A[r]), h[r], local[r]);
+        return h;
+    };
+    // kBatch maps from number p on; those that a run has not are the map that changes nothing
+    constexpr int kBatch = 8;
+    f32x4 local[kBatch];
+    float sum[kBatch];
+    const auto read = [&](int p) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const float *map = place(min(p + i, k.segments - 1));
+            local[i] = *reinterpret_cast<const f32x4 *>(map + 256 * quad + 4 * lane), sum[i] = map[64 * NP + lane];
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const unsigned mask = p + i < to && has_map(p + i) ? 0xffffffffu : 0u;
+            sum[i] = masked(sum[i], mask);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) local[i][r] = masked(local[i][r], mask);
+        }
+    };
+    f32x4 h = {};
+    float total = 0.0f;
+    for (int p = from; p < to; p += kBatch) {
+        read(p);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) h = apply(h, local[i], sum[i]), total += sum[i];
+    }
+    s_local[run][lane] = h;
+    s_sum[run][lane] = total;
+    __syncthreads();
+    const float *first = reverse ? k.a.grad_last : k.a.initial;
+    h = f32x4{};
+    if (first)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int n = NP * slice + 4 * quad + r;
+            h[r] = masked(first[((size_t)b * k.C + channel) * k.N + min(n, k.N - 1)], n < k.N ? lane_mask : 0u);
+        }
+    for (int r = 0; r < run; ++r) h = apply(h, s_local[r][lane], s_sum[r][lane]);
+    for (int p = from; p < to; p += kBatch) {
+        read(p);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (p + i < to) *reinterpret_cast<f32x4 *>(place(p + i) + 256 * quad + 4 * lane) = h;
+            h = apply(h, local[i], sum[i]);
+        }
+    }
+}
+
 // b and c in rows of `padded` fp32 states, zeros behind the N there are: [2][B][T][G][padded].
 template <class E>
 __global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E *b, const E *c, long long bb, long long bt, long long cb, long long ct, int B,
@@ -126,6 +207,30 @@ __global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E
 
 }  // namespace
 
+// From how many segments on their maps are put together by a launch of their own (12 us and 0.035 for each), and not by every wave (0.08 us for each).
+constexpr int kSegmentsAlone = 32;
+
+// How many segments a sequence is cut into, by what its launches take in microseconds, fitted to what they took at 16 states: a piece takes what one wave needs
+// for it and what the other waves of its SIMD need, a wave something to begin with, and a share of the maps before its own; the reverse kernel, of which a
+// SIMD holds two waves, takes whole rounds of them, and leaves sums for every wave.  4 x 4096 x 2048 bf16: forward 371 us with 16 segments, 292 with 32, 278
+// with 40; reverse 633 with 16, 603 with 32, 701 with 24.  1 x 65536 x 256: forward 213 with 512, 198 with 1024, 210 with 1280; reverse 354 with 512, 371 with
+// 1024.  501 x 240 x 50 ragged fp32: forward 91 with 4, 87 with 8, 126 with 30; reverse 139 with 5, 169 with 8, 222 with 30.
+static int best_segments(long long lines, int pieces, bool reverse)
+{
+    int best = 1;
+    double least = 1e30;
+    for (int segments = 1; segments <= pieces && (segments == 1 || lines * segments <= 16384); segments += std::max(1, segments / 32)) {
+        const int span = (pieces + segments - 1) / segments, cut = (pieces + span - 1) / span;
+        const double waves = lines * (double)cut / 1024.0, maps = waves * (cut - 1) / cut;      // of a SIMD
+        const double rounds = std::floor(waves / 2), rest = waves - 2 * rounds, share = cut > kSegmentsAlone ? 0.0 : 0.08 * cut;
+        double time = reverse ? (rounds + (rest > 1 ? 1.0 : rest > 0 ? 0.6 : 0.0)) * (13.8 * span + 3.0 + share) + 2.4 * waves
+                              : 2.8 * span + waves * (1.9 * span + 1.2 + share);
+        if (cut > 1) time += 2.2 * span + maps * (span * (reverse ? 1.8 : 1.5) + 1.2) + 4.0 + (cut > kSegmentsAlone ? 12.0 + 0.035 * cut : 0.0);
+        if (time < least) least = time, best = segments;
+    }
+    return best;
+}
+
 SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse)
 {
     SelectivePlan p{};
@@ -135,10 +240,10 @@ SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse)
     p.tiles = (s.C / s.G + 63) / 64;
     p.pieces = (s.T + kPiece - 1) / kPiece;
     const long long lines = (long long)s.B * s.G * p.tiles * p.slices;
-    const long long wanted = std::min<long long>((2048 + lines - 1) / lines, 64);
-    p.segments = (int)std::max<long long>(1, std::min<long long>(wanted, (p.pieces + 1) / 2));
+    p.segments = best_segments(lines, p.pieces, reverse);
     p.span = (p.pieces + p.segments - 1) / p.segments;
     p.segments = (p.pieces + p.span - 1) / p.span;
+    p.carried = p.segments > kSegmentsAlone;
     const size_t tiles = (size_t)s.G * p.tiles;
     p.maps = p.segments > 1 ? (size_t)s.B * p.segments * tiles * p.slices * (p.states + 1) * 64 : 0;
     p.rows = 2 * (size_t)s.B * s.T * s.G * p.padded;
@@ -175,7 +280,7 @@ Scan scan_arguments(const esrnn_selective_shape &s, const SelectiveArgs &a, Sele
     k.gb = s.grad_out_stride[0], k.gt = s.grad_out_stride[1], k.gxb = s.grad_x_stride[0], k.gxt = s.grad_x_stride[1];
     k.gdb = s.grad_delta_stride[0], k.gdt = s.grad_delta_stride[1];
     k.B = s.B, k.T = s.T, k.C = s.C, k.N = s.N, k.G = s.G, k.softplus = s.delta_kind == ESRNN_DELTA_SOFTPLUS;
-    k.group_channels = s.C / s.G, k.tiles = p.tiles, k.pieces = p.pieces, k.segments = p.segments, k.span = p.span;
+    k.group_channels = s.C / s.G, k.tiles = p.tiles, k.pieces = p.pieces, k.segments = p.segments, k.span = p.span, k.carried = p.carried;
     k.maps = a.workspace;
     float *rows = a.workspace + p.maps;
     k.part_rows = rows + p.rows, k.part_sums = k.part_rows + p.part_rows;
@@ -203,6 +308,22 @@ hipError_t launch_selective_widen(const esrnn_selective_shape &s, const Selectiv
     });
 }
 
+hipError_t launch_selective_carry(const esrnn_selective_shape &s, const SelectivePlan &p, const Scan &k, bool reverse, hipStream_t st)
+{
+    if (!p.carried) return hipSuccess;
+    const unsigned lines = (unsigned)(s.B * s.G * p.tiles);
+    const auto launch = [&](auto states, auto slices) {
+        constexpr int NP = decltype(states)::value, SL = decltype(slices)::value;
+        selective_carry_kernel<NP, SL><<<dim3(lines * SL * (NP / 4)), 64 * kRuns, 0, st>>>(k, reverse);
+        return hipGetLastError();
+    };
+    if (p.slices == 4) return launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
+    if (p.slices == 2) return launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+    if (p.states == 16) return launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+    if (p.states == 8) return launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+    return launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+}
+
 hipError_t launch_selective_forward(const esrnn_selective_shape &s, const SelectiveArgs &a, hipStream_t st)
 {
     SelectivePlan p = selective_plan(s, false);
@@ -213,7 +334,10 @@ hipError_t launch_selective_forward(const esrnn_selective_shape &s, const Select
         typedef decltype(e) E;
         typedef decltype(bc) BC;
         constexpr int NP = decltype(states)::value, SL = decltype(slices)::value;
-        if (p.segments > 1) selective_forward_kernel<E, BC, NP, SL, true><<<dim3(lines * (p.segments - 1)), 64 * SL, 0, st>>>(k);
+        if (p.segments > 1) {
+            selective_forward_kernel<E, BC, NP, SL, true><<<dim3(lines * (p.segments - 1)), 64 * SL, 0, st>>>(k);
+            if (const hipError_t failed = launch_selective_carry(s, p, k, false, st); failed != hipSuccess) return failed;
+        }
         selective_forward_kernel<E, BC, NP, SL, false><<<dim3(lines * p.segments), 64 * SL, 0, st>>>(k);
         return hipGetLastError();
     });

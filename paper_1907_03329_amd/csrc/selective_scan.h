@@ -3,15 +3,17 @@
 //
 // A lane has one channel with its N states in registers (up to 16; a channel of more has two or four lanes of as many waves, the slices), so a
 // wave has 64 channels, and what all of them share, b and c of a position, comes through the scalar cache into scalar registers: the vector
-// ALU takes it from there in the instruction that needs it.  Nothing of a position goes through LDS, and nothing is summed over lanes but the
+// ALU takes it from there in the instruction that needs it.  Nothing is summed over lanes but the
 // gradients of b and c.
 //
 // A sequence is cut into segments, which are as many waves: with a_t = exp(d_t A) a segment's map is h -> exp(A sum d) h + (its own last state from
 // zero), so a first launch leaves the last states and sums of d of all segments, and a second one has every segment put together the maps before its
-// own, and then walk its positions again.  Sequences and channels that fill the chip need no segments, and no first launch.
+// own (where these are many, a launch between the two does that for all of them), and then walk its positions again.  Sequences and channels that fill
+// the chip need no segments, and no first launch.
 //
-// exp(d A) is the hardware's power of two of d (A log2 e).  Channels that a tile lacks and positions past a length have d = x = 0, by a mask on their
-// bits: their states rest, and whatever lies there is never read into arithmetic.
+// exp(d A) is the hardware's power of two of d (A log2 e).  In the place of positions past a length, and of channels that a tile lacks, the last one there is
+// is read again, with d (and in the reverse pass the gradient of out) masked to zero where that matters: states rest behind a sequence, and what lies
+// there is never read.
 #pragma once
 
 #include "state_space_internal.h"
@@ -26,6 +28,7 @@ struct SelectivePlan {
     int tiles;                          // of 64 channels of a group
     int pieces, segments, span;         // of a sequence; pieces of a segment
     bool widened;                       // b and c are copied to fp32 rows of `padded` states first
+    bool carried;                       // the maps of segments are put together by a launch of their own
     size_t maps, rows, part_rows, part_sums;    // floats of the workspace: maps of segments, widened b and c, partial gradients of b and c, of A, D and bias
 };
 SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse);
@@ -38,10 +41,12 @@ struct Scan {
     long long gb, gt, gxb, gxt, gdb, gdt;
     float *maps, *part_rows, *part_sums;
     int B, T, C, N, G;
-    bool softplus;
+    bool softplus, carried;
     int group_channels, tiles, pieces, segments, span;
 };
 Scan scan_arguments(const esrnn_selective_shape &s, const SelectiveArgs &a, SelectivePlan &p);      // (sets p.widened)
+// Puts the state that enters each segment (against time: the gradient behind it) in the place of its map.
+hipError_t launch_selective_carry(const esrnn_selective_shape &s, const SelectivePlan &p, const Scan &k, bool reverse, hipStream_t st);
 // Copies b and c to rows of fp32 where the kernels cannot read them as they are.
 hipError_t launch_selective_widen(const esrnn_selective_shape &s, const SelectiveArgs &a, const SelectivePlan &p, const Scan &k, hipStream_t st);
 
@@ -114,10 +119,12 @@ __device__ __forceinline__ int fresh(int v)
 
 // Values that are complete here: or the compiler moves the whole sums behind the condition under which they are stored, and with them everything
 // that they are made of has to be kept.
-__device__ __forceinline__ void complete(float (&v)[kPiece])
+template <int N>
+__device__ __forceinline__ void complete(float (&v)[N], int from = 0, int count = N)
 {
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) asm volatile("" : "+v"(v[i]));
+    for (int i = 0; i < N; ++i)
+        if (i >= from && i < from + count) asm volatile("" : "+v"(v[i]));
 }
 
 // The elements of one channel at eight positions; behind the sequence's last one that one again.

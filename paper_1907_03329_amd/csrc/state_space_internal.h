@@ -78,51 +78,47 @@ struct Overlapping {
     }
 };
 
-// Sums of `rows` rows of `cols` partial results, in a fixed order, for 64 columns from `first` on: by a workgroup of 1024 threads, sixteen rows at a
-// time; store(column, sum) by the threads of the first row.
-template <class F>
+// Sums of `rows` rows of `cols` partial results, in a fixed order, for kCols columns from `first` on: by a workgroup of 1024 threads, 1024 / kCols rows at
+// a time; store(column, sum) by the threads of the first row.  Few columns need narrow workgroups to be many: 1024 rows of 150 columns take 3.9 us by 16
+// columns and 9.3 by 64.
+template <int kCols, class F>
 __device__ __forceinline__ void sum_columns(const float *__restrict__ parts, long long rows, long long cols, long long first, F &&store)
 {
-    __shared__ float s_sum[16][64];
-    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
+    constexpr int kRows = 1024 / kCols;
+    __shared__ float s_sum[kRows][kCols];
+    const int lane = threadIdx.x % kCols, row = threadIdx.x / kCols;
     const long long col = first + lane;
     float v[4] = {};
     if (col < cols) {
         long long r = row;
-        for (; r + 48 < rows; r += 64)
+        for (; r + 3 * kRows < rows; r += 4 * kRows)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] += parts[(r + 16 * k) * cols + col];
-        for (; r < rows; r += 16) v[0] += parts[r * cols + col];
+            for (int k = 0; k < 4; ++k) v[k] += parts[(r + kRows * k) * cols + col];
+        for (; r < rows; r += kRows) v[0] += parts[r * cols + col];
     }
     s_sum[row][lane] = (v[0] + v[1]) + (v[2] + v[3]);
     __syncthreads();
 #pragma unroll
-    for (int half = 8; half > 0; half /= 2) {
+    for (int half = kRows / 2; half > 0; half /= 2) {
         if (row < half) s_sum[row][lane] += s_sum[row + half][lane];
         __syncthreads();
     }
     if (row == 0 && col < cols) store(col, s_sum[0][lane]);
 }
+constexpr int kSumColumns = 16;
 
-// softplus(v) = max(v, 0) + log(1 + exp(-|v|)) and its derivative sigmoid(v).  log(1 + e) = 2 atanh(e / (2 + e)): the argument is at most 1/3, and
-// seven terms of the series leave 2^-26 of it, at small e too, where the logarithm of 1 + e would have lost e's digits.  exp(-|v|) is zero
-// below 2^-126.
+// softplus(v) = max(v, 0) + log(1 + exp(-|v|)) and its derivative sigmoid(v).  Of w = 1 + e, rounded, log(1 + e) = log(w) + (e - (w - 1)) / (1 + ..),
+// where the second term is what the rounding has lost of e, without which small e would lose all digits; its divisor is left out, as the term is below 2^-24
+// where that is not 1.  The hardware's logarithm is off by 2^-23 of itself at w near 1 too (all floats from 1 to 2 in steps of eight tried).
+// exp(-|v|) is zero below 2^-126.
 struct Softplus {
     float of, slope;
 };
 __device__ __forceinline__ Softplus softplus(float v)
 {
-    const float e = __builtin_amdgcn_exp2f(fabsf(v) * kSigmoidExponent), r = fast_rcp(1.0f + e);
-    const float s = e * fast_rcp(2.0f + e), z = s * s;
-    float p = 1.0f / 13.0f;
-    p = fmaf(p, z, 1.0f / 11.0f);
-    p = fmaf(p, z, 1.0f / 9.0f);
-    p = fmaf(p, z, 1.0f / 7.0f);
-    p = fmaf(p, z, 1.0f / 5.0f);
-    p = fmaf(p, z, 1.0f / 3.0f);
-    p = fmaf(p, z, 1.0f);
-    const float s2 = s + s;
-    return {fmaf(p, s2, fmaxf(v, 0.0f)), v < 0.0f ? e * r : r};
+    const float e = __builtin_amdgcn_exp2f(fabsf(v) * kSigmoidExponent), w = 1.0f + e, r = fast_rcp(w);
+    const float l = fmaf(__builtin_amdgcn_logf(w), 0.69314718055994531f, e - (w - 1.0f));
+    return {fmaxf(v, 0.0f) + l, v < 0.0f ? e * r : r};
 }
 
 // u sigmoid(u) and its derivative, p (1 + u (1 - p)).  An infinite u gives -0 and 0, or itself and 1, not the product of zero and infinity.
