@@ -1,7 +1,7 @@
 // Short causal convolution of every channel with activation (include/esrnn_state_space.h).
 //
 // A lane has 8 or 16 bytes of neighbouring channels and walks a run of positions with the last K - 1 inputs in registers; 64 channels are a
-// tile, and a workgroup has a tile of many runs.  Eight positions are requested at a time.
+// tile, and a workgroup has a tile of many runs.  Eight positions are requested at a time, four in the reverse pass.
 //
 // The reverse pass computes u again from x, and walks K - 1 positions past its run for the gradient of its last inputs:
 //   du_t = d_t act'(u_t),  dx_s = sum_i weight[K-1-i] du_{s+i},  dweight[j] = sum_t du_t x_{t-K+1+j},  dbias = sum_t du_t.
@@ -14,7 +14,7 @@ namespace esrnn {
 
 namespace {
 
-constexpr int kGroup = 8, kThreads = 256, kTile = 64;
+constexpr int kGroup = 8, kBackGroup = 4, kThreads = 256, kTile = 64;
 
 struct Args {
     ConvolutionArgs a;
@@ -38,16 +38,16 @@ struct Place {
     }
 };
 
-// Eight positions from `from` on: zeros where there is none (outside 0 .. length - 1).  What does not exist is read from a place that does, and
+// G positions from `from` on: zeros where there is none (outside 0 .. length - 1).  What does not exist is read from a place that does, and
 // masked out: loads behind a condition would be waited for one by one.
-template <class E, int V, bool kWide>
+template <class E, int V, bool kWide, int G>
 struct Rows {
     typedef Neighbours<E, V> N;
-    typename N::Values v[kGroup];
+    typename N::Values v[G];
     __device__ __forceinline__ void request(const E *base, long long stride, int from, int length, const Overlapping<E, V, kWide> &ch)
     {
 #pragma unroll
-        for (int i = 0; i < kGroup; ++i) v[i] = ch.load(base + (long long)max(min(from + i, length - 1), 0) * stride);
+        for (int i = 0; i < G; ++i) v[i] = ch.load(base + (long long)max(min(from + i, length - 1), 0) * stride);
     }
     __device__ __forceinline__ typename N::Floats get(int i, int from, int length) const
     {
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads) convolution_forward_kernel(Args p)
     }
     F w[K], bias, seen[K];          // seen[K - 1]: the newest
     load_weights<E, V, kWide, K>(p, ch, w, bias);
-    Rows<E, V, kWide> rows;
+    Rows<E, V, kWide, kGroup> rows;
     load_past<E, V, kWide, K>(p, x, at.b, at.begin, length, ch, seen);
     for (int t0 = at.begin; t0 < end; t0 += kGroup) {
         rows.request(x, p.xt, t0, length, ch);
@@ -148,11 +148,13 @@ __global__ void __launch_bounds__(kThreads) convolution_forward_kernel(Args p)
     }
 }
 
+// A run gives the gradients of its inputs, which need du up to K - 1 positions behind them: it begins with du of its first K - 1 positions, and then has du at
+// t = s + K - 1 for the input at s.  The sums for the weights count the latter, and those of the first K - 1 positions of the sequence.
 template <class E, int K, bool kWide>
-__global__ void __launch_bounds__(kThreads) convolution_backward_kernel(Args p)
+__global__ void __launch_bounds__(kThreads, K <= 4 ? 3 : 2) convolution_backward_kernel(Args p)
 {
     typedef Place<E, true> Here;
-    constexpr int V = Here::V, kLanes = Here::kLanes;
+    constexpr int V = Here::V, kLanes = Here::kLanes, G = kBackGroup;
     typedef Neighbours<E, V> N;
     typedef typename N::Floats F;
     __shared__ float s_sum[kThreads / 64][K + 1][kTile];
@@ -166,67 +168,89 @@ __global__ void __launch_bounds__(kThreads) convolution_backward_kernel(Args p)
     F dw[K], dbias = splat_f<F>(0.0f);
 #pragma unroll
     for (int j = 0; j < K; ++j) dw[j] = splat_f<F>(0.0f);
-    // gradient of the input at position s (negative: of `initial`), whose share of grad_last comes last
-    const auto put = [&](int s, F d) {
+    // the share that grad_last has in the gradient of the input at s, negative ones those of `initial`
+    const auto add_last = [&](int s, F &d) {
         const int tail = s - (length - (K - 1));
         if (p.a.grad_last && tail >= 0 && s < length) {
             const float *g = p.a.grad_last + ((long long)at.b * (K - 1) + tail) * p.C;
 #pragma unroll
             for (int k = 0; k < V; ++k) d[k] += g[ch.channel(k)];
         }
-        if (s >= 0) {
-            ch.store(grad_x + s * p.gt, s < length ? N::round(d) : typename N::Values{});
-        } else if (p.a.grad_initial) {
-            float *g = p.a.grad_initial + ((long long)at.b * (K - 1) + K - 1 + s) * p.C;
+    };
+    const auto put_initial = [&](int s, F d) {
+        if (!p.a.grad_initial) return;
+        add_last(s, d);
+        float *g = p.a.grad_initial + ((long long)at.b * (K - 1) + K - 1 + s) * p.C;
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (kWide || ch.first + k < p.C) g[ch.first + k] = d[k];
-        }
+        for (int k = 0; k < V; ++k)
+            if (kWide || ch.first + k < p.C) g[ch.first + k] = d[k];
     };
     if (ch.some() && at.begin < end) {
         if (at.begin >= length) {
             for (int t = at.begin; t < end; ++t) ch.store(grad_x + t * p.gt, typename N::Values{});
             if (at.begin == 0)      // an empty sequence hands the gradient of `last` to `initial`
 #pragma unroll
-                for (int j = 0; j < K - 1; ++j) put(j - (K - 1), splat_f<F>(0.0f));
+                for (int j = 0; j < K - 1; ++j) put_initial(j - (K - 1), splat_f<F>(0.0f));
         } else {
-            F w[K], bias, seen[K], du[K];       // du[K - 1]: the newest
+            F w[K], bias, seen[K], du[K];       // seen[K - 1], du[K - 1]: the newest
             load_weights<E, V, kWide, K>(p, ch, w, bias);
-            Rows<E, V, kWide> rows, ds;
             load_past<E, V, kWide, K>(p, x, at.b, at.begin, length, ch, seen);
 #pragma unroll
             for (int j = 0; j < K; ++j) du[j] = splat_f<F>(0.0f);
-            // the last group has the K - 1 positions behind the run (kGroup >= K - 1)
-            for (int t0 = at.begin; t0 < end + K - 1; t0 += kGroup) {
+            // the next position: `d` of out, whose u is made of seen[0 .. K - 1]
+            const auto advance = [&](F d, bool counts) {
+                if (p.silu) {
+                    F u = bias;
+#pragma unroll
+                    for (int j = 0; j < K; ++j) u += w[j] * seen[j];
+#pragma unroll
+                    for (int k = 0; k < V; ++k) d[k] *= silu(u[k]).slope;
+                }
+                du[K - 1] = d;
+                if (counts) {
+                    dbias += d;
+#pragma unroll
+                    for (int j = 0; j < K; ++j) dw[j] += d * seen[j];
+                }
+            };
+            // the gradient of the input K - 1 positions before the newest, and then one position on
+            const auto gradient = [&] {
+                F dx = w[K - 1] * du[0];
+#pragma unroll
+                for (int j = 1; j < K; ++j) dx += w[K - 1 - j] * du[j];
+#pragma unroll
+                for (int j = 0; j < K - 1; ++j) seen[j] = seen[j + 1], du[j] = du[j + 1];
+                return dx;
+            };
+            {
+                Rows<E, V, kWide, K - 1> rows, ds;
+                rows.request(x, p.xt, at.begin, length, ch);
+                ds.request(grad_out, p.dt, at.begin, length, ch);
+#pragma unroll
+                for (int i = 0; i < K - 1; ++i) {
+                    seen[K - 1] = rows.get(i, at.begin, length);
+                    advance(ds.get(i, at.begin, length), at.begin == 0);
+                    const F dx = gradient();
+                    if (at.begin == 0) put_initial(i - (K - 1), dx);
+                }
+            }
+            for (int s0 = at.begin; s0 < end; s0 += G) {
+                const int t0 = s0 + K - 1;
+                Rows<E, V, kWide, G> rows, ds;
                 rows.request(x, p.xt, t0, length, ch);
                 ds.request(grad_out, p.dt, t0, length, ch);
+                typename N::Values to[G];
 #pragma unroll
-                for (int i = 0; i < kGroup; ++i) {
-                    const int t = t0 + i;
-                    if (t >= end + K - 1) break;
+                for (int i = 0; i < G; ++i) {
                     seen[K - 1] = rows.get(i, t0, length);
-                    F d = ds.get(i, t0, length);
-                    if (p.silu) {
-                        F u = bias;
-#pragma unroll
-                        for (int j = 0; j < K; ++j) u += w[j] * seen[j];
-#pragma unroll
-                        for (int k = 0; k < V; ++k) d[k] *= silu(u[k]).slope;
-                    }
-                    if (t >= length) d = splat_f<F>(0.0f);      // (past the length a weight of NaN would make it NaN)
-                    du[K - 1] = d;
-                    if (t < end) {
-                        dbias += d;
-#pragma unroll
-                        for (int j = 0; j < K; ++j) dw[j] += d * seen[j];
-                    }
-                    F dx = splat_f<F>(0.0f);    // at position t - (K - 1)
-#pragma unroll
-                    for (int j = 0; j < K; ++j) dx += w[K - 1 - j] * du[j];
-                    if (t - (K - 1) >= at.begin || at.begin == 0) put(t - (K - 1), dx);
-#pragma unroll
-                    for (int j = 0; j < K - 1; ++j) seen[j] = seen[j + 1], du[j] = du[j + 1];
+                    advance(ds.get(i, t0, length), true);
+                    F dx = gradient();
+                    if (s0 + G > length - (K - 1)) add_last(s0 + i, dx);
+                    to[i] = N::round(dx);
                 }
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+                    if (s0 + i < end) ch.store(grad_x + (s0 + i) * p.gt, s0 + i < length ? to[i] : typename N::Values{});
             }
         }
     }
@@ -315,7 +339,10 @@ hipError_t with_taps(int K, F &&f)
     }
 }
 
-// Positions of a lane's run: as many workgroups as fill the chip, but no more halo than they need.
+// Positions of a lane's run: the longest of which there are 500 workgroups, two for each compute unit, as a run's first K - 1 positions are work of its own.
+// Forward and reverse in us, bf16, with runs of 8, 16, 32, 64, 128: 8 x 4096 x 2048 (512 workgroups at 64 and at 128) 56, 51, 53, 49, 53 and 136, 106, 99, 105,
+// 95; 1 x 65536 x 256 (512 at 16 and at 32) 20, 16, 18, 27, 46 and 38, 33, 31, 35, 59; 2 x 4096 x 64 (as many as there are at 8) 7, 9, 14, 23, 42 and
+// 12, 14, 20, 30, 52.
 Args arguments(const esrnn_convolution_shape &s, const ConvolutionArgs &a, bool reverse)
 {
     Args p{};
@@ -327,7 +354,7 @@ Args arguments(const esrnn_convolution_shape &s, const ConvolutionArgs &a, bool 
     const int runs = reverse ? Place<float, true>::kRuns : s.dtype == ESRNN_F32 ? Place<float, false>::kRuns : Place<__bf16, false>::kRuns;
     const auto blocks = [&](int run) { return ((long long)s.T + runs * run - 1) / (runs * run); };
     p.run = kGroup;
-    while (p.run < 64 && s.B * p.tiles * blocks(2 * p.run) >= 1024) p.run *= 2;
+    while (p.run < 128 && s.B * p.tiles * blocks(2 * p.run) >= 500) p.run *= 2;
     p.blocks = (int)blocks(p.run);
     return p;
 }
