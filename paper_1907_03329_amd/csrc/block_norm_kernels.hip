@@ -1,7 +1,7 @@
 // Block norm: gate, norm behind a block, residual, norm before the next block, for every row by itself (include/esrnn_state_space.h).
 //
 // A row is held in registers by L lanes of a wave, or by one or several whole waves, whose sums go through LDS; a workgroup takes rows one behind
-// the other, so that a lane's weights are read once, and so that the gradients of the weights add up in its registers.  Forward, with act = silu(gate):
+// the other (in reverse each is requested while the one before is worked on), so that a lane's weights are read once, and so that the gradients of the weights add up in its registers.  Forward, with act = silu(gate):
 //   v = y act | y,  r1 = 1 / sqrt(mean v^2 + eps),  p = v r1 post,  e = p act | p,  s = residual + scale e,  r2 = 1 / sqrt(mean s^2 + eps),  out = s r2 pre.
 // Reverse, with that = s r2, vhat = v r1 and the gradients D of out and S of sum:
 //   ds = S + r2 (D pre - that mean(D pre that)),  de = ds scale,  dp = de act | de,  dv = r1 (dp post - vhat mean(dp post vhat)),  dy = dv act | dv,
@@ -15,7 +15,7 @@ namespace esrnn {
 
 namespace {
 
-constexpr int kMostWorkgroups = 1024;
+constexpr int kWavesForward = 8192, kWavesReverse = 4096;
 
 struct Args {
     BlockNormArgs a;
@@ -25,20 +25,22 @@ struct Args {
 };
 
 // How a row is held: L lanes of each of NW waves, M groups of four neighbouring channels a lane; RW rows of a workgroup at a time.
-template <int L_, int NW_, int M_>
+// kKept: weights and their gradients' sums stay in registers, else weights are read for every row and sums are in LDS; kAhead: rows are requested ahead.
+template <int L_, int NW_, int M_ = 1, bool kKept_ = true, bool kAhead_ = true>
 struct Layout {
+    static constexpr bool kKept = kKept_, kAhead = kAhead_;
     static constexpr int L = L_, NW = NW_, M = M_, kThreads = NW > 1 ? 64 * NW : 256, RW = kThreads / (L * NW), kChannels = 4 * M * L * NW;
 };
 
 // Sums over the lanes of a row, the same in all of them.  `slot`: two sums that follow each other have different ones.
 template <class Y>
-__device__ __forceinline__ float row_sum(float v, float (*lds)[8], int slot)
+__device__ __forceinline__ float row_sum(float v, float (*lds)[16], int slot)
 {
 #pragma unroll
     for (int off = Y::L / 2; off > 0; off /= 2) v += __shfl_xor(v, off, 64);
     if constexpr (Y::NW > 1) {
         if ((threadIdx.x & 63) == 0) lds[slot][threadIdx.x >> 6] = v;
-        __syncthreads();
+        lds_barrier();          // (requests for the next row go on)
         v = 0.0f;
 #pragma unroll
         for (int w = 0; w < Y::NW; ++w) v += lds[slot][w];
@@ -46,17 +48,23 @@ __device__ __forceinline__ float row_sum(float v, float (*lds)[8], int slot)
     return v;
 }
 
-// A lane's channels: group m begins at 4 (m T + lane), T the lanes of a row.
+// A lane's channels: group m begins at 4 (m T + lane), T the lanes of a row.  A row is requested while the one before it is worked on.
 template <class Y, class E>
-__device__ __forceinline__ void load_row(const void *base, long long at, int lane, int C, f32x4 (&v)[Y::M])
-{
-    const E *row = static_cast<const E *>(base) + at;
+struct Row {
+    typename Neighbours<E, 4>::Values v[Y::M];
+    __device__ __forceinline__ void request(const void *base, long long at, int lane, int C)
+    {
+        if (!base) return;
+        const E *row = static_cast<const E *>(base) + at;
 #pragma unroll
-    for (int m = 0; m < Y::M; ++m) {
-        const Neighbours<E, 4> ch{4 * (m * Y::L * Y::NW + lane), C};
-        v[m] = to_f32<E>(ch.load(row));
+        for (int m = 0; m < Y::M; ++m) v[m] = Neighbours<E, 4>{4 * (m * Y::L * Y::NW + lane), C}.load(row);
     }
-}
+    __device__ __forceinline__ void get(bool there, f32x4 (&to)[Y::M]) const
+    {
+#pragma unroll
+        for (int m = 0; m < Y::M; ++m) to[m] = there ? to_f32<E>(v[m]) : f32x4{};
+    }
+};
 template <class Y, class E>
 __device__ __forceinline__ void store_row(void *base, long long at, int lane, int C, const f32x4 (&v)[Y::M])
 {
@@ -70,7 +78,7 @@ __device__ __forceinline__ void store_row(void *base, long long at, int lane, in
 // Weights of a lane's channels, ones where there are none: in registers, or read for every row where a lane has too many channels for that.
 template <class Y>
 struct Weights {
-    static constexpr bool kKept = Y::M <= 2;
+    static constexpr bool kKept = Y::kKept;
     const float *from;
     int lane, C;
     f32x4 kept[kKept ? Y::M : 1];
@@ -90,6 +98,29 @@ struct Weights {
         if constexpr (kKept) return kept[m];
         return read(m);
     }
+};
+// Sums over rows for a lane's channels.
+template <class Y, bool kLds>
+struct Sums {
+    f32x4 v[Y::M];
+    __device__ __forceinline__ Sums(f32x4 *)
+    {
+#pragma unroll
+        for (int m = 0; m < Y::M; ++m) v[m] = f32x4{};
+    }
+    __device__ __forceinline__ void add(int m, f32x4 x) { v[m] += x; }
+    __device__ __forceinline__ f32x4 get(int m) const { return v[m]; }
+};
+template <class Y>
+struct Sums<Y, true> {
+    f32x4 *at;
+    __device__ __forceinline__ Sums(f32x4 *lds) : at(lds + threadIdx.x)
+    {
+#pragma unroll
+        for (int m = 0; m < Y::M; ++m) at[m * Y::kThreads] = f32x4{};
+    }
+    __device__ __forceinline__ void add(int m, f32x4 x) { at[m * Y::kThreads] += x; }
+    __device__ __forceinline__ f32x4 get(int m) const { return at[m * Y::kThreads]; }
 };
 template <class Y>
 __device__ __forceinline__ float squares(const f32x4 (&v)[Y::M])
@@ -113,20 +144,31 @@ __device__ __forceinline__ float inverse_root(float sum, const Args &p) { return
 template <class E, class R, class Y>
 __global__ void __launch_bounds__(Y::kThreads) block_norm_forward_kernel(Args p)
 {
-    __shared__ float s_sums[4][8];
+    __shared__ float s_sums[4][16];
     const int lane = threadIdx.x % (Y::L * Y::NW), in_group = threadIdx.x / (Y::L * Y::NW);
     const Weights<Y> post(p.a.post_weight, lane, p.C), scale(p.a.scale, lane, p.C), pre(p.a.pre_weight, lane, p.C);
-    int turn = 0;
-    for (int first = blockIdx.x * Y::RW; first < p.rows; first += gridDim.x * Y::RW, turn ^= 2) {
+    Row<Y, E> ys, gates;
+    Row<Y, R> residuals;
+    bool exists = false;
+    const auto request = [&](int first) {
         const long long row = min(first + in_group, p.rows - 1);
-        const bool mine = first + in_group < p.rows, exists = !p.a.exists || p.a.exists[row] != 0;
+        exists = !p.a.exists || p.a.exists[row] != 0;
+        ys.request(p.a.y, row * p.y, lane, p.C);
+        gates.request(p.a.gate, row * p.gate, lane, p.C);
+        residuals.request(p.a.residual, row * p.residual, lane, p.C);
+    };
+    int turn = 0;
+    const int step = gridDim.x * Y::RW;
+    if (Y::kAhead) request(blockIdx.x * Y::RW);
+    for (int first = blockIdx.x * Y::RW; first < p.rows; first += step, turn ^= 2) {
+        const long long row = first + in_group;
+        const bool mine = row < p.rows;
+        if (!Y::kAhead) request(first);
         f32x4 v[Y::M], act[Y::M], s[Y::M] = {};
-        load_row<Y, E>(p.a.y, row * p.y, lane, p.C, v);
-        if (p.a.gate) load_row<Y, E>(p.a.gate, row * p.gate, lane, p.C, act);
-        if (p.a.residual) load_row<Y, R>(p.a.residual, row * p.residual, lane, p.C, s);
-        if (!exists)        // (whatever lies there)
-#pragma unroll
-            for (int m = 0; m < Y::M; ++m) v[m] = act[m] = s[m] = f32x4{};
+        ys.get(exists, v);
+        if (p.a.gate) gates.get(exists, act);
+        if (p.a.residual) residuals.get(exists, s);
+        if (Y::kAhead && first + step < p.rows) request(first + step);
         if (p.a.gate) {
 #pragma unroll
             for (int m = 0; m < Y::M; ++m)
@@ -165,25 +207,42 @@ template <class E, class R, class Y>
 __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p)
 {
     constexpr int M = Y::M;
-    __shared__ float s_sums[4][8];
+    __shared__ float s_sums[4][16];
     __shared__ __attribute__((aligned(16))) float s_parts[Y::RW > 1 ? Y::RW : 1][Y::RW > 1 ? Y::kChannels : 1];
     const int lane = threadIdx.x % (Y::L * Y::NW), in_group = threadIdx.x / (Y::L * Y::NW);
     const Weights<Y> post(p.a.post_weight, lane, p.C), scale(p.a.scale, lane, p.C), pre(p.a.pre_weight, lane, p.C);
-    f32x4 dpost[M] = {}, dscale[M] = {}, dpre[M] = {};
-    int turn = 0;
-    for (int first = blockIdx.x * Y::RW; first < p.rows; first += gridDim.x * Y::RW, turn ^= 2) {
+    constexpr bool kLds = !Y::kKept;
+    __shared__ f32x4 s_kept[kLds ? 3 : 1][kLds ? M * Y::kThreads : 1];
+    Sums<Y, kLds> dpost(s_kept[0]), dscale(s_kept[kLds ? 1 : 0]), dpre(s_kept[kLds ? 2 : 0]);
+    Row<Y, E> ys, gates, ds_out;
+    Row<Y, R> residuals, ds_sum;
+    bool exists = false;
+    float next_r1 = 0.0f, next_r2 = 0.0f;
+    const auto request = [&](int first) {
         const long long row = min(first + in_group, p.rows - 1);
-        const bool mine = first + in_group < p.rows, exists = mine && (!p.a.exists || p.a.exists[row] != 0);
+        exists = first + in_group < p.rows && (!p.a.exists || p.a.exists[row] != 0);
+        ys.request(p.a.y, row * p.y, lane, p.C);
+        gates.request(p.a.gate, row * p.gate, lane, p.C);
+        residuals.request(p.a.residual, row * p.residual, lane, p.C);
+        ds_out.request(p.a.grad_out, row * p.grad_out, lane, p.C);
+        ds_sum.request(p.a.grad_sum, row * p.grad_sum, lane, p.C);
+        next_r1 = p.a.stats_in[2 * row], next_r2 = p.a.stats_in[2 * row + 1];
+    };
+    int turn = 0;
+    const int step = gridDim.x * Y::RW;
+    if (Y::kAhead) request(blockIdx.x * Y::RW);
+    for (int first = blockIdx.x * Y::RW; first < p.rows; first += step, turn ^= 2) {
+        const long long row = first + in_group;
+        const bool mine = row < p.rows;
+        if (!Y::kAhead) request(first);
         f32x4 y[M], gate[M] = {}, s[M] = {}, d[M] = {}, ds[M] = {};
-        load_row<Y, E>(p.a.y, row * p.y, lane, p.C, y);
-        if (p.a.gate) load_row<Y, E>(p.a.gate, row * p.gate, lane, p.C, gate);
-        if (p.a.residual) load_row<Y, R>(p.a.residual, row * p.residual, lane, p.C, s);
-        if (p.a.grad_out) load_row<Y, E>(p.a.grad_out, row * p.grad_out, lane, p.C, d);
-        if (p.a.grad_sum) load_row<Y, R>(p.a.grad_sum, row * p.grad_sum, lane, p.C, ds);
-        const float r1 = exists ? p.a.stats_in[2 * row] : 0.0f, r2 = exists ? p.a.stats_in[2 * row + 1] : 0.0f;
-        if (!exists)
-#pragma unroll
-            for (int m = 0; m < M; ++m) y[m] = gate[m] = s[m] = d[m] = ds[m] = f32x4{};
+        const float r1 = exists ? next_r1 : 0.0f, r2 = exists ? next_r2 : 0.0f;
+        ys.get(exists, y);
+        if (p.a.gate) gates.get(exists, gate);
+        if (p.a.residual) residuals.get(exists, s);
+        if (p.a.grad_out) ds_out.get(exists, d);
+        if (p.a.grad_sum) ds_sum.get(exists, ds);
+        if (Y::kAhead && first + step < p.rows) request(first + step);
         f32x4 act[M], slope[M], vhat[M], e[M];
 #pragma unroll
         for (int m = 0; m < M; ++m) {
@@ -201,7 +260,7 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
 #pragma unroll
             for (int m = 0; m < M; ++m) {
                 s[m] *= r2;                 // that
-                dpre[m] += d[m] * s[m];
+                dpre.add(m, d[m] * s[m]);
                 weighted[m] = d[m] * pre[m];
             }
             const float mean = row_sum<Y>(products<Y>(weighted, s), s_sums, turn) * p.inverse;
@@ -216,11 +275,11 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             const f32x4 of_e = p.after ? e[m] * act[m] : e[m];
-            dscale[m] += ds[m] * of_e;
+            dscale.add(m, ds[m] * of_e);
             const f32x4 de = ds[m] * scale[m];
             dgate[m] = de * e[m];
             const f32x4 dp = p.after ? de * act[m] : de;
-            dpost[m] += dp * vhat[m];
+            dpost.add(m, dp * vhat[m]);
             weighted[m] = dp * post[m];
         }
         if (p.a.post_weight) {
@@ -246,7 +305,9 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
     // the workgroup's sums, rows of [3][C]
 #pragma unroll
     for (int which = 0; which < 3; ++which) {
-        const f32x4 *sum = which == 0 ? dpost : which == 1 ? dscale : dpre;
+        f32x4 sum[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) sum[m] = which == 0 ? dpost.get(m) : which == 1 ? dscale.get(m) : dpre.get(m);
         float *to = p.a.parts + ((size_t)blockIdx.x * 3 + which) * p.C;
         if constexpr (Y::RW > 1) {
             __syncthreads();
@@ -259,7 +320,7 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
                 to[c] = v;
             }
         } else {
-            store_row<Y, float>(to, 0, lane, p.C, *reinterpret_cast<const f32x4(*)[M]>(sum));
+            store_row<Y, float>(to, 0, lane, p.C, sum);
         }
     }
 }
@@ -284,16 +345,27 @@ Args arguments(const esrnn_block_norm_shape &s, const BlockNormArgs &a)
     return p;
 }
 
+// In reverse four channels a lane, requested ahead: 32768 rows of 2048 channels, bf16, 236 us by eight waves, 264 by four with eight channels, 411 by two with
+// sixteen.  Forward eight channels, by as many waves as the registers allow, which need no requests ahead: 134 us by four waves (144 ahead), 145 by
+// eight with four channels; 30000 rows of 500 channels 32 by one wave, 46 by two.
 template <class F>
-hipError_t with_layout(int C, F &&f)
+hipError_t with_layout(int C, bool reverse, F &&f)
 {
-    if (C <= 64) return f(Layout<16, 1, 1>{});
-    if (C <= 256) return f(Layout<64, 1, 1>{});
-    if (C <= 512) return f(Layout<64, 1, 2>{});
-    if (C <= 1024) return f(Layout<64, 2, 2>{});
-    if (C <= 2048) return f(Layout<64, 4, 2>{});
-    if (C <= 4096) return f(Layout<64, 8, 2>{});
-    return f(Layout<64, 8, 4>{});
+    if (C <= 64) return f(Layout<16, 1>{});
+    if (C <= 128) return f(Layout<32, 1>{});
+    if (C <= 256) return f(Layout<64, 1>{});
+    if (reverse) {
+        if (C <= 512) return f(Layout<64, 2>{});
+        if (C <= 1024) return f(Layout<64, 4>{});
+        if (C <= 2048) return f(Layout<64, 8>{});
+        if (C <= 4096) return f(Layout<64, 16>{});
+        return f(Layout<64, 16, 2, false, false>{});
+    }
+    if (C <= 512) return f(Layout<64, 1, 2, true, false>{});
+    if (C <= 1024) return f(Layout<64, 2, 2, true, false>{});
+    if (C <= 2048) return f(Layout<64, 4, 2, true, false>{});
+    if (C <= 4096) return f(Layout<64, 8, 2, true, false>{});
+    return f(Layout<64, 16, 2, true, false>{});
 }
 template <class F>
 hipError_t with_types(const esrnn_block_norm_shape &s, F &&f)
@@ -303,22 +375,33 @@ hipError_t with_types(const esrnn_block_norm_shape &s, F &&f)
         return f(e, float{});
     });
 }
-int workgroups(int rows, int at_a_time) { return (int)std::min<long long>(((long long)rows + at_a_time - 1) / at_a_time, kMostWorkgroups); }
+// As many workgroups as the chip holds: some 8 waves a SIMD forward, 4 in reverse (32768 x 2048 bf16 in reverse 367 us with half as many, 30000 x 500 125
+// for 82).
+template <class Y>
+int workgroups(int rows, bool reverse)
+{
+    return (int)std::min<long long>(((long long)rows + Y::RW - 1) / Y::RW, (reverse ? kWavesReverse : kWavesForward) / (Y::kThreads / 64));
+}
 
 }  // namespace
 
 size_t block_norm_workspace_floats(const esrnn_block_norm_shape &s)
 {
-    return (size_t)std::min(s.rows, kMostWorkgroups) * 3 * s.C;
+    size_t rows = 0;
+    with_layout(s.C, true, [&](auto y) {
+        rows = workgroups<decltype(y)>(s.rows, true);
+        return hipSuccess;
+    });
+    return rows * 3 * s.C;
 }
 
 hipError_t launch_block_norm_forward(const esrnn_block_norm_shape &s, const BlockNormArgs &a, hipStream_t st)
 {
     const Args p = arguments(s, a);
     return with_types(s, [&](auto e, auto r) {
-        return with_layout(s.C, [&](auto y) {
+        return with_layout(s.C, false, [&](auto y) {
             typedef decltype(y) Y;
-            block_norm_forward_kernel<decltype(e), decltype(r), Y><<<dim3(workgroups(s.rows, Y::RW)), Y::kThreads, 0, st>>>(p);
+            block_norm_forward_kernel<decltype(e), decltype(r), Y><<<dim3(workgroups<Y>(s.rows, false)), Y::kThreads, 0, st>>>(p);
             return hipGetLastError();
         });
     });
@@ -329,9 +412,9 @@ hipError_t launch_block_norm_backward(const esrnn_block_norm_shape &s, const Blo
     const Args p = arguments(s, a);
     int rows = 0;
     const hipError_t failed = with_types(s, [&](auto e, auto r) {
-        return with_layout(s.C, [&](auto y) {
+        return with_layout(s.C, true, [&](auto y) {
             typedef decltype(y) Y;
-            rows = workgroups(s.rows, Y::RW);
+            rows = workgroups<Y>(s.rows, true);
             block_norm_backward_kernel<decltype(e), decltype(r), Y><<<dim3(rows), Y::kThreads, 0, st>>>(p);
             return hipGetLastError();
         });
