@@ -325,9 +325,10 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
     }
 }
 
+template <int kCols>
 __global__ void __launch_bounds__(1024) block_norm_sum_kernel(const float *__restrict__ parts, int rows, int C, float *grad_post, float *grad_scale, float *grad_pre)
 {
-    sum_columns<kSumColumns>(parts, rows, 3ll * C, (long long)blockIdx.x * kSumColumns, [&](long long col, float v) {
+    sum_columns<kCols>(parts, rows, 3ll * C, (long long)blockIdx.x * kCols, [&](long long col, float v) {
         float *to = col < C ? grad_post : col < 2ll * C ? grad_scale : grad_pre;
         if (to) to[col % C] = v;
     });
@@ -420,8 +421,11 @@ hipError_t launch_block_norm_backward(const esrnn_block_norm_shape &s, const Blo
         });
     });
     if (failed != hipSuccess || !(a.grad_post_weight || a.grad_scale || a.grad_pre_weight)) return failed;
-    block_norm_sum_kernel<<<dim3((3 * s.C + kSumColumns - 1) / kSumColumns), 1024, 0, st>>>(a.parts, rows, s.C, a.grad_post_weight, a.grad_scale, a.grad_pre_weight);
-    return hipGetLastError();
+    return with_columns(3ll * s.C, [&](auto cols) {
+        constexpr int kCols = decltype(cols)::value;
+        block_norm_sum_kernel<kCols><<<dim3((3 * s.C + kCols - 1) / kCols), 1024, 0, st>>>(a.parts, rows, s.C, a.grad_post_weight, a.grad_scale, a.grad_pre_weight);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace esrnn

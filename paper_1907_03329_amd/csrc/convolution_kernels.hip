@@ -278,10 +278,11 @@ __global__ void __launch_bounds__(kThreads, K <= 4 ? 3 : 2) convolution_backward
 }
 
 // Rows of partial sums: [tile][K + 1][64] each.
+template <int kCols>
 __global__ void __launch_bounds__(1024) convolution_sum_kernel(const float *__restrict__ parts, long long rows, int tiles, int K, int C, float *grad_weight,
                                                                float *grad_bias)
 {
-    sum_columns<kSumColumns>(parts, rows, (long long)tiles * (K + 1) * kTile, (long long)blockIdx.x * kSumColumns, [&](long long col, float v) {
+    sum_columns<kCols>(parts, rows, (long long)tiles * (K + 1) * kTile, (long long)blockIdx.x * kCols, [&](long long col, float v) {
         const int j = (int)(col / kTile) % (K + 1), c = (int)(col / ((K + 1) * kTile)) * kTile + (int)(col % kTile);
         if (c >= C) return;
         if (j < K) grad_weight[(long long)c * K + j] = v;
@@ -354,7 +355,7 @@ Args arguments(const esrnn_convolution_shape &s, const ConvolutionArgs &a, bool 
     const int runs = reverse ? Place<float, true>::kRuns : s.dtype == ESRNN_F32 ? Place<float, false>::kRuns : Place<__bf16, false>::kRuns;
     const auto blocks = [&](int run) { return ((long long)s.T + runs * run - 1) / (runs * run); };
     p.run = kGroup;
-    while (p.run < 128 && s.B * p.tiles * blocks(2 * p.run) >= 500) p.run *= 2;
+    while (p.run < 128 && runs * p.run < s.T && s.B * p.tiles * blocks(2 * p.run) >= 500) p.run *= 2;
     p.blocks = (int)blocks(p.run);
     return p;
 }
@@ -396,8 +397,12 @@ hipError_t launch_convolution_backward(const esrnn_convolution_shape &s, const C
         return hipGetLastError();
     });
     if (failed != hipSuccess) return failed;
-    convolution_sum_kernel<<<dim3(p.tiles * (s.K + 1) * (kTile / kSumColumns)), 1024, 0, st>>>(a.parts, (long long)p.B * p.blocks, p.tiles, s.K, s.C, a.grad_weight, a.grad_bias);
-    return hipGetLastError();
+    return with_columns((long long)p.tiles * (s.K + 1) * kTile, [&](auto cols) {
+        constexpr int kCols = decltype(cols)::value;
+        convolution_sum_kernel<kCols><<<dim3(p.tiles * (s.K + 1) * (kTile / kCols)), 1024, 0, st>>>(a.parts, (long long)p.B * p.blocks, p.tiles, s.K, s.C,
+                                                                                                 a.grad_weight, a.grad_bias);
+        return hipGetLastError();
+    });
 }
 
 hipError_t launch_convolution_step(const esrnn_convolution_step_shape &s, const void *x, const float *weight, const float *bias, const int32_t *slots,

@@ -242,15 +242,15 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
 
 // The sums over segments of the gradients of A, D and bias (the first workgroups; rows of [tile][slice][states + 2][64]) and those over tiles of the
 // gradients of b and c (the others; [tile][position][group][2][padded]).
-constexpr int kSumElements = 4096;      // of a workgroup, about: whole positions
-template <class E>
+constexpr int kSumWorkgroups = 768;     // about, each with neighbouring positions of a sequence
+template <class E, int kCols>
 __global__ void __launch_bounds__(1024) selective_sum_kernel(Scan k, int states, int slices, unsigned first_rows, int positions, E *grad_b, E *grad_c,
                                                              long long gbb, long long gbt, long long gcb, long long gct)
 {
     if (blockIdx.x < first_rows) {
         const int wave = (states + 2) * 64;
         const long long cols = (long long)k.G * k.tiles * slices * wave, rows = (long long)k.B * k.segments;
-        sum_columns<kSumColumns>(k.part_sums, rows, cols, (long long)blockIdx.x * kSumColumns, [&](long long col, float v) {
+        sum_columns<kCols>(k.part_sums, rows, cols, (long long)blockIdx.x * kCols, [&](long long col, float v) {
             const int lane = col % 64, n = (int)(col / 64) % (states + 2), slice = (int)(col / wave) % slices, tile = (int)(col / wave / slices);
             const int in_group = tile % k.tiles * 64 + lane, channel = tile / k.tiles * k.group_channels + in_group;
             if (in_group >= k.group_channels) return;
@@ -276,9 +276,12 @@ __global__ void __launch_bounds__(1024) selective_sum_kernel(Scan k, int states,
     for (unsigned i = threadIdx.x; i < min(positions, k.T - t0) * width; i += 1024) {
         const unsigned t = t0 + i / width, within = i % width, n = within % padded, group = within / (2 * padded);
         if (n >= (unsigned)k.N) continue;
-        float v = 0.0f;
-        if (t < (unsigned)length)
-            for (int q = 0; q < k.tiles; ++q) v += from[q * tile_apart + i];
+        float v = t < (unsigned)length ? from[i] : 0.0f;
+        if (t < (unsigned)length && k.tiles > 1) {
+            const float *tile = from + i;
+#pragma unroll 8
+            for (int q = 1; q < k.tiles; ++q) v += *(tile += tile_apart);
+        }
         (within / padded & 1 ? grad_c + t * gct : grad_b + t * gbt)[group * k.N + n] = (E)v;
     }
 }
@@ -303,14 +306,18 @@ hipError_t launch_selective_backward(const esrnn_selective_shape &s, const Selec
         return hipGetLastError();
     });
     if (failed != hipSuccess) return failed;
-    const unsigned columns = (unsigned)(s.G * p.tiles * p.slices * (p.states + 2) * (64 / kSumColumns));
-    const int positions = std::max(1, kSumElements / (s.G * 2 * p.padded));
+    const long long columns = (long long)s.G * p.tiles * p.slices * (p.states + 2) * 64;
+    const int positions = (int)(((long long)s.B * s.T + kSumWorkgroups - 1) / kSumWorkgroups);
     const unsigned runs = (unsigned)s.B * ((s.T + positions - 1) / positions);
     return with_element(s.dtype, [&](auto e) {
-        typedef decltype(e) E;
-        selective_sum_kernel<E><<<dim3(columns + runs), 1024, 0, st>>>(k, p.states, p.slices, columns, positions, static_cast<E *>(a.grad_b), static_cast<E *>(a.grad_c),
-                                                                       s.grad_b_stride[0], s.grad_b_stride[1], s.grad_c_stride[0], s.grad_c_stride[1]);
-        return hipGetLastError();
+        return with_columns(columns, [&](auto cols) {
+            typedef decltype(e) E;
+            constexpr int kCols = decltype(cols)::value;
+            const unsigned first = (unsigned)(columns / kCols);
+            selective_sum_kernel<E, kCols><<<dim3(first + runs), 1024, 0, st>>>(k, p.states, p.slices, first, positions, static_cast<E *>(a.grad_b), static_cast<E *>(a.grad_c),
+                                                                              s.grad_b_stride[0], s.grad_b_stride[1], s.grad_c_stride[0], s.grad_c_stride[1]);
+            return hipGetLastError();
+        });
     });
 }
 

@@ -79,8 +79,8 @@ struct Overlapping {
 };
 
 // Sums of `rows` rows of `cols` partial results, in a fixed order, for kCols columns from `first` on: by a workgroup of 1024 threads, 1024 / kCols rows at
-// a time; store(column, sum) by the threads of the first row.  Few columns need narrow workgroups to be many: 1024 rows of 150 columns take 3.9 us by 16
-// columns and 9.3 by 64.
+// a time; store(column, sum) by the threads of the first row.  Few columns need narrow workgroups to be many, many columns whole cache lines: 1024 rows of 150
+// columns 3.9 us by 16 columns and 9.3 by 64, 512 rows of 6144 columns 20 us by 16 and 14 by 64.
 template <int kCols, class F>
 __device__ __forceinline__ void sum_columns(const float *__restrict__ parts, long long rows, long long cols, long long first, F &&store)
 {
@@ -88,15 +88,20 @@ __device__ __forceinline__ void sum_columns(const float *__restrict__ parts, lon
     __shared__ float s_sum[kRows][kCols];
     const int lane = threadIdx.x % kCols, row = threadIdx.x / kCols;
     const long long col = first + lane;
-    float v[4] = {};
+    constexpr int kBatch = 8;       // loads under way
+    float v[kBatch] = {};
     if (col < cols) {
         long long r = row;
-        for (; r + 3 * kRows < rows; r += 4 * kRows)
+        for (; r + (kBatch - 1) * kRows < rows; r += kBatch * kRows)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] += parts[(r + kRows * k) * cols + col];
+            for (int k = 0; k < kBatch; ++k) v[k] += parts[(r + kRows * k) * cols + col];
         for (; r < rows; r += kRows) v[0] += parts[r * cols + col];
     }
-    s_sum[row][lane] = (v[0] + v[1]) + (v[2] + v[3]);
+#pragma unroll
+    for (int half = kBatch / 2; half > 0; half /= 2)
+#pragma unroll
+        for (int k = 0; k < half; ++k) v[k] += v[k + half];
+    s_sum[row][lane] = v[0];
     __syncthreads();
 #pragma unroll
     for (int half = kRows / 2; half > 0; half /= 2) {
@@ -105,7 +110,14 @@ __device__ __forceinline__ void sum_columns(const float *__restrict__ parts, lon
     }
     if (row == 0 && col < cols) store(col, s_sum[0][lane]);
 }
-constexpr int kSumColumns = 16;
+// f(std::integral_constant<int, kCols>)
+template <class F>
+hipError_t with_columns(long long cols, F &&f)
+{
+    if (cols >= 6000) return f(std::integral_constant<int, 64>{});
+    if (cols >= 2048) return f(std::integral_constant<int, 32>{});
+    return f(std::integral_constant<int, 16>{});
+}
 
 // softplus(v) = max(v, 0) + log(1 + exp(-|v|)) and its derivative sigmoid(v).  Of w = 1 + e, rounded, log(1 + e) = log(w) + (e - (w - 1)) / (1 + ..),
 // where the second term is what the rounding has lost of e, without which small e would lose all digits; its divisor is left out, as the term is below 2^-24
