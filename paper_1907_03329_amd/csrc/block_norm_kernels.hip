@@ -349,24 +349,25 @@ Args arguments(const esrnn_block_norm_shape &s, const BlockNormArgs &a)
 // In reverse four channels a lane, requested ahead: 32768 rows of 2048 channels, bf16, 236 us by eight waves, 264 by four with eight channels, 411 by two with
 // sixteen.  Forward eight channels, by as many waves as the registers allow, which need no requests ahead: 134 us by four waves (144 ahead), 145 by
 // eight with four channels; 30000 rows of 500 channels 32 by one wave, 46 by two.
-template <class F>
-hipError_t with_layout(int C, bool reverse, F &&f)
+template <bool kReverse, class F>
+hipError_t with_layout(int C, F &&f)
 {
     if (C <= 64) return f(Layout<16, 1>{});
     if (C <= 128) return f(Layout<32, 1>{});
     if (C <= 256) return f(Layout<64, 1>{});
-    if (reverse) {
+    if constexpr (kReverse) {
         if (C <= 512) return f(Layout<64, 2>{});
         if (C <= 1024) return f(Layout<64, 4>{});
         if (C <= 2048) return f(Layout<64, 8>{});
         if (C <= 4096) return f(Layout<64, 16>{});
         return f(Layout<64, 16, 2, false, false>{});
+    } else {
+        if (C <= 512) return f(Layout<64, 1, 2, true, false>{});
+        if (C <= 1024) return f(Layout<64, 2, 2, true, false>{});
+        if (C <= 2048) return f(Layout<64, 4, 2, true, false>{});
+        if (C <= 4096) return f(Layout<64, 8, 2, true, false>{});
+        return f(Layout<64, 16, 2, true, false>{});
     }
-    if (C <= 512) return f(Layout<64, 1, 2, true, false>{});
-    if (C <= 1024) return f(Layout<64, 2, 2, true, false>{});
-    if (C <= 2048) return f(Layout<64, 4, 2, true, false>{});
-    if (C <= 4096) return f(Layout<64, 8, 2, true, false>{});
-    return f(Layout<64, 16, 2, true, false>{});
 }
 template <class F>
 hipError_t with_types(const esrnn_block_norm_shape &s, F &&f)
@@ -389,7 +390,7 @@ int workgroups(int rows, bool reverse)
 size_t block_norm_workspace_floats(const esrnn_block_norm_shape &s)
 {
     size_t rows = 0;
-    with_layout(s.C, true, [&](auto y) {
+    with_layout<true>(s.C, [&](auto y) {
         rows = workgroups<decltype(y)>(s.rows, true);
         return hipSuccess;
     });
@@ -400,7 +401,7 @@ hipError_t launch_block_norm_forward(const esrnn_block_norm_shape &s, const Bloc
 {
     const Args p = arguments(s, a);
     return with_types(s, [&](auto e, auto r) {
-        return with_layout(s.C, false, [&](auto y) {
+        return with_layout<false>(s.C, [&](auto y) {
             typedef decltype(y) Y;
             block_norm_forward_kernel<decltype(e), decltype(r), Y><<<dim3(workgroups<Y>(s.rows, false)), Y::kThreads, 0, st>>>(p);
             return hipGetLastError();
@@ -413,7 +414,7 @@ hipError_t launch_block_norm_backward(const esrnn_block_norm_shape &s, const Blo
     const Args p = arguments(s, a);
     int rows = 0;
     const hipError_t failed = with_types(s, [&](auto e, auto r) {
-        return with_layout(s.C, true, [&](auto y) {
+        return with_layout<true>(s.C, [&](auto y) {
             typedef decltype(y) Y;
             rows = workgroups<Y>(s.rows, true);
             block_norm_backward_kernel<decltype(e), decltype(r), Y><<<dim3(rows), Y::kThreads, 0, st>>>(p);

@@ -97,11 +97,7 @@ __device__ __forceinline__ void sum_columns(const float *__restrict__ parts, lon
             for (int k = 0; k < kBatch; ++k) v[k] += parts[(r + kRows * k) * cols + col];
         for (; r < rows; r += kRows) v[0] += parts[r * cols + col];
     }
-#pragma unroll
-    for (int half = kBatch / 2; half > 0; half /= 2)
-#pragma unroll
-        for (int k = 0; k < half; ++k) v[k] += v[k + half];
-    s_sum[row][lane] = v[0];
+    s_sum[row][lane] = ((v[0] + v[4]) + (v[2] + v[6])) + ((v[1] + v[5]) + (v[3] + v[7]));
     __syncthreads();
 #pragma unroll
     for (int half = kRows / 2; half > 0; half /= 2) {
