@@ -328,9 +328,14 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
 template <int kCols>
 __global__ void __launch_bounds__(1024) block_norm_sum_kernel(const float *__restrict__ parts, int rows, int C, float *grad_post, float *grad_scale, float *grad_pre)
 {
-    sum_columns<kCols>(parts, rows, 3ll * C, (long long)blockIdx.x * kCols, [&](long long col, float v) {
-        float *to = col < C ? grad_post : col < 2ll * C ? grad_scale : grad_pre;
-        if (to) to[col % C] = v;
+    sum_columns<kCols>(parts, rows, 3ll * C, (long long)blockIdx.x * kCols, [=](long long col, float v) {
+        if (col < C) {
+            if (grad_post) grad_post[col] = v;
+        } else if (col < 2ll * C) {
+            if (grad_scale) grad_scale[col - C] = v;
+        } else if (grad_pre) {
+            grad_pre[col - 2ll * C] = v;
+        }
     });
 }
 

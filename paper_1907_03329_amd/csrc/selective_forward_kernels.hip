@@ -108,6 +108,107 @@ __global__ void __launch_bounds__(64 * SL) selective_forward_kernel(Scan k)
     }
 }
 
+// A workgroup for a whole line: its waves have neighbouring pieces, whose step sizes stay in registers while the maps of all of them are put together through
+// LDS, four states by each of the first waves, who keep what enters the next block of pieces.
+template <class E, class BC, int NP, int kWaves>
+__global__ void __launch_bounds__(64 * kWaves) selective_line_kernel(Scan k)
+{
+    __shared__ f32x4 s_local[kWaves][NP / 4][64];
+    __shared__ float s_sum[kWaves][64];
+    ScanPlace at(k, 1);
+    const int lane = threadIdx.x & 63, wave = at.slice, waves = blockDim.x >> 6;
+    at.slice = 0;
+    const E *x = static_cast<const E *>(k.a.x) + at.b * k.xb, *delta = static_cast<const E *>(k.a.delta) + at.b * k.db;
+    E *out = static_cast<E *>(k.a.out) + at.b * k.ob;
+    const BC *b = static_cast<const BC *>(k.b) + at.b * k.bb + at.group * k.group, *c = static_cast<const BC *>(k.c) + at.b * k.cb + at.group * k.group;
+    const size_t own = ((size_t)at.b * k.C + at.channel) * k.N;
+    const bool composes = wave < NP / 4;
+
+    float A[NP];
+    load_own<NP>(k.a.A + (size_t)at.channel * k.N, 0, k.N, at.lane_mask, A);
+#pragma unroll
+    for (int n = 0; n < NP; ++n) A[n] *= kLog2e;
+    f32x4 rates = {}, carry = {};       // of states 4 wave ..
+    if (composes)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int n = 4 * wave + r;
+            const unsigned mask = n < k.N ? at.lane_mask : 0u;
+            rates[r] = masked(k.a.A[(size_t)at.channel * k.N + min(n, k.N - 1)], mask) * kLog2e;
+            if (k.a.initial) carry[r] = masked(k.a.initial[own + min(n, k.N - 1)], mask);
+        }
+    const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
+    for (int block = 0; block < at.length; block += waves * kPiece) {
+        const int t = fresh(block + wave * kPiece), left = at.length - 1 - t;
+        const bool active = left >= 0;
+        const BC *b0 = b + t * k.bt, *c0 = c + t * k.ct;
+        float d[kPiece], u[kPiece], y[kPiece], h[NP], sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < NP; ++n) h[n] = 0.0f;
+        if (active) {
+            Column<E> xs, ds;
+            xs.request(x, k.xt, t, at.length, at.channel);
+            ds.request(delta, k.dt, t, at.length, at.channel);
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) {
+                const float xi = (float)xs.v[i];
+                d[i] = masked(step_size(ds.v[i], bias, k.softplus).of, i <= left ? 0xffffffffu : 0u), u[i] = d[i] * xi, y[i] = D * xi;
+                sum += d[i];
+                float bs[NP];
+                load_shared<BC, NP>(b0, k.bt, i, left, bs);
+#pragma unroll
+                for (int n = 0; n < NP; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(d[i] * A[n]), h[n], u[i] * bs[n]);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < NP / 4; ++q) s_local[wave][q][lane] = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
+        s_sum[wave][lane] = sum;
+        lds_barrier();
+        if (composes) {
+#pragma unroll 4
+            for (int w = 0; w < waves; ++w) {
+                const f32x4 local = s_local[w][wave][lane];
+                const float total = s_sum[w][lane];
+                s_local[w][wave][lane] = carry;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) carry[r] = fmaf(__builtin_amdgcn_exp2f(total * rates[r]), carry[r], local[r]);
+            }
+        }
+        lds_barrier();
+        if (!active) continue;
+#pragma unroll
+        for (int q = 0; q < NP / 4; ++q) {
+            const f32x4 entering = s_local[wave][q][lane];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) h[4 * q + r] = entering[r];
+        }
+        if (k.a.saved) store_states<NP>(saved_of<NP, 1>(k, at, t / kPiece), h);
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+            float bs[NP], cs[NP];
+            load_shared<BC, NP>(b0, k.bt, i, left, bs);
+            load_shared<BC, NP>(c0, k.ct, i, left, cs);
+            float part[4] = {y[i], 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int n = 0; n < NP; ++n) {
+                h[n] = fmaf(__builtin_amdgcn_exp2f(d[i] * A[n]), h[n], u[i] * bs[n]);
+                part[n & 3] = fmaf(cs[n], h[n], part[n & 3]);
+            }
+            y[i] = (part[0] + part[1]) + (part[2] + part[3]);
+        }
+        complete(y);
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i)
+            if (t + i < k.T && at.lane_mask) (out + (t + i) * k.ot)[at.channel] = (E)(i <= left ? y[i] : 0.0f);
+    }
+    for (int t = (at.length + kPiece - 1) / kPiece * kPiece + wave; t < k.T; t += waves)
+        if (at.lane_mask) (out + t * k.ot)[at.channel] = (E)0.0f;
+    if (k.a.last && composes && at.lane_mask)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (4 * wave + r < k.N) k.a.last[own + 4 * wave + r] = carry[r];
+}
+
 // A wave has a run of neighbouring segments, in their order or against it, and four states of 64 channels: first the run's own map, then, behind those
 // of the runs before it, what enters each of its segments.
 constexpr int kRuns = 16;
@@ -215,10 +316,10 @@ constexpr int kSegmentsAlone = 32;
 // SIMD holds two waves, takes whole rounds of them, and leaves sums for every wave.  4 x 4096 x 2048 bf16: forward 371 us with 16 segments, 292 with 32, 278
 // with 40; reverse 633 with 16, 603 with 32, 701 with 24.  1 x 65536 x 256: forward 213 with 512, 198 with 1024, 210 with 1280; reverse 354 with 512, 371 with
 // 1024.  501 x 240 x 50 ragged fp32: forward 91 with 4, 87 with 8, 126 with 30; reverse 139 with 5, 169 with 8, 222 with 30.
-static int best_segments(long long lines, int pieces, bool reverse)
+static int best_segments(long long lines, int pieces, bool reverse, double &least)
 {
     int best = 1;
-    double least = 1e30;
+    least = 1e30;
     for (int segments = 1; segments <= pieces && (segments == 1 || lines * segments <= 16384); segments += std::max(1, segments / 32)) {
         const int span = (pieces + segments - 1) / segments, cut = (pieces + span - 1) / span;
         const double waves = lines * (double)cut / 1024.0, maps = waves * (cut - 1) / cut;      // of a SIMD
@@ -231,6 +332,8 @@ static int best_segments(long long lines, int pieces, bool reverse)
     return best;
 }
 
+constexpr int kLineWaves = 16;          // of a workgroup for a whole line
+
 SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse)
 {
     SelectivePlan p{};
@@ -240,7 +343,19 @@ SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse)
     p.tiles = (s.C / s.G + 63) / 64;
     p.pieces = (s.T + kPiece - 1) / kPiece;
     const long long lines = (long long)s.B * s.G * p.tiles * p.slices;
-    p.segments = best_segments(lines, p.pieces, reverse);
+    double cut;
+    p.segments = best_segments(lines, p.pieces, reverse, cut);
+    // A workgroup a line, in the same terms: 16 waves where every line has a compute unit of its own, else 8, two workgroups a compute unit.  In us, forward, cut /
+    // 16 waves / 8 waves: 8 x 1024 x 2048 bf16 (256 lines) 151, 122, 150; 501 x 240 x 50 ragged fp32 88, 75, 66; 200 x 72 x 40 fp32 32, 17, 17; 16 x 72 x 40 17,
+    // 16, 17; 2000 x 72 x 40 74, 118, 108; 4 x 300 x 256 bf16 (16 lines) 26, 42, 47.
+    p.line_waves = 0;
+    if (!reverse && p.slices == 1) {
+        const int most = lines <= 256 ? kLineWaves : kLineWaves / 2, blocks = (p.pieces + most - 1) / most;
+        const int waves = std::max((p.pieces + blocks - 1) / blocks, p.states / 4);
+        const double rounds = std::ceil(std::ceil(lines / 256.0) / 2);
+        const double line = lines <= 256 ? std::max(0.8 * p.pieces, 6.0 * blocks) : rounds * blocks * (1.6 * waves + 2.0);
+        if (line < cut) p.line_waves = waves, p.segments = 1;
+    }
     p.span = (p.pieces + p.segments - 1) / p.segments;
     p.segments = (p.pieces + p.span - 1) / p.span;
     p.carried = p.segments > kSegmentsAlone;
@@ -334,6 +449,11 @@ hipError_t launch_selective_forward(const esrnn_selective_shape &s, const Select
         typedef decltype(e) E;
         typedef decltype(bc) BC;
         constexpr int NP = decltype(states)::value, SL = decltype(slices)::value;
+        if constexpr (SL == 1)
+            if (p.line_waves) {
+                selective_line_kernel<E, BC, NP, kLineWaves><<<dim3(lines), 64 * p.line_waves, 0, st>>>(k);
+                return hipGetLastError();
+            }
         if (p.segments > 1) {
             selective_forward_kernel<E, BC, NP, SL, true><<<dim3(lines * (p.segments - 1)), 64 * SL, 0, st>>>(k);
             if (const hipError_t failed = launch_selective_carry(s, p, k, false, st); failed != hipSuccess) return failed;

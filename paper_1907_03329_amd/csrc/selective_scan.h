@@ -9,7 +9,8 @@
 // A sequence is cut into segments, which are as many waves: with a_t = exp(d_t A) a segment's map is h -> exp(A sum d) h + (its own last state from
 // zero), so a first launch leaves the last states and sums of d of all segments, and a second one has every segment put together the maps before its
 // own (where these are many, a launch between the two does that for all of them), and then walk its positions again.  Sequences and channels that fill
-// the chip need no segments, and no first launch.
+// the chip need no segments, and no first launch.  Forward, where sequences are short or lines (64 channels of a sequence) many, a line is a workgroup, whose
+// waves have neighbouring pieces, and maps go through LDS: one launch, and every position is read once.
 //
 // exp(d A) is the hardware's power of two of d (A log2 e).  In the place of positions past a length, and of channels that a tile lacks, the last one there is
 // is read again, with d (and in the reverse pass the gradient of out) masked to zero where that matters: states rest behind a sequence, and what lies
@@ -29,6 +30,7 @@ struct SelectivePlan {
     int pieces, segments, span;         // of a sequence; pieces of a segment
     bool widened;                       // b and c are copied to fp32 rows of `padded` states first
     bool carried;                       // the maps of segments are put together by a launch of their own
+    int line_waves;                     // forward, a workgroup for a whole sequence of a tile's channels: its waves, or 0
     size_t maps, rows, part_rows, part_sums;    // floats of the workspace: maps of segments, widened b and c, partial gradients of b and c, of A, D and bias
 };
 SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse);
