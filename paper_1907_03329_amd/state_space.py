@@ -109,9 +109,20 @@ def _positions(t, name, size, dtype, device, field, time_major) -> int:
 
 
 def _row_stride(t, name):
-    if t.stride(1) != 1 and t.shape[1] != 1:
+    row, channel = t.stride()
+    if channel != 1 and t.shape[1] != 1:
         raise ValueError(f"{name}: channels have to lie next to each other")
-    return t.stride(0)
+    return row
+
+
+def _remembered(shapes, make, *values):
+    """The shape of a call of single positions: a structure made once for each set of values (a few for a server's batch sizes)."""
+    shape = shapes.get(values)
+    if shape is None:
+        if len(shapes) >= 256:
+            shapes.clear()
+        shape = shapes[values] = C.byref(make(*values))
+    return shape
 
 
 def _held(layer, t, name, size, dtype, own, stream):
@@ -197,6 +208,9 @@ class ShortConvolution:
         return grad_x, self.grad_weight, self.grad_bias, self.grad_initial
 
 
+_convolution_shapes, _selective_shapes = {}, {}
+
+
 def convolution_step(x, weight, state, out, bias=None, slots=None, activation: str = "silu", stream=None) -> None:
     """One position for each row of x and out [rows, C]: state [pool, K - 1, C] in the element type, the inputs before, oldest first, is moved on in
     place.  slots: int32 [rows], the pool's row of every request, distinct (outside the pool: zeros, nothing changes)."""
@@ -208,11 +222,11 @@ def convolution_step(x, weight, state, out, bias=None, slots=None, activation: s
         with torch.cuda.device(device):
             return convolution_step(x, weight, state, out, bias, slots, activation, stream)
     (rows, channels), (pool, past, _) = shape, state.shape
-    s = ConvolutionStepShape(rows, pool, channels, past + 1, _choice(ACTIVATIONS, activation, "activation"), _dtype(dtype), _row_stride(x, "x"),
-                             _row_stride(out, "out"))
+    s = _remembered(_convolution_shapes, ConvolutionStepShape, rows, pool, channels, past + 1, _choice(ACTIVATIONS, activation, "activation"), _dtype(dtype),
+                    _row_stride(x, "x"), _row_stride(out, "out"))
     f = torch.float32
     _raise(_library().esrnn_convolution_step(
-        C.byref(s), x.data_ptr(), _check(weight, "weight", (channels, past + 1), f, device), _check_optional(bias, "bias", (channels,), f, device),
+        s, x.data_ptr(), _check(weight, "weight", (channels, past + 1), f, device), _check_optional(bias, "bias", (channels,), f, device),
         _check_optional(slots, "slots", shape[:1], torch.int32, device), _check(state, "state", (pool, past, channels), dtype, device),
         _check(out, "out", shape, dtype, device, dense=False), _of_device(stream, index, device)), "esrnn_convolution_step")
 
@@ -312,16 +326,15 @@ def selective_step(x, delta, A, b, c, state, out, D=None, bias=None, slots=None,
         with torch.cuda.device(device):
             return selective_step(x, delta, A, b, c, state, out, D, bias, slots, delta_kind, stream)
     (rows, channels), (pool, _, N), groups = shape, state.shape, b.shape[1]
-    f, shared, s = torch.float32, (rows, groups, N), SelectiveStepShape()
+    f, shared = torch.float32, (rows, groups, N)
     for t, name in ((b, "b"), (c, "c")):
         _check(t, name, shared, dtype, device, dense=False)
         if (t.stride(2) != 1 and N != 1) or (t.stride(1) != N and groups != 1):
             raise ValueError(f"{name}: groups and states have to lie next to each other")
-    s.rows, s.pool, s.C, s.N, s.G, s.delta_kind, s.dtype = rows, pool, channels, N, groups, _choice(DELTAS, delta_kind, "delta_kind"), _dtype(dtype)
-    s.x_stride, s.delta_stride, s.out_stride = _row_stride(x, "x"), _row_stride(delta, "delta"), _row_stride(out, "out")
-    s.b_stride, s.c_stride = b.stride(0), c.stride(0)
+    s = _remembered(_selective_shapes, SelectiveStepShape, rows, pool, channels, N, groups, _choice(DELTAS, delta_kind, "delta_kind"), _dtype(dtype),
+                    _row_stride(x, "x"), _row_stride(delta, "delta"), b.stride(0), c.stride(0), _row_stride(out, "out"))
     _raise(_library().esrnn_selective_step(
-        C.byref(s), x.data_ptr(), _check(delta, "delta", shape, dtype, device, dense=False), _check(A, "A", (channels, N), f, device), b.data_ptr(),
+        s, x.data_ptr(), _check(delta, "delta", shape, dtype, device, dense=False), _check(A, "A", (channels, N), f, device), b.data_ptr(),
         c.data_ptr(), _check_optional(D, "D", (channels,), f, device), _check_optional(bias, "bias", (channels,), f, device),
         _check_optional(slots, "slots", shape[:1], torch.int32, device), _check(state, "state", (pool, channels, N), f, device),
         _check(out, "out", shape, dtype, device, dense=False), _of_device(stream, index, device)), "esrnn_selective_step")
@@ -343,7 +356,7 @@ class BlockNorm:
         dtype = torch.float32 if dtype is None else dtype
         stream_dtype = dtype if stream_dtype is None else stream_dtype
         self.device, self.dtype, self.stream_dtype, self.training, self.gate = _cuda(device), dtype, stream_dtype, training, gate
-        self.residual, self.pre = bool(residual), bool(pre)
+        self.residual, self.pre, self._gated = bool(residual), bool(pre), gate != "none"
         self._index, self._lib = self.device.index, _library()
         s = BlockNormShape()
         s.rows, s.C, s.gate, s.dtype, s.stream_dtype, s.eps = int(rows), int(C_), _choice(GATES, gate, "gate"), _dtype(dtype), _dtype(stream_dtype), float(eps)
@@ -367,26 +380,30 @@ class BlockNorm:
             self._out.y = self.grad_y.data_ptr()
             self._out.gate, self._out.residual = (None if t is None else t.data_ptr() for t in (self.grad_gate, self.grad_residual))
 
-    def _row(self, t, name, dtype, wanted, field):
-        """The address of rows that are there if `wanted` says so."""
+    def _row(self, t, name, dtype):
+        """The address and the stride of rows."""
+        return _check(t, name, self._size, dtype, self.device, dense=False), _row_stride(t, name)
+
+    def _absent(self, t, name, wanted):
         if (t is not None) != wanted:
             raise ValueError(f"{name} has to be {'given' if wanted else 'None'}")
-        if t is None:
-            return None
-        at = _check(t, name, self._size, dtype, self.device, dense=False)
-        setattr(self._shape, field, _row_stride(t, name))
-        return at
 
     def _given(self, y, gate, residual, exists, post_weight, scale, pre_weight):
-        o, f, d = self._in, torch.float32, self.device
-        if (pre_weight is not None) != self.pre:
-            raise ValueError(f"pre_weight has to be {'given' if self.pre else 'None'}")
-        o.y = self._row(y, "y", self.dtype, True, "y_stride")
-        o.gate = self._row(gate, "gate", self.dtype, self.gate != "none", "gate_stride")
-        o.residual = self._row(residual, "residual", self.stream_dtype, self.residual, "residual_stride")
-        o.exists = _check_optional(exists, "exists", self._rows, torch.int32, d)
-        o.post_weight, o.scale, o.pre_weight = (_check_optional(t, n, self._channels, f, d)
-                                                for t, n in ((post_weight, "post_weight"), (scale, "scale"), (pre_weight, "pre_weight")))
+        o, s, f, d, size = self._in, self._shape, torch.float32, self.device, self._channels
+        if (gate is not None) != self._gated or (residual is not None) != self.residual or (pre_weight is not None) != self.pre:
+            self._absent(gate, "gate", self._gated)
+            self._absent(residual, "residual", self.residual)
+            self._absent(pre_weight, "pre_weight", self.pre)
+        o.y, s.y_stride = self._row(y, "y", self.dtype)
+        if self._gated:
+            o.gate, s.gate_stride = self._row(gate, "gate", self.dtype)
+        if self.residual:
+            o.residual, s.residual_stride = self._row(residual, "residual", self.stream_dtype)
+        if self.pre:
+            o.pre_weight = _check(pre_weight, "pre_weight", size, f, d)
+        o.post_weight = None if post_weight is None else _check(post_weight, "post_weight", size, f, d)
+        o.scale = None if scale is None else _check(scale, "scale", size, f, d)
+        o.exists = None if exists is None else _check(exists, "exists", self._rows, torch.int32, d)
 
     def forward(self, y, gate=None, residual=None, post_weight=None, scale=None, pre_weight=None, exists=None, in_place: bool = False, stream=None):
         """(sum, out); the one that there is not is None.  in_place: sum takes the place of `residual` (not in a layer for training)."""
@@ -397,7 +414,8 @@ class BlockNorm:
             raise ValueError("in_place needs a residual, and a layer that is not for training")
         self._given(y, gate, residual, exists, post_weight, scale, pre_weight)
         s = self._shape
-        s.sum_stride = s.residual_stride if in_place else s.C
+        if self.residual:
+            s.sum_stride = s.residual_stride if in_place else s.C
         to = _of_device(stream, self._index, self.device)
         _raise(self._lib.esrnn_block_norm_forward(self._ref, self._in_ref, self._in.residual if in_place else self._sum_ptr, self._result_ptr,
                                                   self._stats_ptr, to), "esrnn_block_norm_forward")
@@ -414,8 +432,13 @@ class BlockNorm:
         if not self.training or not self._forward_done:
             raise EsrnnError(4, "BlockNorm.backward")
         self._given(y, gate, residual, exists, post_weight, scale, pre_weight)
-        d_ptr = self._row(grad_out, "grad_out", self.dtype, self.out is not None, "grad_out_stride")
-        ds_ptr = None if grad_sum is None else self._row(grad_sum, "grad_sum", self.stream_dtype, self.residual, "grad_sum_stride")
+        s, d_ptr, ds_ptr = self._shape, None, None
+        self._absent(grad_out, "grad_out", self.out is not None)
+        if grad_out is not None:
+            d_ptr, s.grad_out_stride = self._row(grad_out, "grad_out", self.dtype)
+        if grad_sum is not None:
+            self._absent(grad_sum, "grad_sum", self.residual)
+            ds_ptr, s.grad_sum_stride = self._row(grad_sum, "grad_sum", self.stream_dtype)
         sums = [mine if given is not None else None for mine, given in ((self.grad_post_weight, post_weight), (self.grad_scale, scale),
                                                                         (self.grad_pre_weight, pre_weight))]
         o = self._out
