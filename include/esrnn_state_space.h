@@ -76,7 +76,7 @@ esrnn_status esrnn_convolution_step(const esrnn_convolution_step_shape *shape, c
  * Selective scan: C channels of N states each, 1 <= N <= 64, over T positions of B sequences.  b and c belong to G groups of C / G neighbouring
  * channels.  For a channel of group g, with d = softplus(delta + bias) or delta + bias:
  *   h_t[n] = exp(d_t A[n]) h_{t-1}[n] + d_t x_t b_t[g][n],    out_t = sum_n c_t[g][n] h_t[n] + D x_t
- * A is used as it is (rates of decay are negative).
+ * A is used as it is (rates of decay are negative; minus infinity keeps nothing of a state, but for a step of size zero, which changes nothing).
  */
 typedef enum { ESRNN_DELTA_SOFTPLUS = 0, ESRNN_DELTA_GIVEN = 1 } esrnn_delta_kind;
 
@@ -131,7 +131,7 @@ esrnn_status esrnn_selective_step(const esrnn_selective_step_shape *shape, const
  *   e = p silu(gate) (ESRNN_GATE_AFTER) or p;     sum = residual + scale e  (without residual 0, without scale 1)
  *   out = sum / sqrt(mean(sum^2) + eps) pre_weight
  * Without pre_weight there is no second norm: with a residual `sum` is the result and out is NULL, without one the result is out = scale e.
- * The second norm takes the sum before it is rounded.
+ * The second norm takes the sum before it is rounded.  Squares are summed in fp32: a row whose mean square is beyond it has a root of infinity and gives zeros.
  */
 typedef enum { ESRNN_GATE_NONE = 0, ESRNN_GATE_BEFORE = 1, ESRNN_GATE_AFTER = 2 } esrnn_gate_position;
 

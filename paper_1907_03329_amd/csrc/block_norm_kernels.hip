@@ -8,6 +8,7 @@
 //   dgate = silu'(gate) (dv y | de p),  dpre = sum D that,  dscale = sum ds e,  dpost = sum dp vhat.
 // The reverse pass computes s again from the residual, in fp32, rather than read the rounded sum.
 #include <algorithm>
+#include <limits>
 
 #include "state_space_internal.h"
 
@@ -347,7 +348,8 @@ Args arguments(const esrnn_block_norm_shape &s, const BlockNormArgs &a)
     p.grad_out = s.grad_out_stride, p.grad_sum = s.grad_sum_stride, p.grad_y = s.grad_y_stride, p.grad_gate = s.grad_gate_stride;
     p.grad_residual = s.grad_residual_stride;
     p.rows = s.rows, p.C = s.C, p.before = s.gate == ESRNN_GATE_BEFORE, p.after = s.gate == ESRNN_GATE_AFTER;
-    p.eps = s.eps, p.inverse = 1.0f / s.C;
+    // (at least the smallest normal number, or the root of a row of zeros is zero)
+    p.eps = std::max(s.eps, std::numeric_limits<float>::min()), p.inverse = 1.0f / s.C;
     return p;
 }
 

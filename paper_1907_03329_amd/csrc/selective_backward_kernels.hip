@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(64 * SL) selective_back_maps_kernel(Scan k)
     float A[NP], mu[NP];
     load_own<NP>(k.a.A + (size_t)at.channel * k.N, at.slice, k.N, at.lane_mask, A);
 #pragma unroll
-    for (int n = 0; n < NP; ++n) A[n] *= kLog2e, mu[n] = 0.0f;
+    for (int n = 0; n < NP; ++n) A[n] = exponent_rate(A[n]), mu[n] = 0.0f;
     const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f;
     float sum = 0.0f;
     Column<E> ds, gs, next_ds, next_gs;
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
     float A[NP], mu[NP], dA[NP], dD = 0.0f, dbias = 0.0f;
     load_own<NP>(k.a.A + (size_t)at.channel * k.N, at.slice, k.N, at.lane_mask, A);
 #pragma unroll
-    for (int n = 0; n < NP; ++n) A[n] *= kLog2e, dA[n] = 0.0f;
+    for (int n = 0; n < NP; ++n) A[n] = exponent_rate(A[n]), dA[n] = 0.0f;
     const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
     if (begin < at.length || begin == 0) arriving<NP, SL>(k, at, own, A, mu);
 

@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(64 * SL) selective_forward_kernel(Scan k)
     float A[NP], h[NP];
     load_own<NP>(k.a.A + (size_t)at.channel * k.N, at.slice, k.N, at.lane_mask, A);
 #pragma unroll
-    for (int n = 0; n < NP; ++n) A[n] *= kLog2e, h[n] = 0.0f;
+    for (int n = 0; n < NP; ++n) A[n] = exponent_rate(A[n]), h[n] = 0.0f;
     const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
     if (!kMaps && k.carried && at.segment > 0) {
         if (begin < at.length) load_states<NP>(map_of<NP, SL>(k, at, at.segment), h);
@@ -127,14 +127,14 @@ __global__ void __launch_bounds__(64 * kWaves) selective_line_kernel(Scan k)
     float A[NP];
     load_own<NP>(k.a.A + (size_t)at.channel * k.N, 0, k.N, at.lane_mask, A);
 #pragma unroll
-    for (int n = 0; n < NP; ++n) A[n] *= kLog2e;
+    for (int n = 0; n < NP; ++n) A[n] = exponent_rate(A[n]);
     f32x4 rates = {}, carry = {};       // of states 4 wave ..
     if (composes)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int n = 4 * wave + r;
             const unsigned mask = n < k.N ? at.lane_mask : 0u;
-            rates[r] = masked(k.a.A[(size_t)at.channel * k.N + min(n, k.N - 1)], mask) * kLog2e;
+            rates[r] = exponent_rate(masked(k.a.A[(size_t)at.channel * k.N + min(n, k.N - 1)], mask));
             if (k.a.initial) carry[r] = masked(k.a.initial[own + min(n, k.N - 1)], mask);
         }
     const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(64 * kRuns) selective_carry_kernel(Scan k, int
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int n = NP * slice + 4 * quad + r;
-        A[r] = masked(k.a.A[(size_t)channel * k.N + min(n, k.N - 1)], n < k.N ? lane_mask : 0u) * kLog2e;
+        A[r] = exponent_rate(masked(k.a.A[(size_t)channel * k.N + min(n, k.N - 1)], n < k.N ? lane_mask : 0u));
     }
     const auto apply = [&](f32x4 h, f32x4 local, float sum) {
 #pragma unroll
@@ -371,8 +371,12 @@ SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse)
 
 size_t selective_workspace_floats(const esrnn_selective_shape &s, bool reverse)
 {
-    const SelectivePlan p = selective_plan(s, reverse);
-    return 64 + p.maps + p.rows + p.part_rows + p.part_sums;
+    // (the two passes cut sequences in ways of their own)
+    const auto floats = [&](bool which) {
+        const SelectivePlan p = selective_plan(s, which);
+        return 64 + p.maps + p.rows + p.part_rows + p.part_sums;
+    };
+    return reverse ? std::max(floats(false), floats(true)) : floats(false);
 }
 size_t selective_saved_floats(const esrnn_selective_shape &s)
 {

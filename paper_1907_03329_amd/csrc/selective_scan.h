@@ -179,6 +179,14 @@ __device__ __forceinline__ float *saved_of(const Scan &k, const ScanPlace &at, i
     return k.a.saved + ((((size_t)at.b * k.pieces + piece) * (k.G * k.tiles) + at.tile) * SL + at.slice) * (NP * 64);
 }
 
+// A log2 e, of which exp(d A) is the power of two with d.  An infinite rate of decay forgets everything in a step and nothing in one of size zero, which is
+// what positions past a length are: so it is a finite one.
+__device__ __forceinline__ float exponent_rate(float A)
+{
+    const float rate = A * kLog2e;
+    return rate == -__builtin_inff() ? -0x1p127f : rate;
+}
+
 // This lane's states of arrays [..][C][N]; those that do not exist are zero.
 template <int NP>
 __device__ __forceinline__ void load_own(const float *of_channel, int slice, int N, unsigned lane_mask, float (&v)[NP])

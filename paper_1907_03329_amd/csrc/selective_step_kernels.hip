@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(kThreads) selective_step_kernel(esrnn_selectiv
     const int channel = min(in_tile, s.C - 1), group = channel / (s.C / s.G);
     float A[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) A[r] = n0 + r < s.N ? a.A[(size_t)channel * s.N + n0 + r] * kLog2e : 0.0f;
+    for (int r = 0; r < 4; ++r) A[r] = n0 + r < s.N ? exponent_rate(a.A[(size_t)channel * s.N + n0 + r]) : 0.0f;
     const float bias = a.bias ? a.bias[channel] : 0.0f, D = a.D ? a.D[channel] : 0.0f;
     for (int i = first_row; i < s.rows; i += rows_apart) {
         const int slot = a.slots ? a.slots[i] : i;

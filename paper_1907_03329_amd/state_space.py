@@ -130,13 +130,14 @@ def _held(layer, t, name, size, dtype, own, stream):
     if t is None:
         return None
     at = _check(t, name, size, dtype, layer.device)
-    if own is None or at != own:
+    if at != own:
         return at
-    if layer._carried is None or layer._carried.dtype is not t.dtype:
-        layer._carried = torch.empty_like(t)
+    kept = layer._carried.get(name)
+    if kept is None:
+        kept = layer._carried[name] = torch.empty_like(t)
     with torch.cuda.stream(stream):     # (None: the current one)
-        layer._carried.copy_(t)
-    return layer._carried.data_ptr()
+        kept.copy_(t)
+    return kept.data_ptr()
 
 
 class ShortConvolution:
@@ -160,7 +161,7 @@ class ShortConvolution:
         self._size, self._window = torch.Size((T, B, C_) if time_major else (B, T, C_)), torch.Size((B, taps - 1, C_))
         self._taps, self._channels, self._sequences = torch.Size((C_, taps)), torch.Size((C_,)), torch.Size((B,))
         empty = lambda size, dt=torch.float32: torch.empty(size, dtype=dt, device=self.device)  # noqa: E731
-        self.out, self.last, self._carried = empty(self._size, dtype), empty(self._window, dtype), None
+        self.out, self.last, self._carried, self._own_first = empty(self._size, dtype), empty(self._window, dtype), {}, False
         self._out_ptr, self._last_ptr = self.out.data_ptr(), self.last.data_ptr()
         self._positions(self.out, "out", s.out_stride)
         if training:
@@ -184,13 +185,14 @@ class ShortConvolution:
                 return self.forward(x, weight, bias, lengths, initial, stream)
         given = self._given(x, weight, bias, lengths)
         to = _of_device(stream, self._index, self.device)
-        _raise(self._lib.esrnn_convolution_forward(
-            self._ref, *given, _held(self, initial, "initial", self._window, self.dtype, self._last_ptr, stream), self._out_ptr, self._last_ptr, to),
-            "esrnn_convolution_forward")
+        first = _held(self, initial, "initial", self._window, self.dtype, self._last_ptr, stream)
+        _raise(self._lib.esrnn_convolution_forward(self._ref, *given, first, self._out_ptr, self._last_ptr, to), "esrnn_convolution_forward")
+        self._own_first = initial is not None and initial.data_ptr() == self._last_ptr
         return self.out, self.last
 
     def backward(self, x, weight, grad_out, bias=None, lengths=None, initial=None, grad_last=None, grad_x=None, stream=None):
-        """(grad_x, grad_weight, grad_bias, grad_initial) for the operands of a forward pass (whose last is not `initial` any more)."""
+        """(grad_x, grad_weight, grad_bias, grad_initial) for the operands of a forward pass.  `initial` may be the layer's own `last` if that was what the
+        forward pass last run was given: what it held then."""
         if layers._current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.backward(x, weight, grad_out, bias, lengths, initial, grad_last, grad_x, stream)
@@ -200,6 +202,10 @@ class ShortConvolution:
         given = self._given(x, weight, bias, lengths)
         d_ptr, gx_ptr = self._positions(grad_out, "grad_out", s.grad_out_stride), self._positions(grad_x, "grad_x", s.grad_x_stride)
         first = _check_optional(initial, "initial", self._window, self.dtype, self.device)
+        if first == self._last_ptr:
+            if not self._own_first:
+                raise ValueError("initial is what the forward pass has written to the layer's last")
+            first = self._carried["initial"].data_ptr()
         to = _of_device(stream, self._index, self.device)
         gw, gb, gi, workspace = self._sums
         _raise(self._lib.esrnn_convolution_backward(
@@ -259,7 +265,7 @@ class SelectiveScan:
         self.workspace, self.out, self.last = empty(workspace, torch.uint8), empty(self._size, dtype), empty(self._states)
         self._workspace_ptr, self._out_ptr, self._last_ptr = (t.data_ptr() for t in (self.workspace, self.out, self.last))
         self._wide(self.out, "out", s.out_stride)
-        self._forward_done, self._saved_ptr, self._carried = False, None, None
+        self._forward_done, self._saved_ptr, self._carried = False, None, {}
         if training:
             self.saved = empty(saved // 4)
             self._saved_ptr = self.saved.data_ptr()

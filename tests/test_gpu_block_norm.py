@@ -184,3 +184,26 @@ def test_two_streams_graphs_and_equal_calls():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(results, eager))
+
+
+@pytest.mark.parametrize("eps", [1e-37, 1e-40, 1e-45])
+def test_eps_that_is_no_normal_number(eps):
+    import torch
+    y, w = torch.zeros(2, 70, device="cuda"), torch.ones(70, device="cuda")
+    y[1] = torch.randn(70, device="cuda")
+    layer = state_space.BlockNorm(2, 70, residual=False, pre=False, eps=eps)
+    _, out = layer.forward(y, post_weight=w)
+    grads = layer.backward(y, torch.ones_like(y), post_weight=w)
+    assert not out[0].any() and bool(torch.isfinite(out).all()) and abs(float(out[1].square().mean()) - 1.0) <= 1e-5
+    assert bool(torch.isfinite(grads[0][1]).all()) and bool(torch.isfinite(grads[3]).all())
+
+
+def test_rows_beyond_32_bits():
+    import torch
+    torch.manual_seed(0)
+    near, w = torch.randn(3, 500, device="cuda").half(), torch.rand(500, device="cuda")
+    far = torch.empty(2 * 2_200_000_000 + 500, dtype=torch.float16, device="cuda").as_strided((3, 500), (2_200_000_000, 1))
+    far.copy_(near)
+    layer = state_space.BlockNorm(3, 500, gate="after", dtype=torch.float16)
+    run = lambda t: [r.clone() for r in (*layer.forward(t, t, t, w, w, w), *layer.backward(t, t, t, t, t, w, w, w))]  # noqa: E731
+    assert all(torch.equal(a, b) for a, b in zip(run(near), run(far)))

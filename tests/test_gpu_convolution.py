@@ -210,3 +210,44 @@ def test_two_streams_graphs_and_equal_calls():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(results, eager))
+
+
+def test_windows_carried_from_batch_to_batch_in_training():
+    """The layer's own last as the next initial: forward and reverse passes as with a copy of it; what has been overwritten since is refused."""
+    import torch
+    torch.manual_seed(0)
+    B, T, C, K = 3, 10, 40, 4
+    x, d, w = torch.randn(2, B, T, C, device="cuda").bfloat16(), torch.randn(B, T, C, device="cuda").bfloat16(), torch.randn(C, K, device="cuda")
+    results = []
+    for own in (True, False):
+        layer = state_space.ShortConvolution(B, T, C, K, dtype=torch.bfloat16)
+        last = layer.forward(x[0], w)[1]
+        with pytest.raises(ValueError):
+            layer.backward(x[0], w, d, initial=last)
+        first = last if own else last.clone()
+        out = layer.forward(x[1], w, initial=first)[0]
+        grads = layer.backward(x[1], w, d, initial=first)
+        again = layer.backward(x[1], w, d, initial=first, grad_last=grads[3])       # (its own grad_initial, copied before)
+        results.append([t.clone() for t in (out, *grads, *again)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_a_batch_beyond_32_bits():
+    """Two sequences 2.2e9 elements apart, and rows of one 5e8 apart."""
+    import torch
+    C, T = 64, 9
+    w = torch.randn(C, 4, device="cuda")
+    near = torch.randn(2, T, C, device="cuda").half()
+    layer = state_space.ShortConvolution(2, T, C, dtype=torch.float16)
+    want = [t.clone() for t in (layer.forward(near, w)[0], *layer.backward(near, w, near))]
+    big = torch.empty(2 * 2_200_000_000 + 1000, dtype=torch.float16, device="cuda")
+    for strides in ((2_200_000_000, C, 1), (C, 500_000_000, 1)):
+        x = big.as_strided((2, T, C), strides) if strides[0] > C else big.as_strided((2, T - 1, C), strides)
+        if strides[0] > C:
+            x.copy_(near)
+            got = (layer.forward(x, w)[0], *layer.backward(x, w, x))
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        else:
+            x.copy_(near[:, :T - 1])
+            short = state_space.ShortConvolution(2, T - 1, C, dtype=torch.float16, training=False)
+            assert torch.equal(short.forward(x, w)[0], want[0][:, :T - 1])

@@ -238,3 +238,72 @@ def test_two_streams_graphs_and_equal_calls():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(results, eager))
+
+
+@pytest.mark.parametrize("B,T,C,N", [(300, 72, 40, 16), (300, 40, 64, 8), (4, 130, 64, 16), (257, 9, 60, 3), (20, 200, 130, 16), (600, 33, 40, 16), (1, 128, 64, 16), (1, 129, 64, 16)])
+def test_short_sequences_and_many_lines(B, T, C, N):
+    """Sizes at which a line is a workgroup, of one block of pieces and of several, and some beside them."""
+    check(B, T, C, N, lengths="ragged", initial=True, seed=T)
+    check(B, T, C, N, dtype="bfloat16", D=False, seed=T + 1)
+
+
+@pytest.mark.parametrize("T", [13, 16, 700])
+def test_infinite_rates_of_decay(T):
+    """A state that forgets everything at every position: what it takes in, exactly, at lengths that end inside a piece too; other states do not see it."""
+    import torch
+    torch.manual_seed(0)
+    B, C, N = 2, 70, 4
+    x, delta, d = (torch.randn(B, T, C, device="cuda") for _ in range(3))
+    b, c = torch.randn(B, T, 1, N, device="cuda"), torch.randn(B, T, 1, N, device="cuda")
+    A = -torch.rand(C, N, device="cuda")
+    A[:, 2] = -float("inf")
+    n = torch.tensor([T, T - 5], dtype=torch.int32, device="cuda")
+    h0 = torch.randn(B, C, N, device="cuda")
+    layer = state_space.SelectiveScan(B, T, C, N)
+    out, last = layer.forward(x, delta, A, b, c, lengths=n, initial=h0)
+    step = torch.nn.functional.softplus(delta.double())
+    for i, k in enumerate(n.tolist()):
+        want = (step[i, k - 1] * x[i, k - 1].double() * b[i, k - 1, 0, 2].double())
+        assert float((last[i, :, 2].double() - want).abs().max()) <= 1e-6 * float(want.abs().max())
+    grads = layer.backward(x, delta, A, b, c, d, lengths=n)
+    assert all(bool(torch.isfinite(t).all()) for t in (out, last, *grads))
+    assert not grads[-1][:, :, 2].any() and not grads[2][:, 2].any()
+
+
+def test_a_batch_beyond_32_bits():
+    """Two sequences 2.2e9 elements apart in x, delta and their gradients; states of b and c too."""
+    import torch
+    torch.manual_seed(0)
+    T, C, N = 20, 64, 16
+    far = 2_200_000_000
+    x, delta, d, b, c = (torch.randn(2, T, n, device="cuda").half() for n in (C, C, C, N, N))
+    A = -torch.rand(C, N, device="cuda")
+    layer = state_space.SelectiveScan(2, T, C, N, dtype=torch.float16)
+    want = [t.clone() for t in (*layer.forward(x, delta, A, b[:, :, None], c[:, :, None]), *layer.backward(x, delta, A, b[:, :, None], c[:, :, None], d))]
+    big = torch.empty(far + 20000, dtype=torch.float16, device="cuda")
+    at, views = 0, []
+    for t in (x, delta, d, b, c, x, delta, b, c):
+        v = big.as_strided(t.shape, (far, t.shape[2], 1), at)
+        views.append(v)
+        at += T * t.shape[2]
+    for v, t in zip(views, (x, delta, d, b, c)):
+        v.copy_(t)
+    xs, ds, dd, bs, cs, gx, gd, gb, gc = views
+    operands = (xs, ds, A, bs[:, :, None], cs[:, :, None])
+    got = (*layer.forward(*operands), *layer.backward(*operands, dd, grad_x=gx, grad_delta=gd, grad_b=gb[:, :, None], grad_c=gc[:, :, None]))
+    assert all(torch.equal(p.reshape(q.shape), q) for p, q in zip(got, want))
+
+
+def test_pools_beyond_32_bits():
+    import torch
+    C, N, pool = 1024, 16, 140_000         # 2.3e9 states
+    state = torch.zeros(pool, C, N, device="cuda")
+    torch.manual_seed(0)
+    x, delta, b, c = (torch.randn(3, *s, device="cuda") for s in ((C,), (C,), (1, N), (1, N)))
+    A, out, near = -torch.rand(C, N, device="cuda"), torch.empty(3, C, device="cuda"), torch.zeros(3, C, N, device="cuda")
+    slots = torch.tensor([pool - 1, 0, 131_073], dtype=torch.int32, device="cuda")
+    for _ in range(2):
+        state_space.selective_step(x, delta, A, b, c, state, out, slots=slots)
+        one = out.clone()
+        state_space.selective_step(x, delta, A, b, c, near, out)
+    assert torch.equal(one, out) and torch.equal(state[slots.long()], near) and int((state != 0).any(2).any(1).sum()) == 3
