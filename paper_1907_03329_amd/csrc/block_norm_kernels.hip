@@ -26,10 +26,10 @@ struct Args {
 };
 
 // How a row is held: L lanes of each of NW waves, M groups of four neighbouring channels a lane; RW rows of a workgroup at a time.
-// kKept: weights and their gradients' sums stay in registers, else weights are read for every row and sums are in LDS; kAhead: rows are requested ahead.
-template <int L_, int NW_, int M_ = 1, bool kKept_ = true, bool kAhead_ = true>
+// kAhead: rows are requested ahead.
+template <int L_, int NW_, int M_ = 1, bool kAhead_ = true>
 struct Layout {
-    static constexpr bool kKept = kKept_, kAhead = kAhead_;
+    static constexpr bool kAhead = kAhead_;
     static constexpr int L = L_, NW = NW_, M = M_, kThreads = NW > 1 ? 64 * NW : 256, RW = kThreads / (L * NW), kChannels = 4 * M * L * NW;
 };
 
@@ -76,52 +76,22 @@ __device__ __forceinline__ void store_row(void *base, long long at, int lane, in
         ch.store(row, from_f32<E>(v[m]));
     }
 }
-// Weights of a lane's channels, ones where there are none: in registers, or read for every row where a lane has too many channels for that.
+// Weights of a lane's channels, ones where there are none.
+template <class Y>
+__device__ __forceinline__ f32x4 load_weight(const float *w, int m, int lane, int C)
+{
+    if (!w) return f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+    return Neighbours<float, 4>{4 * (m * Y::L * Y::NW + lane), C}.load(w);
+}
 template <class Y>
 struct Weights {
-    static constexpr bool kKept = Y::kKept;
-    const float *from;
-    int lane, C;
-    f32x4 kept[kKept ? Y::M : 1];
-    __device__ __forceinline__ f32x4 read(int m) const
-    {
-        if (!from) return f32x4{1.0f, 1.0f, 1.0f, 1.0f};
-        return Neighbours<float, 4>{4 * (m * Y::L * Y::NW + lane), C}.load(from);
-    }
-    __device__ __forceinline__ Weights(const float *w, int lane_, int C_) : from(w), lane(lane_), C(C_)
-    {
-        if constexpr (kKept)
-#pragma unroll
-            for (int m = 0; m < Y::M; ++m) kept[m] = read(m);
-    }
-    __device__ __forceinline__ f32x4 operator[](int m) const
-    {
-        if constexpr (kKept) return kept[m];
-        return read(m);
-    }
-};
-// Sums over rows for a lane's channels.
-template <class Y, bool kLds>
-struct Sums {
     f32x4 v[Y::M];
-    __device__ __forceinline__ Sums(f32x4 *)
+    __device__ __forceinline__ Weights(const float *w, int lane, int C)
     {
 #pragma unroll
-        for (int m = 0; m < Y::M; ++m) v[m] = f32x4{};
+        for (int m = 0; m < Y::M; ++m) v[m] = load_weight<Y>(w, m, lane, C);
     }
-    __device__ __forceinline__ void add(int m, f32x4 x) { v[m] += x; }
-    __device__ __forceinline__ f32x4 get(int m) const { return v[m]; }
-};
-template <class Y>
-struct Sums<Y, true> {
-    f32x4 *at;
-    __device__ __forceinline__ Sums(f32x4 *lds) : at(lds + threadIdx.x)
-    {
-#pragma unroll
-        for (int m = 0; m < Y::M; ++m) at[m * Y::kThreads] = f32x4{};
-    }
-    __device__ __forceinline__ void add(int m, f32x4 x) { at[m * Y::kThreads] += x; }
-    __device__ __forceinline__ f32x4 get(int m) const { return at[m * Y::kThreads]; }
+    __device__ __forceinline__ f32x4 operator[](int m) const { return v[m]; }
 };
 template <class Y>
 __device__ __forceinline__ float squares(const f32x4 (&v)[Y::M])
@@ -212,9 +182,9 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
     __shared__ __attribute__((aligned(16))) float s_parts[Y::RW > 1 ? Y::RW : 1][Y::RW > 1 ? Y::kChannels : 1];
     const int lane = threadIdx.x % (Y::L * Y::NW), in_group = threadIdx.x / (Y::L * Y::NW);
     const Weights<Y> post(p.a.post_weight, lane, p.C), scale(p.a.scale, lane, p.C), pre(p.a.pre_weight, lane, p.C);
-    constexpr bool kLds = !Y::kKept;
-    __shared__ f32x4 s_kept[kLds ? 3 : 1][kLds ? M * Y::kThreads : 1];
-    Sums<Y, kLds> dpost(s_kept[0]), dscale(s_kept[kLds ? 1 : 0]), dpre(s_kept[kLds ? 2 : 0]);
+    // (sixteen waves of a row have at most 128 registers, which requests in fp32 would exceed)
+    constexpr bool kAhead = Y::kAhead && !(Y::NW == 16 && sizeof(R) == 4);
+    f32x4 dpost[M] = {}, dscale[M] = {}, dpre[M] = {};
     Row<Y, E> ys, gates, ds_out;
     Row<Y, R> residuals, ds_sum;
     bool exists = false;
@@ -231,11 +201,11 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
     };
     int turn = 0;
     const int step = gridDim.x * Y::RW;
-    if (Y::kAhead) request(blockIdx.x * Y::RW);
+    if (kAhead) request(blockIdx.x * Y::RW);
     for (int first = blockIdx.x * Y::RW; first < p.rows; first += step, turn ^= 2) {
         const long long row = first + in_group;
         const bool mine = row < p.rows;
-        if (!Y::kAhead) request(first);
+        if (!kAhead) request(first);
         f32x4 y[M], gate[M] = {}, s[M] = {}, d[M] = {}, ds[M] = {};
         const float r1 = exists ? next_r1 : 0.0f, r2 = exists ? next_r2 : 0.0f;
         ys.get(exists, y);
@@ -243,7 +213,7 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
         if (p.a.residual) residuals.get(exists, s);
         if (p.a.grad_out) ds_out.get(exists, d);
         if (p.a.grad_sum) ds_sum.get(exists, ds);
-        if (Y::kAhead && first + step < p.rows) request(first + step);
+        if (kAhead && first + step < p.rows) request(first + step);
         f32x4 act[M], slope[M], vhat[M], e[M];
 #pragma unroll
         for (int m = 0; m < M; ++m) {
@@ -261,7 +231,7 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
 #pragma unroll
             for (int m = 0; m < M; ++m) {
                 s[m] *= r2;                 // that
-                dpre.add(m, d[m] * s[m]);
+                dpre[m] += d[m] * s[m];
                 weighted[m] = d[m] * pre[m];
             }
             const float mean = row_sum<Y>(products<Y>(weighted, s), s_sums, turn) * p.inverse;
@@ -276,11 +246,11 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             const f32x4 of_e = p.after ? e[m] * act[m] : e[m];
-            dscale.add(m, ds[m] * of_e);
+            dscale[m] += ds[m] * of_e;
             const f32x4 de = ds[m] * scale[m];
             dgate[m] = de * e[m];
             const f32x4 dp = p.after ? de * act[m] : de;
-            dpost.add(m, dp * vhat[m]);
+            dpost[m] += dp * vhat[m];
             weighted[m] = dp * post[m];
         }
         if (p.a.post_weight) {
@@ -308,7 +278,7 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
     for (int which = 0; which < 3; ++which) {
         f32x4 sum[M];
 #pragma unroll
-        for (int m = 0; m < M; ++m) sum[m] = which == 0 ? dpost.get(m) : which == 1 ? dscale.get(m) : dpre.get(m);
+        for (int m = 0; m < M; ++m) sum[m] = which == 0 ? dpost[m] : which == 1 ? dscale[m] : dpre[m];
         float *to = p.a.parts + ((size_t)blockIdx.x * 3 + which) * p.C;
         if constexpr (Y::RW > 1) {
             __syncthreads();
@@ -324,6 +294,100 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
             store_row<Y, float>(to, 0, lane, p.C, sum);
         }
     }
+}
+
+// Rows of more channels than registers hold with all that is made of them: every one of the three steps (the sum for the second norm, that for the first, the
+// gradients) reads the row again, from the caches, and the sums over rows are in LDS.  4000 rows of 8192 channels, bf16: some 250 us of 102 at the rate of a copy.
+template <class E, class R, class Y>
+__global__ void __launch_bounds__(Y::kThreads) block_norm_wide_backward_kernel(Args p)
+{
+    constexpr int M = Y::M;
+    __shared__ float s_sums[4][16];
+    __shared__ f32x4 s_weights[3][M][Y::kThreads];
+    const int lane = threadIdx.x;
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int which = 0; which < 3; ++which) s_weights[which][m][lane] = f32x4{};
+    int turn = 0;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 2) {
+        const bool exists = !p.a.exists || p.a.exists[row] != 0;
+        const float r1 = exists ? p.a.stats_in[2 * row] : 0.0f, r2 = exists ? p.a.stats_in[2 * row + 1] : 0.0f;
+        const auto ch = [&](int m) { return 4 * (m * Y::kThreads + lane); };
+        // (converted behind the condition on `base`, and all requests of a step together, or each would be waited for by itself)
+        const auto read = [&](auto e, const void *base, long long at, int m) {
+            typedef decltype(e) T;
+            Vec4<T> v = {};
+            if (base) v = Neighbours<T, 4>{ch(m), p.C}.load(static_cast<const T *>(base) + at);
+            return v;
+        };
+        const auto widen = [&](auto v) { return exists ? __builtin_convertvector(v, f32x4) : f32x4{}; };
+        struct Terms {
+            f32x4 y, act, slope, vhat, e, that, d, ds;  // e: p, before a gate behind the norm
+        };
+        const auto terms = [&](int m, bool with_sum) {
+            Terms t;
+            const auto y = read(E{}, p.a.y, row * p.y, m), d = read(E{}, p.a.grad_out, row * p.grad_out, m), g = read(E{}, p.a.gate, row * p.gate, m);
+            const auto residual = read(R{}, p.a.residual, row * p.residual, m), ds = read(R{}, with_sum ? p.a.grad_sum : nullptr, row * p.grad_sum, m);
+            const f32x4 gate = widen(g);
+            t.y = widen(y), t.d = widen(d), t.ds = widen(ds);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const Silu a = silu(gate[k]);
+                t.act[k] = a.of, t.slope[k] = a.slope;
+            }
+            t.vhat = (p.before ? t.y * t.act : t.y) * r1;
+            t.e = t.vhat * load_weight<Y>(p.a.post_weight, m, lane, p.C);
+            t.that = (widen(residual) + load_weight<Y>(p.a.scale, m, lane, p.C) * (p.after ? t.e * t.act : t.e)) * r2;
+            return t;
+        };
+        const auto dot = [](f32x4 a, f32x4 b) {
+            const f32x4 v = a * b;
+            return (v[0] + v[1]) + (v[2] + v[3]);
+        };
+        float mean2 = 0.0f, mean1 = 0.0f;
+        if (p.a.pre_weight) {
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                const Terms t = terms(m, false);
+                mean2 += dot(t.d * load_weight<Y>(p.a.pre_weight, m, lane, p.C), t.that);
+            }
+            mean2 = row_sum<Y>(mean2, s_sums, turn) * p.inverse;
+        }
+        const auto of_sum = [&](int m, const Terms &t) {
+            if (!p.a.residual && !p.a.pre_weight) return t.d;
+            return p.a.pre_weight ? t.ds + r2 * (t.d * load_weight<Y>(p.a.pre_weight, m, lane, p.C) - t.that * mean2) : t.ds;
+        };
+        if (p.a.post_weight) {
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                const Terms t = terms(m, true);
+                const f32x4 de = of_sum(m, t) * load_weight<Y>(p.a.scale, m, lane, p.C);
+                mean1 += dot((p.after ? de * t.act : de) * load_weight<Y>(p.a.post_weight, m, lane, p.C), t.vhat);
+            }
+            mean1 = row_sum<Y>(mean1, s_sums, turn + 1) * p.inverse;
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const Terms t = terms(m, true);
+            const f32x4 ds = of_sum(m, t), de = ds * load_weight<Y>(p.a.scale, m, lane, p.C), dp = p.after ? de * t.act : de;
+            if (p.a.pre_weight) s_weights[2][m][lane] += t.d * t.that;
+            s_weights[1][m][lane] += ds * (p.after ? t.e * t.act : t.e);
+            s_weights[0][m][lane] += dp * t.vhat;
+            f32x4 dv = dp * load_weight<Y>(p.a.post_weight, m, lane, p.C);
+            if (p.a.post_weight) dv = r1 * (dv - t.vhat * mean1);
+            const f32x4 dgate = (p.before ? dv * t.y : de * t.e) * t.slope;
+            if (p.before) dv *= t.act;
+            if (p.a.grad_residual) Neighbours<R, 4>{ch(m), p.C}.store(static_cast<R *>(p.a.grad_residual) + row * p.grad_residual, from_f32<R>(ds));
+            Neighbours<E, 4>{ch(m), p.C}.store(static_cast<E *>(p.a.grad_y) + row * p.grad_y, from_f32<E>(dv));
+            if (p.a.grad_gate) Neighbours<E, 4>{ch(m), p.C}.store(static_cast<E *>(p.a.grad_gate) + row * p.grad_gate, from_f32<E>(dgate));
+        }
+    }
+#pragma unroll
+    for (int which = 0; which < 3; ++which)
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+            Neighbours<float, 4>{4 * (m * Y::kThreads + lane), p.C}.store(p.a.parts + ((size_t)blockIdx.x * 3 + which) * p.C, s_weights[which][m][lane]);
 }
 
 template <int kCols>
@@ -367,13 +431,13 @@ hipError_t with_layout(int C, F &&f)
         if (C <= 1024) return f(Layout<64, 4>{});
         if (C <= 2048) return f(Layout<64, 8>{});
         if (C <= 4096) return f(Layout<64, 16>{});
-        return f(Layout<64, 16, 2, false, false>{});
+        return f(Layout<64, 16, 2, false>{});
     } else {
-        if (C <= 512) return f(Layout<64, 1, 2, true, false>{});
-        if (C <= 1024) return f(Layout<64, 2, 2, true, false>{});
-        if (C <= 2048) return f(Layout<64, 4, 2, true, false>{});
-        if (C <= 4096) return f(Layout<64, 8, 2, true, false>{});
-        return f(Layout<64, 16, 2, true, false>{});
+        if (C <= 512) return f(Layout<64, 1, 2, false>{});
+        if (C <= 1024) return f(Layout<64, 2, 2, false>{});
+        if (C <= 2048) return f(Layout<64, 4, 2, false>{});
+        if (C <= 4096) return f(Layout<64, 8, 2, false>{});
+        return f(Layout<64, 16, 2, false>{});
     }
 }
 template <class F>
@@ -424,7 +488,8 @@ hipError_t launch_block_norm_backward(const esrnn_block_norm_shape &s, const Blo
         return with_layout<true>(s.C, [&](auto y) {
             typedef decltype(y) Y;
             rows = workgroups<Y>(s.rows, true);
-            block_norm_backward_kernel<decltype(e), decltype(r), Y><<<dim3(rows), Y::kThreads, 0, st>>>(p);
+            if constexpr (Y::M > 1) block_norm_wide_backward_kernel<decltype(e), decltype(r), Y><<<dim3(rows), Y::kThreads, 0, st>>>(p);
+            else block_norm_backward_kernel<decltype(e), decltype(r), Y><<<dim3(rows), Y::kThreads, 0, st>>>(p);
             return hipGetLastError();
         });
     });
