@@ -101,6 +101,26 @@ __global__ void __launch_bounds__(64 * SL) selective_back_maps_kernel(Scan k)
     map[64 * NP + lane] = sum;
 }
 
+// b and c in the order of PieceRows, zeros for states and positions that there are not: [B][pieces][G][fours of states][8][2][4].
+template <class E, class BC>
+__global__ void __launch_bounds__(256) selective_arrange_kernel(Scan k, const E *b, const E *c, long long bb, long long bt, long long cb, long long ct, int fours,
+                                                                long long count, BC *to)
+{
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= count) return;
+    const int r = i & 3, which = i >> 2 & 1, position = i >> 3 & 7;
+    long long rest = i >> 6;
+    const int n = 4 * (int)(rest % fours) + r;
+    rest /= fours;
+    const int group = rest % k.G;
+    rest /= k.G;
+    const int t = (int)(rest % k.pieces) * kPiece + position, s = (int)(rest / k.pieces);
+    const int length = k.a.lengths ? min(max(k.a.lengths[s], 0), k.T) : k.T;
+    BC v = (BC)0.0f;
+    if (n < k.N && t < length) v = (BC)(float)(which ? c + s * cb + t * ct : b + s * bb + t * bt)[(long long)group * k.N + n];
+    to[i] = v;
+}
+
 template <class E, class BC, int NP, int SL>
 __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_kernel(Scan k)
 {
@@ -113,8 +133,7 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
     const E *x = static_cast<const E *>(k.a.x) + at.b * k.xb, *delta = static_cast<const E *>(k.a.delta) + at.b * k.db;
     const E *grad = static_cast<const E *>(k.a.grad_out) + at.b * k.gb;
     E *grad_x = static_cast<E *>(k.a.grad_x) + at.b * k.gxb, *grad_delta = static_cast<E *>(k.a.grad_delta) + at.b * k.gdb;
-    const BC *b = static_cast<const BC *>(k.b) + at.b * k.bb + at.group * k.group + NP * at.slice;
-    const BC *c = static_cast<const BC *>(k.c) + at.b * k.cb + at.group * k.group + NP * at.slice;
+    const BC *shared_rows = static_cast<const BC *>(k.arranged) + ((size_t)at.b * k.pieces * k.G + at.group) * (kPadded / 4 * 64) + at.slice * (NP / 4 * 64);
     const size_t own = ((size_t)at.b * k.C + at.channel) * k.N;
 
     float A[NP], mu[NP], dA[NP], dD = 0.0f, dbias = 0.0f;
@@ -135,14 +154,16 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
     const int last = min(end, at.length);
     if (begin < last) {
         const int top = begin + (last - 1 - begin) / kPiece * kPiece;
+        // the next piece's elements are requested while this one is worked on, and the next four states while these are
+        Column<E> xs, ds, gs;
+        xs.request(x, k.xt, top, at.length, at.channel);
+        ds.request(delta, k.dt, top, at.length, at.channel);
+        gs.request(grad, k.gt, top, at.length, at.channel);
+        f32x4 next_states = *reinterpret_cast<const f32x4 *>(saved_of<NP, SL>(k, at, top / kPiece) + 4 * lane);
         for (int t0 = top; t0 >= begin; t0 -= kPiece, turn ^= 1) {
-            Column<E> xs, ds, gs;
-            xs.request(x, k.xt, t0, at.length, at.channel);
-            ds.request(delta, k.dt, t0, at.length, at.channel);
-            gs.request(grad, k.gt, t0, at.length, at.channel);
             const int t = fresh(t0), left = at.length - 1 - t;
             const float *saved = saved_of<NP, SL>(k, at, t / kPiece);
-            const BC *b0 = b + t * k.bt, *c0 = c + t * k.ct;
+            const BC *rows = shared_rows + (size_t)(t / kPiece) * k.G * (kPadded / 4 * 64);
             const buf_rsrc to_parts = make_base(parts + (size_t)t * part_position);
             float d[kPiece], slope[kPiece], xi[kPiece], g[kPiece], through[kPiece], rate[kPiece];   // through: sum lambda b; rate: sum mu h_{t-1} A log2(e)
 #pragma unroll
@@ -153,39 +174,39 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
                 slope[i] = masked(s.slope, mask), xi[i] = (float)xs.v[i];
                 through[i] = rate[i] = 0.0f;
             }
+            const int before_t = max(t0 - kPiece, begin);
+            xs.request(x, k.xt, before_t, at.length, at.channel);
+            ds.request(delta, k.dt, before_t, at.length, at.channel);
+            gs.request(grad, k.gt, before_t, at.length, at.channel);
 #pragma unroll
             for (int n0 = 0; n0 < NP; n0 += kPart) {
                 // (or the parts' registers add up, and the loads of all of them become one)
                 __builtin_amdgcn_sched_barrier(0);
-                const int part = fresh(n0);
-                const BC *b_part = b0 + part, *c_part = c0 + part;
+                const PieceRows<BC> bc(rows + 64 * fresh(n0 / 4));
                 float h[kPiece + 1][kPart], decay[kPiece][kPart];
-                const f32x4 before = *reinterpret_cast<const f32x4 *>(saved + 64 * n0 + 4 * lane);
+                const f32x4 before = next_states;
+                next_states = *reinterpret_cast<const f32x4 *>((n0 + kPart < NP ? saved + 64 * (n0 + kPart) : saved_of<NP, SL>(k, at, before_t / kPiece)) + 4 * lane);
 #pragma unroll
                 for (int n = 0; n < kPart; ++n) h[0][n] = before[n];
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i) {
-                    float bs[kPart];
-                    load_shared<BC, kPart>(b_part, k.bt, i, left, bs);
                     const float u = d[i] * xi[i];
 #pragma unroll
                     for (int n = 0; n < kPart; ++n) {
                         decay[i][n] = __builtin_amdgcn_exp2f(d[i] * A[n0 + n]);
-                        h[i + 1][n] = fmaf(decay[i][n], h[i][n], u * bs[n]);
+                        h[i + 1][n] = fmaf(decay[i][n], h[i][n], u * bc.get(i, 0, n));
                     }
                 }
 #pragma unroll
                 for (int i = kPiece - 1; i >= 0; --i) {
-                    float bs[kPart], cs[kPart], of_b[kPart], of_c[kPart];
-                    load_shared<BC, kPart>(b_part, k.bt, i, left, bs);
-                    load_shared<BC, kPart>(c_part, k.ct, i, left, cs);
+                    float of_b[kPart], of_c[kPart];
                     const float u = d[i] * xi[i];
 #pragma unroll
                     for (int n = 0; n < kPart; ++n) {
-                        const float lambda = fmaf(cs[n], g[i], mu[n0 + n]);
+                        const float lambda = fmaf(bc.get(i, 1, n), g[i], mu[n0 + n]);
                         of_c[n] = g[i] * h[i + 1][n];
                         of_b[n] = u * lambda;
-                        through[i] = fmaf(bs[n], lambda, through[i]);
+                        through[i] = fmaf(bc.get(i, 0, n), lambda, through[i]);
                         mu[n0 + n] = decay[i][n] * lambda;
                         const float m = mu[n0 + n] * h[i][n];
                         rate[i] = fmaf(m, A[n0 + n], rate[i]);
@@ -302,6 +323,10 @@ hipError_t launch_selective_backward(const esrnn_selective_shape &s, const Selec
             selective_back_maps_kernel<E, BC, NP, SL><<<dim3(lines * (p.segments - 1)), 64 * SL, 0, st>>>(k);
             if (const hipError_t stopped = launch_selective_carry(s, p, k, true, st); stopped != hipSuccess) return stopped;
         }
+        const long long count = (long long)s.B * p.pieces * s.G * p.padded / 4 * 64;
+        selective_arrange_kernel<E, BC><<<dim3((unsigned)((count + 255) / 256)), 256, 0, st>>>(
+            k, static_cast<const E *>(a.b), static_cast<const E *>(a.c), s.b_stride[0], s.b_stride[1], s.c_stride[0], s.c_stride[1], p.padded / 4, count,
+            static_cast<BC *>(const_cast<void *>(k.arranged)));
         selective_backward_kernel<E, BC, NP, SL><<<dim3(lines * p.segments), 64 * SL, 0, st>>>(k);
         return hipGetLastError();
     });

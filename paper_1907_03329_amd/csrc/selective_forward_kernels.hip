@@ -363,6 +363,7 @@ SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse)
     p.maps = p.segments > 1 ? (size_t)s.B * p.segments * tiles * p.slices * (p.states + 1) * 64 : 0;
     p.rows = 2 * (size_t)s.B * s.T * s.G * p.padded;
     if (reverse) {
+        p.arranged = (size_t)s.B * p.pieces * s.G * p.padded / 4 * 64;      // (or half of it in bf16)
         p.part_rows = (size_t)p.tiles * s.B * p.pieces * kPiece * s.G * 2 * p.padded;
         p.part_sums = (size_t)s.B * p.segments * tiles * p.slices * (p.states + 2) * 64;
     }
@@ -374,7 +375,7 @@ size_t selective_workspace_floats(const esrnn_selective_shape &s, bool reverse)
     // (the two passes cut sequences in ways of their own)
     const auto floats = [&](bool which) {
         const SelectivePlan p = selective_plan(s, which);
-        return 64 + p.maps + p.rows + p.part_rows + p.part_sums;
+        return 64 + p.maps + p.rows + p.arranged + p.part_rows + p.part_sums;
     };
     return reverse ? std::max(floats(false), floats(true)) : floats(false);
 }
@@ -402,7 +403,7 @@ Scan scan_arguments(const esrnn_selective_shape &s, const SelectiveArgs &a, Sele
     k.group_channels = s.C / s.G, k.tiles = p.tiles, k.pieces = p.pieces, k.segments = p.segments, k.span = p.span, k.carried = p.carried;
     k.maps = a.workspace;
     float *rows = a.workspace + p.maps;
-    k.part_rows = rows + p.rows, k.part_sums = k.part_rows + p.part_rows;
+    k.arranged = rows + p.rows, k.part_rows = rows + p.rows + p.arranged, k.part_sums = k.part_rows + p.part_rows;
     p.widened = !(shared_as_given(s, p, a.b, s.b_stride) && shared_as_given(s, p, a.c, s.c_stride));
     if (p.widened) {
         const long long position = (long long)s.G * p.padded, sequence = s.T * position;

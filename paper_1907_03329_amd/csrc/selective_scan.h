@@ -31,7 +31,7 @@ struct SelectivePlan {
     bool widened;                       // b and c are copied to fp32 rows of `padded` states first
     bool carried;                       // the maps of segments are put together by a launch of their own
     int line_waves;                     // forward, a workgroup for a whole sequence of a tile's channels: its waves, or 0
-    size_t maps, rows, part_rows, part_sums;    // floats of the workspace: maps of segments, widened b and c, partial gradients of b and c, of A, D and bias
+    size_t maps, rows, arranged, part_rows, part_sums;  // floats of the workspace: maps of segments, widened b and c, both by pieces, partial gradients of b and c, of A, D and bias
 };
 SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse);
 
@@ -41,6 +41,7 @@ struct Scan {
     long long xb, xt, db, dt, ob, ot;   // strides of a sequence and of a position
     long long bb, bt, cb, ct, group;    // of rows of b and c, and of a group in both
     long long gb, gt, gxb, gxt, gdb, gdt;
+    const void *arranged;               // in the reverse pass: b and c by pieces and fours of states, [..][8 positions][4 of b, 4 of c]
     float *maps, *part_rows, *part_sums;
     int B, T, C, N, G;
     bool softplus, carried;
@@ -128,6 +129,29 @@ __device__ __forceinline__ void complete(float (&v)[N], int from = 0, int count 
     for (int i = 0; i < N; ++i)
         if (i >= from && i < from + count) asm volatile("" : "+v"(v[i]));
 }
+
+// Four states of b and c at the eight positions of a piece, [8][4 of b, 4 of c] in memory: few wide loads, as every wait for the scalar cache is one for all
+// that is under way.
+template <class BC>
+struct PieceRows {
+    static constexpr int kLoads = 4 * (int)sizeof(BC) / 4;
+    typedef unsigned Whole __attribute__((ext_vector_type(16), aligned(4)));
+    Whole w[kLoads];
+    __device__ __forceinline__ explicit PieceRows(const BC *p)
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) w[i] = *(Constant<Whole> *)(uintptr_t)(p + i * (64 / sizeof(BC)));
+    }
+    // of position i, b (0) or c (1), state n
+    __device__ __forceinline__ float get(int i, int which, int n) const
+    {
+        const int at = 8 * i + 4 * which + n;
+        // (a copy first: the builtin takes an element of a vector for the vector's first)
+        unsigned bits = sizeof(BC) == 4 ? w[at / 16][at % 16] : w[at / 32][at / 2 % 16];
+        if (sizeof(BC) == 2) bits = at & 1 ? bits & 0xffff0000u : bits << 16;
+        return __builtin_bit_cast(float, bits);
+    }
+};
 
 // The elements of one channel at eight positions; behind the sequence's last one that one again.
 template <class E>
