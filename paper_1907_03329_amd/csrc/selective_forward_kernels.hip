@@ -209,19 +209,27 @@ __global__ void __launch_bounds__(64 * kWaves) selective_line_kernel(Scan k)
             if (4 * wave + r < k.N) k.a.last[own + 4 * wave + r] = carry[r];
 }
 
-// A wave has a run of neighbouring segments, in their order or against it, and four states of 64 channels: first the run's own map, then, behind those
-// of the runs before it, what enters each of its segments.
-constexpr int kRuns = 16;
-template <int NP, int SL>
-__global__ void __launch_bounds__(64 * kRuns) selective_carry_kernel(Scan k, int reverse)
+// A lane has a run of neighbouring segments, in their order or against it, and four states of a channel: first the run's own map, then, behind those of the
+// runs before it, what enters each of its segments.  A workgroup has kColumns channels, 64 and 16 runs or, where segments are many, 8 and 128 runs: maps stay
+// in registers between the two where a run has no more than kBatch.  That is the rule between both, for it is reads that bound this: 1 x 65536 x 256, 1024
+// segments, whole forward pass 202 us with 64 channels, of which one compute unit reads the maps of 64 channels for four states, and 160 with 8; 4 x 4096 x 2048,
+// 86 segments, 275 and 363, as every read is an eighth of a row.
+constexpr int kCarryWaves = 16, kBatch = 8;
+template <int NP, int SL, int kColumns>
+__global__ void __launch_bounds__(64 * kCarryWaves) selective_carry_kernel(Scan k, int reverse)
 {
-    __shared__ __attribute__((aligned(16))) f32x4 s_local[kRuns][64];
-    __shared__ float s_sum[kRuns][64];
-    const int lane = threadIdx.x & 63, run = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int quad = blockIdx.x % (NP / 4), slice = blockIdx.x / (NP / 4) % SL;
-    const unsigned line = blockIdx.x / (NP / 4 * SL);
+    constexpr int kWaveRuns = 64 / kColumns, kRuns = kCarryWaves * kWaveRuns;
+    __shared__ __attribute__((aligned(16))) f32x4 s_local[kCarryWaves][kColumns];
+    __shared__ float s_sum[kCarryWaves][kColumns];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int column = lane % kColumns, wave_run = lane / kColumns, run = wave * kWaveRuns + wave_run;
+    unsigned rest = blockIdx.x;
+    const int in_tile = rest % kWaveRuns * kColumns + column;
+    rest /= kWaveRuns;
+    const int quad = rest % (NP / 4), slice = rest / (NP / 4) % SL;
+    const unsigned line = rest / (NP / 4 * SL);
     const int tiles = k.G * k.tiles, tile = line % tiles, b = line / tiles;
-    const int in_group = tile % k.tiles * 64 + lane, channel = tile / k.tiles * k.group_channels + min(in_group, k.group_channels - 1);
+    const int in_group = tile % k.tiles * 64 + in_tile, channel = tile / k.tiles * k.group_channels + min(in_group, k.group_channels - 1);
     const unsigned lane_mask = in_group < k.group_channels ? 0xffffffffu : 0u;
     const int length = k.a.lengths ? min(max(__builtin_amdgcn_readfirstlane(k.a.lengths[b]), 0), k.T) : k.T;
     const int last_segment = max(length - 1, 0) / (k.span * kPiece);
@@ -242,14 +250,13 @@ __global__ void __launch_bounds__(64 * kRuns) selective_carry_kernel(Scan k, int
         return h;
     };
     // kBatch maps from number p on; those that a run has not are the map that changes nothing
-    constexpr int kBatch = 8;
     f32x4 local[kBatch];
     float sum[kBatch];
     const auto read = [&](int p) {
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const float *map = place(min(p + i, k.segments - 1));
-            local[i] = *reinterpret_cast<const f32x4 *>(map + 256 * quad + 4 * lane), sum[i] = map[64 * NP + lane];
+            local[i] = *reinterpret_cast<const f32x4 *>(map + 256 * quad + 4 * in_tile), sum[i] = map[64 * NP + in_tile];
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
@@ -261,13 +268,32 @@ __global__ void __launch_bounds__(64 * kRuns) selective_carry_kernel(Scan k, int
     };
     f32x4 h = {};
     float total = 0.0f;
-    for (int p = from; p < to; p += kBatch) {
-        read(p);
+    for (int p = 0; p < each; p += kBatch) {
+        read(from + p);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) h = apply(h, local[i], sum[i]), total += sum[i];
     }
-    s_local[run][lane] = h;
-    s_sum[run][lane] = total;
+    // the runs of a wave: each one's map behind those before it, and then only those before it
+    const auto from_before = [&](float v, int off) {
+        const float other = __shfl_up(v, off, 64);      // (of all lanes, so outside the condition)
+        return masked(other, lane >= off ? 0xffffffffu : 0u);
+    };
+#pragma unroll
+    for (int off = kColumns; off < 64; off *= 2) {
+        f32x4 before;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) before[r] = from_before(h[r], off);
+        const float sum_before = from_before(total, off);
+        h = apply(before, h, total), total += sum_before;
+    }
+    if (wave_run == kWaveRuns - 1) s_local[wave][column] = h, s_sum[wave][column] = total;
+    f32x4 in_wave = {};
+    float sum_in_wave = 0.0f;
+    if constexpr (kWaveRuns > 1) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) in_wave[r] = from_before(h[r], kColumns);
+        sum_in_wave = from_before(total, kColumns);
+    }
     __syncthreads();
     const float *first = reverse ? k.a.grad_last : k.a.initial;
     h = f32x4{};
@@ -277,12 +303,13 @@ __global__ void __launch_bounds__(64 * kRuns) selective_carry_kernel(Scan k, int
             const int n = NP * slice + 4 * quad + r;
             h[r] = masked(first[((size_t)b * k.C + channel) * k.N + min(n, k.N - 1)], n < k.N ? lane_mask : 0u);
         }
-    for (int r = 0; r < run; ++r) h = apply(h, s_local[r][lane], s_sum[r][lane]);
-    for (int p = from; p < to; p += kBatch) {
-        read(p);
+    for (int r = 0; r < wave; ++r) h = apply(h, s_local[r][column], s_sum[r][column]);
+    if constexpr (kWaveRuns > 1) h = apply(h, in_wave, sum_in_wave);
+    for (int p = 0; p < each; p += kBatch) {
+        if (each > kBatch) read(from + p);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            if (p + i < to) *reinterpret_cast<f32x4 *>(place(p + i) + 256 * quad + 4 * lane) = h;
+            if (from + p + i < to) *reinterpret_cast<f32x4 *>(place(from + p + i) + 256 * quad + 4 * in_tile) = h;
             h = apply(h, local[i], sum[i]);
         }
     }
@@ -308,14 +335,16 @@ __global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E
 
 }  // namespace
 
-// From how many segments on their maps are put together by a launch of their own (12 us and 0.035 for each), and not by every wave (0.08 us for each).
+// From how many segments on their maps are put together by a launch of their own (8 us), and not by every wave (0.08 us for each).
 constexpr int kSegmentsAlone = 32;
 
 // How many segments a sequence is cut into, by what its launches take in microseconds, fitted to what they took at 16 states: a piece takes what one wave needs
 // for it and what the other waves of its SIMD need, a wave something to begin with, and a share of the maps before its own; the reverse kernel, of which a
-// SIMD holds two waves, takes whole rounds of them, and leaves sums for every wave.  4 x 4096 x 2048 bf16: forward 371 us with 16 segments, 292 with 32, 278
-// with 40; reverse 633 with 16, 603 with 32, 701 with 24.  1 x 65536 x 256: forward 213 with 512, 198 with 1024, 210 with 1280; reverse 354 with 512, 371 with
-// 1024.  501 x 240 x 50 ragged fp32: forward 91 with 4, 87 with 8, 126 with 30; reverse 139 with 5, 169 with 8, 222 with 30.
+// SIMD holds two waves, takes whole rounds of them, and leaves sums for every wave.  Measured, * what this takes:
+//   4 x 4096 x 2048 bf16   forward 371 us with 16 segments, 291 with 32, 275 with 86, 288 with 103*; reverse 543 with 16, 661 with 20, 511 with 32*, 502 with 64
+//   1 x 65536 x 256 bf16   forward 185 with 512, 160 with 1024, 164 with 2048*; reverse 315 with 512, 295 with 1024*, 323 with 1280
+//   1 x 3000 x 256 bf16    forward 43 with 96, 33 with 188*, 35 with 375; reverse 78 with 96, 59 with 188*, 53 with 375
+//   16 x 1024 x 1024 bf16  reverse 282 with 8, 272 with 16*, 306 with 20
 static int best_segments(long long lines, int pieces, bool reverse, double &least)
 {
     int best = 1;
@@ -326,7 +355,7 @@ static int best_segments(long long lines, int pieces, bool reverse, double &leas
         const double rounds = std::floor(waves / 2), rest = waves - 2 * rounds, share = cut > kSegmentsAlone ? 0.0 : 0.08 * cut;
         double time = reverse ? (rounds + (rest > 1 ? 1.0 : rest > 0 ? 0.6 : 0.0)) * (13.8 * span + 3.0 + share) + 2.4 * waves
                               : 2.8 * span + waves * (1.9 * span + 1.2 + share);
-        if (cut > 1) time += 2.2 * span + maps * (span * (reverse ? 1.8 : 1.5) + 1.2) + 4.0 + (cut > kSegmentsAlone ? 12.0 + 0.035 * cut : 0.0);
+        if (cut > 1) time += 2.2 * span + maps * (span * (reverse ? 1.8 : 1.5) + 1.2) + 4.0 + (cut > kSegmentsAlone ? 8.0 : 0.0);
         if (time < least) least = time, best = segments;
     }
     return best;
@@ -434,7 +463,9 @@ hipError_t launch_selective_carry(const esrnn_selective_shape &s, const Selectiv
     const unsigned lines = (unsigned)(s.B * s.G * p.tiles);
     const auto launch = [&](auto states, auto slices) {
         constexpr int NP = decltype(states)::value, SL = decltype(slices)::value;
-        selective_carry_kernel<NP, SL><<<dim3(lines * SL * (NP / 4)), 64 * kRuns, 0, st>>>(k, reverse);
+        const unsigned columns = lines * SL * (NP / 4);
+        if (p.segments > kCarryWaves * kBatch) selective_carry_kernel<NP, SL, 8><<<dim3(columns * 8), 64 * kCarryWaves, 0, st>>>(k, reverse);
+        else selective_carry_kernel<NP, SL, 64><<<dim3(columns), 64 * kCarryWaves, 0, st>>>(k, reverse);
         return hipGetLastError();
     };
     if (p.slices == 4) return launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});

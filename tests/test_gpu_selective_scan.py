@@ -102,6 +102,13 @@ def test_many_lines_and_segments():
     check(1, 1000, 30, 40, lengths=[777], initial=True, seed=6)
 
 
+@pytest.mark.parametrize("T,C,N,groups,lengths", [(2000, 64, 16, 1, None), (3000, 140, 8, 2, None), (2600, 9, 20, 1, [1500, 2600]), (12000, 20, 4, 1, None),
+                                                  (12000, 70, 16, 1, [11003])])
+def test_segments_by_the_hundred(T, C, N, groups, lengths):
+    """Maps of many segments are put together by a launch of their own, in runs of neighbours, ends of sequences among them."""
+    check(len(lengths or [0]), T, C, N, groups, lengths=lengths, initial=True, seed=7)
+
+
 def test_step_sizes_from_nothing_to_large():
     """softplus from where it is e^v to where it is v, element by element, as the output of one position that begins at zero: d b c x."""
     import torch
