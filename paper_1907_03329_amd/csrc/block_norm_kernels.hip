@@ -1,12 +1,16 @@
 // Block norm: gate, norm behind a block, residual, norm before the next block, for every row by itself (include/esrnn_state_space.h).
 //
 // A row is held in registers by L lanes of a wave, or by one or several whole waves, whose sums go through LDS; a workgroup takes rows one behind
-// the other (in reverse each is requested while the one before is worked on), so that a lane's weights are read once, and so that the gradients of the weights add up in its registers.  Forward, with act = silu(gate):
+// the other (in reverse each is requested while the one before is worked on), so that a lane's weights are read once, and so that the gradients of the
+// weights add up in its registers.  Forward, with act = silu(gate):
 //   v = y act | y,  r1 = 1 / sqrt(mean v^2 + eps),  p = v r1 post,  e = p act | p,  s = residual + scale e,  r2 = 1 / sqrt(mean s^2 + eps),  out = s r2 pre.
 // Reverse, with that = s r2, vhat = v r1 and the gradients D of out and S of sum:
 //   ds = S + r2 (D pre - that mean(D pre that)),  de = ds scale,  dp = de act | de,  dv = r1 (dp post - vhat mean(dp post vhat)),  dy = dv act | dv,
 //   dgate = silu'(gate) (dv y | de p),  dpre = sum D that,  dscale = sum ds e,  dpost = sum dp vhat.
 // The reverse pass computes s again from the residual, in fp32, rather than read the rounded sum.
+//
+// Reads and writes are the bound, every operand once: 32768 rows of 2048, bf16, gate and both norms, forward 137-144 us (673 MB, 4.8 TB/s), reverse 226-256 + 5 us
+// (1089 MB, 4.5 TB/s); 120240 rows of 50, fp32, 21 and 28 + 5 us.
 #include <algorithm>
 #include <limits>
 
@@ -297,7 +301,7 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
 }
 
 // Rows of more channels than registers hold with all that is made of them: every one of the three steps (the sum for the second norm, that for the first, the
-// gradients) reads the row again, from the caches, and the sums over rows are in LDS.  4000 rows of 8192 channels, bf16: some 250 us of 102 at the rate of a copy.
+// gradients) reads the row again, from the caches, and the sums over rows are in LDS.  4000 rows of 8192 channels, bf16: some 250 us, where 109 would be those of a copy.
 template <class E, class R, class Y>
 __global__ void __launch_bounds__(Y::kThreads) block_norm_wide_backward_kernel(Args p)
 {

@@ -1,4 +1,9 @@
-// Selective scan over whole sequences, forward (include/esrnn_state_space.h; selective_scan.h has the way it is cut up).
+// Selective scan over whole sequences, forward (include/esrnn_state_space.h; selective_scan.h has the way it is cut up):
+//   h_t = exp(d_t A) h_{t-1} + d_t x_t b_t,  out_t = c_t . h_t + D x_t.
+// A state costs a power of two, which takes the vector ALU as long as four other instructions, and four of these, where x, delta and out are six bytes for sixteen
+// states: instructions are the bound, and no matrix instruction fits, for every channel has decays of its own.  4 x 4096 x 2048, 16 states, bf16, 103 segments:
+// maps 110 us, of which the SIMDs issue vector instructions for 104, putting them together 24 (122 MB), outputs 153 (127 of instructions; 336 MB written, of them
+// 268 states for the reverse pass).  1 x 65536 x 256: 160 us in all.  501 x 240 x 50 ragged fp32 in one launch: 67 us.
 #include <algorithm>
 #include <cmath>
 
@@ -214,7 +219,7 @@ __global__ void __launch_bounds__(64 * kWaves) selective_line_kernel(Scan k)
 // in registers between the two where a run has no more than kBatch.  That is the rule between both, for it is reads that bound this: 1 x 65536 x 256, 1024
 // segments, whole forward pass 202 us with 64 channels, of which one compute unit reads the maps of 64 channels for four states, and 160 with 8; 4 x 4096 x 2048,
 // 86 segments, 275 and 363, as every read is an eighth of a row.
-constexpr int kCarryWaves = 16, kBatch = 8;
+constexpr int kCarryWaves = 16, kBatch = 8, kFewColumns = 8;
 template <int NP, int SL, int kColumns>
 __global__ void __launch_bounds__(64 * kCarryWaves) selective_carry_kernel(Scan k, int reverse)
 {
@@ -335,14 +340,14 @@ __global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E
 
 }  // namespace
 
-// From how many segments on their maps are put together by a launch of their own (8 us), and not by every wave (0.08 us for each).
-constexpr int kSegmentsAlone = 32;
+// From how many segments on their maps are put together by a launch of their own (8 us for every kReadOnce), and not by every wave (0.08 us for each).
+constexpr int kSegmentsAlone = 32, kReadOnce = 64 / kFewColumns * kCarryWaves * kBatch;
 
 // How many segments a sequence is cut into, by what its launches take in microseconds, fitted to what they took at 16 states: a piece takes what one wave needs
 // for it and what the other waves of its SIMD need, a wave something to begin with, and a share of the maps before its own; the reverse kernel, of which a
 // SIMD holds two waves, takes whole rounds of them, and leaves sums for every wave.  Measured, * what this takes:
 //   4 x 4096 x 2048 bf16   forward 371 us with 16 segments, 291 with 32, 275 with 86, 288 with 103*; reverse 543 with 16, 661 with 20, 511 with 32*, 502 with 64
-//   1 x 65536 x 256 bf16   forward 185 with 512, 160 with 1024, 164 with 2048*; reverse 315 with 512, 295 with 1024*, 323 with 1280
+//   1 x 65536 x 256 bf16   forward 185 with 512, 160 with 1024*, 164 with 2048; reverse 315 with 512, 295 with 1024*, 323 with 1280
 //   1 x 3000 x 256 bf16    forward 43 with 96, 33 with 188*, 35 with 375; reverse 78 with 96, 59 with 188*, 53 with 375
 //   16 x 1024 x 1024 bf16  reverse 282 with 8, 272 with 16*, 306 with 20
 static int best_segments(long long lines, int pieces, bool reverse, double &least)
@@ -355,7 +360,7 @@ static int best_segments(long long lines, int pieces, bool reverse, double &leas
         const double rounds = std::floor(waves / 2), rest = waves - 2 * rounds, share = cut > kSegmentsAlone ? 0.0 : 0.08 * cut;
         double time = reverse ? (rounds + (rest > 1 ? 1.0 : rest > 0 ? 0.6 : 0.0)) * (13.8 * span + 3.0 + share) + 2.4 * waves
                               : 2.8 * span + waves * (1.9 * span + 1.2 + share);
-        if (cut > 1) time += 2.2 * span + maps * (span * (reverse ? 1.8 : 1.5) + 1.2) + 4.0 + (cut > kSegmentsAlone ? 8.0 : 0.0);
+        if (cut > 1) time += 2.2 * span + maps * (span * (reverse ? 1.8 : 1.5) + 1.2) + 4.0 + (cut > kSegmentsAlone ? 8.0 * ((cut + kReadOnce - 1) / kReadOnce) : 0.0);
         if (time < least) least = time, best = segments;
     }
     return best;
@@ -464,7 +469,7 @@ hipError_t launch_selective_carry(const esrnn_selective_shape &s, const Selectiv
     const auto launch = [&](auto states, auto slices) {
         constexpr int NP = decltype(states)::value, SL = decltype(slices)::value;
         const unsigned columns = lines * SL * (NP / 4);
-        if (p.segments > kCarryWaves * kBatch) selective_carry_kernel<NP, SL, 8><<<dim3(columns * 8), 64 * kCarryWaves, 0, st>>>(k, reverse);
+        if (p.segments > kCarryWaves * kBatch) selective_carry_kernel<NP, SL, kFewColumns><<<dim3(columns * (64 / kFewColumns)), 64 * kCarryWaves, 0, st>>>(k, reverse);
         else selective_carry_kernel<NP, SL, 64><<<dim3(columns), 64 * kCarryWaves, 0, st>>>(k, reverse);
         return hipGetLastError();
     };

@@ -3,8 +3,7 @@
 //
 // A lane has one channel with its N states in registers (up to 16; a channel of more has two or four lanes of as many waves, the slices), so a
 // wave has 64 channels, and what all of them share, b and c of a position, comes through the scalar cache into scalar registers: the vector
-// ALU takes it from there in the instruction that needs it.  Nothing is summed over lanes but the
-// gradients of b and c.
+// ALU takes it from there in the instruction that needs it.  Nothing is summed over lanes but the gradients of b and c.
 //
 // A sequence is cut into segments, which are as many waves: with a_t = exp(d_t A) a segment's map is h -> exp(A sum d) h + (its own last state from
 // zero), so a first launch leaves the last states and sums of d of all segments, and a second one has every segment put together the maps before its
@@ -31,7 +30,8 @@ struct SelectivePlan {
     bool widened;                       // b and c are copied to fp32 rows of `padded` states first
     bool carried;                       // the maps of segments are put together by a launch of their own
     int line_waves;                     // forward, a workgroup for a whole sequence of a tile's channels: its waves, or 0
-    size_t maps, rows, arranged, part_rows, part_sums;  // floats of the workspace: maps of segments, widened b and c, both by pieces, partial gradients of b and c, of A, D and bias
+    // floats of the workspace: maps of segments, widened b and c, both by pieces, partial gradients of b and c, of A, D and bias
+    size_t maps, rows, arranged, part_rows, part_sums;
 };
 SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse);
 
