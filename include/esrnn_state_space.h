@@ -35,7 +35,7 @@ extern "C" {
 /*
  * Short causal convolution of every channel with K taps of its own, 2 <= K <= 8, over T positions of B sequences:
  *   u_t = bias + sum_{j < K} weight[j] x_{t-K+1+j},   out = u  or  u sigmoid(u)      (esrnn_norm_activation)
- * The K - 1 inputs before the first position are `initial`, oldest first, or zero.
+ * The K - 1 inputs before the first position are `initial`, oldest first, or zero.  At most 2^24 - 1 tiles of 64 channels of 128 positions of a sequence.
  */
 typedef struct {
     int32_t B, T, C, K;
@@ -77,6 +77,8 @@ esrnn_status esrnn_convolution_step(const esrnn_convolution_step_shape *shape, c
  * channels.  For a channel of group g, with d = softplus(delta + bias) or delta + bias:
  *   h_t[n] = exp(d_t A[n]) h_{t-1}[n] + d_t x_t b_t[g][n],    out_t = sum_n c_t[g][n] h_t[n] + D x_t
  * A is used as it is (rates of decay are negative; minus infinity keeps nothing of a state, but for a step of size zero, which changes nothing).
+ * Operands that exist are finite; an infinity makes its channel's states, or its group's, infinite or NaN from there on.  At most 2^20 lines, of 64 channels of a
+ * sequence and of a group, and 2^15 of them side by side.
  */
 typedef enum { ESRNN_DELTA_SOFTPLUS = 0, ESRNN_DELTA_GIVEN = 1 } esrnn_delta_kind;
 

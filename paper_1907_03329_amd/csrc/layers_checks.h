@@ -1,6 +1,7 @@
 // Argument checks that the entry points of the layer operators share (layers_api.cpp, state_space_api.cpp).
 #pragma once
 
+#include <initializer_list>
 #include <utility>
 
 #include "layers_internal.h"
@@ -70,6 +71,18 @@ template <class S>
 bool rows_overlap(const S &s, const void *written, const int64_t written_stride[2], const void *other, const int64_t other_stride[2])
 {
     return rows_overlap(s, written, written_stride, other, other_stride, s.C);
+}
+// Whether an array that is written begins where another one does.  Null pointers are no arrays.
+inline bool one_place(std::initializer_list<const void *> written, std::initializer_list<const void *> read)
+{
+    for (const void *const *w = written.begin(); w != written.end(); ++w) {
+        if (!*w) continue;
+        for (const void *const *o = w + 1; o != written.end(); ++o)
+            if (*o == *w) return true;
+        for (const void *o : read)
+            if (o == *w) return true;
+    }
+    return false;
 }
 // of fp32 arrays of n and m elements, either of which may be null
 inline bool floats_overlap(const float *a, size_t n, const float *b, size_t m) { return a && b && a < b + m && b < a + n; }

@@ -112,24 +112,24 @@ template <class E, class BC>
 __global__ void __launch_bounds__(256) selective_arrange_kernel(Scan k, const E *b, const E *c, long long bb, long long bt, long long cb, long long ct, int fours,
                                                                 long long count, Vec4<BC> *to)
 {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= count) return;
-    const int which = i & 1, position = i >> 1 & 7;
-    long long rest = i >> 4;
-    const int n = 4 * (int)(rest % fours);
-    rest /= fours;
-    const int group = rest % k.G;
-    rest /= k.G;
-    const int t = (int)(rest % k.pieces) * kPiece + position, s = (int)(rest / k.pieces);
-    const int length = k.a.lengths ? min(max(k.a.lengths[s], 0), k.T) : k.T;
-    const E *from = (which ? c + s * cb + (long long)min(t, k.T - 1) * ct : b + s * bb + (long long)min(t, k.T - 1) * bt) + (long long)group * k.N;
-    Vec4<BC> v;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < count; i += (long long)gridDim.x * 256) {
+        const int which = i & 1, position = i >> 1 & 7;
+        long long rest = i >> 4;
+        const int n = 4 * (int)(rest % fours);
+        rest /= fours;
+        const int group = rest % k.G;
+        rest /= k.G;
+        const int t = (int)(rest % k.pieces) * kPiece + position, s = (int)(rest / k.pieces);
+        const int length = k.a.lengths ? min(max(k.a.lengths[s], 0), k.T) : k.T;
+        const E *from = (which ? c + s * cb + (long long)min(t, k.T - 1) * ct : b + s * bb + (long long)min(t, k.T - 1) * bt) + (long long)group * k.N;
+        Vec4<BC> v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float value = (float)from[min(n + r, k.N - 1)];
-        v[r] = (BC)(n + r < k.N && t < length ? value : 0.0f);
+        for (int r = 0; r < 4; ++r) {
+            const float value = (float)from[min(n + r, k.N - 1)];
+            v[r] = (BC)(n + r < k.N && t < length ? value : 0.0f);
+        }
+        to[i] = v;
     }
-    to[i] = v;
 }
 
 template <class E, class BC, int NP, int SL>
@@ -335,7 +335,7 @@ hipError_t launch_selective_backward(const esrnn_selective_shape &s, const Selec
             if (const hipError_t stopped = launch_selective_carry(s, p, k, true, st); stopped != hipSuccess) return stopped;
         }
         const long long count = (long long)s.B * p.pieces * s.G * p.padded / 4 * 16;
-        selective_arrange_kernel<E, BC><<<dim3((unsigned)((count + 255) / 256)), 256, 0, st>>>(
+        selective_arrange_kernel<E, BC><<<dim3((unsigned)std::min((count + 255) / 256, kCopyWorkgroups)), 256, 0, st>>>(
             k, static_cast<const E *>(a.b), static_cast<const E *>(a.c), s.b_stride[0], s.b_stride[1], s.c_stride[0], s.c_stride[1], p.padded / 4, count,
             static_cast<Vec4<BC> *>(const_cast<void *>(k.arranged)));
         selective_backward_kernel<E, BC, NP, SL><<<dim3(lines * p.segments), 64 * SL, 0, st>>>(k);

@@ -325,17 +325,18 @@ template <class E>
 __global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E *b, const E *c, long long bb, long long bt, long long cb, long long ct, int B,
                                                                          int T, int G, int N, int padded, float *rows)
 {
-    const long long half = (long long)B * T * G * padded, i = (long long)blockIdx.x * kThreadsOfRows + threadIdx.x;
-    if (i >= 2 * half) return;
-    const bool second = i >= half;
-    long long rest = second ? i - half : i;
-    const int n = rest % padded;
-    rest /= padded;
-    const int g = rest % G;
-    rest /= G;
-    const int t = rest % T, s = rest / T;
-    const E *from = second ? c + s * cb + t * ct : b + s * bb + t * bt;
-    rows[i] = n < N ? (float)from[(long long)g * N + n] : 0.0f;
+    const long long half = (long long)B * T * G * padded;
+    for (long long i = (long long)blockIdx.x * kThreadsOfRows + threadIdx.x; i < 2 * half; i += (long long)gridDim.x * kThreadsOfRows) {
+        const bool second = i >= half;
+        long long rest = second ? i - half : i;
+        const int n = rest % padded;
+        rest /= padded;
+        const int g = rest % G;
+        rest /= G;
+        const int t = rest % T, s = rest / T;
+        const E *from = second ? c + s * cb + t * ct : b + s * bb + t * bt;
+        rows[i] = n < N ? (float)from[(long long)g * N + n] : 0.0f;
+    }
 }
 
 }  // namespace
@@ -455,7 +456,7 @@ hipError_t launch_selective_widen(const esrnn_selective_shape &s, const Selectiv
     if (!p.widened) return hipSuccess;
     return with_element(s.dtype, [&](auto e) {
         typedef decltype(e) E;
-        selective_widen_kernel<E><<<dim3((unsigned)((p.rows + kThreadsOfRows - 1) / kThreadsOfRows)), kThreadsOfRows, 0, st>>>(
+        selective_widen_kernel<E><<<dim3((unsigned)std::min<long long>((p.rows + kThreadsOfRows - 1) / kThreadsOfRows, kCopyWorkgroups)), kThreadsOfRows, 0, st>>>(
             static_cast<const E *>(a.b), static_cast<const E *>(a.c), s.b_stride[0], s.b_stride[1], s.c_stride[0], s.c_stride[1], s.B, s.T, s.G, s.N,
             p.padded, const_cast<float *>(static_cast<const float *>(k.b)));
         return hipGetLastError();

@@ -20,6 +20,7 @@
 
 namespace esrnn {
 
+constexpr long long kCopyWorkgroups = 1 << 20;      // at most, of 256 threads, that copy b and c
 constexpr int kPiece = 8;               // positions of a piece; the forward pass leaves the state before each for the reverse pass
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 

@@ -6,7 +6,7 @@ using namespace esrnn;
 
 namespace {
 
-constexpr int64_t kMostWorkgroups = int64_t(1) << 30;
+constexpr int64_t kMostWorkgroups = (int64_t(1) << 24) - 1;     // of 256 threads: a launch has less than 2^32
 
 bool sequences(int64_t B, int64_t T, int64_t C) { return B >= 1 && T >= 1 && C >= 1 && T <= (1 << 30) && C <= (1 << 24) && B <= (1 << 30); }
 bool activation(int kind) { return kind == ESRNN_NORM_NONE || kind == ESRNN_NORM_SILU; }
@@ -22,9 +22,9 @@ bool convolution_sizes(const esrnn_convolution_shape &s)
 bool selective_sizes(const esrnn_selective_shape &s)
 {
     if (!sequences(s.B, s.T, s.C) || s.N < 1 || s.N > 64 || s.G < 1 || s.C % s.G != 0 || !delta(s.delta_kind) || !element_type(s.dtype)) return false;
-    // waves, rows of partial sums for b and c, widened rows: counts of 32 bits; a group's row of states 16 bits' worth of bytes many times over
+    // lines of 64 channels, and their columns of partial sums (up to 72 x 64): workgroups of up to 1024 threads, less than 2^32 in a launch
     const int64_t tiles = (int64_t)s.G * ((s.C / s.G + 63) / 64), positions = (int64_t)s.B * (s.T + 7);
-    return s.G <= (1 << 16) && tiles <= (1 << 20) && (int64_t)s.B * tiles <= (1 << 22) && positions <= (int64_t(1) << 36) / (s.G * int64_t(64)) &&
+    return tiles <= (1 << 15) && (int64_t)s.B * tiles <= (1 << 20) && positions <= (int64_t(1) << 36) / (s.G * int64_t(64)) &&
            (int64_t)s.B * tiles * 64 <= kMostElements / s.T;
 }
 
@@ -87,8 +87,8 @@ esrnn_status esrnn_convolution_forward(const esrnn_convolution_shape *shape, con
     // (windows of all sequences are one row)
     const RowsShape windows{1, 1, (int64_t)s.B * (s.K - 1) * s.C, s.dtype};
     const int64_t none[2] = {0, 0};
-    if (rows_overlap(s, out, s.out_stride, x, s.x_stride) || (last && initial && rows_overlap(windows, last, none, initial, none)) || last == x || last == out ||
-        (initial && out == initial))
+    if (rows_overlap(s, out, s.out_stride, x, s.x_stride) || (last && initial && rows_overlap(windows, last, none, initial, none)) ||
+        one_place({out, last}, {x, lengths, weight, bias, initial}))
         return ESRNN_ERR_CONFIG;
     ConvolutionArgs a{};
     a.x = x, a.lengths = lengths, a.weight = weight, a.bias = bias, a.initial = initial, a.out = out, a.last = last;
@@ -111,7 +111,8 @@ esrnn_status esrnn_convolution_backward(const esrnn_convolution_shape *shape, co
     if (!aligned_to(workspace, 256)) return ESRNN_ERR_WORKSPACE;
     const size_t windows = (size_t)s.B * (s.K - 1) * s.C, taps = (size_t)s.C * s.K;
     if (rows_overlap(s, grad_x, s.grad_x_stride, x, s.x_stride) || rows_overlap(s, grad_x, s.grad_x_stride, grad_out, s.grad_out_stride) ||
-        (initial && grad_x == initial) || floats_overlap(grad_initial, windows, grad_last, windows) || floats_overlap(grad_weight, taps, weight, taps) ||
+        one_place({grad_x, grad_weight, grad_bias, grad_initial, workspace}, {x, lengths, weight, bias, initial, grad_out, grad_last}) ||
+        floats_overlap(grad_initial, windows, grad_last, windows) || floats_overlap(grad_weight, taps, weight, taps) ||
         floats_overlap(grad_bias, s.C, bias, s.C) || floats_overlap(grad_weight, taps, grad_bias, s.C) || floats_overlap(grad_weight, taps, bias, s.C) ||
         floats_overlap(grad_bias, s.C, weight, taps))
         return ESRNN_ERR_CONFIG;
@@ -134,7 +135,7 @@ esrnn_status esrnn_convolution_step(const esrnn_convolution_step_shape *shape, c
     if (!x || !weight || !state || !out) return ESRNN_ERR_NULL;
     if (s.x_stride < 0 || s.out_stride < 0 || s.x_stride > kMostElements / s.rows || s.out_stride > kMostElements / s.rows ||
         (s.rows > 1 && s.out_stride < s.C) || !element_aligned(x, s.dtype) || !element_aligned(out, s.dtype) || !element_aligned(state, s.dtype) ||
-        !floats_aligned(weight) || !floats_aligned(bias) || !floats_aligned(slots) || out == x || state == x || state == out)
+        !floats_aligned(weight) || !floats_aligned(bias) || !floats_aligned(slots) || one_place({state, out}, {x, weight, bias, slots}))
         return ESRNN_ERR_CONFIG;
     ESRNN_TRY(launch_convolution_step(s, x, weight, bias, slots, state, out, static_cast<hipStream_t>(stream)));
     return ESRNN_OK;
@@ -172,7 +173,8 @@ esrnn_status esrnn_selective_forward(const esrnn_selective_shape *shape, const v
     if (!floats_aligned(A) || !floats_aligned(D) || !floats_aligned(bias) || !floats_aligned(lengths) || !floats_aligned(initial) || !floats_aligned(last))
         return ESRNN_ERR_CONFIG;
     if (!aligned_to(workspace, 256) || !aligned_to(saved, 256)) return ESRNN_ERR_WORKSPACE;
-    if (rows_overlap(s, out, s.out_stride, x, s.x_stride) || rows_overlap(s, out, s.out_stride, delta, s.delta_stride) ||
+    if (one_place({out, last, saved, workspace}, {x, delta, A, b, c, D, bias, lengths, initial}) || rows_overlap(s, out, s.out_stride, x, s.x_stride) ||
+        rows_overlap(s, out, s.out_stride, delta, s.delta_stride) ||
         rows_overlap(s, out, s.out_stride, b, s.b_stride, shared.C) || rows_overlap(s, out, s.out_stride, c, s.c_stride, shared.C) ||
         floats_overlap(last, states_of(s), initial, states_of(s)) || floats_overlap(last, states_of(s), A, (size_t)s.C * s.N))
         return ESRNN_ERR_CONFIG;
@@ -211,6 +213,8 @@ esrnn_status esrnn_selective_backward(const esrnn_selective_shape *shape, const 
     for (const auto &w : arrays)
         for (const auto &o : arrays)
             if (w.written && &w != &o && rows_overlap(w.rows, w.p, w.stride, o.p, o.stride, o.rows.C)) return ESRNN_ERR_CONFIG;
+    if (one_place({g.x, g.delta, g.b, g.c, g.A, g.D, g.bias, g.initial, workspace}, {x, delta, A, b, c, D, bias, lengths, saved, grad_out, grad_last}))
+        return ESRNN_ERR_CONFIG;
     const size_t n = states_of(s), rates = (size_t)s.C * s.N, channels = s.C;
     if (floats_overlap(g.initial, n, grad_last, n) || floats_overlap(g.A, rates, A, rates) || floats_overlap(g.D, channels, D, channels) ||
         floats_overlap(g.bias, channels, bias, channels) || floats_overlap(g.D, channels, g.bias, channels) || floats_overlap(g.A, rates, g.D, channels) ||
@@ -240,8 +244,7 @@ esrnn_status esrnn_selective_step(const esrnn_selective_step_shape *shape, const
         if (stride < 0 || stride > kMostElements / s.rows) return ESRNN_ERR_CONFIG;
     for (const void *p : {x, delta_, b, c, static_cast<const void *>(out)})
         if (!element_aligned(p, s.dtype)) return ESRNN_ERR_CONFIG;
-    for (const void *p : {x, delta_, b, c})
-        if (p == out) return ESRNN_ERR_CONFIG;
+    if (one_place({state, out}, {x, delta_, A, b, c, D, bias, slots})) return ESRNN_ERR_CONFIG;
     if ((s.rows > 1 && s.out_stride < s.C) || !floats_aligned(A) || !floats_aligned(D) || !floats_aligned(bias) || !floats_aligned(slots) || !floats_aligned(state))
         return ESRNN_ERR_CONFIG;
     const SelectiveStep a{x, delta_, b, c, A, D, bias, slots, state, out};
@@ -276,7 +279,8 @@ esrnn_status esrnn_block_norm_forward(const esrnn_block_norm_shape *shape, const
     if (const esrnn_status e = check_rows(s, with_sum, 4, false); e != ESRNN_OK) return e;
     const Rows residual_and_sum[] = {rows[2], rows[4]};
     if (const esrnn_status e = check_rows(s, residual_and_sum, 2, true); e != ESRNN_OK) return e;
-    if (!floats_aligned(in->exists) || !floats_aligned(in->post_weight) || !floats_aligned(in->scale) || !floats_aligned(in->pre_weight) || !floats_aligned(stats))
+    if (!floats_aligned(in->exists) || !floats_aligned(in->post_weight) || !floats_aligned(in->scale) || !floats_aligned(in->pre_weight) || !floats_aligned(stats) ||
+        one_place({sum, out, stats}, {in->y, in->gate, sum == in->residual ? nullptr : in->residual, in->exists, in->post_weight, in->scale, in->pre_weight}))
         return ESRNN_ERR_CONFIG;
     BlockNormArgs a{};
     a.y = in->y, a.gate = in->gate, a.residual = in->residual, a.exists = in->exists;
@@ -305,7 +309,10 @@ esrnn_status esrnn_block_norm_backward(const esrnn_block_norm_shape *shape, cons
                          {g.gate, s.grad_gate_stride, s.dtype, true}, {g.residual, s.grad_residual_stride, s.stream_dtype, true}};
     if (const esrnn_status e = check_rows(s, rows, 8, false); e != ESRNN_OK) return e;
     const float *weights[] = {in->post_weight, in->scale, in->pre_weight}, *sums[] = {g.post_weight, g.scale, g.pre_weight};
-    if (!floats_aligned(in->exists) || !floats_aligned(stats)) return ESRNN_ERR_CONFIG;
+    if (!floats_aligned(in->exists) || !floats_aligned(stats) ||
+        one_place({g.y, g.gate, g.residual, g.post_weight, g.scale, g.pre_weight, workspace},
+                  {in->y, in->gate, in->residual, in->exists, in->post_weight, in->scale, in->pre_weight, stats, grad_out, grad_sum}))
+        return ESRNN_ERR_CONFIG;
     for (int i = 0; i < 3; ++i) {
         if (!floats_aligned(weights[i]) || !floats_aligned(sums[i])) return ESRNN_ERR_CONFIG;
         for (int j = 0; j < 3; ++j)

@@ -287,6 +287,48 @@ def test_block_norm_arguments_that_are_refused(lib):
     assert block_backward(lib, ok, grads={"scale": GRADS["post_weight"]}) == CONFIG and block_backward(lib, ok, grads={"gate": GRADS["y"]}) == CONFIG
 
 
+# ---- arrays of different kinds at one place, and sizes that no launch has ----
+def test_arrays_at_one_place_are_refused(lib):
+    c, s, n = conv(), select(), block()
+    for written, read in ((dict(out=P[1]), "weight"), (dict(out=P[2]), "bias"), (dict(last=P[1]), "weight"), (dict(last=P[0]), "x"), (dict(last=P[4]), "out")):
+        assert conv_forward(lib, c, **written) == CONFIG, read
+    for written in (dict(gx=P[1]), dict(gx=P[7]), dict(gw=P[0]), dict(gw=P[6]), dict(gi=P[3]), dict(gi=P[9]), dict(ws=P[0]), dict(ws=P[8])):
+        assert conv_backward(lib, c, **written) == CONFIG, written
+    for written in (dict(out=P[2]), dict(last=P[0]), dict(last=P[8]), dict(saved=P[0]), dict(saved=P[7]), dict(saved=P[11]), dict(ws=P[2]), dict(ws=P[8])):
+        assert select_forward(lib, s, **written) == CONFIG, written
+    for at in (P[7], P[8], P[11]):
+        assert select_backward(lib, s, ws=at) == CONFIG
+    places = dict(x=P[11], delta=P[12], b=P[13], c=P[14], A=P[15], D=odd(P[15], 1 << 30), bias=odd(P[15], 1 << 31), initial=odd(P[15], 1 << 32))
+    for name, at in (("x", P[7]), ("A", P[9]), ("b", P[2]), ("D", P[6]), ("bias", P[5]), ("initial", P[7]), ("c", P[10]), ("delta", P[4])):
+        g = ss.SelectiveGrads(**values(places | {name: at}))
+        assert lib.esrnn_selective_backward(C.byref(s), *P[:7], None, P[7], P[8], P[9], C.byref(g), P[10], None) == CONFIG, name
+    for written in (dict(stats=P[0]), dict(stats=P[2]), dict(stats=P[5]), dict(stats=P[7]), dict(out=P[3]), dict(sum=P[4])):
+        assert block_forward(lib, n, **written) == CONFIG, written
+    for at in (P[0], P[3], P[6], P[7], P[8], P[9], P[12]):
+        assert block_backward(lib, n, ws=at) == CONFIG
+    assert block_backward(lib, n, grads={"y": P[8]}) == CONFIG and block_backward(lib, n, grads={"scale": P[6]}) == CONFIG
+    step = ss.SelectiveStepShape(2, 4, 8, 4, 2, 0, 0, 8, 8, 8, 8, 8)
+    for state in (*P[:8], P[9]):
+        assert lib.esrnn_selective_step(C.byref(step), *P[:8], state, P[9], None) == CONFIG
+    for out in P[:8]:
+        assert lib.esrnn_selective_step(C.byref(step), *P[:8], P[8], out, None) == CONFIG
+    step = ss.ConvolutionStepShape(2, 4, 8, 4, 1, 0, 8, 8)
+    for state, out in ((P[0], P[5]), (P[1], P[5]), (P[2], P[5]), (P[3], P[5]), (P[4], P[4]), (P[4], P[0]), (P[4], P[1]), (P[4], P[2]), (P[4], P[3])):
+        assert lib.esrnn_convolution_step(C.byref(step), *P[:4], state, out, None) == CONFIG
+
+
+def test_launches_have_fewer_than_2_to_the_32_threads(lib):
+    n = C.c_size_t()
+    for most, more in ((dict(B=(1 << 24) - 1, T=3, C_=5), dict(B=1 << 24, T=3, C_=5)), (dict(B=1, T=128, C_=1 << 24), dict(B=64, T=129, C_=1 << 24)),
+                       (dict(B=1 << 23, T=1, C_=64), dict(B=1 << 23, T=1, C_=65))):
+        assert lib.esrnn_convolution_workspace_bytes(C.byref(conv(**most)), C.byref(n)) == OK
+        assert lib.esrnn_convolution_workspace_bytes(C.byref(conv(**more)), C.byref(n)) == CONFIG and conv_forward(lib, conv(**more)) == CONFIG
+    for most, more in ((dict(B=1 << 20, T=1, C_=64), dict(B=(1 << 20) + 1, T=1, C_=64)), (dict(B=1, T=1, C_=64 << 15), dict(B=1, T=1, C_=(64 << 15) + 64)),
+                       (dict(B=1, T=1, C_=1 << 15, G=1 << 15), dict(B=1, T=1, C_=1 << 16, G=1 << 16))):
+        assert lib.esrnn_selective_workspace_bytes(C.byref(select(**most)), 1, C.byref(n)) == OK
+        assert lib.esrnn_selective_workspace_bytes(C.byref(select(**more)), 1, C.byref(n)) == CONFIG and select_forward(lib, select(**more)) == CONFIG
+
+
 def test_null_shapes(lib):
     n = C.c_size_t()
     assert lib.esrnn_selective_workspace_bytes(None, 0, C.byref(n)) == NULL and lib.esrnn_selective_saved_bytes(C.byref(select()), None) == NULL
