@@ -1,6 +1,6 @@
 // Selective scan over whole sequences, forward (include/esrnn_state_space.h; selective_scan.h has the way it is cut up):
 //   h_t = exp(d_t A) h_{t-1} + d_t x_t b_t,  out_t = c_t . h_t + D x_t.
-// A state costs a power of two, which takes the vector ALU as long as four other instructions, and four of these, where x, delta and out are six bytes for sixteen
+// A state costs a power of two, which takes the vector ALU as long as two other instructions, and four of these, where x, delta and out are six bytes for sixteen
 // states: instructions are the bound, and no matrix instruction fits, for every channel has decays of its own.  4 x 4096 x 2048, 16 states, bf16, 103 segments:
 // maps 110 us, of which the SIMDs issue vector instructions for 104, putting them together 24 (122 MB), outputs 153 (127 of instructions; 336 MB written, of them
 // 268 states for the reverse pass).  1 x 65536 x 256: 160 us in all.  501 x 240 x 50 ragged fp32 in one launch: 67 us.
