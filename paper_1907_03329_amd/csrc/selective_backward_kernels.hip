@@ -136,7 +136,6 @@ template <class E, class BC, int NP, int SL>
 __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_kernel(Scan k)
 {
     constexpr int kPart = 4, kPadded = NP * SL;     // (states at a time: theirs at nine positions and their decays at eight take 68 registers)
-    __shared__ float s_sums[SL > 1 ? 2 : 1][SL > 1 ? SL : 1][2 * kPiece][64];
     __shared__ __attribute__((aligned(16))) float s_shared[SL][2 * kPiece][kSumRow];
     const ScanPlace at(k, k.segments);
     const int lane = threadIdx.x & 63;
@@ -161,7 +160,6 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
     float(*shared)[kSumRow] = s_shared[at.slice];
     const float *shared_read = &shared[lane >> 2][4 * (lane & 3)];
 
-    int turn = 0;
     const int last = min(end, at.length);
     if (begin < last) {
         const int top = begin + (last - 1 - begin) / kPiece * kPiece;
@@ -171,7 +169,7 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
         ds.request(delta, k.dt, top, at.length, at.channel);
         gs.request(grad, k.gt, top, at.length, at.channel);
         f32x4 next_states = *reinterpret_cast<const f32x4 *>(saved_of<NP, SL>(k, at, top / kPiece) + 4 * lane);
-        for (int t0 = top; t0 >= begin; t0 -= kPiece, turn ^= 1) {
+        for (int t0 = top; t0 >= begin; t0 -= kPiece) {
             const int t = fresh(t0), left = at.length - 1 - t;
             const float *saved = saved_of<NP, SL>(k, at, t / kPiece);
             const BC *rows = shared_rows + (size_t)(t / kPiece) * k.G * (kPadded / 4 * 64);
@@ -235,16 +233,18 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
                 complete(dA, n0, kPart);
             }
             if constexpr (SL > 1) {
+                // the wave has read its rows: they hold its shares of the sums over all states until every slice has read those of its positions
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) s_sums[turn][at.slice][i][lane] = through[i], s_sums[turn][at.slice][kPiece + i][lane] = rate[i];
-                __syncthreads();
+                for (int i = 0; i < kPiece; ++i) shared[i][lane] = through[i], shared[kPiece + i][lane] = rate[i];
+                lds_barrier();      // (requests for the next piece go on)
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i)
                     if (i % SL == at.slice) {
                         through[i] = rate[i] = 0.0f;
 #pragma unroll
-                        for (int s = 0; s < SL; ++s) through[i] += s_sums[turn][s][i][lane], rate[i] += s_sums[turn][s][kPiece + i][lane];
+                        for (int s = 0; s < SL; ++s) through[i] += s_shared[s][i][lane], rate[i] += s_shared[s][kPiece + i][lane];
                     }
+                lds_barrier();
             }
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) {

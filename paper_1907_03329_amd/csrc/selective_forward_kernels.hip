@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(64 * SL) selective_forward_kernel(Scan k)
             if constexpr (SL > 1) {
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i) s_y[turn][at.slice][i][lane] = y[i];
-                __syncthreads();
+                lds_barrier();      // (requests for the next piece go on)
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i)
                     if (i % SL == at.slice) {
