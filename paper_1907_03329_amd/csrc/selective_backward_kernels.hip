@@ -265,6 +265,14 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
             (grad_x + t * k.gxt)[at.channel] = (E)0.0f;
             (grad_delta + t * k.gdt)[at.channel] = (E)0.0f;
         }
+    if constexpr (SL > 1) {
+        // (every slice has its share of the positions; the first one leaves the sums)
+        shared[0][lane] = dD, shared[1][lane] = dbias;
+        lds_barrier();
+        if (at.slice == 0)
+#pragma unroll
+            for (int s = 1; s < SL; ++s) dD += s_shared[s][0][lane], dbias += s_shared[s][1][lane];
+    }
     float *sums = k.part_sums + ((((size_t)at.b * k.segments + at.segment) * (k.G * k.tiles) + at.tile) * SL + at.slice) * ((NP + 2) * 64);
 #pragma unroll
     for (int n = 0; n < NP; ++n) sums[64 * n + lane] = dA[n];
@@ -289,12 +297,7 @@ __global__ void __launch_bounds__(1024) selective_sum_kernel(Scan k, int states,
             if (n < states) {
                 if (slice * states + n < k.N) k.a.grad_A[(size_t)channel * k.N + slice * states + n] = v;
             } else if (float *to = n == states ? k.a.grad_D : k.a.grad_bias) {
-                // every slice has its share of the positions
-                if (slice == 0) {
-                    for (int s = 1; s < slices; ++s)
-                        for (long long r = 0; r < rows; ++r) v += k.part_sums[r * cols + col + s * wave];
-                    to[channel] = v;
-                }
+                if (slice == 0) to[channel] = v;
             }
         });
         return;
