@@ -341,16 +341,17 @@ __global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E
 
 }  // namespace
 
-// From how many segments on their maps are put together by a launch of their own (8 us for every kReadOnce), and not by every wave (0.08 us for each).
+// From how many segments on their maps are put together by a launch of their own, and not by every wave (0.08 us for each).
 constexpr int kSegmentsAlone = 32, kReadOnce = 64 / kFewColumns * kCarryWaves * kBatch;
 
-// How many segments a sequence is cut into, by what its launches take in microseconds, fitted to what they took at 16 states: a piece takes what one wave needs
-// for it and what the other waves of its SIMD need, a wave something to begin with, and a share of the maps before its own; the reverse kernel, of which a
-// SIMD holds two waves, takes whole rounds of them, and leaves sums for every wave.  Measured, * what this takes:
-//   4 x 4096 x 2048 bf16   forward 371 us with 16 segments, 291 with 32, 275 with 86, 288 with 103*; reverse 543 with 16, 661 with 20, 511 with 32*, 502 with 64
-//   1 x 65536 x 256 bf16   forward 185 with 512, 160 with 1024*, 164 with 2048; reverse 315 with 512, 295 with 1024*, 323 with 1280
-//   1 x 3000 x 256 bf16    forward 43 with 96, 33 with 188*, 35 with 375; reverse 78 with 96, 59 with 188*, 53 with 375
-//   16 x 1024 x 1024 bf16  reverse 282 with 8, 272 with 16*, 306 with 20
+// How many segments a sequence is cut into, by what its launches take in microseconds, fitted to what they took (14 shapes, 1 to 1024 segments): a piece takes
+// what one wave needs for it and what the other waves of its SIMD need, a wave something to begin with, and a share of the maps before its own; the reverse
+// kernel, of which a SIMD holds two waves, takes whole rounds of them, one wave little less than two, and leaves sums for every wave.  Measured in us, * what this takes:
+//   4 x 4096 x 2048 bf16, 16 states    forward 371 with 16 segments, 291 with 32, 275 with 86 and with 103*; reverse 543 with 16, 510 with 32, 499 with 64*
+//   1 x 65536 x 256 bf16, 16 states    forward 185 with 512, 160 with 1024*, 164 with 2048; reverse 315 with 512, 294 with 1024*, 323 with 1280
+//   1 x 3000 x 256 bf16, 16 states     forward 43 with 96, 33 with 188*, 35 with 375; reverse 78 with 96, 59 with 188*, 53 with 375
+//   240 x 122 x 240 bf16, 16 states    reverse 188 with 1, 157 with 2*, 179 with 8
+//   4 x 4096 x 1024 bf16, 32 states    reverse 513 with 16, 578 with 32, 506 with 47, 527 with 64*
 static int best_segments(long long lines, int pieces, bool reverse, double &least)
 {
     int best = 1;
@@ -359,9 +360,10 @@ static int best_segments(long long lines, int pieces, bool reverse, double &leas
         const int span = (pieces + segments - 1) / segments, cut = (pieces + span - 1) / span;
         const double waves = lines * (double)cut / 1024.0, maps = waves * (cut - 1) / cut;      // of a SIMD
         const double rounds = std::floor(waves / 2), rest = waves - 2 * rounds, share = cut > kSegmentsAlone ? 0.0 : 0.08 * cut;
-        double time = reverse ? (rounds + (rest > 1 ? 1.0 : rest > 0 ? 0.6 : 0.0)) * (13.8 * span + 3.0 + share) + 2.4 * waves
+        double time = reverse ? (rounds + (rest > 1 ? 1.0 : rest > 0 ? 0.9 : 0.0)) * (11.5 * span + 3.0 + share) + 1.1 * waves
                               : 2.8 * span + waves * (1.9 * span + 1.2 + share);
-        if (cut > 1) time += 2.2 * span + maps * (span * (reverse ? 1.8 : 1.5) + 1.2) + 4.0 + (cut > kSegmentsAlone ? 8.0 * ((cut + kReadOnce - 1) / kReadOnce) : 0.0);
+        if (cut > 1) time += (reverse ? 2.0 : 2.2) * span + maps * (span * 1.5 + 1.2) + 4.0;
+        if (cut > kSegmentsAlone) time += (reverse ? 4.0 : 8.0) * ((cut + kReadOnce - 1) / kReadOnce);
         if (time < least) least = time, best = segments;
     }
     return best;
