@@ -308,16 +308,27 @@ __global__ void __launch_bounds__(1024) selective_sum_kernel(Scan k, int states,
     const size_t tile_apart = (size_t)k.B * whole * width;
     const float *from = k.part_rows + ((size_t)b * whole + t0) * width;
     grad_b += b * gbb, grad_c += b * gcb;
-    for (unsigned i = threadIdx.x; i < min(positions, k.T - t0) * width; i += 1024) {
-        const unsigned t = t0 + i / width, within = i % width, n = within % padded, group = within / (2 * padded);
+    // (four states a thread, which share the divisions: rows are whole fours of them)
+    const unsigned fours = width / 4;
+    for (unsigned i = threadIdx.x; i < min(positions, k.T - t0) * fours; i += 1024) {
+        const unsigned t = t0 + i / fours, within = 4 * (i % fours), n = within % padded, group = within / (2 * padded);
         if (n >= (unsigned)k.N) continue;
-        float v = t < (unsigned)length ? from[i] : 0.0f;
-        if (t < (unsigned)length && k.tiles > 1) {
-            const float *tile = from + i;
+        f32x4 v = {};
+        if (t < (unsigned)length) {
+            const float *tile = from + 4 * (size_t)i;
+            v = *reinterpret_cast<const f32x4 *>(tile);
 #pragma unroll 8
-            for (int q = 1; q < k.tiles; ++q) v += *(tile += tile_apart);
+            for (int q = 1; q < k.tiles; ++q) v += *reinterpret_cast<const f32x4 *>(tile += tile_apart);
         }
-        (within / padded & 1 ? grad_c + t * gct : grad_b + t * gbt)[group * k.N + n] = (E)v;
+        E *to = (within / padded & 1 ? grad_c + t * gct : grad_b + t * gbt) + (size_t)group * k.N + n;
+        typedef E Four __attribute__((ext_vector_type(4), aligned(sizeof(E))));
+        if (n + 4 <= (unsigned)k.N) {
+            *reinterpret_cast<Four *>(to) = Four{(E)v[0], (E)v[1], (E)v[2], (E)v[3]};
+        } else {
+#pragma unroll
+            for (unsigned r = 0; r < 3; ++r)
+                if (n + r < (unsigned)k.N) to[r] = (E)v[r];
+        }
     }
 }
 

@@ -348,7 +348,7 @@ constexpr int kSegmentsAlone = 32, kReadOnce = 64 / kFewColumns * kCarryWaves * 
 // what one wave needs for it and what the other waves of its SIMD need, a wave something to begin with, and a share of the maps before its own; the reverse
 // kernel, of which a SIMD holds two waves, takes whole rounds of them, one wave little less than two, and leaves sums for every wave.  Measured in us, * what this takes:
 //   4 x 4096 x 2048 bf16, 16 states    forward 371 with 16 segments, 291 with 32, 275 with 86 and with 103*; reverse 543 with 16, 510 with 32, 499 with 64*
-//   1 x 65536 x 256 bf16, 16 states    forward 185 with 512, 160 with 1024*, 164 with 2048; reverse 315 with 512, 294 with 1024*, 323 with 1280
+//   1 x 65536 x 256 bf16, 16 states    forward 185 with 512, 160 with 1024, 164 with 2048*; reverse 315 with 512, 294 with 1024*, 323 with 1280
 //   1 x 3000 x 256 bf16, 16 states     forward 43 with 96, 33 with 188*, 35 with 375; reverse 78 with 96, 59 with 188*, 53 with 375
 //   240 x 122 x 240 bf16, 16 states    reverse 188 with 1, 157 with 2*, 179 with 8
 //   4 x 4096 x 1024 bf16, 32 states    reverse 513 with 16, 578 with 32, 506 with 47, 527 with 64*
