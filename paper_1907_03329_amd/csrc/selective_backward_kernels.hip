@@ -9,11 +9,11 @@
 // registers, four of a lane's states at a time.  Sums over channels go through LDS within a wave and over tiles in a second launch; those over positions
 // stay in a lane and go over segments in the same.
 //
-// A state takes a power of two and some 13 instructions, with the sums over channels, of the vector ALU, which is the bound: 4 x 4096 x 2048, 16 states, bf16, 32
-// segments: 511 us in all, of them maps 130 (98 of instructions), b and c by pieces 5, gradients 370 (293 of instructions; 512 MB read), sums 24.  1 x 65536 x 256:
-// 295 us; 501 x 240 x 50 ragged fp32: 165.  Tried and slower: two states at a time (699 us for the gradients, for twice the scalar loads and sums); b and c as they
-// are given, 559 us in all, for a piece's are 32 narrow scalar loads and not 8 wide ones; one tile's gradients of b and c without the second launch, which takes
-// 40 registers that there are not.
+// A state takes a power of two and some 13 instructions, with the sums over channels, of the vector ALU, which is the bound: 4 x 4096 x 2048, 16 states,
+// bf16, 64 segments: 495 us in all, of them maps 113 (101 of instructions), putting them together 21, b and c by pieces 5, gradients 373 (288 of instructions;
+// 531 MB read), sums 23.  1 x 65536 x 256: 288 us; 501 x 240 x 50 ragged fp32: 157; 4 x 2048 x 1024, 64 states, bf16: 477.  Tried and slower: two states at a
+// time (699 us for the gradients, for twice the scalar loads and sums); b and c as they are given, 559 us in all, for a piece's are 32 narrow scalar loads and
+// not 8 wide ones; one tile's gradients of b and c without the second launch, which takes 40 registers that there are not.
 #include <algorithm>
 
 #include "selective_scan.h"
