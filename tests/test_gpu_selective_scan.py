@@ -88,6 +88,13 @@ def test_short_and_empty_sequences(lengths, N):
     check(3, 40, 66, N, lengths=lengths, initial=True, seed=1)
 
 
+@pytest.mark.parametrize("N,C,groups", [(6, 140, 1), (33, 140, 1), (40, 300, 2), (64, 66, 1)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_gradients_of_several_tiles_at_odd_places(N, C, groups, dtype):
+    """States that are no whole fours or slices, gradients with gaps between their rows, and positions past the lengths."""
+    check(3, 29, C, N, groups, dtype=dtype, lengths=[29, 0, 18], initial=True, layout="gaps", own_places=True, seed=9)
+
+
 @pytest.mark.parametrize("kind", ["softplus", "given"])
 @pytest.mark.parametrize("D,bias", [(True, False), (False, True), (False, False)])
 def test_operands_that_are_left_out(kind, D, bias):
