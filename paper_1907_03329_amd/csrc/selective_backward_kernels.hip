@@ -27,6 +27,14 @@ namespace {
 // That is 8.6 vector instructions for a position's eight values where exchanges between lanes alone, each of which halves the lanes and the values, take
 // 18; the vector ALU is the bound here and LDS is not.  Rows are 64 lanes x 16 bytes and 64 bytes more, so that the sixteen lanes of a read have all banks.
 constexpr int kSumRow = 64 * 4 + 16;
+// Between accesses of a wave's lanes to what other lanes of it have: the hardware serves a wave's LDS accesses in their order, and the compiler has to keep it.
+// (No instruction of its own.)
+__device__ __forceinline__ void ordered_in_wave()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 // Sums of the quad's lanes, the first value in the lane 0, ..
 __device__ __forceinline__ float exchanged(float keep, float send, std::integral_constant<int, 2>)
 {
@@ -224,9 +232,11 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
                     *reinterpret_cast<f32x4 *>(&shared[2 * i][4 * lane]) = f32x4{of_b[0], of_b[1], of_b[2], of_b[3]};
                     *reinterpret_cast<f32x4 *>(&shared[2 * i + 1][4 * lane]) = f32x4{of_c[0], of_c[1], of_c[2], of_c[3]};
                 }
+                ordered_in_wave();
                 f32x4 sum[2] = {*reinterpret_cast<const f32x4 *>(shared_read), *reinterpret_cast<const f32x4 *>(shared_read + 16)};
 #pragma unroll
                 for (int c = 2; c < 16; ++c) sum[c & 1] += *reinterpret_cast<const f32x4 *>(shared_read + 16 * c);
+                ordered_in_wave();
                 buf_store(to_parts, part_at, 4 * n0, sum_of_quad(sum[0] + sum[1]));
                 complete(through);
                 complete(rate);
