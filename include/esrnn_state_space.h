@@ -76,7 +76,8 @@ esrnn_status esrnn_convolution_step(const esrnn_convolution_step_shape *shape, c
  * Selective scan: C channels of N states each, 1 <= N <= 64, over T positions of B sequences.  b and c belong to G groups of C / G neighbouring
  * channels.  For a channel of group g, with d = softplus(delta + bias) or delta + bias:
  *   h_t[n] = exp(d_t A[n]) h_{t-1}[n] + d_t x_t b_t[g][n],    out_t = sum_n c_t[g][n] h_t[n] + D x_t
- * A is used as it is (rates of decay are negative; minus infinity keeps nothing of a state, but for a step of size zero, which changes nothing).
+ * A is used as it is (rates of decay are negative; minus infinity keeps nothing of a state from steps of 2^-119 on, and a step of size zero changes nothing.  The
+ * gradient of a smaller step of a channel with an infinite rate leaves out what decays: it has no derivative there).
  * Operands that exist are finite; an infinity makes its channel's states, or its group's, infinite or NaN from there on.  At most 2^20 lines, of 64 channels of a
  * sequence and of a group, and 2^15 of them side by side.
  */

@@ -160,6 +160,16 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
     for (int n = 0; n < NP; ++n) A[n] = exponent_rate(A[n]), dA[n] = 0.0f;
     const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
     if (begin < at.length || begin == 0) arriving<NP, SL>(k, at, own, A, mu);
+    // Smaller steps get no gradient from decays where one of the channel's rates is infinite (each slice looks at all of them): such a rate has no derivative there, and
+    // behind larger ones it leaves nothing, so that its states have no part.
+    float least = 0.0f;
+    const auto look_at = [&](float rate) { least = rate == kForgetsAll ? kLeastStep : least; };
+    if constexpr (SL == 1) {
+#pragma unroll
+        for (int n = 0; n < NP; ++n) look_at(A[n]);
+    } else {
+        for (int n = 0; n < k.N; ++n) look_at(exponent_rate(k.a.A[(size_t)at.channel * k.N + n]));
+    }
 
     // what a lane has after all additions: position lane / 8, b or c, state lane % 4; rows of [2][padded] for every position and group
     const float *parts = k.part_rows + (((size_t)(at.tile % k.tiles) * k.B + at.b) * k.pieces * kPiece * k.G + at.group) * (2 * kPadded) + NP * at.slice;
@@ -259,7 +269,9 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) {
                 if (i % SL != at.slice || t + i >= end) continue;
-                const float to_x = fmaf(d[i], through[i], D * g[i]), to_delta = fmaf(rate[i], kLn2, xi[i] * through[i]) * slope[i];
+                // (selections: a large rate may have made an infinity of what would be multiplied by zero, past the length too)
+                const float of_rates = fabsf(d[i]) < least ? 0.0f : rate[i], to_x = fmaf(d[i], through[i], D * g[i]);
+                const float to_step = fmaf(of_rates, kLn2, xi[i] * through[i]), to_delta = slope[i] == 0.0f ? 0.0f : to_step * slope[i];
                 dbias += to_delta;
                 dD = fmaf(g[i], xi[i], dD);
                 if (at.lane_mask) {

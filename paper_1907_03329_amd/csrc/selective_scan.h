@@ -205,11 +205,12 @@ __device__ __forceinline__ float *saved_of(const Scan &k, const ScanPlace &at, i
 }
 
 // A log2 e, of which exp(d A) is the power of two with d.  An infinite rate of decay forgets everything in a step and nothing in one of size zero, which is
-// what positions past a length are: so it is a finite one.
+// what positions past a length are: so it is a finite one, which leaves nothing from a step of kLeastStep on (2^-256 is zero).
+constexpr float kForgetsAll = -0x1p127f, kLeastStep = 0x1p-119f;
 __device__ __forceinline__ float exponent_rate(float A)
 {
     const float rate = A * kLog2e;
-    return rate == -__builtin_inff() ? -0x1p127f : rate;
+    return rate == -__builtin_inff() ? kForgetsAll : rate;
 }
 
 // This lane's states of arrays [..][C][N]; those that do not exist are zero.
