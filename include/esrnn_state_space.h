@@ -15,8 +15,8 @@
  * Element types: activations and their gradients in fp32, bf16 or fp16, all of one call alike (the residual stream may be fp32 beside
  * 16-bit activations); states, statistics, parameters, their gradients and every sum in fp32.  Results are rounded to the element type
  * once, to nearest.  Alignment: that of one element (workspaces and saved states 256 bytes).
- * Arrays that a call writes must not overlap others; those that begin at one place, or that share elements as far as equal strides show it, are
- * refused.
+ * Arrays that a call writes must not overlap others; those that begin at one place, or that share elements as far as equal strides of rows or positions show it, and
+ * rows that reach into a pool of states, are refused.
  *
  * lengths [B] int32 or NULL (all T): positions that exist; values outside 0 .. T are clamped.  Past its length a sequence is not read into
  * arithmetic, and results are zero there.

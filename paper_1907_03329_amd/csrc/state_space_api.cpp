@@ -63,6 +63,30 @@ esrnn_status check_rows(const esrnn_block_norm_shape &s, const Rows *rows, int n
     return ESRNN_OK;
 }
 
+// What single positions read or write of each request: `width` elements next to each other.
+struct StepRows {
+    const void *p;
+    int64_t stride, width;
+};
+// Whether one of them shares elements with a pool of states, which has no gaps.
+bool reach_into(const StepRows &r, int64_t rows, int64_t element, const void *pool, int64_t bytes)
+{
+    const int64_t first = reinterpret_cast<intptr_t>(r.p) - reinterpret_cast<intptr_t>(pool), step = r.stride * element, end = first + r.width * element;
+    if (bytes == 0 || (end <= 0 && step == 0)) return false;
+    const int64_t i = end > 0 ? 0 : -end / step + 1;        // the first that ends behind the pool's beginning
+    return i < rows && first + i * step < bytes;
+}
+bool step_overlaps(int64_t rows, int dtype, const StepRows &out, std::initializer_list<StepRows> read, const void *pool, int64_t bytes)
+{
+    const int64_t element = (int64_t)element_bytes(dtype), written[2] = {0, out.stride};
+    if (reach_into(out, rows, element, pool, bytes)) return true;
+    for (const StepRows &r : read) {
+        const int64_t stride[2] = {0, r.stride};
+        if (rows_overlap(RowsShape{1, rows, out.width, dtype}, out.p, written, r.p, stride, r.width) || reach_into(r, rows, element, pool, bytes)) return true;
+    }
+    return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -135,7 +159,8 @@ esrnn_status esrnn_convolution_step(const esrnn_convolution_step_shape *shape, c
     if (!x || !weight || !state || !out) return ESRNN_ERR_NULL;
     if (s.x_stride < 0 || s.out_stride < 0 || s.x_stride > kMostElements / s.rows || s.out_stride > kMostElements / s.rows ||
         (s.rows > 1 && s.out_stride < s.C) || !element_aligned(x, s.dtype) || !element_aligned(out, s.dtype) || !element_aligned(state, s.dtype) ||
-        !floats_aligned(weight) || !floats_aligned(bias) || !floats_aligned(slots) || one_place({state, out}, {x, weight, bias, slots}))
+        !floats_aligned(weight) || !floats_aligned(bias) || !floats_aligned(slots) || one_place({state, out}, {x, weight, bias, slots}) ||
+        step_overlaps(s.rows, s.dtype, {out, s.out_stride, s.C}, {{x, s.x_stride, s.C}}, state, (int64_t)s.pool * (s.K - 1) * s.C * (int64_t)element_bytes(s.dtype)))
         return ESRNN_ERR_CONFIG;
     ESRNN_TRY(launch_convolution_step(s, x, weight, bias, slots, state, out, static_cast<hipStream_t>(stream)));
     return ESRNN_OK;
@@ -246,6 +271,10 @@ esrnn_status esrnn_selective_step(const esrnn_selective_step_shape *shape, const
         if (!element_aligned(p, s.dtype)) return ESRNN_ERR_CONFIG;
     if (one_place({state, out}, {x, delta_, A, b, c, D, bias, slots})) return ESRNN_ERR_CONFIG;
     if ((s.rows > 1 && s.out_stride < s.C) || !floats_aligned(A) || !floats_aligned(D) || !floats_aligned(bias) || !floats_aligned(slots) || !floats_aligned(state))
+        return ESRNN_ERR_CONFIG;
+    const int64_t shared = (int64_t)s.G * s.N;
+    if (step_overlaps(s.rows, s.dtype, {out, s.out_stride, s.C}, {{x, s.x_stride, s.C}, {delta_, s.delta_stride, s.C}, {b, s.b_stride, shared}, {c, s.c_stride, shared}},
+                      state, (int64_t)s.pool * s.C * s.N * (int64_t)sizeof(float)))
         return ESRNN_ERR_CONFIG;
     const SelectiveStep a{x, delta_, b, c, A, D, bias, slots, state, out};
     ESRNN_TRY(launch_selective_step(s, a, static_cast<hipStream_t>(stream)));
