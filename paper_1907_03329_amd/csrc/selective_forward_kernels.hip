@@ -320,15 +320,15 @@ __global__ void __launch_bounds__(64 * kCarryWaves) selective_carry_kernel(Scan 
     }
 }
 
-// b and c in rows of `padded` fp32 states, zeros behind the N there are: [2][B][T][G][padded].
+// b and c, or c alone, in rows of `padded` fp32 states, zeros behind the N there are: [copies][B][T][G][padded].
 template <class E>
-__global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E *b, const E *c, long long bb, long long bt, long long cb, long long ct, int B,
-                                                                         int T, int G, int N, int padded, float *rows)
+__global__ void __launch_bounds__(kThreadsOfRows) selective_widen_kernel(const E *b, const E *c, long long bb, long long bt, long long cb, long long ct, int copies,
+                                                                         int B, int T, int G, int N, int padded, float *rows)
 {
-    const long long half = (long long)B * T * G * padded;
-    for (long long i = (long long)blockIdx.x * kThreadsOfRows + threadIdx.x; i < 2 * half; i += (long long)gridDim.x * kThreadsOfRows) {
-        const bool second = i >= half;
-        long long rest = second ? i - half : i;
+    const long long half = (long long)B * T * G * padded, first_of_c = (copies - 1) * half;
+    for (long long i = (long long)blockIdx.x * kThreadsOfRows + threadIdx.x; i < copies * half; i += (long long)gridDim.x * kThreadsOfRows) {
+        const bool second = i >= first_of_c;
+        long long rest = second ? i - first_of_c : i;
         const int n = rest % padded;
         rest /= padded;
         const int g = rest % G;
@@ -398,7 +398,8 @@ SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse)
     p.carried = p.segments > kSegmentsAlone;
     const size_t tiles = (size_t)s.G * p.tiles;
     p.maps = p.segments > 1 ? (size_t)s.B * p.segments * tiles * p.slices * (p.states + 1) * 64 : 0;
-    p.rows = 2 * (size_t)s.B * s.T * s.G * p.padded;
+    p.copies = !reverse ? 2 : p.segments > 1 ? 1 : 0;
+    p.rows = p.copies * (size_t)s.B * s.T * s.G * p.padded;
     if (reverse) {
         p.arranged = (size_t)s.B * p.pieces * s.G * p.padded / 4 * 64;      // (or half of it in bf16)
         p.part_rows = (size_t)p.tiles * s.B * p.pieces * kPiece * s.G * 2 * p.padded;
@@ -444,7 +445,7 @@ Scan scan_arguments(const esrnn_selective_shape &s, const SelectiveArgs &a, Sele
     p.widened = !(shared_as_given(s, p, a.b, s.b_stride) && shared_as_given(s, p, a.c, s.c_stride));
     if (p.widened) {
         const long long position = (long long)s.G * p.padded, sequence = s.T * position;
-        k.b = rows, k.c = rows + s.B * sequence;
+        k.b = rows, k.c = p.copies == 2 ? rows + s.B * sequence : rows;
         k.bb = k.cb = sequence, k.bt = k.ct = position, k.group = p.padded;
     } else {
         k.b = a.b, k.c = a.c;
@@ -455,12 +456,12 @@ Scan scan_arguments(const esrnn_selective_shape &s, const SelectiveArgs &a, Sele
 
 hipError_t launch_selective_widen(const esrnn_selective_shape &s, const SelectiveArgs &a, const SelectivePlan &p, const Scan &k, hipStream_t st)
 {
-    if (!p.widened) return hipSuccess;
+    if (!p.widened || p.copies == 0) return hipSuccess;
     return with_element(s.dtype, [&](auto e) {
         typedef decltype(e) E;
         selective_widen_kernel<E><<<dim3((unsigned)std::min<long long>((p.rows + kThreadsOfRows - 1) / kThreadsOfRows, kCopyWorkgroups)), kThreadsOfRows, 0, st>>>(
-            static_cast<const E *>(a.b), static_cast<const E *>(a.c), s.b_stride[0], s.b_stride[1], s.c_stride[0], s.c_stride[1], s.B, s.T, s.G, s.N,
-            p.padded, const_cast<float *>(static_cast<const float *>(k.b)));
+            static_cast<const E *>(a.b), static_cast<const E *>(a.c), s.b_stride[0], s.b_stride[1], s.c_stride[0], s.c_stride[1], p.copies, s.B, s.T, s.G,
+            s.N, p.padded, const_cast<float *>(static_cast<const float *>(k.b)));
         return hipGetLastError();
     });
 }

@@ -28,7 +28,8 @@ struct SelectivePlan {
     int states, slices, padded;         // states of a lane, slices of a channel, and their product
     int tiles;                          // of 64 channels of a group
     int pieces, segments, span;         // of a sequence; pieces of a segment
-    bool widened;                       // b and c are copied to fp32 rows of `padded` states first
+    bool widened;                       // b and c, as far as the pass reads rows of them, are copied to fp32 rows of `padded` states first
+    int copies;                         // of how many it does: both forward; in reverse the maps read those of c, and nothing else does
     bool carried;                       // the maps of segments are put together by a launch of their own
     int line_waves;                     // forward, a workgroup for a whole sequence of a tile's channels: its waves, or 0
     // floats of the workspace: maps of segments, widened b and c, both by pieces, partial gradients of b and c, of A, D and bias
@@ -38,7 +39,7 @@ SelectivePlan selective_plan(const esrnn_selective_shape &s, bool reverse);
 
 struct Scan {
     SelectiveArgs a;
-    const void *b, *c;                  // of which the kernels read rows: as given, or widened
+    const void *b, *c;                  // of which the kernels read rows: as given, or widened (where they do)
     long long xb, xt, db, dt, ob, ot;   // strides of a sequence and of a position
     long long bb, bt, cb, ct, group;    // of rows of b and c, and of a group in both
     long long gb, gt, gxb, gxt, gdb, gdt;
@@ -51,7 +52,7 @@ struct Scan {
 Scan scan_arguments(const esrnn_selective_shape &s, const SelectiveArgs &a, SelectivePlan &p);      // (sets p.widened)
 // Puts the state that enters each segment (against time: the gradient behind it) in the place of its map.
 hipError_t launch_selective_carry(const esrnn_selective_shape &s, const SelectivePlan &p, const Scan &k, bool reverse, hipStream_t st);
-// Copies b and c to rows of fp32 where the kernels cannot read them as they are.
+// Copies b and c, or c alone, to rows of fp32 where the kernels cannot read them as they are.
 hipError_t launch_selective_widen(const esrnn_selective_shape &s, const SelectiveArgs &a, const SelectivePlan &p, const Scan &k, hipStream_t st);
 
 // f(element type tag, type of b and c, states of a lane, slices)
