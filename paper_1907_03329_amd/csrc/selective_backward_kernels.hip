@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
 {
     constexpr int kPart = 4, kPadded = NP * SL;     // (states at a time: theirs at nine positions and their decays at eight take 68 registers)
     __shared__ __attribute__((aligned(16))) float s_shared[SL][2 * kPiece][kSumRow];
+    __shared__ float s_steepest[SL > 1 ? SL : 1][64];
     const ScanPlace at(k, k.segments);
     const int lane = threadIdx.x & 63;
     const int begin = at.segment * k.span * kPiece, end = min(begin + k.span * kPiece, k.T);
@@ -160,22 +161,17 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
     for (int n = 0; n < NP; ++n) A[n] = exponent_rate(A[n]), dA[n] = 0.0f;
     const float bias = k.a.bias ? k.a.bias[at.channel] : 0.0f, D = k.a.D ? k.a.D[at.channel] : 0.0f;
     if (begin < at.length || begin == 0) arriving<NP, SL>(k, at, own, A, mu);
-    // Smaller steps get no gradient from decays where one of the channel's rates is infinite (each slice looks at all of them): such a rate has no derivative there, and
-    // behind larger ones it leaves nothing, so that its states have no part.
-    float least = 0.0f;
-    const auto look_at = [&](float rate) { least = rate == kForgetsAll ? kLeastStep : least; };
-    if constexpr (SL == 1) {
-#pragma unroll
-        for (int n = 0; n < NP; ++n) look_at(A[n]);
-    } else {
-        for (int n = 0; n < k.N; ++n) look_at(exponent_rate(k.a.A[(size_t)at.channel * k.N + n]));
-    }
 
     // what a lane has after all additions: position lane / 8, b or c, state lane % 4; rows of [2][padded] for every position and group
     const float *parts = k.part_rows + (((size_t)(at.tile % k.tiles) * k.B + at.b) * k.pieces * kPiece * k.G + at.group) * (2 * kPadded) + NP * at.slice;
     const unsigned part_position = (unsigned)k.G * (2 * kPadded);
     const unsigned part_at = 4 * ((lane >> 3) * part_position + (lane >> 2 & 1) * kPadded + (lane & 3));
     float(*shared)[kSumRow] = s_shared[at.slice];
+    // The largest rate of the channel, which may make an infinity of what a slope of zero is multiplied by.
+    float steepest = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) steepest = fminf(steepest, A[n]);
+    if constexpr (SL > 1) s_steepest[at.slice][lane] = steepest;        // (the other slices read it behind the barrier of a piece)
     const float *shared_read = &shared[lane >> 2][4 * (lane & 3)];
 
     const int last = min(end, at.length);
@@ -252,11 +248,14 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
                 complete(rate);
                 complete(dA, n0, kPart);
             }
+            float of_channel = SL > 1 ? 0.0f : steepest;
             if constexpr (SL > 1) {
                 // the wave has read its rows: they hold its shares of the sums over all states until every slice has read those of its positions
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i) shared[i][lane] = through[i], shared[kPiece + i][lane] = rate[i];
                 lds_barrier();      // (requests for the next piece go on)
+#pragma unroll
+                for (int s = 0; s < SL; ++s) of_channel = fminf(of_channel, s_steepest[s][lane]);
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i)
                     if (i % SL == at.slice) {
@@ -266,12 +265,17 @@ __global__ void __launch_bounds__(64 * SL, SL > 1 ? 1 : 2) selective_backward_ke
                     }
                 lds_barrier();
             }
+            // Slopes are zero past the length, too.  And steps below kLeastStep get no gradient from decays where a rate is infinite: it has no derivative there, and behind
+            // larger steps nothing is left that would go by it.  (Behind a condition for the wave: selections at every piece cost 1 to 5 % of the kernel.)
+            if (__any(of_channel < -0x1p64f)) {
+                const float least = of_channel == kForgetsAll ? kLeastStep : 0.0f;
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) rate[i] = fabsf(d[i]) < least || slope[i] == 0.0f ? 0.0f : rate[i];
+            }
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) {
                 if (i % SL != at.slice || t + i >= end) continue;
-                // (selections: a large rate may have made an infinity of what would be multiplied by zero, past the length too)
-                const float of_rates = fabsf(d[i]) < least ? 0.0f : rate[i], to_x = fmaf(d[i], through[i], D * g[i]);
-                const float to_step = fmaf(of_rates, kLn2, xi[i] * through[i]), to_delta = slope[i] == 0.0f ? 0.0f : to_step * slope[i];
+                const float to_x = fmaf(d[i], through[i], D * g[i]), to_delta = fmaf(rate[i], kLn2, xi[i] * through[i]) * slope[i];
                 dbias += to_delta;
                 dD = fmaf(g[i], xi[i], dD);
                 if (at.lane_mask) {
