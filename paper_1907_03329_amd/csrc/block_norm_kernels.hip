@@ -300,8 +300,10 @@ __global__ void __launch_bounds__(Y::kThreads) block_norm_backward_kernel(Args p
     }
 }
 
-// Rows of more channels than registers hold with all that is made of them: every one of the three steps (the sum for the second norm, that for the first, the
-// gradients) reads the row again, from the caches, and the sums over rows are in LDS.  4000 rows of 8192 channels, bf16: some 250 us, where 109 would be those of a copy.
+// Rows of more than 4096 channels, of which registers do not hold what is made of them: every one of the three steps (the sum for the second norm, that for the first,
+// the gradients) reads the row again, from the caches, and the sums over rows are in LDS.  4000 rows of 8192 channels, bf16: some 250 us, where 109 would be those of a
+// copy.  The operands alone would fit (eight channels of five arrays: 20 registers in 16 bits, 40 in fp32, of 128) and could be read once, the terms made of them at every
+// step: not built.
 template <class E, class R, class Y>
 __global__ void __launch_bounds__(Y::kThreads) block_norm_wide_backward_kernel(Args p)
 {

@@ -10,8 +10,9 @@
 // stay in a lane and go over segments in the same.
 //
 // A state takes a power of two and some 13 instructions, with the sums over channels, of the vector ALU, which is the bound: 4 x 4096 x 2048, 16 states,
-// bf16, 64 segments: 495 us in all, of them maps 113 (101 of instructions), putting them together 21, b and c by pieces 5, gradients 373 (288 of instructions;
-// 531 MB read), sums 23.  1 x 65536 x 256: 288 us; 501 x 240 x 50 ragged fp32: 157; 4 x 2048 x 1024, 64 states, bf16: 477.  Tried and slower: two states at a
+// bf16, 64 segments: 493 us in all.  Dispatch by dispatch under the profiler, where they take a tenth longer together: maps 114 (101 of instructions), putting them
+// together 21, b and c by pieces 5, gradients 379 (285 of instructions; 531 MB read), sums 23.  1 x 65536 x 256: 281 us in all; 501 x 240 x 50 ragged fp32: 159;
+// 4 x 2048 x 1024, 64 states, bf16: 474.  Tried and slower: two states at a
 // time (699 us for the gradients, for twice the scalar loads and sums); b and c as they are given, 559 us in all, for a piece's are 32 narrow scalar loads and
 // not 8 wide ones; one tile's gradients of b and c without the second launch, which takes 40 registers that there are not.
 #include <algorithm>
